@@ -1,0 +1,563 @@
+"""Sequence operators as cases that can be timed: what one layer over event
+histories is made of.
+
+  norm             t = x + r, y = t / rms(t) * w, in the inputs' type or in 8
+                   bits (e4m3) with one scale a row
+  norm_backward    its gradients in t and w
+  linear           y = act(x W^T + b) + r; 8-bit x and W with a scale a row
+  linear_backward  dx, dW and db from dy and the saved pre-activation z
+  scan             h_t = a_t h_(t-1) + (1 - a_t) x_t, a_t = sigmoid(g_t), along
+                   every sequence of a packed or padded batch
+  scan_train       the scan and its gradients in g, x and h_0
+  scan_step        one row of the scan for each of n slots of a state table
+
+Sizes are the repository's own (memories of 100, time codes of 100, messages of
+372 and 472 columns, 12,000 roots of 10 neighbours, tables of 9,228 nodes) and
+generic ones: one row to 16,384 in products and norms, one row to a million in
+a scan, widths of 64 to 8,192 with odd ones among them.
+
+``own`` picks the form that ``run`` takes: elementary torch operations in 32
+bits, or the framework's entry points.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+F32, F64 = torch.float32, torch.float64
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16,
+         "e4m3": torch.float8_e4m3fn}
+BYTES = {"f32": 4, "bf16": 2, "f16": 2, "e4m3": 1}
+EPS = 1e-6
+E4M3_MAX = 448.0
+TINY = 2.0 ** -126
+
+
+# ------------------------------------------------------------------- cases
+def listed():
+    return [
+        # a few rows of a model that answers: only latency counts
+        dict(name="norm_few_bf16", op="norm", rows=4, D=2048, dtype="bf16", out="bf16", res=True),
+        # the rows that 8-bit products read, with the residual stream that goes on
+        dict(name="norm_8bit_bf16", op="norm", rows=8192, D=4096, dtype="bf16", out="e4m3",
+             res=True),
+        # training on node rows of the framework's memory width
+        dict(name="norm_backward_f32", op="norm_backward", rows=12000, D=100, dtype="f32",
+             dt=False),
+        # a few rows through a wide layer: bound by reading the weights once
+        dict(name="linear_few_f16", op="linear", rows=4, N=4096, K=2048, dtype="f16", out="f16",
+             act="silu", bias=True, res=False),
+        # gates and candidates from messages and time codes (472 columns), in the framework's type
+        dict(name="linear_gates_f32", op="linear", rows=12000, N=200, K=472, dtype="f32",
+             out="f32", act="none", bias=True, res=False),
+        # a wide layer in 8 bits, added to the residual stream: the largest product
+        dict(name="linear_8bit", op="linear", rows=16384, N=4096, K=8192, dtype="e4m3",
+             out="bf16", act="none", bias=True, res=True),
+        # an ordinary layer's training step
+        dict(name="linear_backward_bf16", op="linear_backward", rows=8192, N=4096, K=2048,
+             dtype="bf16", act="gelu"),
+        # one event for each of a batch's nodes, into the table of node states
+        dict(name="scan_step_f32", op="scan_step", rows=600, slots=9228, D=100, dtype="f32"),
+        # sampled neighbours of 12,000 roots, newest first, padded to 10
+        dict(name="scan_padded_f32", op="scan", S=12000, L=10, rows=120000, D=100, dtype="f32",
+             layout="padded", reverse=True, h0=False),
+        # one long history
+        dict(name="scan_long_bf16", op="scan", S=1, L=0, rows=1000003, D=128, dtype="bf16",
+             layout="packed", reverse=False, h0=True),
+        # packed histories of uneven length through a training step
+        dict(name="scan_train_bf16", op="scan_train", S=64, L=0, rows=131072, D=512, dtype="bf16",
+             layout="packed", reverse=False, h0=True),
+        # many short histories in the framework's type through a training step
+        dict(name="scan_train_f32", op="scan_train", S=4000, L=0, rows=44001, D=100, dtype="f32",
+             layout="packed", reverse=False, h0=True),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["norm", "norm_backward", "linear", "linear", "linear_backward", "scan",
+                     "scan", "scan_train", "scan_step"])
+    flag = lambda: rng.random() < 0.5
+    odd = lambda v, m: max(1, v if rng.random() < 0.35 else m * max(1, v // m))
+    if op in ("norm", "norm_backward"):
+        rows = _log(rng, 1, 16384)
+        c = dict(op=op, rows=rows, D=odd(_log(rng, 64, 8192), 8),
+                 dtype=rng.choice(["f32", "bf16", "f16"]))
+        while c["rows"] * c["D"] > 2 ** 26:
+            c["rows"] //= 2
+        if op == "norm":
+            c.update(out=rng.choice([c["dtype"], "e4m3"]), res=flag())
+        else:
+            c.update(dt=flag())
+        return c
+    if op in ("linear", "linear_backward"):
+        c = dict(op=op, rows=_log(rng, 1, 16384), N=odd(_log(rng, 64, 4096), 8),
+                 K=odd(_log(rng, 64, 4096), 8),
+                 dtype=rng.choice(["f32", "bf16", "bf16", "f16"] +
+                                  (["e4m3"] * 2 if op == "linear" else [])),
+                 act=rng.choice(["none", "silu", "gelu"]))
+        most = 2e10 if c["dtype"] == "f32" else 2e11
+        while c["rows"] * c["N"] * c["K"] > most:
+            c["rows"] //= 2
+        if op == "linear":
+            c.update(out="bf16" if c["dtype"] == "e4m3" else c["dtype"], bias=flag(), res=flag())
+        return c
+    if op == "scan_step":
+        rows = _log(rng, 1, 16384)
+        return dict(op=op, rows=rows, slots=rows + _log(rng, 1, 10000),
+                    D=odd(_log(rng, 32, 2048), 8), dtype=rng.choice(["f32", "bf16", "f16"]))
+    D = odd(_log(rng, 32, 1024), 8)
+    layout = rng.choice(["packed", "padded"])
+    most = 2 ** 27 if op == "scan" else 2 ** 26
+    c = dict(op=op, S=_log(rng, 1, 8192), L=0, rows=0, D=D,
+             dtype=rng.choice(["f32", "bf16", "f16"]), layout=layout, reverse=flag(), h0=flag())
+    L = _log(rng, 1, 16384)
+    while c["S"] * L * D > most:
+        c["S"], L = max(1, c["S"] // 2), max(1, int(L / 1.3))
+    c["L"], c["rows"] = (L if layout == "padded" else 0), c["S"] * L
+    return c
+
+
+# ------------------------------------------------------------------ inputs
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(int(seed))
+    dt = TYPES[case["dtype"]]
+    randn = lambda *shape: torch.randn(*shape, generator=gen, device="cuda")
+    empty = lambda *shape, dtype=dt: torch.zeros(*shape, device="cuda", dtype=dtype)
+    op = case["op"]
+    s = dict(case=case)
+    if op in ("norm", "norm_backward"):
+        R, D = case["rows"], case["D"]
+        # rows of different size, as a residual stream has
+        x = randn(R, D) * torch.exp(randn(R, 1))
+        s["w"] = (1 + 0.2 * randn(D)).to(dt)
+        if op == "norm":
+            s["x"] = x.to(dt)
+            s["res"] = randn(R, D).to(dt) if case["res"] else None
+            s["total"] = empty(R, D) if case["res"] else None
+            s["y"] = empty(R, D, dtype=TYPES[case["out"]])
+            s["scale"] = empty(R, dtype=F32) if case["out"] == "e4m3" else None
+        else:
+            s["t"], s["dy"] = x.to(dt), randn(R, D).to(dt)
+            s["dtotal"] = randn(R, D).to(dt) if case["dt"] else None
+            s["dx"], s["dw"] = empty(R, D), empty(D)
+    elif op in ("linear", "linear_backward"):
+        R, N, K = case["rows"], case["N"], case["K"]
+        x, w = randn(R, K), randn(N, K) / math.sqrt(K)
+        if dt == TYPES["e4m3"]:
+            for name, v in (("x", x), ("w", w)):
+                scale = v.abs().amax(1) / E4M3_MAX
+                s[name], s["scale_" + name] = (v / scale[:, None]).to(dt), scale
+        else:
+            s["x"], s["w"] = x.to(dt), w.to(dt)
+            s["scale_x"] = s["scale_w"] = None
+        if op == "linear":
+            out = TYPES[case["out"]]
+            s["bias"] = (0.5 * randn(N)).to(out) if case["bias"] else None
+            s["res"] = randn(R, N).to(out) if case["res"] else None
+            s["y"] = empty(R, N, dtype=out)
+        else:
+            s["z"] = randn(R, N).to(dt) if case["act"] != "none" else None
+            s["dy"] = randn(R, N).to(dt)
+            s["dx"], s["dw"], s["db"] = empty(R, K), empty(N, K), empty(N)
+    elif op == "scan_step":
+        n, D = case["rows"], case["D"]
+        s["g"], s["x"] = _gates(randn, n, D).to(dt), randn(n, D).to(dt)
+        s["slots"] = torch.randperm(case["slots"], generator=gen, device="cuda")[:n].to(
+            torch.int32)
+        s["state"], s["y"] = randn(case["slots"], D), empty(n, D)
+    else:
+        R, S, D = case["rows"], case["S"], case["D"]
+        s["g"], s["x"] = _gates(randn, R, D).to(dt), randn(R, D).to(dt)
+        s["y"] = empty(R, D)
+        s["h0"] = randn(S, D) if case["h0"] else None
+        s["h_last"] = empty(S, D, dtype=F32)
+        if case["layout"] == "padded":
+            # neighbour counts: some roots have none, most are full
+            s["offsets"] = None
+            u = torch.rand(S, generator=gen, device="cuda") * 1.5 * case["L"]
+            s["length"] = u.to(torch.int32).clamp_(max=case["L"])
+        else:
+            # uneven lengths, empty ones among them, and rows behind the last
+            cut = torch.rand(S, generator=gen, device="cuda").square_().add_(1e-3)
+            cut[S // 3] = cut[S // 3] * (S == 1)
+            cut = torch.cumsum(cut.to(F64), 0)
+            used = R - (R // 50 if S > 1 else 0)
+            ends = (cut / cut[-1].clamp_min(1e-9) * used).round_().to(torch.int64)
+            s["offsets"] = torch.cat([ends.new_zeros(1), ends])
+            s["length"] = None
+        if op == "scan_train":
+            s["dy"], s["dh_last"] = randn(R, D).to(dt), randn(S, D)
+            s["dg"], s["dx"] = empty(R, D), empty(R, D)
+            s["dh0"] = empty(S, D, dtype=F32)
+    if own:
+        _prepare_own(s, case)
+    return s
+
+
+def _gates(randn, rows, D):
+    # channels that forget within a few rows next to ones that hold hundreds
+    return randn(rows, D) + torch.linspace(-1.0, 5.0, D, device="cuda")
+
+
+def _prepare_own(s, case):
+    from paper_2402_15113_amd import tgm
+    op, n = case["op"], 0
+    if op == "norm_backward":
+        n = tgm.tgm_norm_work_bytes(case["rows"], case["D"])
+    elif op in ("linear", "linear_backward"):
+        n = tgm.tgm_linear_work_bytes(case["rows"], case["N"], case["K"], TYPES[case["dtype"]],
+                                      backward=op == "linear_backward", act=case["act"])
+    elif op in ("scan", "scan_train"):
+        n = tgm.tgm_scan_work_bytes(case["rows"], case["D"], case["S"])
+    s["work"] = torch.empty(n, dtype=torch.uint8, device="cuda") if n else None
+    if op == "scan_train":
+        s["carry"] = torch.empty(tgm.tgm_scan_carry_rows(case["rows"], case["S"],
+                                                         packed=case["layout"] == "packed"),
+                                 case["D"], device="cuda")
+
+
+# -------------------------------------------------------------------- a pass
+def run(s):
+    return _run_own(s) if own else _PLAIN[s["case"]["op"]](s)
+
+
+def _run_own(s):
+    from paper_2402_15113_amd import tgm
+    c = s["case"]
+    op = c["op"]
+    if op == "norm":
+        tgm.tgm_norm(s["x"], s["w"], s["y"], EPS, res=s["res"], total=s["total"],
+                     scale=s["scale"])
+        return dict(y=s["y"], total=s["total"], scale=s["scale"])
+    if op == "norm_backward":
+        tgm.tgm_norm_backward(s["t"], s["w"], s["dy"], EPS, s["dx"], s["dw"], s["work"],
+                              dtotal=s["dtotal"])
+        return dict(dx=s["dx"], dw=s["dw"])
+    if op == "linear":
+        tgm.tgm_linear(s["x"], s["w"], s["y"], s["work"], act=c["act"], bias=s["bias"],
+                       residual=s["res"], scale_x=s["scale_x"], scale_w=s["scale_w"])
+        return dict(y=s["y"])
+    if op == "linear_backward":
+        tgm.tgm_linear_backward(s["x"], s["w"], s["dy"], s["work"], act=c["act"], z=s["z"],
+                                dx=s["dx"], dw=s["dw"], db=s["db"])
+        return dict(dx=s["dx"], dw=s["dw"], db=s["db"])
+    if op == "scan_step":
+        tgm.tgm_scan_step(s["g"], s["x"], s["state"], s["y"], slots=s["slots"])
+        return dict(y=s["y"], state=s["state"])
+    seq = dict(offsets=s["offsets"], length=s["length"], reverse=c["reverse"])
+    if op == "scan":
+        tgm.tgm_scan(s["g"], s["x"], s["y"], c["S"], s["work"], h0=s["h0"], h_last=s["h_last"],
+                     **seq)
+        return dict(y=s["y"], h_last=s["h_last"])
+    tgm.tgm_scan(s["g"], s["x"], s["y"], c["S"], s["work"], h0=s["h0"], h_last=s["h_last"],
+                 carry=s["carry"], **seq)
+    tgm.tgm_scan_backward(s["g"], s["x"], s["dy"], s["carry"], s["dg"], s["dx"], c["S"],
+                          s["work"], dh_last=s["dh_last"], dh0=s["dh0"], **seq)
+    return dict(y=s["y"], h_last=s["h_last"], dg=s["dg"], dx=s["dx"], dh0=s["dh0"])
+
+
+def _plain_norm(s):
+    t = s["x"].to(F32)
+    if s["res"] is not None:
+        t = t + s["res"].to(F32)
+    y = t * torch.rsqrt((t * t).mean(1, keepdim=True) + EPS) * s["w"].to(F32)
+    total = None if s["res"] is None else t.to(s["x"].dtype)
+    if s["scale"] is None:
+        return dict(y=y.to(s["y"].dtype), total=total, scale=None)
+    scale = (y.abs().amax(1) / E4M3_MAX).clamp_min(TINY)
+    q = (y / scale[:, None]).clamp(-E4M3_MAX, E4M3_MAX)
+    return dict(y=q.to(s["y"].dtype), total=total, scale=scale)
+
+
+def _plain_norm_backward(s):
+    t, w, dy = s["t"].to(F32), s["w"].to(F32), s["dy"].to(F32)
+    r = torch.rsqrt((t * t).mean(1, keepdim=True) + EPS)
+    wdy = w * dy
+    dx = r * (wdy - t * (r * r) * (wdy * t).mean(1, keepdim=True))
+    if s["dtotal"] is not None:
+        dx = dx + s["dtotal"].to(F32)
+    return dict(dx=dx.to(s["dx"].dtype), dw=(dy * t * r).sum(0).to(s["dw"].dtype))
+
+
+def _plain_act(z, act):
+    if act == "relu":
+        return z.clamp_min(0)
+    if act == "silu":
+        return z * torch.sigmoid(z)
+    if act == "gelu":
+        return 0.5 * z * (1 + torch.erf(z * math.sqrt(0.5)))
+    return z
+
+
+def _plain_act_grad(z, act):
+    if act == "relu":
+        return (z > 0).to(z.dtype)
+    if act == "silu":
+        p = torch.sigmoid(z)
+        return p * (1 + z * (1 - p))
+    return 0.5 * (1 + torch.erf(z * math.sqrt(0.5))) + \
+        z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)
+
+
+def _plain_linear(s):
+    z = s["x"].to(F32) @ s["w"].to(F32).t()
+    if s["scale_x"] is not None:
+        z = z * (s["scale_x"][:, None] * s["scale_w"][None])
+    if s["bias"] is not None:
+        z = z + s["bias"].to(F32)
+    y = _plain_act(z, s["case"]["act"])
+    if s["res"] is not None:
+        y = y + s["res"].to(F32)
+    return dict(y=y.to(s["y"].dtype))
+
+
+def _plain_linear_backward(s):
+    dz = s["dy"].to(F32)
+    if s["z"] is not None:
+        dz = dz * _plain_act_grad(s["z"].to(F32), s["case"]["act"])
+    dt = s["x"].dtype
+    return dict(dx=(dz @ s["w"].to(F32)).to(dt), dw=(dz.t() @ s["x"].to(F32)).to(dt),
+                db=dz.sum(0).to(dt))
+
+
+def _rows_of(s):
+    """Each row's sequence, whether it is in it, and whether it is its first and
+    its last in the scan's order; each sequence's bounds."""
+    c = s["case"]
+    S, R = c["S"], c["rows"]
+    if s["offsets"] is None:
+        begin = torch.arange(S, device="cuda") * c["L"]
+        end = begin + s["length"].to(torch.int64)
+    else:
+        begin, end = s["offsets"][:-1], s["offsets"][1:]
+    r = torch.arange(R, device="cuda")
+    # the last sequence that begins at or before the row: empty ones before it share its place
+    seq = torch.searchsorted(begin.contiguous(), r, right=True) - 1
+    inside = r < end[seq]
+    first, last = inside & (r == begin[seq]), inside & (r == end[seq] - 1)
+    if c["reverse"]:
+        first, last = last, first
+    return seq, inside, first, last, begin, end
+
+
+def _doubling(a, b, span):
+    """b_t <- a_t b_(t-1) + b_t along the rows, by steps of 1, 2, 4, ..."""
+    k = 1
+    while k < span:
+        b[k:] = b[k:] + a[k:] * b[:-k]
+        a[k:] = a[k:] * a[:-k]
+        k *= 2
+    return b
+
+
+def _plain_scan(s, gradients=False):
+    c = s["case"]
+    span = c["L"] or c["rows"]
+    seq, inside, first, last, begin, end = _rows_of(s)
+    turn = (lambda v: v.flip(0)) if c["reverse"] else (lambda v: v)
+    g, x = s["g"].to(F32), s["x"].to(F32)
+    a, i = torch.sigmoid(g), torch.sigmoid(-g)
+    zero = torch.zeros((), device="cuda")
+    h0 = s["h0"] if s["h0"] is not None else zero.expand(c["S"], c["D"])
+    start = torch.where(first[:, None], h0[seq], zero)
+    b = torch.where(inside[:, None], i * x + a * start, zero)
+    keep = torch.where((inside & ~first)[:, None], a, zero)
+    h = turn(_doubling(turn(keep).clone(), turn(b).clone(), span))
+    some = (end > begin)[:, None]
+    at = (begin if c["reverse"] else end - 1).clamp(0, c["rows"] - 1)
+    out = dict(y=h.to(s["y"].dtype), h_last=torch.where(some, h[at], h0))
+    if not gradients:
+        return out
+    back = (lambda v: v) if c["reverse"] else (lambda v: v.flip(0))
+    # the gate of the row that follows in the scan's order
+    follows = torch.zeros_like(a)
+    if c["reverse"]:
+        follows[1:] = a[:-1]
+    else:
+        follows[:-1] = a[1:]
+    follows = torch.where((inside & ~last)[:, None], follows, zero)
+    dh = torch.where(inside[:, None], s["dy"].to(F32) +
+                     torch.where(last[:, None], s["dh_last"][seq], zero), zero)
+    dh = back(_doubling(back(follows).clone(), back(dh).clone(), span))
+    before = torch.zeros_like(h)
+    if c["reverse"]:
+        before[:-1] = h[1:]
+    else:
+        before[1:] = h[:-1]
+    before = torch.where(first[:, None], start, before)
+    # (1 - a) a (h_(t-1) - x), zero outside
+    out["dg"] = (dh * a * i * (before - x)).to(s["dg"].dtype)
+    out["dx"] = (dh * i).to(s["dx"].dtype)
+    at = (end - 1 if c["reverse"] else begin).clamp(0, c["rows"] - 1)
+    out["dh0"] = torch.where(some, (a * dh)[at], s["dh_last"])
+    return out
+
+
+def _plain_scan_step(s):
+    slots = s["slots"].to(torch.int64)
+    g, x, h = s["g"].to(F32), s["x"].to(F32), s["state"][slots]
+    h = torch.sigmoid(g) * h + torch.sigmoid(-g) * x
+    s["state"][slots] = h
+    return dict(y=h.to(s["y"].dtype), state=s["state"])
+
+
+_PLAIN = dict(norm=_plain_norm, norm_backward=_plain_norm_backward, linear=_plain_linear,
+              linear_backward=_plain_linear_backward, scan=_plain_scan,
+              scan_train=lambda s: _plain_scan(s, gradients=True), scan_step=_plain_scan_step)
+
+
+# ---------------------------------------------------------------------- work
+def work(case):
+    op, b = case["op"], BYTES[case["dtype"]]
+    if op in ("norm", "norm_backward"):
+        n, D = case["rows"] * case["D"], case["D"]
+        if op == "norm":
+            o = BYTES[case["out"]]
+            extra = 4 * case["rows"] if case["out"] == "e4m3" else 0
+            return dict(bytes=n * (b + o + (2 * b if case["res"] else 0)) + D * b + extra,
+                        flops=5 * n)
+        return dict(bytes=n * b * (4 if case["dt"] else 3) + 2 * D * b, flops=10 * n)
+    if op == "linear":
+        R, N, K, o = case["rows"], case["N"], case["K"], BYTES[case["out"]]
+        scales = 4 * (R + N) if case["dtype"] == "e4m3" else 0
+        return dict(bytes=(R * K + N * K) * b + R * N * o * (2 if case["res"] else 1) +
+                    (N * o if case["bias"] else 0) + scales, flops=2 * R * N * K)
+    if op == "linear_backward":
+        R, N, K = case["rows"], case["N"], case["K"]
+        return dict(bytes=(2 * R * K + 2 * N * K + R * N * (1 if case["act"] == "none" else 2) +
+                           N) * b, flops=4 * R * N * K)
+    if op == "scan_step":
+        n = case["rows"] * case["D"]
+        return dict(bytes=n * (3 * b + 8) + 4 * case["rows"], flops=6 * n)
+    n, s = case["rows"] * case["D"], case["S"] * case["D"]
+    if op == "scan":
+        return dict(bytes=3 * n * b + 4 * s * (2 if case["h0"] else 1), flops=6 * n)
+    # forward: g, x in, y out; backward: g, x, dy in, dg, dx out
+    return dict(bytes=8 * n * b + 4 * s * (4 if case["h0"] else 3), flops=20 * n)
+
+
+# ------------------------------------------------------------------ in 64 bits
+def exact(case, seed):
+    s = prepare(case, seed)
+    D = lambda name: None if s.get(name) is None else s[name].to(F64)
+    op = case["op"]
+    if op == "norm":
+        t = D("x") if s["res"] is None else D("x") + D("res")
+        y = t / (t.square().sum(1, keepdim=True) / case["D"] + EPS).sqrt() * D("w")
+        total = None if s["res"] is None else t
+        if s["scale"] is None:
+            return dict(y=y, total=total, scale=None)
+        scale = torch.maximum(y.amax(1), -y.amin(1)) / E4M3_MAX
+        # the 8-bit values nearest to y / scale, ties to the even one: three bits behind the
+        # leading one, down to steps of 2^-9
+        q = y / scale.clamp_min(TINY)[:, None]
+        step = torch.exp2(torch.floor(torch.log2(q.abs().clamp_min(2.0 ** -6))) - 3)
+        return dict(y=torch.round(q / step) * step, total=total, scale=scale.clamp_min(TINY))
+    if op == "norm_backward":
+        t, w = D("t").requires_grad_(), D("w").requires_grad_()
+        y = t / (t.square().sum(1, keepdim=True) / case["D"] + EPS).sqrt() * w
+        dx, dw = torch.autograd.grad(y, (t, w), D("dy"))
+        return dict(dx=dx if s["dtotal"] is None else dx + D("dtotal"), dw=dw)
+    if op == "linear":
+        x, w = D("x"), D("w")
+        if s["scale_x"] is not None:
+            x, w = x * D("scale_x")[:, None], w * D("scale_w")[:, None]
+        z = torch.matmul(x, w.t().contiguous())
+        z = z if s["bias"] is None else z + D("bias")
+        if case["act"] == "silu":
+            z = z / (1 + torch.exp(-z))
+        elif case["act"] == "gelu":
+            z = z * torch.erfc(-z / math.sqrt(2)) / 2
+        elif case["act"] == "relu":
+            z = torch.where(z > 0, z, torch.zeros_like(z))
+        return dict(y=z if s["res"] is None else z + D("res"))
+    if op == "linear_backward":
+        dz = D("dy")
+        if s["z"] is not None:
+            z = D("z").requires_grad_()
+            v = z / (1 + torch.exp(-z)) if case["act"] == "silu" else \
+                z * torch.erfc(-z / math.sqrt(2)) / 2 if case["act"] == "gelu" else \
+                torch.where(z > 0, z, torch.zeros_like(z))
+            dz, = torch.autograd.grad(v, z, dz)
+        return dict(dx=torch.matmul(dz, D("w")), dw=torch.matmul(dz.t().contiguous(), D("x")),
+                    db=dz.sum(0))
+    if op == "scan_step":
+        slots = s["slots"].long()
+        z = 1 / (1 + torch.exp(-D("g")))
+        state = D("state")
+        state[slots] = z * state[slots] + (1 - z) * D("x")
+        return dict(y=state[slots].clone(), state=state)
+    return _exact_scan(case, s)
+
+
+def _linear_recurrence(a, b):
+    """h_t = a_t h_(t-1) + b_t row by row, h_(-1) = 0, for the pieces of about
+    the square root of the rows side by side, and then from piece to piece."""
+    rows, D = a.shape
+    C = max(1, math.isqrt(rows))
+    P = -(-rows // C)
+    pad = P * C - rows
+    a = torch.cat([a, a.new_zeros(pad, D)]).view(P, C, D)
+    h = torch.cat([b, b.new_zeros(pad, D)]).view(P, C, D)
+    gain = a.clone()
+    for t in range(1, C):
+        h[:, t] += a[:, t] * h[:, t - 1]
+        gain[:, t] *= gain[:, t - 1]
+    end = torch.zeros(P, D, dtype=h.dtype, device=h.device)
+    for p in range(1, P):
+        end[p] = h[p - 1, -1] + gain[p - 1, -1] * end[p - 1]
+    return (h + gain * end[:, None]).view(P * C, D)[:rows]
+
+
+def _exact_scan(case, s):
+    S, R, D, rev = case["S"], case["rows"], case["D"], case["reverse"]
+    if s["offsets"] is None:
+        lo = [k * case["L"] for k in range(S)]
+        hi = [b + n for b, n in zip(lo, s["length"].tolist())]
+    else:
+        lo, hi = s["offsets"].tolist()[:-1], s["offsets"].tolist()[1:]
+    some = [k for k in range(S) if hi[k] > lo[k]]
+    dev = s["g"].device
+    at = lambda v: torch.tensor(v, dtype=torch.int64, device=dev)
+    seqs, los, his = at(some), at([lo[k] for k in some]), at([hi[k] - 1 for k in some])
+    head, tail = (his, los) if rev else (los, his)
+    mark = torch.zeros(R + 1, dtype=torch.int64, device=dev)
+    mark[los] += 1
+    mark[his + 1] -= 1
+    inside = (mark.cumsum(0)[:R] > 0)[:, None].to(F64)
+    z = 1 / (1 + torch.exp(-s["g"].to(F64)))
+    x = s["x"].to(F64)
+    h0 = s["h0"].to(F64) if s["h0"] is not None else torch.zeros(S, D, dtype=F64, device=dev)
+    a, b = z * inside, (1 - z) * x * inside
+    b[head] += a[head] * h0[seqs]
+    a[head] = 0
+    order = (lambda v: v.flip(0)) if rev else (lambda v: v)
+    h = order(_linear_recurrence(order(a), order(b)))
+    h_last = h0.clone()
+    h_last[seqs] = h[tail]
+    if case["op"] == "scan":
+        return dict(y=h, h_last=h_last)
+    # the adjoint runs the other way: what row t hands back is z_t times its own
+    dh = s["dy"].to(F64) * inside
+    dh[tail] += s["dh_last"].to(F64)[seqs]
+    hand = z * inside
+    shifted = torch.zeros_like(hand)
+    if rev:
+        shifted[1:] = hand[:-1]
+    else:
+        shifted[:-1] = hand[1:]
+    shifted[tail] = 0
+    order = (lambda v: v) if rev else (lambda v: v.flip(0))
+    dh = order(_linear_recurrence(order(shifted * inside), order(dh)))
+    before = torch.roll(h, -1 if rev else 1, 0)
+    before[head] = h0[seqs]
+    dh0 = s["dh_last"].to(F64).clone()
+    dh0[seqs] = (z * dh)[head]
+    return dict(y=h, h_last=h_last, dg=dh * (before - x) * z * (1 - z), dx=dh * (1 - z), dh0=dh0)
