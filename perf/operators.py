@@ -259,7 +259,7 @@ def _run_own(s):
     tgm.tgm_scan(s["g"], s["x"], s["y"], c["S"], s["work"], h0=s["h0"], h_last=s["h_last"],
                  carry=s["carry"], **seq)
     tgm.tgm_scan_backward(s["g"], s["x"], s["dy"], s["carry"], s["dg"], s["dx"], c["S"],
-                          s["work"], dh_last=s["dh_last"], dh0=s["dh0"], **seq)
+                          s["work"], h0=s["h0"], dh_last=s["dh_last"], dh0=s["dh0"], **seq)
     return dict(y=s["y"], h_last=s["h_last"], dg=s["dg"], dx=s["dx"], dh0=s["dh0"])
 
 
