@@ -626,6 +626,81 @@ tgm_status_t tgm_min_staleness(const double *tau, int64_t n, int32_t k_max, int3
                                double *fetch_start, double *stall, double *b, double *e);
 
 /* ------------------------------------------------------------------------
+ * Sequence operators.  The memory update above takes one recurrent step of a
+ * node per batch, from its latest message (Eq. 1).  The calls below make up a
+ * layer that runs over every event of a history instead, in the forms that
+ * training (a gradient) and serving (a few rows, one event per node) need:
+ *
+ *   tgm_norm           root-mean-square norm with the residual's addition
+ *   tgm_linear         matrix product with bias, activation and residual
+ *   tgm_scan           gated linear recurrence along packed or padded histories
+ *   tgm_scan_step      one row of it for each of n slots of a state table
+ *   tgm_..._backward   their gradients
+ *
+ * Conventions, besides those at the top of this file:
+ *  - Rows are events (or nodes, or roots), columns channels.  A row stride
+ *    (ld_*, in elements) of 0 stands for dense rows; columns are contiguous.
+ *    No alignment beyond the element's own is required.  Strides are below
+ *    2^24 elements, and at least the row's width, so rows do not overlap;
+ *    any number of rows times stride is addressed in 64 bits.
+ *  - Every sum, statistic and state is held in fp32; results are rounded once,
+ *    to the output's type, unless a call says otherwise.  Reductions have a
+ *    fixed order: results are bit-reproducible.  Infinities and NaN go through
+ *    as the formulas have them.
+ *  - n_rows (device int32, may be NULL: all rows) is a row count that only the
+ *    device knows, like *n_nodes above, clamped to [0, rows]: the rows from it
+ *    on are not read, and what a call would write for them is left as it is.
+ *  - work / work_bytes: a device buffer of the caller, of at least the size
+ *    that the operator's ..._work_bytes call gives (else TGM_ESIZE), 16-byte
+ *    aligned (else TGM_EINVAL).  Its content carries nothing from one call to
+ *    the next; calls that may run at the same time (other streams, other
+ *    captured graphs) need a buffer each.  The calls allocate nothing, copy
+ *    nothing to the host, and can be captured into a graph.
+ *  - The calling thread's current device must be the stream's device.
+ *  - Outputs may not overlap inputs or one another unless a call says so.
+ */
+#define TGM_F32 0
+#define TGM_BF16 1
+#define TGM_F16 2
+#define TGM_E4M3 3   /* 8 bits: 4 of exponent, 3 of mantissa, largest value 448, no infinity */
+
+/* Root-mean-square norm with the residual's addition:
+ *   t = x + res (t = x where res is NULL),
+ *   y = t (mean_j t_j^2 + eps)^(-1/2) w.
+ * x, res, total [rows x D] and w [D] have type dtype (f32, bf16 or f16); total
+ * (may be NULL) receives t rounded to it, y is formed from t before that
+ * rounding.  y has type out_dtype: dtype, or TGM_E4M3 with one scale a row
+ * (scale [rows] fp32, NULL for the other types):
+ *   scale = max(max_j |y_j| / 448, 2^-126), stored y = y / scale to the nearest
+ *   8-bit value (ties to even).  The maximum passes over NaN; a row with an
+ *   infinite y has an infinite scale, and NaN or 0 for values.
+ * total may be x or res, and y (of out_dtype == dtype) may be x or res unless
+ * total is that one, each with the same stride.  1 <= D <= 32768.
+ * Errors: TGM_EINVAL (null, sizes, types, strides, eps negative or NaN). */
+typedef struct {
+    int32_t rows, D;
+    int32_t dtype, out_dtype;
+    float eps;
+    int64_t ld_x, ld_res, ld_total, ld_y;
+} tgm_norm_desc;
+tgm_status_t tgm_norm(const tgm_norm_desc *d, const void *x, const void *res, const void *w,
+                      const int32_t *n_rows, void *total, void *y, float *scale, void *stream);
+
+/* Gradients of tgm_norm's y (before any rounding to 8 bits) in t and w, from t
+ * as stored (x, or total), with q = (mean t^2 + eps)^(-1/2):
+ *   dx = q (w dy - t q^2 mean_j(w_j dy_j t_j)) + dtotal,  dw = sum_rows dy t q.
+ * dx is the gradient in x and in res alike; dtotal (may be NULL) the gradient
+ * that reaches t by the residual stream.  All of type dtype; d's strides are
+ * ld_x of t, ld_y of dy, ld_res of dtotal, ld_total of dx; out_dtype is not
+ * read.  dx may be dy, dtotal or t, with the same stride.  dw [D] (may be
+ * NULL) is zero where there are no rows.  work as tgm_norm_work_bytes gives.
+ * Errors: TGM_EINVAL, TGM_ESIZE (work). */
+tgm_status_t tgm_norm_work_bytes(int32_t rows, int32_t D, size_t *bytes);
+tgm_status_t tgm_norm_backward(const tgm_norm_desc *d, const void *t, const void *w,
+                               const void *dy, const void *dtotal, const int32_t *n_rows,
+                               void *dx, void *dw, void *work, size_t work_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * Per-kernel timing.  When enabled, every kernel the library launches is
  * bracketed by two HIP events recorded on its own stream; tgm_profile_get
  * synchronises those events and reports, per kernel name, the number of

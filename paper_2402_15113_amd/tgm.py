@@ -35,6 +35,7 @@ SYMBOLS = ["tgm_status_str", "tgm_last_device_error", "tgm_version", "tgm_alloc_
            "tgm_apan_reset", "tgm_apan_load",
            "tgm_apan_read", "tgm_apan_fetched",
            "tgm_embed_projection",
+           "tgm_norm", "tgm_norm_work_bytes", "tgm_norm_backward",
            "tgm_profile_enable", "tgm_profile_reset", "tgm_profile_count", "tgm_profile_get"]
 
 
@@ -93,6 +94,14 @@ class Optimizer(C.Structure):
 TGM_OPT_SGD, TGM_OPT_ADAM = 0, 1
 OPTIMIZERS = {"sgd": TGM_OPT_SGD, "adam": TGM_OPT_ADAM}
 N_PARAM_TENSORS = 17   # TGM_N_PARAM_TENSORS
+
+class NormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32),
+                ("out_dtype", C.c_int32), ("eps", C.c_float), ("ld_x", C.c_int64),
+                ("ld_res", C.c_int64), ("ld_total", C.c_int64), ("ld_y", C.c_int64)]
+
+
+TGM_F32, TGM_BF16, TGM_F16, TGM_E4M3 = 0, 1, 2, 3
 
 _lib = None
 V, I32, I64, P = C.c_void_p, C.c_int32, C.c_int64, C.c_void_p
@@ -162,6 +171,9 @@ def lib():
             "tgm_state_set_mitigation": [V, V, C.c_double, C.c_float],
             "tgm_min_staleness": [P, I64, I32, P, P, P, P, P],
             "tgm_embed_projection": [V, I32, P, P, P, P, P, I32, P, V],
+            "tgm_norm": [C.POINTER(NormDesc), P, P, P, P, P, P, P, V],
+            "tgm_norm_work_bytes": [I32, I32, C.POINTER(C.c_size_t)],
+            "tgm_norm_backward": [C.POINTER(NormDesc), P, P, P, P, P, P, P, P, C.c_size_t, V],
         }
         sig["tgm_profile_enable"] = [I32]
         sig["tgm_profile_reset"] = []
@@ -574,3 +586,119 @@ def tgm_embed(m, g, R, nb, root_pos, root_ts, nbr_pos, eid, nts, cnt, mem_new, n
     _check("tgm_embed", lib().tgm_embed(m, g, R, nb, _p(root_pos), _p(root_ts), _p(nbr_pos),
                                         _p(eid), _p(nts), _p(cnt), _p(mem_new), _p(n_nodes), cap,
                                         _p(h), _s(stream)))
+
+
+# ------------------------------------------------------------------ sequence operators
+def _types():
+    import torch
+    return {torch.float32: TGM_F32, torch.bfloat16: TGM_BF16, torch.float16: TGM_F16,
+            torch.float8_e4m3fn: TGM_E4M3}
+
+
+def dtype_code(dtype) -> int:
+    """TGM_F32, ... of a torch type."""
+    try:
+        return _types()[dtype]
+    except KeyError:
+        raise ValueError(f"no operator takes {dtype}") from None
+
+
+def _arg(name, t, dtype, shape, device, optional=False):
+    """Check a tensor argument and return (pointer, row stride).  The stride is
+    0 where there is no second row for it to lead to."""
+    if t is None:
+        if not optional:
+            raise ValueError(f"{name} is missing")
+        return None, 0
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has type {t.dtype}, not {dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    if t.device != device or device.type != "cuda":
+        raise ValueError(f"{name} is on {t.device}: every tensor of a call is on one GPU")
+    ld = 0
+    if t.dim() == 2 and t.numel():
+        if shape[1] > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name}'s columns are not contiguous")
+        if shape[0] > 1:
+            ld = t.stride(0)
+            if ld < shape[1]:
+                raise ValueError(f"{name}'s rows overlap (stride {ld}, width {shape[1]})")
+    elif t.numel() > 1 and not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+    return C.c_void_p(t.data_ptr()), ld
+
+
+def _work_arg(work, device):
+    import torch
+    if work is None:
+        return None, 0
+    if work.device != device or work.dtype != torch.uint8 or not work.is_contiguous():
+        raise ValueError("work is a contiguous uint8 tensor on the call's GPU")
+    return C.c_void_p(work.data_ptr()), work.numel()
+
+
+def _call(fn, device, stream, *args):
+    """fn(*args, stream) with the tensors' device current."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError(f"{fn}: tensors on {device}; the operators run on a GPU")
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    if s.device != device:
+        raise ValueError(f"{fn}: a stream of {s.device} for tensors on {device}")
+    f = getattr(lib(), fn)
+    if torch.cuda.current_device() == device.index:
+        _check(fn, f(*args, C.c_void_p(s.cuda_stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(fn, f(*args, C.c_void_p(s.cuda_stream)))
+
+
+def _bytes(fn, *args) -> int:
+    n = C.c_size_t(0)
+    _check(fn, getattr(lib(), fn)(*args, C.byref(n)))
+    return int(n.value)
+
+
+def _shape2(name, t):
+    if t is None or t.dim() != 2:
+        raise ValueError(f"{name} is a matrix")
+    return tuple(t.shape)
+
+
+def tgm_norm(x, w, y, eps, res=None, total=None, scale=None, n_rows=None, stream=None):
+    """y = t / rms(t) * w with t = x + res; ``y`` of x's type, or float8_e4m3fn
+    with ``scale`` [rows] fp32; ``total`` receives t."""
+    import torch
+    rows, D = _shape2("x", x)
+    dev, dt = x.device, x.dtype
+    out = y.dtype if y is not None and y.dtype == torch.float8_e4m3fn else dt
+    px, lx = _arg("x", x, dt, (rows, D), dev)
+    pr, lr = _arg("res", res, dt, (rows, D), dev, optional=True)
+    pw, _ = _arg("w", w, dt, (D,), dev)
+    pt, lt = _arg("total", total, dt, (rows, D), dev, optional=True)
+    py, ly = _arg("y", y, out, (rows, D), dev)
+    ps, _ = _arg("scale", scale, torch.float32, (rows,), dev, optional=True)
+    pn, _ = _arg("n_rows", n_rows, torch.int32, (1,), dev, optional=True)
+    d = NormDesc(rows, D, dtype_code(dt), dtype_code(out), eps, lx, lr, lt, ly)
+    _call("tgm_norm", dev, stream, C.byref(d), px, pr, pw, pn, pt, py, ps)
+
+
+def tgm_norm_work_bytes(rows, D) -> int:
+    return _bytes("tgm_norm_work_bytes", rows, D)
+
+
+def tgm_norm_backward(t, w, dy, eps, dx, dw, work, dtotal=None, n_rows=None, stream=None):
+    import torch
+    rows, D = _shape2("t", t)
+    dev, dt = t.device, t.dtype
+    px, lx = _arg("t", t, dt, (rows, D), dev)
+    pw, _ = _arg("w", w, dt, (D,), dev)
+    py, ly = _arg("dy", dy, dt, (rows, D), dev)
+    pd, ld = _arg("dtotal", dtotal, dt, (rows, D), dev, optional=True)
+    po, lo = _arg("dx", dx, dt, (rows, D), dev)
+    pg, _ = _arg("dw", dw, dt, (D,), dev, optional=True)
+    pn, _ = _arg("n_rows", n_rows, torch.int32, (1,), dev, optional=True)
+    pk, nk = _work_arg(work, dev)
+    d = NormDesc(rows, D, dtype_code(dt), dtype_code(dt), eps, lx, ld, lo, ly)
+    _call("tgm_norm_backward", dev, stream, C.byref(d), px, pw, py, pd, pn, po, pg, pk, nk)
