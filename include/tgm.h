@@ -700,6 +700,70 @@ tgm_status_t tgm_norm_backward(const tgm_norm_desc *d, const void *t, const void
                                const void *dy, const void *dtotal, const int32_t *n_rows,
                                void *dx, void *dw, void *work, size_t work_bytes, void *stream);
 
+/* Gated linear recurrence along sequences (histories) of rows:
+ *   a_t = sigmoid(g_t),  h_t = a_t h_(t-1) + (1 - a_t) x_t,  y_t = h_t,
+ * channel by channel, from h_(before the first row) = h0 (zero where h0 is
+ * NULL): the update gate and the candidate of the GRU above, with a gate that
+ * does not read the state, so that a history runs as a scan.
+ *
+ * g, x, y [rows x D] have type dtype (f32, bf16 or f16); h0 and h_last [S x D]
+ * (dense fp32; h_last may be NULL) are the states that sequence s starts from
+ * and ends with (h0's for a sequence without rows).  The sequences are
+ *   packed: offsets [S + 1] int64, not decreasing, within [0, rows]: sequence s
+ *     is the rows offsets[s] .. offsets[s + 1] - 1 (max(0, len[s]) of them at
+ *     most where length [S] int32 is given);
+ *   padded: offsets NULL, rows divisible by S: with L = rows / S, rows s L ..
+ *     s L + L - 1 (the first min(L, max(0, length[s])) of them where length is
+ *     given, as tgm_sample's cnt for its [R x nb] outputs).
+ * Rows of no sequence are not read and their y is left as it is.  (Offsets that
+ * decrease or leave the range give unspecified values, never an access out of
+ * range.)  reverse != 0 runs every sequence from its last row to its first, as
+ * sampled neighbours need, which lie newest first.
+ * carry (may be NULL) [tgm_scan_carry_rows x D] fp32 receives the states inside
+ * the sequences that tgm_scan_backward starts from.
+ * y may be g or x, with the same stride.  rows < 2^31, D <= 65536.
+ * Errors: TGM_EINVAL (null, sizes, types, strides, S < 0, S = 0 with rows in
+ * the padded form or rows not divisible by it), TGM_ESIZE (work). */
+typedef struct {
+    int64_t rows;
+    int32_t S, D;
+    int32_t dtype, reverse;
+    int64_t ld_g, ld_x, ld_y;       /* y; in tgm_scan_backward dy */
+    int64_t ld_dg, ld_dx;           /* tgm_scan_backward only */
+} tgm_scan_desc;
+/* packed: 1 for sequences by offsets, 0 for padded ones. */
+tgm_status_t tgm_scan_carry_rows(int64_t rows, int32_t S, int32_t packed, int64_t *n);
+/* Enough for the calls of both forms. */
+tgm_status_t tgm_scan_work_bytes(int64_t rows, int32_t D, int32_t S, size_t *bytes);
+tgm_status_t tgm_scan(const tgm_scan_desc *d, const void *g, const void *x,
+                      const int64_t *offsets, const int32_t *length, const float *h0, void *y,
+                      float *h_last, float *carry, void *work, size_t work_bytes, void *stream);
+
+/* Gradients of tgm_scan in g, x and h0, from dy [rows x D] of type dtype and
+ * dh_last [S x D] (fp32, may be NULL: zero), with the forward call's desc,
+ * inputs, sequences and carry (which hold the states' values; y is not read):
+ *   e_t = dy_t + a_(t+1) e_(t+1)  (dh_last for the second term at the last row),
+ *   dx_t = (1 - a_t) e_t,  dg_t = (h_(t-1) - x_t) a_t (1 - a_t) e_t,
+ *   dh0 = a_1 e_1  (dh_last for a sequence without rows).
+ * dg, dx [rows x D] of type dtype (rows of no sequence are left as they are),
+ * dh0 [S x D] fp32 (may be NULL).  dg and dx may be dy, g or x (each another
+ * one), with the same stride.  Errors as tgm_scan. */
+tgm_status_t tgm_scan_backward(const tgm_scan_desc *d, const void *g, const void *x,
+                               const int64_t *offsets, const int32_t *length, const float *h0,
+                               const float *carry, const void *dy, const float *dh_last, void *dg,
+                               void *dx, float *dh0, void *work, size_t work_bytes, void *stream);
+
+/* One row for each of n = d->rows sequences whose states are rows of a table
+ * (node states): with h = state[slots[p]] (row p where slots is NULL),
+ *   h <- a h + (1 - a) x,  y[p] = h, state[slots[p]] = h,  a = sigmoid(g[p]),
+ * for the rows p < *n_rows.  state [d->S x D] dense fp32, updated in place;
+ * slots [n] int32 are distinct among the rows in use; a slot outside
+ * [0, S) stands for a state of zeros that is not kept.  y may be NULL, or g or
+ * x with the same stride.  reverse is not read. */
+tgm_status_t tgm_scan_step(const tgm_scan_desc *d, const void *g, const void *x,
+                           const int32_t *slots, const int32_t *n_rows, float *state, void *y,
+                           void *stream);
+
 /* ------------------------------------------------------------------------
  * Per-kernel timing.  When enabled, every kernel the library launches is
  * bracketed by two HIP events recorded on its own stream; tgm_profile_get

@@ -36,6 +36,8 @@ SYMBOLS = ["tgm_status_str", "tgm_last_device_error", "tgm_version", "tgm_alloc_
            "tgm_apan_read", "tgm_apan_fetched",
            "tgm_embed_projection",
            "tgm_norm", "tgm_norm_work_bytes", "tgm_norm_backward",
+           "tgm_scan", "tgm_scan_carry_rows", "tgm_scan_work_bytes", "tgm_scan_backward",
+           "tgm_scan_step",
            "tgm_profile_enable", "tgm_profile_reset", "tgm_profile_count", "tgm_profile_get"]
 
 
@@ -99,6 +101,12 @@ class NormDesc(C.Structure):
     _fields_ = [("rows", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32),
                 ("out_dtype", C.c_int32), ("eps", C.c_float), ("ld_x", C.c_int64),
                 ("ld_res", C.c_int64), ("ld_total", C.c_int64), ("ld_y", C.c_int64)]
+
+
+class ScanDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("S", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32),
+                ("reverse", C.c_int32), ("ld_g", C.c_int64), ("ld_x", C.c_int64),
+                ("ld_y", C.c_int64), ("ld_dg", C.c_int64), ("ld_dx", C.c_int64)]
 
 
 TGM_F32, TGM_BF16, TGM_F16, TGM_E4M3 = 0, 1, 2, 3
@@ -171,6 +179,12 @@ def lib():
             "tgm_state_set_mitigation": [V, V, C.c_double, C.c_float],
             "tgm_min_staleness": [P, I64, I32, P, P, P, P, P],
             "tgm_embed_projection": [V, I32, P, P, P, P, P, I32, P, V],
+            "tgm_scan": [C.POINTER(ScanDesc), P, P, P, P, P, P, P, P, P, C.c_size_t, V],
+            "tgm_scan_carry_rows": [I64, I32, I32, C.POINTER(I64)],
+            "tgm_scan_work_bytes": [I64, I32, I32, C.POINTER(C.c_size_t)],
+            "tgm_scan_backward": [C.POINTER(ScanDesc), P, P, P, P, P, P, P, P, P, P, P, P,
+                                  C.c_size_t, V],
+            "tgm_scan_step": [C.POINTER(ScanDesc), P, P, P, P, P, P, V],
             "tgm_norm": [C.POINTER(NormDesc), P, P, P, P, P, P, P, V],
             "tgm_norm_work_bytes": [I32, I32, C.POINTER(C.c_size_t)],
             "tgm_norm_backward": [C.POINTER(NormDesc), P, P, P, P, P, P, P, P, C.c_size_t, V],
@@ -702,3 +716,85 @@ def tgm_norm_backward(t, w, dy, eps, dx, dw, work, dtotal=None, n_rows=None, str
     pk, nk = _work_arg(work, dev)
     d = NormDesc(rows, D, dtype_code(dt), dtype_code(dt), eps, lx, ld, lo, ly)
     _call("tgm_norm_backward", dev, stream, C.byref(d), px, pw, py, pd, pn, po, pg, pk, nk)
+
+
+def tgm_scan_carry_rows(rows, S, packed) -> int:
+    n = I64()
+    _check("tgm_scan_carry_rows", lib().tgm_scan_carry_rows(rows, S, 1 if packed else 0,
+                                                            C.byref(n)))
+    return int(n.value)
+
+
+def tgm_scan_work_bytes(rows, D, S) -> int:
+    return _bytes("tgm_scan_work_bytes", rows, D, S)
+
+
+def _scan_args(g, x, S, offsets, length, h0):
+    import torch
+    rows, D = _shape2("g", g)
+    dev, dt = g.device, g.dtype
+    pg, lg = _arg("g", g, dt, (rows, D), dev)
+    px, lx = _arg("x", x, dt, (rows, D), dev)
+    po, _ = _arg("offsets", offsets, torch.int64, (S + 1,), dev, optional=True)
+    pl, _ = _arg("length", length, torch.int32, (S,), dev, optional=True)
+    ph, _ = _arg("h0", _dense("h0", h0), torch.float32, (S, D), dev, optional=True)
+    return rows, D, dev, dt, pg, lg, px, lx, po, pl, ph
+
+
+def _dense(name, t):
+    if t is not None and not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+    return t
+
+
+def tgm_scan(g, x, y, S, work, offsets=None, length=None, h0=None, h_last=None, carry=None,
+             reverse=False, stream=None):
+    """h_t = a_t h_(t-1) + (1 - a_t) x_t, a = sigmoid(g), along S sequences:
+    packed by ``offsets`` [S + 1], or padded (rows / S rows each)."""
+    import torch
+    rows, D, dev, dt, pg, lg, px, lx, po, pl, ph = _scan_args(g, x, S, offsets, length, h0)
+    py, ly = _arg("y", y, dt, (rows, D), dev)
+    pe, _ = _arg("h_last", _dense("h_last", h_last), torch.float32, (S, D), dev, optional=True)
+    pc = None
+    if carry is not None:
+        n = tgm_scan_carry_rows(rows, S, offsets is not None)
+        pc, _ = _arg("carry", _dense("carry", carry), torch.float32, (n, D), dev)
+    pk, nk = _work_arg(work, dev)
+    d = ScanDesc(rows, S, D, dtype_code(dt), 1 if reverse else 0, lg, lx, ly, 0, 0)
+    _call("tgm_scan", dev, stream, C.byref(d), pg, px, po, pl, ph, py, pe, pc, pk, nk)
+
+
+def tgm_scan_backward(g, x, dy, carry, dg, dx, S, work, offsets=None, length=None, h0=None,
+                      dh_last=None, dh0=None, reverse=False, stream=None):
+    """Gradients of tgm_scan with the same inputs, sequences and the ``carry``
+    that it left."""
+    import torch
+    rows, D, dev, dt, pg, lg, px, lx, po, pl, ph = _scan_args(g, x, S, offsets, length, h0)
+    n = tgm_scan_carry_rows(rows, S, offsets is not None)
+    pc, _ = _arg("carry", _dense("carry", carry), torch.float32, (n, D), dev)
+    py, ly = _arg("dy", dy, dt, (rows, D), dev)
+    pe, _ = _arg("dh_last", _dense("dh_last", dh_last), torch.float32, (S, D), dev, optional=True)
+    pdg, ldg = _arg("dg", dg, dt, (rows, D), dev)
+    pdx, ldx = _arg("dx", dx, dt, (rows, D), dev)
+    p0, _ = _arg("dh0", _dense("dh0", dh0), torch.float32, (S, D), dev, optional=True)
+    pk, nk = _work_arg(work, dev)
+    d = ScanDesc(rows, S, D, dtype_code(dt), 1 if reverse else 0, lg, lx, ly, ldg, ldx)
+    _call("tgm_scan_backward", dev, stream, C.byref(d), pg, px, po, pl, ph, pc, py, pe, pdg, pdx,
+          p0, pk, nk)
+
+
+def tgm_scan_step(g, x, state, y, slots=None, n_rows=None, stream=None):
+    """One row of the scan for each row of g and x, into ``state`` [slots x D]
+    in place."""
+    import torch
+    rows, D = _shape2("g", g)
+    dev, dt = g.device, g.dtype
+    S, _ = _shape2("state", state)
+    pg, lg = _arg("g", g, dt, (rows, D), dev)
+    px, lx = _arg("x", x, dt, (rows, D), dev)
+    ps, _ = _arg("state", _dense("state", state), torch.float32, (S, D), dev)
+    py, ly = _arg("y", y, dt, (rows, D), dev, optional=True)
+    pt, _ = _arg("slots", slots, torch.int32, (rows,), dev, optional=True)
+    pn, _ = _arg("n_rows", n_rows, torch.int32, (1,), dev, optional=True)
+    d = ScanDesc(rows, S, D, dtype_code(dt), 0, lg, lx, ly, 0, 0)
+    _call("tgm_scan_step", dev, stream, C.byref(d), pg, px, pt, pn, ps, py)

@@ -63,3 +63,60 @@ def norm_grads(t, w, dy, eps, dtotal=None):
     if dtotal is not None:
         dx, sx = dx + dtotal, sx + dtotal.abs()
     return dx, (dy * t * q).sum(0), sx, (dy * t * q).abs().sum(0)
+
+
+# ------------------------------------------------------------------- scan
+def scan(g, x, begin, end, h0=None, reverse=False, dy=None, dh_last=None):
+    """Row by row.  ``begin``, ``end``: the rows of each sequence.  Returns a
+    dict of results, and under "err_" the fp32 error that they may have: every
+    step's own roundings (GATE for each gate, one for each operation), carried
+    along by the gates as the states are."""
+    g, x, h0, dy, dh_last = cpu64(g, x, h0, dy, dh_last)
+    S, (R, D) = len(begin), g.shape
+    h0 = torch.zeros(S, D, dtype=F64) if h0 is None else h0
+    a = torch.sigmoid(g)
+    i = torch.sigmoid(-g)
+    # a gate's error in units of U: exp's argument (|g| log2 e) rounded, exp, 1 + e, the
+    # reciprocal (1 step), a product
+    gate = U * (g.abs().nan_to_num(0, 0, 0).clamp(max=90) + 8)
+    out = {k: torch.full((R, D), float("nan"), dtype=F64) for k in ("y", "dg", "dx")}
+    err = {k: torch.zeros(R, D, dtype=F64) for k in ("y", "dg", "dx")}
+    out["h_last"], err["h_last"] = h0.clone(), torch.zeros(S, D, dtype=F64)
+    before = torch.zeros(R, D, dtype=F64)
+    err_before = torch.zeros(R, D, dtype=F64)
+    inside = torch.zeros(R, dtype=torch.bool)
+    for s in range(S):
+        rows = list(range(begin[s], end[s]))
+        rows = rows[::-1] if reverse else rows
+        h, e = h0[s], torch.zeros(D, dtype=F64)
+        for t in rows:
+            inside[t] = True
+            before[t], err_before[t] = h, e
+            # the state may also come by the tile's map (P, Q): as many roundings again
+            e = a[t] * e + (gate[t] + 6 * U) * ((a[t] * h).abs() + (i[t] * x[t]).abs())
+            h = a[t] * h + i[t] * x[t]
+            out["y"][t], err["y"][t] = h, 2 * e
+        out["h_last"][s], err["h_last"][s] = h, 2 * e
+    out["inside"] = inside
+    if dy is None:
+        return out, err
+    dh_last = torch.zeros(S, D, dtype=F64) if dh_last is None else dh_last
+    out["dh0"], err["dh0"] = dh_last.clone(), torch.zeros(S, D, dtype=F64)
+    for s in range(S):
+        rows = list(range(begin[s], end[s]))
+        rows = rows if reverse else rows[::-1]
+        c, e = dh_last[s], torch.zeros(D, dtype=F64)
+        for t in rows:
+            v = dy[t] + c
+            e = e + 2 * U * (dy[t].abs() + c.abs())
+            out["dx"][t] = i[t] * v
+            err["dx"][t] = 2 * (i[t] * e + gate[t] * (i[t] * v).abs())
+            d = before[t] - x[t]
+            out["dg"][t] = v * a[t] * i[t] * d
+            err["dg"][t] = 2 * a[t] * i[t] * (
+                e * d.abs() + v.abs() * (2 * err_before[t] + (2 * gate[t] + 4 * U) *
+                                         (before[t].abs() + x[t].abs())))
+            c = a[t] * v
+            e = a[t] * e + (gate[t] + 4 * U) * c.abs()
+        out["dh0"][s], err["dh0"][s] = c, 2 * e
+    return out, err

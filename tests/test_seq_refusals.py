@@ -68,6 +68,69 @@ def test_norm_backward_work(L):
                                None) == tgm.TGM_EINVAL
 
 
+def scan_desc(**kw):
+    d = dict(rows=96, S=3, D=64, dtype=tgm.TGM_BF16, reverse=0, ld_g=0, ld_x=0, ld_y=0, ld_dg=0,
+             ld_dx=0)
+    d.update(kw)
+    return C.byref(tgm.ScanDesc(*[d[n] for n, _ in tgm.ScanDesc._fields_]))
+
+
+BAD_SCAN = [dict(rows=-1), dict(rows=1 << 31), dict(S=-1), dict(D=0), dict(D=65537),
+            dict(dtype=3), dict(dtype=-1), dict(ld_g=63), dict(ld_x=-64), dict(ld_y=1 << 24)]
+
+
+@pytest.mark.parametrize("off", [None, X])
+@pytest.mark.parametrize("bad", BAD_SCAN + [dict(ld_dg=1), dict(ld_dx=-1)])
+def test_scan_sizes(L, bad, off):
+    E = tgm.TGM_EINVAL
+    assert L.tgm_scan(scan_desc(**bad), X, X, off, X, X, X, X, X, X, BIG, None) == E
+    assert L.tgm_scan_backward(scan_desc(**bad), X, X, off, X, X, X, X, X, X, X, X, X, BIG,
+                               None) == E
+
+
+def test_scan_pointers_and_work(L):
+    E = tgm.TGM_EINVAL
+    ok = [scan_desc(), X, X, X, None, None, X, None, None, X, BIG, None]
+    for k in (0, 1, 2, 6, 9):
+        assert L.tgm_scan(*[None if j == k else v for j, v in enumerate(ok)]) == E, k
+    assert L.tgm_scan(*ok[:9], X + 8, BIG, None) == E
+    assert L.tgm_scan(*ok[:9], X, 3 * 64 * 12 - 1, None) == tgm.TGM_ESIZE
+    back = [scan_desc(), X, X, X, None, None, X, X, None, X, X, None, X, BIG, None]
+    for k in (0, 1, 2, 6, 7, 9, 10, 12):
+        assert L.tgm_scan_backward(*[None if j == k else v for j, v in enumerate(back)]) == E, k
+    assert L.tgm_scan_backward(*back[:12], X, 10, None) == tgm.TGM_ESIZE
+    # padded sequences divide the rows
+    for bad in (dict(rows=97), dict(S=0)):
+        assert L.tgm_scan(scan_desc(**bad), X, X, None, None, None, X, None, None, X, BIG,
+                          None) == E
+
+
+def test_scan_sizes_of_buffers():
+    assert tgm.tgm_scan_carry_rows(100, 7, True) == 4
+    assert tgm.tgm_scan_carry_rows(0, 0, True) == 0
+    assert tgm.tgm_scan_carry_rows(200, 2, False) == 8     # 100 rows: 4 tiles each
+    assert tgm.tgm_scan_carry_rows(70, 7, False) == 3      # 10 rows: 3 sequences a tile
+    for bad in ((-1, 1, True), (10, 3, False), (1 << 31, 1, True), (5, 0, False), (5, -1, True)):
+        with pytest.raises(tgm.TgmError):
+            tgm.tgm_scan_carry_rows(*bad)
+    with pytest.raises(tgm.TgmError):
+        tgm.tgm_scan_work_bytes(10, 0, 1)
+    assert tgm.lib().tgm_scan_carry_rows(5, 1, 1, None) == tgm.TGM_EINVAL
+    assert tgm.lib().tgm_scan_work_bytes(5, 1, 1, None) == tgm.TGM_EINVAL
+
+
+@pytest.mark.parametrize("bad", BAD_SCAN)
+def test_scan_step_sizes(L, bad):
+    assert L.tgm_scan_step(scan_desc(**bad), X, X, X, X, X, X, None) == tgm.TGM_EINVAL
+
+
+def test_scan_step_pointers(L):
+    ok = [scan_desc(), X, X, None, None, X, X, None]
+    for k in (0, 1, 2, 5):
+        assert L.tgm_scan_step(*[None if j == k else v
+                                 for j, v in enumerate(ok)]) == tgm.TGM_EINVAL, k
+
+
 def test_binding_checks_tensors():
     x, w = torch.zeros(4, 8), torch.ones(8)
     with pytest.raises(ValueError, match="GPU"):
