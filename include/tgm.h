@@ -700,6 +700,48 @@ tgm_status_t tgm_norm_backward(const tgm_norm_desc *d, const void *t, const void
                                const void *dy, const void *dtotal, const int32_t *n_rows,
                                void *dx, void *dw, void *work, size_t work_bytes, void *stream);
 
+/* Matrix product with bias, activation and residual in one pass over its output:
+ *   z = x W^T + bias,  y = act(z) + res,  x [rows x K], W [N x K], y [rows x N].
+ * dtype f32, bf16 or f16: every matrix and bias [N] has that type (out_dtype ==
+ * dtype; scale_x, scale_w NULL).  dtype TGM_E4M3: x and W hold 8-bit values with
+ * a scale a row (scale_x [rows], scale_w [N] fp32, as tgm_norm writes them), z =
+ * scale_x_r scale_w_n (x W^T)_rn + bias_n, and bias, res, z, y have out_dtype
+ * (f32, bf16 or f16).  bias, res may be NULL (zero); z (may be NULL) receives the
+ * pre-activation for tgm_linear_backward.  y may be res, with the same stride.
+ * Products are exact and added in fp32; those of 8-bit values, for a 16-bit
+ * result, by the 8-bit matrix instructions, which first add 8 neighbouring
+ * columns' products aligned to the largest one and cut below 2^-13 of it.
+ * 1 <= N, K <= 2^20.
+ * Errors: TGM_EINVAL (null, sizes, types, strides, scales), TGM_ESIZE (work). */
+#define TGM_ACT_NONE 0
+#define TGM_ACT_RELU 1   /* max(z, 0) */
+#define TGM_ACT_SILU 2   /* z sigmoid(z) */
+#define TGM_ACT_GELU 3   /* z (1 + erf(z / sqrt 2)) / 2 */
+typedef struct {
+    int32_t rows, N, K;
+    int32_t dtype, out_dtype, act;
+    int64_t ld_x, ld_w, ld_res, ld_z, ld_y;
+    int64_t ld_dx, ld_dw;   /* tgm_linear_backward only */
+} tgm_linear_desc;
+/* For tgm_linear (backward 0) and tgm_linear_backward (1). */
+tgm_status_t tgm_linear_work_bytes(int32_t rows, int32_t N, int32_t K, int32_t dtype,
+                                   int32_t act, int32_t backward, size_t *bytes);
+tgm_status_t tgm_linear(const tgm_linear_desc *d, const void *x, const float *scale_x,
+                        const void *W, const float *scale_w, const void *bias, const void *res,
+                        const int32_t *n_rows, void *z, void *y, void *work, size_t work_bytes,
+                        void *stream);
+
+/* Gradients of tgm_linear's y in x, W and bias (the one in res is dy), for dtype
+ * f32, bf16 or f16, from dy [rows x N] (stride ld_y) and, unless act is none, z
+ * as the forward call wrote it:
+ *   dz = dy act'(z),  dx = dz W,  dW = dz^T x,  db = sum_rows dz.
+ * dx [rows x K], dW [N x K], db [N]; each may be NULL.  act' of ReLU is 0 at 0.
+ * dz is rounded to dtype for the products, which take operands of that type;
+ * db adds it unrounded.  With no rows dW and db are zero. */
+tgm_status_t tgm_linear_backward(const tgm_linear_desc *d, const void *x, const void *W,
+                                 const void *z, const void *dy, const int32_t *n_rows, void *dx,
+                                 void *dW, void *db, void *work, size_t work_bytes, void *stream);
+
 /* Gated linear recurrence along sequences (histories) of rows:
  *   a_t = sigmoid(g_t),  h_t = a_t h_(t-1) + (1 - a_t) x_t,  y_t = h_t,
  * channel by channel, from h_(before the first row) = h0 (zero where h0 is

@@ -36,6 +36,7 @@ SYMBOLS = ["tgm_status_str", "tgm_last_device_error", "tgm_version", "tgm_alloc_
            "tgm_apan_read", "tgm_apan_fetched",
            "tgm_embed_projection",
            "tgm_norm", "tgm_norm_work_bytes", "tgm_norm_backward",
+           "tgm_linear", "tgm_linear_work_bytes", "tgm_linear_backward",
            "tgm_scan", "tgm_scan_carry_rows", "tgm_scan_work_bytes", "tgm_scan_backward",
            "tgm_scan_step",
            "tgm_profile_enable", "tgm_profile_reset", "tgm_profile_count", "tgm_profile_get"]
@@ -103,6 +104,13 @@ class NormDesc(C.Structure):
                 ("ld_res", C.c_int64), ("ld_total", C.c_int64), ("ld_y", C.c_int64)]
 
 
+class LinearDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("dtype", C.c_int32),
+                ("out_dtype", C.c_int32), ("act", C.c_int32), ("ld_x", C.c_int64),
+                ("ld_w", C.c_int64), ("ld_res", C.c_int64), ("ld_z", C.c_int64),
+                ("ld_y", C.c_int64), ("ld_dx", C.c_int64), ("ld_dw", C.c_int64)]
+
+
 class ScanDesc(C.Structure):
     _fields_ = [("rows", C.c_int64), ("S", C.c_int32), ("D", C.c_int32), ("dtype", C.c_int32),
                 ("reverse", C.c_int32), ("ld_g", C.c_int64), ("ld_x", C.c_int64),
@@ -110,6 +118,8 @@ class ScanDesc(C.Structure):
 
 
 TGM_F32, TGM_BF16, TGM_F16, TGM_E4M3 = 0, 1, 2, 3
+TGM_ACT_NONE, TGM_ACT_RELU, TGM_ACT_SILU, TGM_ACT_GELU = 0, 1, 2, 3
+ACTS = {"none": TGM_ACT_NONE, "relu": TGM_ACT_RELU, "silu": TGM_ACT_SILU, "gelu": TGM_ACT_GELU}
 
 _lib = None
 V, I32, I64, P = C.c_void_p, C.c_int32, C.c_int64, C.c_void_p
@@ -179,6 +189,10 @@ def lib():
             "tgm_state_set_mitigation": [V, V, C.c_double, C.c_float],
             "tgm_min_staleness": [P, I64, I32, P, P, P, P, P],
             "tgm_embed_projection": [V, I32, P, P, P, P, P, I32, P, V],
+            "tgm_linear_work_bytes": [I32, I32, I32, I32, I32, I32, C.POINTER(C.c_size_t)],
+            "tgm_linear": [C.POINTER(LinearDesc), P, P, P, P, P, P, P, P, P, P, C.c_size_t, V],
+            "tgm_linear_backward": [C.POINTER(LinearDesc), P, P, P, P, P, P, P, P, P,
+                                    C.c_size_t, V],
             "tgm_scan": [C.POINTER(ScanDesc), P, P, P, P, P, P, P, P, P, C.c_size_t, V],
             "tgm_scan_carry_rows": [I64, I32, I32, C.POINTER(I64)],
             "tgm_scan_work_bytes": [I64, I32, I32, C.POINTER(C.c_size_t)],
@@ -716,6 +730,61 @@ def tgm_norm_backward(t, w, dy, eps, dx, dw, work, dtotal=None, n_rows=None, str
     pk, nk = _work_arg(work, dev)
     d = NormDesc(rows, D, dtype_code(dt), dtype_code(dt), eps, lx, ld, lo, ly)
     _call("tgm_norm_backward", dev, stream, C.byref(d), px, pw, py, pd, pn, po, pg, pk, nk)
+
+
+def _act(name) -> int:
+    if name not in ACTS:
+        raise ValueError(f"act is one of {sorted(ACTS)}, not {name!r}")
+    return ACTS[name]
+
+
+def tgm_linear_work_bytes(rows, N, K, dtype, act="none", backward=False) -> int:
+    return _bytes("tgm_linear_work_bytes", rows, N, K, dtype_code(dtype), _act(act),
+                  1 if backward else 0)
+
+
+def tgm_linear(x, w, y, work, act="none", bias=None, residual=None, z=None, scale_x=None,
+               scale_w=None, n_rows=None, stream=None):
+    """y = act(x w^T + bias) + residual; float8_e4m3fn x and w with ``scale_x``
+    [rows] and ``scale_w`` [N]; ``z`` receives the pre-activation."""
+    import torch
+    (rows, K), (N, _), out = _shape2("x", x), _shape2("w", w), None if y is None else y.dtype
+    dev, dt = x.device, x.dtype
+    px, lx = _arg("x", x, dt, (rows, K), dev)
+    pw, lw = _arg("w", w, dt, (N, K), dev)
+    psx, _ = _arg("scale_x", scale_x, torch.float32, (rows,), dev, optional=True)
+    psw, _ = _arg("scale_w", scale_w, torch.float32, (N,), dev, optional=True)
+    pb, _ = _arg("bias", bias, out, (N,), dev, optional=True)
+    pr, lr = _arg("residual", residual, out, (rows, N), dev, optional=True)
+    pz, lz = _arg("z", z, out, (rows, N), dev, optional=True)
+    py, ly = _arg("y", y, out, (rows, N), dev)
+    pn, _ = _arg("n_rows", n_rows, torch.int32, (1,), dev, optional=True)
+    pk, nk = _work_arg(work, dev)
+    d = LinearDesc(rows, N, K, dtype_code(dt), dtype_code(out), _act(act), lx, lw, lr, lz, ly, 0,
+                   0)
+    _call("tgm_linear", dev, stream, C.byref(d), px, psx, pw, psw, pb, pr, pn, pz, py, pk, nk)
+
+
+def tgm_linear_backward(x, w, dy, work, act="none", z=None, dx=None, dw=None, db=None,
+                        n_rows=None, stream=None):
+    """dx, dw and db (each optional) from dy and, unless act is none, the ``z``
+    that tgm_linear wrote."""
+    import torch
+    (rows, K), (N, _) = _shape2("x", x), _shape2("w", w)
+    dev, dt = x.device, x.dtype
+    px, lx = _arg("x", x, dt, (rows, K), dev)
+    pw, lw = _arg("w", w, dt, (N, K), dev)
+    pz, lz = _arg("z", z, dt, (rows, N), dev, optional=True)
+    py, ly = _arg("dy", dy, dt, (rows, N), dev)
+    pdx, ldx = _arg("dx", dx, dt, (rows, K), dev, optional=True)
+    pdw, ldw = _arg("dw", dw, dt, (N, K), dev, optional=True)
+    pdb, _ = _arg("db", db, dt, (N,), dev, optional=True)
+    pn, _ = _arg("n_rows", n_rows, torch.int32, (1,), dev, optional=True)
+    pk, nk = _work_arg(work, dev)
+    d = LinearDesc(rows, N, K, dtype_code(dt), dtype_code(dt), _act(act), lx, lw, 0, lz, ly, ldx,
+                   ldw)
+    _call("tgm_linear_backward", dev, stream, C.byref(d), px, pw, pz, py, pn, pdx, pdw, pdb, pk,
+          nk)
 
 
 def tgm_scan_carry_rows(rows, S, packed) -> int:

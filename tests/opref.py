@@ -120,3 +120,83 @@ def scan(g, x, begin, end, h0=None, reverse=False, dy=None, dh_last=None):
             e = a[t] * e + (gate[t] + 4 * U) * c.abs()
         out["dh0"][s], err["dh0"][s] = c, 2 * e
     return out, err
+
+
+# ------------------------------------------------------------------- product
+def act(z, name):
+    """(value, derivative, error of either in units of U relative to |z| + 1)."""
+    if name == "relu":
+        return torch.where(z > 0, z, torch.where(torch.isnan(z), z, 0 * z.nan_to_num(0, 0, 0))), \
+            (z > 0).to(F64)
+    if name == "silu":
+        p = torch.sigmoid(z)
+        return z * p, p * (1 + z * (1 - p))
+    if name == "gelu":
+        c = torch.erfc(-z / 2 ** 0.5) / 2
+        return z * c, c + z * torch.exp(-z * z / 2) / (2 * torch.pi) ** 0.5
+    return z, torch.ones_like(z)
+
+
+# |act'| <= 1.13; fp32 evaluation: exp's argument is rounded ((2 |z| + 8) U of a factor
+# that is at most 1) and 1 + erf cancels (4 U of its scale, times |z|)
+def act_err(z, err_z):
+    return 1.13 * err_z + (2 * z.abs() + 12) * U * z.abs()
+
+
+def act_grad_err(z):
+    return (2 * z.abs() + 12) * U * (1 + z.abs())
+
+
+def cut(x, w):
+    """What the 8-bit matrix instructions may lose of x w^T: they align 8
+    neighbouring products to the largest, whose exponent E they keep 13 binary
+    places of, and cut the rest (read off the instruction: next to 2^14, a
+    product of 2^1 is kept and 1.75 is not, of either sign).  A product of two
+    values of 4 significant bits has 8, so the largest loses nothing, and each of
+    the 7 others less than a unit of 2^(E - 13) <= 2^-13 of the largest."""
+    R, K = x.shape
+    x, w = (torch.nn.functional.pad(v.abs(), (0, -K % 8)).view(v.shape[0], -1, 8) for v in (x, w))
+    lost = torch.zeros(R, w.shape[0], dtype=F64)
+    for g in range(x.shape[1]):
+        lost += (x[:, None, g] * w[None, :, g]).amax(-1)
+    return 7 * 2.0 ** -13 * lost
+
+
+def linear(x, w, name, bias=None, res=None, scale_x=None, scale_w=None, cut8=False):
+    """(z, error of z, y, error of y), before the rounding to the output's type.
+    Sums of K terms and a bias in any order; the scales' products; with cut8
+    what the 8-bit instructions lose."""
+    x, w, bias, res, sx, sw = cpu64(x, w, bias, res, scale_x, scale_w)
+    K = x.shape[1]
+    z, size = x @ w.t(), x.abs() @ w.abs().t()
+    lost = cut(x, w) if cut8 else 0
+    if sx is not None:
+        s = sx[:, None] * sw[None]
+        z, size, lost = z * s, size * s, lost * s
+    if bias is not None:
+        z, size = z + bias, size + bias.abs()
+    ez = (K + 8) * U * size + lost
+    y, _ = act(z, name)
+    ey = act_err(z, ez) if name != "none" else ez
+    if res is not None:
+        y = y + res
+        ey = ey + U * y.abs()
+    return z, ez, y, ey
+
+
+def linear_grads(x, w, dy, name, z=None):
+    """{name: (value, error)} before the rounding to the output's type."""
+    dtype = dy.dtype
+    x, w, dy, z = cpu64(x, w, dy, z)
+    R, N = dy.shape
+    dz, e, exact = dy, torch.zeros_like(dy), torch.zeros_like(dy)
+    if name != "none":
+        g = act(z, name)[1]
+        dz = dy * g
+        exact = dy.abs() * act_grad_err(z)      # before dz's rounding to the operands' type
+        e = exact + rounded(dz.abs() + exact, dtype)
+    out = {}
+    out["dx"] = dz @ w, e @ w.abs() + (N + 8) * U * ((dz.abs() + e) @ w.abs())
+    out["dw"] = dz.t() @ x, e.t() @ x.abs() + (R + 8) * U * ((dz.abs() + e).t() @ x.abs())
+    out["db"] = dz.sum(0), (exact + (R + 8) * U * (dz.abs() + exact)).sum(0)
+    return out

@@ -68,6 +68,63 @@ def test_norm_backward_work(L):
                                None) == tgm.TGM_EINVAL
 
 
+def linear_desc(**kw):
+    d = dict(rows=8, N=32, K=64, dtype=tgm.TGM_BF16, out_dtype=tgm.TGM_BF16, act=0, ld_x=0,
+             ld_w=0, ld_res=0, ld_z=0, ld_y=0, ld_dx=0, ld_dw=0)
+    d.update(kw)
+    return C.byref(tgm.LinearDesc(*[d[n] for n, _ in tgm.LinearDesc._fields_]))
+
+
+BAD_LINEAR = [dict(rows=-1), dict(N=0), dict(K=0), dict(N=(1 << 20) + 1), dict(K=(1 << 20) + 1),
+              dict(act=4), dict(act=-1), dict(dtype=0), dict(out_dtype=2), dict(dtype=5),
+              dict(ld_x=63), dict(ld_w=-64), dict(ld_y=31), dict(ld_z=1 << 24), dict(ld_res=1)]
+
+
+@pytest.mark.parametrize("bad", BAD_LINEAR + [dict(ld_dx=63), dict(ld_dw=1)])
+def test_linear_sizes(L, bad):
+    E = tgm.TGM_EINVAL
+    assert L.tgm_linear(linear_desc(**bad), X, None, X, None, X, X, None, X, X, X, BIG, None) == E
+    assert L.tgm_linear_backward(linear_desc(**bad), X, X, X, X, None, X, X, X, X, BIG, None) == E
+
+
+def test_linear_pointers_and_scales(L):
+    E = tgm.TGM_EINVAL
+    ok = [linear_desc(), X, None, X, None, None, None, None, None, X, X, BIG, None]
+    for k in (0, 1, 3, 9):
+        assert L.tgm_linear(*[None if j == k else v for j, v in enumerate(ok)]) == E, k
+    # scales go with 8 bits, and with nothing else
+    for k in (2, 4):
+        assert L.tgm_linear(*[X if j == k else v for j, v in enumerate(ok)]) == E, k
+    ok[0], ok[2], ok[4] = linear_desc(dtype=tgm.TGM_E4M3), X, X
+    for k in (1, 2, 3, 4, 9):
+        assert L.tgm_linear(*[None if j == k else v for j, v in enumerate(ok)]) == E, k
+    ok[0] = linear_desc(dtype=tgm.TGM_E4M3, out_dtype=tgm.TGM_E4M3)
+    assert L.tgm_linear(*ok) == E
+
+
+def test_linear_backward_pointers_and_work(L):
+    E = tgm.TGM_EINVAL
+    ok = [linear_desc(act=2), X, X, X, X, None, X, X, X, X, BIG, None]
+    for k in (0, 1, 2, 3, 4, 9):
+        assert L.tgm_linear_backward(*[None if j == k else v for j, v in enumerate(ok)]) == E, k
+    assert L.tgm_linear_backward(*ok[:9], X + 2, BIG, None) == E
+    need = tgm.tgm_linear_work_bytes(8, 32, 64, torch.bfloat16, act="silu", backward=True)
+    assert need >= 8 * 32 * 2
+    assert L.tgm_linear_backward(*ok[:10], need - 1, None) == tgm.TGM_ESIZE
+    ok[0] = linear_desc(dtype=tgm.TGM_E4M3, out_dtype=tgm.TGM_E4M3)
+    assert L.tgm_linear_backward(*ok) == E
+
+
+def test_linear_work_bytes():
+    for bad in ((-1, 1, 1, 0, 0, 0), (1, 0, 1, 0, 0, 0), (1, 1, 0, 0, 0, 0), (1, 1, 1, 4, 0, 0),
+                (1, 1, 1, 0, 4, 0), (1, 1, 1, 3, 0, 1)):
+        with pytest.raises(tgm.TgmError):
+            tgm._bytes("tgm_linear_work_bytes", *bad)
+    assert tgm.lib().tgm_linear_work_bytes(1, 1, 1, 0, 0, 0, None) == tgm.TGM_EINVAL
+    with pytest.raises(ValueError, match="act"):
+        tgm.tgm_linear_work_bytes(1, 1, 1, torch.float32, act="tanh")
+
+
 def scan_desc(**kw):
     d = dict(rows=96, S=3, D=64, dtype=tgm.TGM_BF16, reverse=0, ld_g=0, ld_x=0, ld_y=0, ld_dg=0,
              ld_dx=0)
