@@ -2,13 +2,14 @@
 // gradient and its single-row form.
 //
 // h_t = a_t h_(t-1) + (1 - a_t) x_t is an affine map of h_(t-1), so the rows of
-// a tile of 32 compose to h_out = P h_in + Q with P the product of the gates.
-// Three launches: every tile's (P, Q), the state that enters every tile, and
-// the rows themselves.  A wavefront takes one tile and 64 V channels (V
-// neighbouring ones a lane) with all of the tile's loads in flight; the tiles
-// run over the rows as they lie, whatever sequences they belong to, so uneven
-// lengths cost nothing.  Bound by memory: the operator has to read g and x and
-// write y once.
+// a tile of 32 compose to h_out = P h_in + Q with P the product of the gates,
+// and tiles compose likewise.  One pass over the data: a wavefront takes one
+// tile and 64 V channels (V neighbouring ones a lane), a workgroup 8 tiles in a
+// row; rows stay in registers between the tile's map and its states, so g and x
+// are read once and y is written once, which is what bounds the operator.
+// Between workgroups the states go along a chain (below).  The tiles run over
+// the rows as they lie, whatever sequences they belong to, so uneven lengths
+// cost nothing.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -20,7 +21,7 @@ using namespace tgm;
 namespace {
 
 constexpr int kRows = 32;   // rows of a tile
-constexpr int kWaves = 4;   // wavefronts (tiles) of a workgroup
+constexpr int kWaves = 8;   // wavefronts (tiles) of a workgroup
 
 // The sequences, and their rows' division into tiles: packed sequences share
 // tiles of consecutive rows; padded ones have tiles of their own (`chunks` of
@@ -148,111 +149,181 @@ template <int V> __device__ __forceinline__ Lane lane_at(int32_t D, int32_t widt
 
 struct ScanArgs {
     Seqs q;
-    int32_t D, width;
+    int32_t D, width, blocks;   // channels, those of a wavefront, wavefronts for a row
+    int32_t groups;             // workgroups along the rows
     const void *g, *x, *dy;
     const float *h0;      // backward: also the forward's
     const float *last;    // backward: dh_last
     void *y, *dg, *dx;
     float *h_last;        // backward: dh0
-    float *carry;         // states entering the tiles
-    float *agg;           // (P, Q) of the tiles; P = -1: nothing of the state before gets through
-    float *back;          // backward: what is handed back into the tiles
+    float *carry;         // states entering the tiles (may be null in the forward)
+    uint64_t *maps, *states;    // [groups x D]: the chain's words
+    int32_t *ticket;            // [blocks]
     int64_t ld_g, ld_x, ld_y, ld_dg, ld_dx;
 };
 
-__device__ __forceinline__ int64_t tile_index()
+// ---------------------------------------------------------------- the chain
+// A map (P, Q) is one 64-bit word, P in the upper half: a word is written and
+// read whole, so no other ordering is needed.  P = -1 stands for a map that
+// ignores the state before (a sequence begins inside it), all bits set for a
+// word that is not there yet (a computed NaN never has them all set).
+//
+// Workgroups take their places in the rows' order by a counter as they start.
+// The first of each channel block's chain is its runner: it composes the
+// others' maps in order and hands every workgroup the state before its rows,
+// 32 words a load.  A workgroup writes its map without waiting for anyone, and
+// the runner waits only for the lowest place whose map is missing, which a
+// workgroup that has started holds or the next one to start will hold; so
+// every wait ends, however few workgroups run at once.
+constexpr uint64_t kAbsent = ~(uint64_t)0;
+
+__device__ __forceinline__ uint64_t word_of(float P, float Q)
 {
-    return ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kWaves + (threadIdx.x >> 6);
+    const uint32_t p = P != P ? 0x7fc00000u : __float_as_uint(P);
+    return (uint64_t)p << 32 | __float_as_uint(Q);
+}
+__device__ __forceinline__ uint64_t word_load(const uint64_t *p)
+{
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void word_store(uint64_t *p, uint64_t w)
+{
+    __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float upper(uint64_t w) { return __uint_as_float((uint32_t)(w >> 32)); }
+__device__ __forceinline__ float lower(uint64_t w) { return __uint_as_float((uint32_t)w); }
+
+// (P, Q) after (p, q): the map of both.
+__device__ __forceinline__ void compose(float &P, float &Q, float p, float q)
+{
+    Q = p < 0.f ? q : fmaf(p, Q, q);
+    P = p < 0.f || P < 0.f ? -1.f : P * p;
 }
 
-// Tile k's (P, Q) for every channel.  BWD: of the adjoint, whose rows run the
-// other way: c_out = a (dy + c_in).
-template <class T, int V, bool BWD>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_agg(ScanArgs A)
+__device__ void run_chain(const ScanArgs &A, int b)
 {
-    const int64_t k = tile_index();
-    if (k >= A.q.tiles)
+    constexpr int kAhead = 32;
+    const int32_t c0 = b * A.width, c1 = min(A.D, c0 + A.width);
+    const int32_t ch = c0 + (int32_t)threadIdx.x;
+    if ((int)(threadIdx.x & ~63u) + c0 >= c1)   // one wavefront for every 64 channels
         return;
-    const Tile t = tile_at(A.q, k);
-    const Lane c = lane_at<V>(A.D, A.width, blockIdx.z);
-    const T *g = (const T *)A.g + c.ch, *x = (const T *)(BWD ? A.dy : A.x) + c.ch;
-    const int64_t ld_x = BWD ? A.ld_y : A.ld_x;
-    const RowInfo in = rows_of(A.q, t);
-    float P[V], Q[V];
+    const uint64_t *maps = A.maps + min(ch, c1 - 1);
+    uint64_t *states = A.states + min(ch, c1 - 1);
+    float h = 0.f;
+    for (int32_t done = 0; done < A.groups;) {
+        uint64_t w[kAhead];
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        P[v] = 1.f, Q[v] = 0.f;
-    if (in.valid) {
-#pragma unroll 8
-        for (int j = 0; j < kRows; ++j) {
-            const int r = BWD ? kRows - 1 - j : j;
-            if (!((in.valid >> r) & 1))
-                continue;
-            const int64_t p = A.q.rev ? t.p0 - r : t.p0 + r;
-            const Pack<T, V> pg = load_pack<T, V>(g + p * A.ld_g);
-            const Pack<T, V> px = load_pack<T, V>(x + p * ld_x);
-            const int32_t s = __builtin_amdgcn_readlane(in.seq, r);
-            const bool cut = ((BWD ? in.last : in.first) >> r) & 1;
+        for (int i = 0; i < kAhead; ++i)
+            w[i] = word_load(maps + (int64_t)min(done + i, A.groups - 1) * A.D);
+        const int32_t from = done;
+        bool ready = true;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const Gate G = gate_of(to_f32(pg.v[v]));
-                const float u = to_f32(px.v[v]);
-                if (cut) {
-                    const float *from = BWD ? A.last : A.h0;
-                    P[v] = -1.f;
-                    Q[v] = from ? from[(int64_t)s * A.D + c.ch + v] : 0.f;
-                }
-                P[v] = P[v] < 0.f ? -1.f : P[v] * G.a;
-                Q[v] = BWD ? G.a * (u + Q[v]) : fmaf(G.a, Q[v], G.i * u);
+        for (int i = 0; i < kAhead; ++i) {
+            ready = ready && __all(w[i] != kAbsent);
+            if (ready && from + i < A.groups) {
+                word_store(states + (int64_t)(from + i) * A.D, word_of(-1.f, h));
+                const float p = upper(w[i]);
+                h = p < 0.f ? lower(w[i]) : fmaf(p, h, lower(w[i]));
+                ++done;
             }
         }
+        if (done == from)
+            __builtin_amdgcn_s_sleep(2);
     }
-    if (c.on) {
+}
+
+// This workgroup's place and channel block; false: it was a runner and is done.
+__device__ __forceinline__ bool take_place(const ScanArgs &A, int &place, int &b)
+{
+    __shared__ int32_t t;
+    b = (int)(blockIdx.x % (uint32_t)A.blocks);
+    place = (int)(blockIdx.x / (uint32_t)A.blocks);
+    if (!A.ticket)
+        return true;
+    if (threadIdx.x == 0)
+        t = __hip_atomic_fetch_add(A.ticket + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    place = t - 1;
+    if (place < 0) {
+        run_chain(A, b);
+        return false;
+    }
+    return true;
+}
+
+// The state before this wavefront's tile, from its and its workgroup's maps:
+// `need` where its first row continues a sequence.  P, Q: the tile's map.
+template <int V>
+__device__ __forceinline__ void enter(const ScanArgs &A, int place, const Lane &c, bool need,
+                                      const float (&P)[V], const float (&Q)[V], float (&h)[V])
+{
+    __shared__ f2 maps[kWaves][64 * V];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        maps[w][lane * V + v] = f2{P[v], Q[v]};
+    __syncthreads();
+    float p[V], q[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        p[v] = 1.f, q[v] = 0.f;
+    for (int u = 0; u < w; ++u)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            float *o = A.agg + (k * A.D + c.ch + v) * 2;
-            o[0] = P[v];
-            o[1] = Q[v];
+            const f2 m = maps[u][lane * V + v];
+            compose(p[v], q[v], m.x, m.y);
+        }
+    if (A.ticket && w == kWaves - 1 && c.on) {   // the workgroup's map, as soon as it is known
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float ap = p[v], aq = q[v];
+            compose(ap, aq, P[v], Q[v]);
+            word_store(A.maps + (int64_t)place * A.D + c.ch + v, word_of(ap, aq));
         }
     }
-}
-
-// The state that enters each tile, one thread a channel.
-template <bool BWD> __global__ __launch_bounds__(64) void k_scan_carry(ScanArgs A)
-{
-    const int32_t ch = blockIdx.x * 64 + threadIdx.x;
-    if (ch >= A.D)
+    if (!need)
         return;
-    float *to = BWD ? A.back : A.carry;
-    float h = 0.f;
-#pragma unroll 8
-    for (int64_t j = 0; j < A.q.tiles; ++j) {
-        const int64_t k = BWD ? A.q.tiles - 1 - j : j;
-        const float *o = A.agg + (k * A.D + ch) * 2;
-        const float P = o[0], Q = o[1];
-        to[k * A.D + ch] = h;
-        h = P < 0.f ? Q : fmaf(P, h, Q);
+    float before[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        before[v] = 0.f;
+    // a sequence that begins in the workgroup before this tile cuts every channel alike
+    if (A.ticket && place > 0 && __any(p[0] >= 0.f || p[0] != p[0])) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint64_t *at = A.states + (int64_t)place * A.D + c.ch + v;
+            uint64_t s = word_load(at);
+            while (__any(s == kAbsent)) {
+                __builtin_amdgcn_s_sleep(1);
+                s = word_load(at);
+            }
+            before[v] = lower(s);
+        }
     }
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        h[v] = p[v] < 0.f ? q[v] : fmaf(p[v], before[v], q[v]);
 }
 
-template <class T, int V> __global__ __launch_bounds__(64 * kWaves) void k_scan_rows(ScanArgs A)
+// ---------------------------------------------------------------- the passes
+// ALONE: no sequence leaves its tile (short padded ones).
+template <class T, int V, bool ALONE>
+__global__ __launch_bounds__(64 * kWaves) void k_scan(ScanArgs A)
 {
-    const int64_t k = tile_index();
-    if (k >= A.q.tiles)
+    int place, b;
+    if (!take_place(A, place, b))
         return;
-    const Tile t = tile_at(A.q, k);
-    const Lane c = lane_at<V>(A.D, A.width, blockIdx.z);
+    const int64_t k = (int64_t)place * kWaves + (threadIdx.x >> 6);
+    const bool some = k < A.q.tiles;
+    if (ALONE && !some)
+        return;
+    const Tile t = tile_at(A.q, some ? k : 0);
+    const Lane c = lane_at<V>(A.D, A.width, b);
     const T *g = (const T *)A.g + c.ch, *x = (const T *)A.x + c.ch;
     T *y = (T *)A.y + c.ch;
-    const RowInfo in = rows_of(A.q, t);
-    if (!in.valid)
-        return;
-    float h[V];
-    if (in.valid & ~in.first & 1) {
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            h[v] = A.carry[k * A.D + c.ch + v];
-    }
+    RowInfo in = rows_of(A.q, t);
+    if (!some)
+        in.valid = in.first = in.last = 0;
     // y may be g or x: every row is loaded before the first one is stored
     Pack<T, V> pg[kRows], px[kRows];
 #pragma unroll
@@ -262,6 +333,41 @@ template <class T, int V> __global__ __launch_bounds__(64 * kWaves) void k_scan_
             pg[r] = load_pack<T, V>(g + p * A.ld_g);
             px[r] = load_pack<T, V>(x + p * A.ld_x);
         }
+    float h[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        h[v] = 0.f;
+    if constexpr (!ALONE) {
+        float P[V], Q[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            P[v] = 1.f, Q[v] = 0.f;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            if ((in.valid >> r) & 1) {
+                if ((in.first >> r) & 1) {
+                    const int32_t s = __builtin_amdgcn_readlane(in.seq, r);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        P[v] = -1.f;
+                        Q[v] = A.h0 ? A.h0[(int64_t)s * A.D + c.ch + v] : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const Gate G = gate_of(to_f32(pg[r].v[v]));
+                    P[v] = P[v] < 0.f ? -1.f : P[v] * G.a;
+                    Q[v] = fmaf(G.a, Q[v], G.i * to_f32(px[r].v[v]));
+                }
+            }
+        const bool need = in.valid & ~in.first & 1;
+        enter<V>(A, place, c, need, P, Q, h);
+        if (need && A.carry && c.on) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                A.carry[k * A.D + c.ch + v] = h[v];
+        }
+    }
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
         if ((in.valid >> r) & 1) {
@@ -284,55 +390,88 @@ template <class T, int V> __global__ __launch_bounds__(64 * kWaves) void k_scan_
         }
 }
 
-template <class T, int V>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_rows_bwd(ScanArgs A)
+// The gradient's pass, tiles and rows in the other order: a row hands a e back
+// to the one before it, with e = dy + what it was handed itself.
+template <class T, int V, bool ALONE>
+__global__ __launch_bounds__(64 * kWaves) void k_scan_bwd(ScanArgs A)
 {
-    const int64_t k = tile_index();
-    if (k >= A.q.tiles)
+    int place, b;
+    if (!take_place(A, place, b))
         return;
-    const Tile t = tile_at(A.q, k);
-    const Lane c = lane_at<V>(A.D, A.width, blockIdx.z);
+    const int64_t k = A.q.tiles - 1 - ((int64_t)place * kWaves + (threadIdx.x >> 6));
+    const bool some = k >= 0;
+    if (ALONE && !some)
+        return;
+    const Tile t = tile_at(A.q, some ? k : 0);
+    const Lane c = lane_at<V>(A.D, A.width, b);
     const T *g = (const T *)A.g + c.ch, *x = (const T *)A.x + c.ch, *dy = (const T *)A.dy + c.ch;
     T *dg = (T *)A.dg + c.ch, *dx = (T *)A.dx + c.ch;
-    const RowInfo in = rows_of(A.q, t);
-    if (!in.valid)
-        return;
+    RowInfo in = rows_of(A.q, t);
+    if (!some)
+        in.valid = in.first = in.last = 0;
     float h[V], e[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        h[v] = e[v] = 0.f;
     if (in.valid & ~in.first & 1) {
 #pragma unroll
         for (int v = 0; v < V; ++v)
             h[v] = A.carry[k * A.D + c.ch + v];
     }
-    const int32_t end = t.n - 1;
-    if ((in.valid & ~in.last) >> end & 1) {
+    Pack<T, V> pg[kRows], py[kRows];
+    float d[kRows][V];   // x, then (h_(t-1) - x) a (1 - a)
+    {
+        Pack<T, V> px[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            if ((in.valid >> r) & 1) {
+                const int64_t p = A.q.rev ? t.p0 - r : t.p0 + r;
+                pg[r] = load_pack<T, V>(g + p * A.ld_g);
+                px[r] = load_pack<T, V>(x + p * A.ld_x);
+                py[r] = load_pack<T, V>(dy + p * A.ld_y);
+            }
+        // the states before the rows again, as the forward call formed them
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            if ((in.valid >> r) & 1) {
+                const int32_t s = __builtin_amdgcn_readlane(in.seq, r);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    if ((in.first >> r) & 1)
+                        h[v] = A.h0 ? A.h0[(int64_t)s * A.D + c.ch + v] : 0.f;
+                    const Gate G = gate_of(to_f32(pg[r].v[v]));
+                    const float u = to_f32(px[r].v[v]);
+                    d[r][v] = (h[v] - u) * (G.a * G.i);
+                    h[v] = fmaf(G.a, h[v], G.i * u);
+                }
+            }
+    }
+    if constexpr (!ALONE) {
+        float P[V], Q[V];
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            e[v] = A.back[k * A.D + c.ch + v];
-    }
-    Pack<T, V> pg[kRows], px[kRows], py[kRows];
+            P[v] = 1.f, Q[v] = 0.f;
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
-        if ((in.valid >> r) & 1) {
-            const int64_t p = A.q.rev ? t.p0 - r : t.p0 + r;
-            pg[r] = load_pack<T, V>(g + p * A.ld_g);
-            px[r] = load_pack<T, V>(x + p * A.ld_x);
-            py[r] = load_pack<T, V>(dy + p * A.ld_y);
-        }
-    // the states before the rows again, as the forward call formed them
-    float before[kRows][V];
+        for (int r = kRows - 1; r >= 0; --r)
+            if ((in.valid >> r) & 1) {
+                if ((in.last >> r) & 1) {
+                    const int32_t s = __builtin_amdgcn_readlane(in.seq, r);
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
-        if ((in.valid >> r) & 1) {
-            const int32_t s = __builtin_amdgcn_readlane(in.seq, r);
+                    for (int v = 0; v < V; ++v) {
+                        P[v] = -1.f;
+                        Q[v] = A.last ? A.last[(int64_t)s * A.D + c.ch + v] : 0.f;
+                    }
+                }
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if ((in.first >> r) & 1)
-                    h[v] = A.h0 ? A.h0[(int64_t)s * A.D + c.ch + v] : 0.f;
-                before[r][v] = h[v];
-                const Gate G = gate_of(to_f32(pg[r].v[v]));
-                h[v] = fmaf(G.a, h[v], G.i * to_f32(px[r].v[v]));
+                for (int v = 0; v < V; ++v) {
+                    const Gate G = gate_of(to_f32(pg[r].v[v]));
+                    P[v] = P[v] < 0.f ? -1.f : P[v] * G.a;
+                    Q[v] = G.a * (to_f32(py[r].v[v]) + Q[v]);
+                }
             }
-        }
+        const bool need = ((in.valid & ~in.last) >> (t.n - 1)) & 1;
+        enter<V>(A, place, c, need, P, Q, e);
+    }
 #pragma unroll
     for (int r = kRows - 1; r >= 0; --r)
         if ((in.valid >> r) & 1) {
@@ -346,10 +485,9 @@ __global__ __launch_bounds__(64 * kWaves) void k_scan_rows_bwd(ScanArgs A)
                     e[v] = A.last ? A.last[at] : 0.f;
                 e[v] += to_f32(py[r].v[v]);
                 const Gate G = gate_of(to_f32(pg[r].v[v]));
-                const float d = G.i * e[v];
-                ox.v[v] = from_f32<T>(d);
+                ox.v[v] = from_f32<T>(G.i * e[v]);
+                og.v[v] = from_f32<T>(d[r][v] * e[v]);
                 e[v] *= G.a;
-                og.v[v] = from_f32<T>((before[r][v] - to_f32(px[r].v[v])) * G.a * d);
                 if (((in.first >> r) & 1) && A.h_last && c.on)
                     A.h_last[at] = e[v];
             }
@@ -360,16 +498,23 @@ __global__ __launch_bounds__(64 * kWaves) void k_scan_rows_bwd(ScanArgs A)
         }
 }
 
-// A sequence without rows ends with the state that it starts from (backward:
-// hands its end's gradient to its start): a wavefront looks 64 of them over.
-__global__ __launch_bounds__(256) void k_scan_empty(Seqs q, int32_t D,
-                                                    const float *__restrict__ from,
-                                                    float *__restrict__ to)
+// Before a pass: no word of the chain is there and no place is taken; and a
+// sequence without rows ends with the state that it starts from (backward:
+// hands its end's gradient to its start), which a wavefront does for 64 of them.
+__global__ __launch_bounds__(256) void k_scan_begin(Seqs q, int32_t D,
+                                                    const float *__restrict__ from, float *to,
+                                                    uint64_t *words, int64_t n, int32_t *ticket,
+                                                    int32_t blocks)
 {
+    const int64_t threads = (int64_t)gridDim.x * 256, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    for (int64_t i = id; i < n; i += threads)
+        words[i] = kAbsent;
+    if (ticket && id < blocks)
+        ticket[id] = 0;
+    if (!to)
+        return;
     const int lane = threadIdx.x & 63;
-    const int64_t waves = (int64_t)gridDim.x * 4;
-    for (int64_t s0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * 64; s0 < q.S;
-         s0 += waves * 64) {
+    for (int64_t s0 = id - lane; s0 < q.S; s0 += threads) {
         const int64_t s = s0 + lane;
         bool none = false;
         if (s < q.S) {
@@ -416,7 +561,8 @@ __global__ __launch_bounds__(256) void k_scan_step(const T *g, const T *x,
     }
 }
 
-constexpr int64_t kMaxRows = (int64_t)1 << 31;
+constexpr int64_t kMaxRows = ((int64_t)1 << 30) + 1;
+constexpr int64_t kMaxGrid = ((int64_t)1 << 32) / (64 * kWaves);   // threads of a launch: 32 bits
 constexpr int kMaxD = 65536;
 
 // Fills q's division into tiles; false where the sequences cannot be.
@@ -473,41 +619,61 @@ int pick_width(int32_t D, int want, int32_t *width)
     return 1;
 }
 
-dim3 tile_grid(const ScanArgs &A)
-{
-    const int64_t wg = cdiv(A.q.tiles, kWaves), x = std::min<int64_t>(wg, 1 << 20);
-    return dim3((uint32_t)x, (uint32_t)cdiv(wg, x), (uint32_t)cdiv(A.D, A.width));
-}
-
 template <class T, int V, bool BWD> tgm_status_t launch_scan(const ScanArgs &A, hipStream_t s)
 {
-    if (!A.q.tiles)
-        return TGM_OK;
-    const dim3 grid = tile_grid(A);
-    if (!A.q.per) {   // short padded sequences lie inside their tiles
-        TGM_LAUNCH((k_scan_agg<T, V, BWD>), grid, dim3(64 * kWaves), 0, s, A);
-        TGM_LAUNCH((k_scan_carry<BWD>), dim3((uint32_t)cdiv(A.D, 64)), dim3(64), 0, s, A);
+    // a runner more for every chain
+    const dim3 grid((uint32_t)(((int64_t)A.groups + (A.ticket ? 1 : 0)) * A.blocks));
+    const dim3 block(64 * kWaves);
+    if (BWD) {
+        if (A.q.per)
+            TGM_LAUNCH((k_scan_bwd<T, V, true>), grid, block, 0, s, A);
+        else
+            TGM_LAUNCH((k_scan_bwd<T, V, false>), grid, block, 0, s, A);
+    } else {
+        if (A.q.per)
+            TGM_LAUNCH((k_scan<T, V, true>), grid, block, 0, s, A);
+        else
+            TGM_LAUNCH((k_scan<T, V, false>), grid, block, 0, s, A);
     }
-    if (BWD)
-        TGM_LAUNCH((k_scan_rows_bwd<T, V>), grid, dim3(64 * kWaves), 0, s, A);
-    else
-        TGM_LAUNCH((k_scan_rows<T, V>), grid, dim3(64 * kWaves), 0, s, A);
     return TGM_OK;
 }
 
-template <class T, bool BWD> tgm_status_t run_scan(ScanArgs A, hipStream_t s)
+// Lays the chain out in the work space: maps and states, [groups x D] words
+// each, and the places' counters.
+size_t chain_bytes(int64_t groups, int64_t D) { return (size_t)groups * D * 16 + 2048 * 4; }
+
+template <class T, bool BWD>
+tgm_status_t run_scan(ScanArgs A, void *work, size_t work_bytes, hipStream_t s)
 {
     // a lane of fp32 pairs would hold more rows than registers in the gradient
     const int V = pick_width(A.D, BWD && sizeof(T) == 4 ? 1 : 2, &A.width);
+    A.blocks = (int32_t)cdiv(A.D, A.width);
+    A.groups = (int32_t)cdiv(A.q.tiles, kWaves);
+    if (((int64_t)A.groups + 1) * A.blocks >= kMaxGrid)
+        return TGM_EINVAL;
+    if (A.q.rows) {
+        if (!work || ((uintptr_t)work & 15))
+            return TGM_EINVAL;
+        if (work_bytes < chain_bytes(cdiv(most_tiles(A.q.rows, A.q.S), kWaves), A.D))
+            return TGM_ESIZE;
+    }
+    int64_t words = 0;
+    if (!A.q.per && A.groups > 1) {
+        words = (int64_t)A.groups * A.D * 2;
+        A.maps = (uint64_t *)work;
+        A.states = A.maps + words / 2;
+        A.ticket = (int32_t *)(A.maps + words);
+    }
+    const bool empty = A.h_last && A.q.S && (A.q.offsets || A.q.length || A.q.L == 0);
+    if (words || empty) {
+        const int64_t wg = std::min<int64_t>(cdiv(std::max<int64_t>(words, A.q.S), 256), 2048);
+        TGM_LAUNCH(k_scan_begin, dim3((uint32_t)wg), dim3(256), 0, s, A.q, A.D,
+                   BWD ? A.last : A.h0, empty ? A.h_last : nullptr, A.maps, words, A.ticket,
+                   A.blocks);
+    }
+    if (!A.q.tiles)
+        return TGM_OK;
     return V == 2 ? launch_scan<T, 2, BWD>(A, s) : launch_scan<T, 1, BWD>(A, s);
-}
-
-tgm_status_t empties(const ScanArgs &A, const float *from, hipStream_t s)
-{
-    if (A.h_last && A.q.S && (A.q.offsets || A.q.length || A.q.L == 0))
-        TGM_LAUNCH(k_scan_empty, dim3((uint32_t)std::min<int64_t>(cdiv(A.q.S, 256), 4096)),
-                   dim3(256), 0, s, A.q, A.D, from, A.h_last);
-    return TGM_OK;
 }
 
 tgm_status_t scan_args(const tgm_scan_desc *d, const void *g, const void *x,
@@ -534,22 +700,6 @@ tgm_status_t scan_args(const tgm_scan_desc *d, const void *g, const void *x,
     return TGM_OK;
 }
 
-// Splits the work space: the tiles' maps, and their states (`carry` or `back`).
-tgm_status_t take_work(ScanArgs *A, void *work, size_t work_bytes, float **states)
-{
-    const size_t need = (size_t)A->q.tiles * A->D * 12;
-    if (!need || A->q.per)
-        return TGM_OK;
-    if (!work || ((uintptr_t)work & 15))
-        return TGM_EINVAL;
-    if (work_bytes < need)
-        return TGM_ESIZE;
-    A->agg = (float *)work;
-    if (!*states)
-        *states = A->agg + (size_t)A->q.tiles * A->D * 2;
-    return TGM_OK;
-}
-
 }  // namespace
 
 extern "C" tgm_status_t tgm_scan_carry_rows(int64_t rows, int32_t S, int32_t packed, int64_t *n)
@@ -567,7 +717,7 @@ extern "C" tgm_status_t tgm_scan_work_bytes(int64_t rows, int32_t D, int32_t S, 
     const int64_t n = most_tiles(rows, S);
     if (!bytes || n < 0 || D < 1 || D > kMaxD)
         return TGM_EINVAL;
-    *bytes = (size_t)n * D * 12;
+    *bytes = n ? chain_bytes(cdiv(n, kWaves), D) : 0;
     return TGM_OK;
 }
 
@@ -581,13 +731,11 @@ extern "C" tgm_status_t tgm_scan(const tgm_scan_desc *d, const void *g, const vo
     if (d->rows && !y)
         return TGM_EINVAL;
     A.y = y, A.h_last = h_last, A.carry = carry;
-    TGM_TRY_STATUS(take_work(&A, work, work_bytes, &A.carry));
     const hipStream_t s = as_stream(stream);
-    TGM_TRY_STATUS(empties(A, h0, s));
     switch (d->dtype) {
-    case TGM_F32: return run_scan<float, false>(A, s);
-    case TGM_BF16: return run_scan<bf16, false>(A, s);
-    default: return run_scan<f16, false>(A, s);
+    case TGM_F32: return run_scan<float, false>(A, work, work_bytes, s);
+    case TGM_BF16: return run_scan<bf16, false>(A, work, work_bytes, s);
+    default: return run_scan<f16, false>(A, work, work_bytes, s);
     }
 }
 
@@ -602,14 +750,12 @@ extern "C" tgm_status_t tgm_scan_backward(const tgm_scan_desc *d, const void *g,
     if (d->rows && (!dy || !dg || !dx || !carry))
         return TGM_EINVAL;
     A.dy = dy, A.dg = dg, A.dx = dx, A.last = dh_last, A.h_last = dh0;
-    A.carry = const_cast<float *>(carry);   // read only: the states go to `back`
-    TGM_TRY_STATUS(take_work(&A, work, work_bytes, &A.back));
+    A.carry = const_cast<float *>(carry);   // read only here
     const hipStream_t s = as_stream(stream);
-    TGM_TRY_STATUS(empties(A, dh_last, s));
     switch (d->dtype) {
-    case TGM_F32: return run_scan<float, true>(A, s);
-    case TGM_BF16: return run_scan<bf16, true>(A, s);
-    default: return run_scan<f16, true>(A, s);
+    case TGM_F32: return run_scan<float, true>(A, work, work_bytes, s);
+    case TGM_BF16: return run_scan<bf16, true>(A, work, work_bytes, s);
+    default: return run_scan<f16, true>(A, work, work_bytes, s);
     }
 }
 
