@@ -4,7 +4,7 @@
 // h_t = a_t h_(t-1) + (1 - a_t) x_t is an affine map of h_(t-1), so the rows of
 // a tile of 32 compose to h_out = P h_in + Q with P the product of the gates,
 // and tiles compose likewise.  One pass over the data: a wavefront takes one
-// tile and 64 V channels (V neighbouring ones a lane), a workgroup 8 tiles in a
+// tile and 64 V channels (V neighbouring ones a lane), a workgroup several tiles in a
 // row; rows stay in registers between the tile's map and its states, so g and x
 // are read once and y is written once, which is what bounds the operator.
 // Between workgroups the states go along a chain (below).  The tiles run over
@@ -13,6 +13,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "seq.h"
 
@@ -21,7 +22,12 @@ using namespace tgm;
 namespace {
 
 constexpr int kRows = 32;   // rows of a tile
-constexpr int kWaves = 8;   // wavefronts (tiles) of a workgroup
+// Wavefronts (tiles) of a workgroup, so that two or more workgroups' rows fit a
+// CU's registers: 128 a lane forward, 256 in the gradient.  One history of
+// 1,000,003 rows of 128 bf16 channels: 224 us with 8 (361 with 4: twice the maps
+// for its chain, 293 with 10: one workgroup a CU); the gradient of 131,072 rows
+// of 512: 203 us with 4, 246 with 8 (one workgroup a CU).
+constexpr int kWaves = 8, kWavesBwd = 4;
 
 // The sequences, and their rows' division into tiles: packed sequences share
 // tiles of consecutive rows; padded ones have tiles of their own (`chunks` of
@@ -83,16 +89,59 @@ struct RowInfo {
     uint32_t valid, first, last;
 };
 
-__device__ __forceinline__ RowInfo rows_of(const Seqs &q, const Tile &t)
+__device__ __forceinline__ int64_t row_at(const Seqs &q, const Tile &t, int r)
+{
+    return q.rev ? t.p0 - r : t.p0 + r;
+}
+
+__device__ __forceinline__ RowInfo info_of(const Seqs &q, int32_t s, int64_t p, int64_t begin,
+                                           int64_t end, bool in)
+{
+    in = in && p >= begin && p < end;
+    const bool head = in && p == begin, tail = in && p == end - 1;
+    RowInfo i;
+    i.seq = s;
+    i.valid = (uint32_t)__ballot(in);
+    i.first = (uint32_t)__ballot(q.rev ? tail : head);
+    i.last = (uint32_t)__ballot(q.rev ? head : tail);
+    return i;
+}
+
+__device__ __forceinline__ RowInfo rows_padded(const Seqs &q, const Tile &t)
 {
     const int r = threadIdx.x & 31;
-    const int64_t p = q.rev ? t.p0 - min(r, t.n - 1) : t.p0 + min(r, t.n - 1);
-    int64_t begin, end;
+    const int64_t p = row_at(q, t, min(r, t.n - 1));
+    const int32_t s = (int32_t)(p / q.L);
+    const int64_t begin = s * q.L;
+    const int64_t end = begin + (q.length ? min(q.L, (int64_t)max(0, q.length[s])) : q.L);
+    return info_of(q, s, p, begin, end, r < t.n);
+}
+
+__device__ __forceinline__ RowInfo rows_packed(const Seqs &q, const Tile &t)
+{
+    const int lane = threadIdx.x & 63, r = lane & 31;
+    const int64_t p = row_at(q, t, min(r, t.n - 1));
+    const int64_t p1 = q.rev ? t.p0 - (t.n - 1) : t.p0, p2 = q.rev ? t.p0 : t.p0 + (t.n - 1);
+    const int32_t n = count_le(q.offsets, q.S, p1);   // sequences that begin up to the tile
+    // the beginnings after those, 64 of them in the lanes, and the one before
+    const bool at = lane <= q.S - n;
+    const int64_t next = at ? q.offsets[n + lane] : INT64_MAX;
+    const int64_t here = n > 0 ? q.offsets[n - 1] : 0;
     int32_t s;
-    if (q.offsets) {
-        const int64_t p1 = q.rev ? t.p0 - (t.n - 1) : t.p0, p2 = q.rev ? t.p0 : t.p0 + (t.n - 1);
-        int32_t lo = count_le(q.offsets, q.S, p1) - 1;
-        int32_t hi = max(lo, count_le(q.offsets, q.S, p2) - 1);
+    int64_t begin, end;
+    if (__popcll(__ballot(lane < q.S - n && next <= p2)) < 64) {
+        int c = 0;   // those up to p
+#pragma unroll
+        for (int step = 32; step; step >>= 1) {
+            const int64_t v = __shfl(next, c + step - 1);
+            c += c + step - 1 < q.S - n && v <= p ? step : 0;
+        }
+        s = n - 1 + c;
+        const int64_t before = __shfl(next, max(c - 1, 0));
+        begin = c ? before : here;
+        end = __shfl(next, c);
+    } else {   // more than 64 begin inside the tile: empty ones among them
+        int32_t lo = n - 1, hi = max(lo, count_le(q.offsets, q.S, p2) - 1);
         while (lo < hi) {   // the last sequence that begins at or before p
             const int32_t mid = lo + (hi - lo + 1) / 2;
             if (q.offsets[mid] <= p)
@@ -103,21 +152,10 @@ __device__ __forceinline__ RowInfo rows_of(const Seqs &q, const Tile &t)
         s = lo;
         begin = s >= 0 ? q.offsets[s] : 0;
         end = s >= 0 ? q.offsets[s + 1] : 0;
-        if (q.length && s >= 0)
-            end = min(end, begin + max(0, q.length[s]));
-    } else {
-        s = (int32_t)(p / q.L);
-        begin = s * q.L;
-        end = begin + (q.length ? min(q.L, (int64_t)max(0, q.length[s])) : q.L);
     }
-    const bool in = r < t.n && s >= 0 && p >= begin && p < end;
-    const bool head = in && p == begin, tail = in && p == end - 1;
-    RowInfo i;
-    i.seq = s;
-    i.valid = (uint32_t)__ballot(in);
-    i.first = (uint32_t)__ballot(q.rev ? tail : head);
-    i.last = (uint32_t)__ballot(q.rev ? head : tail);
-    return i;
+    if (q.length && s >= 0)
+        end = min(end, begin + max(0, q.length[s]));
+    return info_of(q, s, p, begin, end, r < t.n && s >= 0);
 }
 
 // The gates.  exp(-|g|) lies in (0, 1], so neither gate loses its small values
@@ -146,6 +184,103 @@ template <int V> __device__ __forceinline__ Lane lane_at(int32_t D, int32_t widt
     const int32_t ch = c0 + V * (int32_t)(threadIdx.x & 63);
     return Lane{min(ch, c1 - V), ch < c1};
 }
+// This lane's elements of a row of a dense array.
+template <class T> __device__ __forceinline__ T *in_row(T *X, int64_t p, int64_t ld, int32_t ch)
+{
+    return X + p * ld + (uint32_t)ch;
+}
+// A tile's rows of a matrix: one 64-bit base, the wavefront's, and an offset of
+// 32 bits for row r of the scan's order (32 rows of less than 2^24 elements).
+template <class T> struct Rows {
+    char *base;
+    uint32_t first, step;
+    __device__ __forceinline__ Rows(const void *X, const Seqs &q, const Tile &t, int64_t ld)
+    {
+        const int64_t lo = q.rev ? t.p0 - (t.n - 1) : t.p0;
+        base = (char *)const_cast<void *>(X) + lo * ld * (int64_t)sizeof(T);
+        const uint32_t b = (uint32_t)ld * (uint32_t)sizeof(T);
+        first = q.rev ? (uint32_t)(t.n - 1) * b : 0u;
+        step = q.rev ? 0u - b : b;
+    }
+    __device__ __forceinline__ T *at(int r, int32_t ch) const
+    {
+        return reinterpret_cast<T *>(base + (first + (uint32_t)r * step)) + (uint32_t)ch;
+    }
+};
+__device__ __forceinline__ int wave_id()
+{
+    return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+}
+
+// A row's elements in a lane, as they came: between the passes over a tile they
+// stay packed, which the compiler is kept from undoing (unpacked 16-bit
+// elements take twice the registers).
+template <class T, int V> struct Held {
+    Pack<T, V> v;
+    __device__ __forceinline__ float at(int i) const { return to_f32(v.v[i]); }
+    __device__ __forceinline__ void keep() {}
+};
+template <class T> struct HeldPair {
+    uint32_t w;
+    __device__ __forceinline__ float at(int i) const
+    {
+        const uint16_t u = (uint16_t)(w >> (16 * i));
+        return to_f32(__builtin_bit_cast(T, u));
+    }
+    __device__ __forceinline__ void keep() { asm volatile("" : "+v"(w)); }
+};
+template <> struct Held<f16, 2> : HeldPair<f16> {};
+template <> struct Held<bf16, 2> : HeldPair<bf16> {};
+template <class T, int V> __device__ __forceinline__ Held<T, V> hold(const T *p)
+{
+    using HeldT = Held<T, V>;
+    return __builtin_bit_cast(HeldT, load_pack<T, V>(p));
+}
+
+// The states that a tile's sequences start from (or hand back from), one for
+// each row in `mask`: the first two are loaded ahead, before the rows are gone
+// through; the others, in tiles of short sequences, when met.
+template <int V> struct Starts {
+    float v0[V], v1[V];
+    __device__ __forceinline__ void load(const float *X, uint32_t mask, int32_t seq, int32_t D,
+                                         int32_t ch)
+    {
+        one(v0, X, mask, seq, D, ch);
+        one(v1, X, mask & (mask - 1), seq, D, ch);
+    }
+    // that of row r of the mask
+    __device__ __forceinline__ void get(float (&h)[V], const float *X, uint32_t mask, int r,
+                                        int32_t seq, int32_t D, int32_t ch) const
+    {
+        const int j = __builtin_popcount(mask & ((1u << r) - 1));
+        float other[V];
+#pragma unroll
+        for (int u = 0; u < V; ++u)
+            other[u] = 0.f;
+        if (j >= 2)
+            one(other, X, mask & ~((1u << r) - 1), seq, D, ch);
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+            const float a = v0[u], b = v1[u];
+            h[u] = j == 0 ? a : j == 1 ? b : other[u];
+        }
+    }
+
+private:
+    static __device__ __forceinline__ void one(float (&to)[V], const float *X, uint32_t mask,
+                                               int32_t seq, int32_t D, int32_t ch)
+    {
+#pragma unroll
+        for (int u = 0; u < V; ++u)
+            to[u] = 0.f;
+        if (X && mask) {
+            const float *x = in_row(X, __builtin_amdgcn_readlane(seq, __builtin_ctz(mask)), D, ch);
+#pragma unroll
+            for (int u = 0; u < V; ++u)
+                to[u] = x[u];
+        }
+    }
+};
 
 struct ScanArgs {
     Seqs q;
@@ -170,8 +305,7 @@ struct ScanArgs {
 //
 // Workgroups take their places in the rows' order by a counter as they start.
 // The first of each channel block's chain is its runner: it composes the
-// others' maps in order and hands every workgroup the state before its rows,
-// 32 words a load.  A workgroup writes its map without waiting for anyone, and
+// others' maps in order and hands every workgroup the state before its rows.  A workgroup writes its map without waiting for anyone, and
 // the runner waits only for the lowest place whose map is missing, which a
 // workgroup that has started holds or the next one to start will hold; so
 // every wait ends, however few workgroups run at once.
@@ -200,52 +334,100 @@ __device__ __forceinline__ void compose(float &P, float &Q, float p, float q)
     P = p < 0.f || P < 0.f ? -1.f : P * p;
 }
 
-__device__ void run_chain(const ScanArgs &A, int b)
+// A runner takes 64 channels.  Its wavefronts take a block of 16 maps each at a
+// time: a block that is there is composed on its own, the state before each
+// block comes from the maps of the blocks before it, and the states inside
+// follow one by one: the same operations whichever words were there at which
+// look, so results do not depend on timing.
+template <int W> __device__ void run_chain(const ScanArgs &A, int b, int part)
 {
-    constexpr int kAhead = 32;
-    const int32_t c0 = b * A.width, c1 = min(A.D, c0 + A.width);
-    const int32_t ch = c0 + (int32_t)threadIdx.x;
-    if ((int)(threadIdx.x & ~63u) + c0 >= c1)   // one wavefront for every 64 channels
-        return;
-    const uint64_t *maps = A.maps + min(ch, c1 - 1);
-    uint64_t *states = A.states + min(ch, c1 - 1);
-    float h = 0.f;
-    for (int32_t done = 0; done < A.groups;) {
-        uint64_t w[kAhead];
+    constexpr int kBlock = 16;
+    __shared__ f2 block[2][W][64];
+    __shared__ int32_t there[2][W];
+    const int lane = threadIdx.x & 63, u = wave_id();
+    const int32_t c0 = b * A.width + 64 * part, c1 = min(A.D, (b + 1) * A.width);
+    const uint32_t ch = (uint32_t)min(c0 + lane, c1 - 1);
+    float base = 0.f;             // the state before the first block not done
+    int32_t at = 0, known = 0;    // the first map of that block; how many of it are done
+    for (int turn = 0; at < A.groups; turn ^= 1) {
+        const int32_t first = at + kBlock * u, left = min(kBlock, A.groups - first);
+        const uint64_t *maps = A.maps + (int64_t)first * A.D + ch;
+        uint64_t w[kBlock];
+        uint32_t absent = 0;   // bit i: word i is not there for every lane
+        if (left > 0) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            w[i] = word_load(maps + (int64_t)min(done + i, A.groups - 1) * A.D);
-        const int32_t from = done;
-        bool ready = true;
+            for (int i = 0; i < kBlock; ++i)
+                w[i] = word_load(maps + (uint64_t)((uint32_t)min(i, left - 1) * (uint32_t)A.D));
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            ready = ready && __all(w[i] != kAbsent);
-            if (ready && from + i < A.groups) {
-                word_store(states + (int64_t)(from + i) * A.D, word_of(-1.f, h));
-                const float p = upper(w[i]);
-                h = p < 0.f ? lower(w[i]) : fmaf(p, h, lower(w[i]));
-                ++done;
-            }
+            for (int i = 0; i < kBlock; ++i)
+                absent |= __ballot((uint32_t)(w[i] >> 32) == ~0u) ? 1u << i : 0u;
         }
-        if (done == from)
-            __builtin_amdgcn_s_sleep(2);
+        const int n = left <= 0 ? 0 : absent ? min(left, __builtin_ctz(absent)) : left;
+        if (n == kBlock) {
+            float P = 1.f, Q = 0.f;
+#pragma unroll
+            for (int i = 0; i < kBlock; ++i)
+                compose(P, Q, upper(w[i]), lower(w[i]));
+            block[turn][u][lane] = f2{P, Q};
+        }
+        if (lane == 0)
+            there[turn][u] = n;
+        __syncthreads();   // one a turn: two turns' words are apart
+        f2 m[W];
+        int32_t count[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k)
+            m[k] = block[turn][k][lane], count[k] = there[turn][k];
+        float h = base;
+        int32_t whole = 0, rest = 0;   // blocks there from the first on; of the one after
+#pragma unroll
+        for (int k = 0; k < W; ++k)
+            if (whole == k) {
+                rest = __builtin_amdgcn_readfirstlane(count[k]);
+                if (rest == kBlock) {
+                    ++whole;
+                    rest = 0;
+                    base = m[k].x < 0.f ? m[k].y : fmaf(m[k].x, base, m[k].y);
+                    h = k < u ? base : h;
+                }
+            }
+        if (u <= whole) {   // the state before this wavefront's block is known
+            uint64_t *states = A.states + (int64_t)first * A.D + ch;
+            const int done = u ? 0 : known;
+#pragma unroll
+            for (int i = 0; i < kBlock; ++i)
+                if (i < n) {
+                    if (i >= done)
+                        word_store(states + (uint64_t)((uint32_t)i * (uint32_t)A.D),
+                                   word_of(-1.f, h));
+                    const float p = upper(w[i]), q = lower(w[i]);
+                    h = p < 0.f ? q : fmaf(p, h, q);
+                }
+        }
+        if (!whole && rest <= known)
+            __builtin_amdgcn_s_sleep(1);
+        at += kBlock * whole;
+        known = rest;
+        if (at + rest >= A.groups)
+            break;
     }
 }
 
 // This workgroup's place and channel block; false: it was a runner and is done.
+template <int V, int W, bool ALONE>
 __device__ __forceinline__ bool take_place(const ScanArgs &A, int &place, int &b)
 {
     __shared__ int32_t t;
     b = (int)(blockIdx.x % (uint32_t)A.blocks);
     place = (int)(blockIdx.x / (uint32_t)A.blocks);
-    if (!A.ticket)
+    if (ALONE || !A.ticket)
         return true;
     if (threadIdx.x == 0)
         t = __hip_atomic_fetch_add(A.ticket + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    place = t - 1;
+    place = __builtin_amdgcn_readfirstlane(t) - V;   // V runners
     if (place < 0) {
-        run_chain(A, b);
+        run_chain<W>(A, b, place + V);
         return false;
     }
     return true;
@@ -253,15 +435,19 @@ __device__ __forceinline__ bool take_place(const ScanArgs &A, int &place, int &b
 
 // The state before this wavefront's tile, from its and its workgroup's maps:
 // `need` where its first row continues a sequence.  P, Q: the tile's map.
-template <int V>
+template <int V, int W>
 __device__ __forceinline__ void enter(const ScanArgs &A, int place, const Lane &c, bool need,
                                       const float (&P)[V], const float (&Q)[V], float (&h)[V])
 {
-    __shared__ f2 maps[kWaves][64 * V];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    __shared__ f2 maps[W][64 * V];
+    __shared__ float state[64 * V];
+    __shared__ bool wanted;
+    const int lane = threadIdx.x & 63, w = wave_id();
 #pragma unroll
     for (int v = 0; v < V; ++v)
         maps[w][lane * V + v] = f2{P[v], Q[v]};
+    if (threadIdx.x == 0)
+        wanted = need && A.ticket && place > 0;
     __syncthreads();
     float p[V], q[V];
 #pragma unroll
@@ -273,7 +459,7 @@ __device__ __forceinline__ void enter(const ScanArgs &A, int place, const Lane &
             const f2 m = maps[u][lane * V + v];
             compose(p[v], q[v], m.x, m.y);
         }
-    if (A.ticket && w == kWaves - 1 && c.on) {   // the workgroup's map, as soon as it is known
+    if (A.ticket && w == W - 1 && c.on) {   // the workgroup's map, as soon as it is known
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             float ap = p[v], aq = q[v];
@@ -281,226 +467,274 @@ __device__ __forceinline__ void enter(const ScanArgs &A, int place, const Lane &
             word_store(A.maps + (int64_t)place * A.D + c.ch + v, word_of(ap, aq));
         }
     }
-    if (!need)
-        return;
-    float before[V];
+    if (__builtin_amdgcn_readfirstlane((int)wanted)) {
+        // one wavefront looks for the state: eight would take the memory's time
+        if (w == 0) {
+            const uint64_t *at = A.states + (int64_t)place * A.D + c.ch;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        before[v] = 0.f;
-    // a sequence that begins in the workgroup before this tile cuts every channel alike
-    if (A.ticket && place > 0 && __any(p[0] >= 0.f || p[0] != p[0])) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const uint64_t *at = A.states + (int64_t)place * A.D + c.ch + v;
-            uint64_t s = word_load(at);
-            while (__any(s == kAbsent)) {
-                __builtin_amdgcn_s_sleep(1);
-                s = word_load(at);
+            for (int v = 0; v < V; ++v) {
+                uint64_t s = word_load(at + v);
+                while (__any(s == kAbsent)) {
+                    __builtin_amdgcn_s_sleep(4);
+                    s = word_load(at + v);
+                }
+                state[lane * V + v] = lower(s);
             }
-            before[v] = lower(s);
         }
-    }
+        __syncthreads();
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-        h[v] = p[v] < 0.f ? q[v] : fmaf(p[v], before[v], q[v]);
+        for (int v = 0; v < V; ++v)
+            h[v] = state[lane * V + v];
+    }
+    if (need)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            h[v] = p[v] < 0.f ? q[v] : fmaf(p[v], h[v], q[v]);
 }
 
 // ---------------------------------------------------------------- the passes
 // ALONE: no sequence leaves its tile (short padded ones).
-template <class T, int V, bool ALONE>
-__global__ __launch_bounds__(64 * kWaves) void k_scan(ScanArgs A)
+template <class T, int V, int W, bool ALONE>
+__global__ __launch_bounds__(64 * W, 4) void k_scan(ScanArgs A)
 {
     int place, b;
-    if (!take_place(A, place, b))
+    if (!take_place<V, W, ALONE>(A, place, b))
         return;
-    const int64_t k = (int64_t)place * kWaves + (threadIdx.x >> 6);
+    const int64_t k = (int64_t)place * W + wave_id();
     const bool some = k < A.q.tiles;
     if (ALONE && !some)
         return;
     const Tile t = tile_at(A.q, some ? k : 0);
     const Lane c = lane_at<V>(A.D, A.width, b);
-    const T *g = (const T *)A.g + c.ch, *x = (const T *)A.x + c.ch;
-    T *y = (T *)A.y + c.ch;
-    RowInfo in = rows_of(A.q, t);
-    if (!some)
-        in.valid = in.first = in.last = 0;
-    // y may be g or x: every row is loaded before the first one is stored
-    Pack<T, V> pg[kRows], px[kRows];
+    // All loads go out at once, without a branch between them: packed rows before
+    // the search for their sequences; a padded row of no sequence is another one
+    // again.  y may be g or x: every row is loaded before the first is stored.
+    RowInfo in{};
+    uint32_t wanted = ~0u >> (kRows - t.n);
+    if (some && !A.q.offsets) {
+        in = rows_padded(A.q, t);
+        wanted = in.valid;
+    }
+    if (ALONE && !wanted)
+        return;
+    const int other = wanted ? __builtin_ctz(wanted) : 0;
+    const Rows<const T> gs(A.g, A.q, t, A.ld_g), xs(A.x, A.q, t, A.ld_x);
+    const Rows<T> ys(A.y, A.q, t, A.ld_y);
+    Held<T, V> pg[kRows], px[kRows];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
-        if ((in.valid >> r) & 1) {
-            const int64_t p = A.q.rev ? t.p0 - r : t.p0 + r;
-            pg[r] = load_pack<T, V>(g + p * A.ld_g);
-            px[r] = load_pack<T, V>(x + p * A.ld_x);
-        }
+    for (int r = 0; r < kRows; ++r) {
+        const int from = (wanted >> r) & 1 ? r : other;
+        pg[r] = hold<T, V>(gs.at(from, c.ch));
+        px[r] = hold<T, V>(xs.at(from, c.ch));
+    }
+    if (some && A.q.offsets)
+        in = rows_packed(A.q, t);
+    Starts<V> starts;
+    starts.load(A.h0, in.first, in.seq, A.D, c.ch);
     float h[V];
 #pragma unroll
     for (int v = 0; v < V; ++v)
         h[v] = 0.f;
+    // most tiles of long sequences are plain: no row of them begins or ends one
+    const bool plain = in.valid == ~0u && !in.first && !in.last;
     if constexpr (!ALONE) {
         float P[V], Q[V];
 #pragma unroll
         for (int v = 0; v < V; ++v)
             P[v] = 1.f, Q[v] = 0.f;
+        auto map = [&](auto is_plain) __attribute__((always_inline)) {
 #pragma unroll
-        for (int r = 0; r < kRows; ++r)
-            if ((in.valid >> r) & 1) {
-                if ((in.first >> r) & 1) {
-                    const int32_t s = __builtin_amdgcn_readlane(in.seq, r);
+            for (int r = 0; r < kRows; ++r)
+                if (is_plain || ((in.valid >> r) & 1)) {
+                    if (!is_plain && ((in.first >> r) & 1))
+                        starts.get(Q, A.h0, in.first, r, in.seq, A.D, c.ch);
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        P[v] = -1.f;
-                        Q[v] = A.h0 ? A.h0[(int64_t)s * A.D + c.ch + v] : 0.f;
+                        const Gate G = gate_of(pg[r].at(v));
+                        P[v] *= G.a;
+                        Q[v] = fmaf(G.a, Q[v], G.i * px[r].at(v));
                     }
                 }
+        };
+        if (plain)
+            map(std::true_type{});
+        else
+            map(std::false_type{});
+        if (in.first)
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const Gate G = gate_of(to_f32(pg[r].v[v]));
-                    P[v] = P[v] < 0.f ? -1.f : P[v] * G.a;
-                    Q[v] = fmaf(G.a, Q[v], G.i * to_f32(px[r].v[v]));
-                }
-            }
+            for (int v = 0; v < V; ++v)
+                P[v] = -1.f;
         const bool need = in.valid & ~in.first & 1;
-        enter<V>(A, place, c, need, P, Q, h);
+        enter<V, W>(A, place, c, need, P, Q, h);
         if (need && A.carry && c.on) {
 #pragma unroll
             for (int v = 0; v < V; ++v)
-                A.carry[k * A.D + c.ch + v] = h[v];
+                in_row(A.carry, k, A.D, c.ch)[v] = h[v];
         }
     }
+    auto rows = [&](auto is_plain) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
-        if ((in.valid >> r) & 1) {
-            const int64_t p = A.q.rev ? t.p0 - r : t.p0 + r;
-            const int32_t s = __builtin_amdgcn_readlane(in.seq, r);
-            Pack<T, V> py;
+        for (int r = 0; r < kRows; ++r)
+            if (is_plain || ((in.valid >> r) & 1)) {
+                if (!is_plain && ((in.first >> r) & 1))
+                    starts.get(h, A.h0, in.first, r, in.seq, A.D, c.ch);
+                Pack<T, V> py;
+                pg[r].keep(), px[r].keep();
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int64_t at = (int64_t)s * A.D + c.ch + v;
-                if ((in.first >> r) & 1)
-                    h[v] = A.h0 ? A.h0[at] : 0.f;
-                const Gate G = gate_of(to_f32(pg[r].v[v]));
-                h[v] = fmaf(G.a, h[v], G.i * to_f32(px[r].v[v]));
-                py.v[v] = from_f32<T>(h[v]);
-                if (((in.last >> r) & 1) && A.h_last && c.on)
-                    A.h_last[at] = h[v];
+                for (int v = 0; v < V; ++v) {
+                    const Gate G = gate_of(pg[r].at(v));
+                    h[v] = fmaf(G.a, h[v], G.i * px[r].at(v));
+                    py.v[v] = from_f32<T>(h[v]);
+                }
+                if (c.on)
+                    store_pack(ys.at(r, c.ch), py);
+                if (!is_plain && ((in.last >> r) & 1) && A.h_last && c.on) {
+                    float *to = in_row(A.h_last, __builtin_amdgcn_readlane(in.seq, r), A.D, c.ch);
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        to[v] = h[v];
+                }
             }
-            if (c.on)
-                store_pack(y + p * A.ld_y, py);
-        }
+    };
+    if (plain)
+        rows(std::true_type{});
+    else
+        rows(std::false_type{});
 }
 
-// The gradient's pass, tiles and rows in the other order: a row hands a e back
-// to the one before it, with e = dy + what it was handed itself.
-template <class T, int V, bool ALONE>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_bwd(ScanArgs A)
+// The gradient's pass, tiles in the other order: a row hands a e back to the
+// one before it, with e = dy + what it was handed itself.
+template <class T, int V, int W, bool ALONE>
+__global__ __launch_bounds__(64 * W, 2) void k_scan_bwd(ScanArgs A)
 {
     int place, b;
-    if (!take_place(A, place, b))
+    if (!take_place<V, W, ALONE>(A, place, b))
         return;
-    const int64_t k = A.q.tiles - 1 - ((int64_t)place * kWaves + (threadIdx.x >> 6));
+    const int64_t k = A.q.tiles - 1 - ((int64_t)place * W + wave_id());
     const bool some = k >= 0;
     if (ALONE && !some)
         return;
     const Tile t = tile_at(A.q, some ? k : 0);
     const Lane c = lane_at<V>(A.D, A.width, b);
-    const T *g = (const T *)A.g + c.ch, *x = (const T *)A.x + c.ch, *dy = (const T *)A.dy + c.ch;
-    T *dg = (T *)A.dg + c.ch, *dx = (T *)A.dx + c.ch;
-    RowInfo in = rows_of(A.q, t);
-    if (!some)
-        in.valid = in.first = in.last = 0;
-    float h[V], e[V];
+    RowInfo in{};
+    uint32_t wanted = ~0u >> (kRows - t.n);
+    if (some && !A.q.offsets) {
+        in = rows_padded(A.q, t);
+        wanted = in.valid;
+    }
+    if (ALONE && !wanted)
+        return;
+    const int other = wanted ? __builtin_ctz(wanted) : 0;
+    const Rows<const T> gs(A.g, A.q, t, A.ld_g), xs(A.x, A.q, t, A.ld_x), dys(A.dy, A.q, t, A.ld_y);
+    const Rows<T> dgs(A.dg, A.q, t, A.ld_dg), dxs(A.dx, A.q, t, A.ld_dx);
+    // kept between the passes: g, dy and (h_(t-1) - x) a; the gates are formed twice
+    // (kept, they would take the registers of a third of the rows)
+    float d[kRows][V];
+    float h[V], e[V], P[V], Q[V];
 #pragma unroll
     for (int v = 0; v < V; ++v)
-        h[v] = e[v] = 0.f;
+        h[v] = e[v] = Q[v] = 0.f, P[v] = 1.f;
+    Starts<V> ends;
+    Held<T, V> pg[kRows], px[kRows], py[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {   // as in k_scan
+        const int from = (wanted >> r) & 1 ? r : other;
+        pg[r] = hold<T, V>(gs.at(from, c.ch));
+        px[r] = hold<T, V>(xs.at(from, c.ch));
+        py[r] = hold<T, V>(dys.at(from, c.ch));
+    }
+    if (some && A.q.offsets)
+        in = rows_packed(A.q, t);
+    const bool plain = in.valid == ~0u && !in.first && !in.last;
+    Starts<V> starts;
+    starts.load(A.h0, in.first, in.seq, A.D, c.ch);
+    ends.load(A.last, in.last, in.seq, A.D, c.ch);
     if (in.valid & ~in.first & 1) {
+        const float *from = in_row(A.carry, k, A.D, c.ch);
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            h[v] = A.carry[k * A.D + c.ch + v];
+            h[v] = from[v];
     }
-    Pack<T, V> pg[kRows], py[kRows];
-    float d[kRows][V];   // x, then (h_(t-1) - x) a (1 - a)
-    {
-        Pack<T, V> px[kRows];
+    // the states before the rows again, as the forward call formed them, and
+    // what the tile hands back: the sum over its first sequence's rows of dy
+    // times the gates up to the row, and the end's share
+    auto map = [&](auto is_plain) __attribute__((always_inline)) {
 #pragma unroll
         for (int r = 0; r < kRows; ++r)
-            if ((in.valid >> r) & 1) {
-                const int64_t p = A.q.rev ? t.p0 - r : t.p0 + r;
-                pg[r] = load_pack<T, V>(g + p * A.ld_g);
-                px[r] = load_pack<T, V>(x + p * A.ld_x);
-                py[r] = load_pack<T, V>(dy + p * A.ld_y);
-            }
-        // the states before the rows again, as the forward call formed them
+            if (is_plain || ((in.valid >> r) & 1)) {
+                if (!is_plain && ((in.first >> r) & 1))
+                    starts.get(h, A.h0, in.first, r, in.seq, A.D, c.ch);
+                const bool open = is_plain || !(in.last & ((1u << r) - 1));
+                float end[V];
 #pragma unroll
-        for (int r = 0; r < kRows; ++r)
-            if ((in.valid >> r) & 1) {
-                const int32_t s = __builtin_amdgcn_readlane(in.seq, r);
+                for (int v = 0; v < V; ++v)
+                    end[v] = 0.f;
+                if (!ALONE && !is_plain && open && ((in.last >> r) & 1))
+                    ends.get(end, A.last, in.last, r, in.seq, A.D, c.ch);
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    if ((in.first >> r) & 1)
-                        h[v] = A.h0 ? A.h0[(int64_t)s * A.D + c.ch + v] : 0.f;
-                    const Gate G = gate_of(to_f32(pg[r].v[v]));
-                    const float u = to_f32(px[r].v[v]);
-                    d[r][v] = (h[v] - u) * (G.a * G.i);
+                    const Gate G = gate_of(pg[r].at(v));
+                    const float u = px[r].at(v);
+                    d[r][v] = (h[v] - u) * G.a;
                     h[v] = fmaf(G.a, h[v], G.i * u);
-                }
-            }
-    }
-    if constexpr (!ALONE) {
-        float P[V], Q[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            P[v] = 1.f, Q[v] = 0.f;
-#pragma unroll
-        for (int r = kRows - 1; r >= 0; --r)
-            if ((in.valid >> r) & 1) {
-                if ((in.last >> r) & 1) {
-                    const int32_t s = __builtin_amdgcn_readlane(in.seq, r);
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        P[v] = -1.f;
-                        Q[v] = A.last ? A.last[(int64_t)s * A.D + c.ch + v] : 0.f;
+                    if (!ALONE && open) {
+                        P[v] *= G.a;
+                        Q[v] = fmaf(P[v], py[r].at(v) + end[v], Q[v]);
                     }
                 }
+            }
+    };
+    if (plain)
+        map(std::true_type{});
+    else
+        map(std::false_type{});
+    if constexpr (!ALONE) {
+        if (in.last)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                P[v] = -1.f;
+        const bool need = ((in.valid & ~in.last) >> (t.n - 1)) & 1;
+        enter<V, W>(A, place, c, need, P, Q, e);
+    }
+    auto rows = [&](auto is_plain) __attribute__((always_inline)) {
+#pragma unroll
+        for (int r = kRows - 1; r >= 0; --r)
+            if (is_plain || ((in.valid >> r) & 1)) {
+                if (!is_plain && ((in.last >> r) & 1))
+                    ends.get(e, A.last, in.last, r, in.seq, A.D, c.ch);
+                pg[r].keep(), py[r].keep();
+                Pack<T, V> og, ox;
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const Gate G = gate_of(to_f32(pg[r].v[v]));
-                    P[v] = P[v] < 0.f ? -1.f : P[v] * G.a;
-                    Q[v] = G.a * (to_f32(py[r].v[v]) + Q[v]);
+                    e[v] += py[r].at(v);
+                    const Gate G = gate_of(pg[r].at(v));
+                    const float back = G.i * e[v];
+                    ox.v[v] = from_f32<T>(back);
+                    og.v[v] = from_f32<T>(d[r][v] * back);
+                    e[v] *= G.a;
+                }
+                if (c.on) {
+                    store_pack(dgs.at(r, c.ch), og);
+                    store_pack(dxs.at(r, c.ch), ox);
+                }
+                if (!is_plain && ((in.first >> r) & 1) && A.h_last && c.on) {
+                    float *to = in_row(A.h_last, __builtin_amdgcn_readlane(in.seq, r), A.D, c.ch);
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        to[v] = e[v];
                 }
             }
-        const bool need = ((in.valid & ~in.last) >> (t.n - 1)) & 1;
-        enter<V>(A, place, c, need, P, Q, e);
-    }
-#pragma unroll
-    for (int r = kRows - 1; r >= 0; --r)
-        if ((in.valid >> r) & 1) {
-            const int64_t p = A.q.rev ? t.p0 - r : t.p0 + r;
-            const int32_t s = __builtin_amdgcn_readlane(in.seq, r);
-            Pack<T, V> og, ox;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int64_t at = (int64_t)s * A.D + c.ch + v;
-                if ((in.last >> r) & 1)
-                    e[v] = A.last ? A.last[at] : 0.f;
-                e[v] += to_f32(py[r].v[v]);
-                const Gate G = gate_of(to_f32(pg[r].v[v]));
-                ox.v[v] = from_f32<T>(G.i * e[v]);
-                og.v[v] = from_f32<T>(d[r][v] * e[v]);
-                e[v] *= G.a;
-                if (((in.first >> r) & 1) && A.h_last && c.on)
-                    A.h_last[at] = e[v];
-            }
-            if (c.on) {
-                store_pack(dg + p * A.ld_dg, og);
-                store_pack(dx + p * A.ld_dx, ox);
-            }
-        }
+    };
+    if (plain)
+        rows(std::true_type{});
+    else
+        rows(std::false_type{});
 }
 
 // Before a pass: no word of the chain is there and no place is taken; and a
 // sequence without rows ends with the state that it starts from (backward:
-// hands its end's gradient to its start), which a wavefront does for 64 of them.
+// hands its end's gradient to its start), which a wavefront does for 8 of them.
+constexpr int kSeqs = 8;
 __global__ __launch_bounds__(256) void k_scan_begin(Seqs q, int32_t D,
                                                     const float *__restrict__ from, float *to,
                                                     uint64_t *words, int64_t n, int32_t *ticket,
@@ -514,10 +748,10 @@ __global__ __launch_bounds__(256) void k_scan_begin(Seqs q, int32_t D,
     if (!to)
         return;
     const int lane = threadIdx.x & 63;
-    for (int64_t s0 = id - lane; s0 < q.S; s0 += threads) {
+    for (int64_t s0 = (id >> 6) * kSeqs; s0 < q.S; s0 += (threads >> 6) * kSeqs) {
         const int64_t s = s0 + lane;
         bool none = false;
-        if (s < q.S) {
+        if (lane < kSeqs && s < q.S) {
             none = q.offsets ? q.offsets[s + 1] <= q.offsets[s] : q.L == 0;
             none |= q.length && q.length[s] <= 0;
         }
@@ -619,21 +853,22 @@ int pick_width(int32_t D, int want, int32_t *width)
     return 1;
 }
 
-template <class T, int V, bool BWD> tgm_status_t launch_scan(const ScanArgs &A, hipStream_t s)
+template <class T, int V, int W, bool BWD>
+tgm_status_t launch_scan(const ScanArgs &A, hipStream_t s)
 {
-    // a runner more for every chain
-    const dim3 grid((uint32_t)(((int64_t)A.groups + (A.ticket ? 1 : 0)) * A.blocks));
-    const dim3 block(64 * kWaves);
-    if (BWD) {
+    // and the chains' runners
+    const dim3 grid((uint32_t)(((int64_t)A.groups + (A.ticket ? V : 0)) * A.blocks));
+    const dim3 block(64 * W);
+    if constexpr (BWD) {
         if (A.q.per)
-            TGM_LAUNCH((k_scan_bwd<T, V, true>), grid, block, 0, s, A);
+            TGM_LAUNCH((k_scan_bwd<T, V, W, true>), grid, block, 0, s, A);
         else
-            TGM_LAUNCH((k_scan_bwd<T, V, false>), grid, block, 0, s, A);
+            TGM_LAUNCH((k_scan_bwd<T, V, W, false>), grid, block, 0, s, A);
     } else {
         if (A.q.per)
-            TGM_LAUNCH((k_scan<T, V, true>), grid, block, 0, s, A);
+            TGM_LAUNCH((k_scan<T, V, W, true>), grid, block, 0, s, A);
         else
-            TGM_LAUNCH((k_scan<T, V, false>), grid, block, 0, s, A);
+            TGM_LAUNCH((k_scan<T, V, W, false>), grid, block, 0, s, A);
     }
     return TGM_OK;
 }
@@ -645,16 +880,16 @@ size_t chain_bytes(int64_t groups, int64_t D) { return (size_t)groups * D * 16 +
 template <class T, bool BWD>
 tgm_status_t run_scan(ScanArgs A, void *work, size_t work_bytes, hipStream_t s)
 {
-    // a lane of fp32 pairs would hold more rows than registers in the gradient
-    const int V = pick_width(A.D, BWD && sizeof(T) == 4 ? 1 : 2, &A.width);
+    const int V = pick_width(A.D, sizeof(T) == 4 ? 1 : 2, &A.width);
+    constexpr int W = BWD ? kWavesBwd : kWaves;
     A.blocks = (int32_t)cdiv(A.D, A.width);
-    A.groups = (int32_t)cdiv(A.q.tiles, kWaves);
-    if (((int64_t)A.groups + 1) * A.blocks >= kMaxGrid)
+    A.groups = (int32_t)cdiv(A.q.tiles, W);
+    if (((int64_t)A.groups + 2) * A.blocks >= kMaxGrid)
         return TGM_EINVAL;
     if (A.q.rows) {
         if (!work || ((uintptr_t)work & 15))
             return TGM_EINVAL;
-        if (work_bytes < chain_bytes(cdiv(most_tiles(A.q.rows, A.q.S), kWaves), A.D))
+        if (work_bytes < chain_bytes(cdiv(most_tiles(A.q.rows, A.q.S), kWavesBwd), A.D))
             return TGM_ESIZE;
     }
     int64_t words = 0;
@@ -666,14 +901,17 @@ tgm_status_t run_scan(ScanArgs A, void *work, size_t work_bytes, hipStream_t s)
     }
     const bool empty = A.h_last && A.q.S && (A.q.offsets || A.q.length || A.q.L == 0);
     if (words || empty) {
-        const int64_t wg = std::min<int64_t>(cdiv(std::max<int64_t>(words, A.q.S), 256), 2048);
+        const int64_t wg = std::min<int64_t>(cdiv(std::max<int64_t>(words, empty ? A.q.S * (int64_t)(64 / kSeqs) : 0), 256), 2048);
         TGM_LAUNCH(k_scan_begin, dim3((uint32_t)wg), dim3(256), 0, s, A.q, A.D,
                    BWD ? A.last : A.h0, empty ? A.h_last : nullptr, A.maps, words, A.ticket,
                    A.blocks);
     }
     if (!A.q.tiles)
         return TGM_OK;
-    return V == 2 ? launch_scan<T, 2, BWD>(A, s) : launch_scan<T, 1, BWD>(A, s);
+    if constexpr (sizeof(T) == 2)
+        if (V == 2)
+            return launch_scan<T, 2, W, BWD>(A, s);
+    return launch_scan<T, 1, W, BWD>(A, s);
 }
 
 tgm_status_t scan_args(const tgm_scan_desc *d, const void *g, const void *x,
@@ -717,7 +955,7 @@ extern "C" tgm_status_t tgm_scan_work_bytes(int64_t rows, int32_t D, int32_t S, 
     const int64_t n = most_tiles(rows, S);
     if (!bytes || n < 0 || D < 1 || D > kMaxD)
         return TGM_EINVAL;
-    *bytes = n ? chain_bytes(cdiv(n, kWaves), D) : 0;
+    *bytes = n ? chain_bytes(cdiv(n, kWavesBwd), D) : 0;
     return TGM_OK;
 }
 
