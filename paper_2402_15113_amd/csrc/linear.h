@@ -103,58 +103,126 @@ struct LinearOut {
     const int32_t *n_rows;  // bounds M where given
 };
 
-// Columns n .. n + 3 of row m from their sums.
-template <class O> __device__ __forceinline__ void finish(const LinearOut &o, int64_t m, int32_t n, f4 c)
-{
-    float v[4] = {c.x, c.y, c.z, c.w};
-    const int left = o.N - n;
-    if (o.sm) {
-        const float s = o.sm[m];
+// W neighbouring columns of C, from n on: what they share in every row, and their
+// results in row m.  `left` of them exist (all of them if that is W or more).
+template <class O, int W> struct Columns {
+    float bias[W], scale[W];
+    int left;
+
+    __device__ __forceinline__ void load(const LinearOut &o, int32_t n)
+    {
+        left = o.N - n;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < left)
-                v[j] *= s * o.sn[n + j];
-    }
-    const O *bias = (const O *)o.bias + n, *res = (const O *)o.res + m * o.ld_res + n;
-    O *z = (O *)o.z + m * o.ld_z + n, *y = (O *)o.y + m * o.ld_y + n;
-    if (left >= 4) {
-        Pack<O, 4> p;
-        if (o.bias) {
-            p = load_pack<O, 4>(bias);
+        for (int j = 0; j < W; ++j)
+            bias[j] = 0.f, scale[j] = 1.f;
+        if (left >= W) {
+            if (o.bias) {
+                const Pack<O, W> p = load_wide((const O *)o.bias + n);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                v[j] += to_f32(p.v[j]);
-        }
-        if (o.z) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                p.v[j] = from_f32<O>(v[j]);
-            store_pack(z, p);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            v[j] = act_of(v[j], o.act);
-        if (o.res) {
-            p = load_pack<O, 4>(res);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                v[j] += to_f32(p.v[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            p.v[j] = from_f32<O>(v[j]);
-        store_pack(y, p);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 3; ++j)
-            if (j < left) {
-                float u = v[j] + (o.bias ? to_f32(bias[j]) : 0.f);
-                if (o.z)
-                    z[j] = from_f32<O>(u);
-                u = act_of(u, o.act) + (o.res ? to_f32(res[j]) : 0.f);
-                y[j] = from_f32<O>(u);
+                for (int j = 0; j < W; ++j)
+                    bias[j] = to_f32(p.v[j]);
             }
+            if (o.sn)
+#pragma unroll
+                for (int j = 0; j < W; j += 4) {
+                    const Pack<float, 4> p = load_pack<float, 4>(o.sn + n + j);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        scale[j + i] = p.v[i];
+                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j)
+                if (j < left) {
+                    if (o.bias)
+                        bias[j] = to_f32(((const O *)o.bias)[n + j]);
+                    if (o.sn)
+                        scale[j] = o.sn[n + j];
+                }
+        }
     }
+    __device__ __forceinline__ Pack<O, W> residual(const LinearOut &o, int64_t m, int32_t n) const
+    {
+        const O *res = (const O *)o.res + m * o.ld_res + n;
+        if (left >= W)
+            return load_wide(res);
+        Pack<O, W> p;
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j)
+            if (j < left)
+                p.v[j] = res[j];
+        return p;
+    }
+    // v: the sums; sm: the row's scale
+    __device__ __forceinline__ void finish(const LinearOut &o, int64_t m, int32_t n, float (&v)[W],
+                                           float sm, const Pack<O, W> &res) const
+    {
+        Pack<O, W> p;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            if (o.sm)
+                v[j] *= sm * scale[j];
+            v[j] += bias[j];
+            p.v[j] = from_f32<O>(v[j]);
+        }
+        if (o.z)
+            store((O *)o.z + m * o.ld_z + n, p);
+        if (o.act != TGM_ACT_NONE)
+#pragma unroll
+            for (int j = 0; j < W; ++j)
+                v[j] = act_of(v[j], o.act);
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            p.v[j] = from_f32<O>(o.res ? v[j] + to_f32(res.v[j]) : v[j]);
+        store((O *)o.y + m * o.ld_y + n, p);
+    }
+
+private:
+    // 16 bytes a load and store at most
+    static constexpr int PART = sizeof(O) * W <= 16 ? W : 16 / (int)sizeof(O);
+    static __device__ __forceinline__ Pack<O, W> load_wide(const O *from)
+    {
+        Pack<O, W> p;
+#pragma unroll
+        for (int j = 0; j < W; j += PART) {
+            const Pack<O, PART> q = load_pack<O, PART>(from + j);
+#pragma unroll
+            for (int i = 0; i < PART; ++i)
+                p.v[j + i] = q.v[i];
+        }
+        return p;
+    }
+    __device__ __forceinline__ void store(O *to, const Pack<O, W> &p) const
+    {
+        if (left >= W) {
+#pragma unroll
+            for (int j = 0; j < W; j += PART) {
+                Pack<O, PART> q;
+#pragma unroll
+                for (int i = 0; i < PART; ++i)
+                    q.v[i] = p.v[j + i];
+                store_pack(to + j, q);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j)
+                if (j < left)
+                    to[j] = p.v[j];
+        }
+    }
+};
+
+// Columns n .. n + 3 of row m from their sums.
+template <class O>
+__device__ __forceinline__ void finish(const LinearOut &o, int64_t m, int32_t n, f4 c)
+{
+    Columns<O, 4> q;
+    q.load(o, n);
+    Pack<O, 4> res;
+    if (o.res)
+        res = q.residual(o, m, n);
+    float v[4] = {c.x, c.y, c.z, c.w};
+    q.finish(o, m, n, v, o.sm ? o.sm[m] : 1.f, res);
 }
 
 // C[m, n] = sum_k P(n, k) Q(m, k), C of o.M rows and o.N columns.
@@ -175,7 +243,12 @@ tgm_status_t linear_tile_bf16(const LinearProduct &p, int which, int out);
 tgm_status_t linear_tile_f16(const LinearProduct &p, int which, int out);
 tgm_status_t linear_tile_e4m3(const LinearProduct &p, int which, int out);
 
-// Parts that the sum of a product of this size and type is split into.
-int linear_splits(int64_t M, int64_t N, int64_t K, int code);
+// The tile of a product and the parts that its sum is split into, by its size and
+// type.
+struct LinearPlan {
+    bool large;
+    int parts;
+};
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int code);
 
 }  // namespace tgm

@@ -20,58 +20,80 @@ namespace {
 
 constexpr int kMaxDim = 1 << 20;
 
-// ---------------------------------------------------------------- operands from memory
-// Element (c, k) lies at X[c ld + k] (KC) or X[k ld + c].
-template <class T, bool KC>
-__device__ __forceinline__ Frag<T> load_frag(const T *X, int64_t ld, int64_t c, int64_t k,
-                                             int64_t K)
+// ---------------------------------------------------------------- few rows
+// 16 bytes of an operand's row from k on; zeros from K on.
+template <class T> __device__ __forceinline__ Frag<T> load_frag(const T *row, int32_t k, int32_t K)
 {
     constexpr int VEC = Frag<T>::VEC;
     Frag<T> f;
-    if (KC && k + VEC <= K) {
-        f.v = load_pack<T, VEC>(X + c * ld + k);
+    if (k + VEC <= K) {
+        f.v = load_pack<T, VEC>(row + k);
         return f;
     }
     __builtin_memset(&f, 0, sizeof(f));
 #pragma unroll
     for (int j = 0; j < VEC; ++j)
         if (k + j < K)
-            f.v.v[j] = KC ? X[c * ld + k + j] : X[(k + j) * ld + c];
+            f.v.v[j] = row[k + j];
     return f;
 }
 
-// A workgroup takes 16 columns and 16 MB rows of C; its wavefronts share the
-// sum and add up through LDS.  Operands come straight from memory.
-template <class T, class O, bool PK, bool QK, int MB, int W>
+// Few rows: bound by reading W once.  A workgroup takes 16 columns and 16 MB rows of
+// C; its wavefronts share the sum, each a run of it, and add up through LDS.
+// Operands come straight from memory into the matrix instructions, eight loads of
+// a row of W at a time.
+template <class T, class O, int MB, int W>
 __global__ __launch_bounds__(64 * W) void k_linear_few(const T *__restrict__ P,
                                                        const T *__restrict__ Q, int64_t ld_p,
                                                        int64_t ld_q, int32_t K, LinearOut o,
-                                                       const int32_t *k_rows)
+                                                       int32_t tn)
 {
-    constexpr int VEC = Frag<T>::VEC;
+    constexpr int VEC = Frag<T>::VEC, STEP = 4 * VEC, AHEAD = MB == 1 ? 8 : 4;
     __shared__ f4 lds[W][MB][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r = lane & 15, q = lane >> 4;
     const int32_t M = rows_in_use(o.M, o.n_rows);
-    K = rows_in_use(K, k_rows);
-    const int32_t n0 = blockIdx.x * 16, m0 = blockIdx.y * (16 * MB);
+    const int32_t n0 = (int32_t)(blockIdx.x % tn) * 16, m0 = (int32_t)(blockIdx.x / tn) * (16 * MB);
     if (m0 >= M)
         return;
-    const int32_t n = min(n0 + r, o.N - 1);
+    const T *p = P + (int64_t)min(n0 + r, o.N - 1) * ld_p;
+    const T *x[MB];
     f4 acc[MB];
 #pragma unroll
-    for (int b = 0; b < MB; ++b)
+    for (int b = 0; b < MB; ++b) {
+        x[b] = Q + (int64_t)min(m0 + 16 * b + r, M - 1) * ld_q;
         acc[b] = f4{0.f, 0.f, 0.f, 0.f};
-    for (int32_t k = (w * 4 + q) * VEC; k - q * VEC < K; k += W * 4 * VEC) {
-        const Frag<T> p = load_frag<T, PK>(P, ld_p, n, k, K);
+    }
+    const int32_t steps = (K + STEP - 1) / STEP, per = (steps + W - 1) / W;
+    const int32_t s1 = min(steps, (w + 1) * per);
+    auto multiply = [&](const Frag<T> &f, const Frag<T> &g, int b) __attribute__((always_inline)) {
+        if constexpr (sizeof(T) == 1 && sizeof(O) == 4)
+            acc[b] = mfma_wide(f, g, acc[b]);
+        else
+            acc[b] = mfma(f, g, acc[b]);
+    };
+    int32_t s = w * per;
+    for (; s + AHEAD <= s1 && (s + AHEAD) * STEP <= K; s += AHEAD) {
+        Frag<T> f[AHEAD], g[AHEAD][MB];
 #pragma unroll
-        for (int b = 0; b < MB; ++b) {
-            const int32_t m = min(m0 + 16 * b + r, M - 1);
-            const Frag<T> f = load_frag<T, QK>(Q, ld_q, m, k, K);
-            if constexpr (sizeof(T) == 1 && sizeof(O) == 4)
-                acc[b] = mfma_wide(p, f, acc[b]);
-            else
-                acc[b] = mfma(p, f, acc[b]);
+        for (int u = 0; u < AHEAD; ++u) {
+            const int32_t k = (s + u) * STEP + q * VEC;
+            f[u].v = load_pack<T, VEC>(p + k);
+#pragma unroll
+            for (int b = 0; b < MB; ++b)
+                g[u][b].v = load_pack<T, VEC>(x[b] + k);
         }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int b = 0; b < MB; ++b)
+                multiply(f[u], g[u][b], b);
+    }
+    for (; s < s1; ++s) {
+        const int32_t k = s * STEP + q * VEC;
+        const Frag<T> f = load_frag<T>(p, k, K);
+#pragma unroll
+        for (int b = 0; b < MB; ++b)
+            multiply(f, load_frag<T>(x[b], k, K), b);
     }
 #pragma unroll
     for (int b = 0; b < MB; ++b)
@@ -90,35 +112,64 @@ __global__ __launch_bounds__(64 * W) void k_linear_few(const T *__restrict__ P,
 
 // ---------------------------------------------------------------- dz and db
 // dz = dy act'(z) (stored where `dz` is given) and, with `part`, partial
-// column sums of it: a workgroup takes 64 columns and every gridDim.y-th set
-// of 4 rows.
-template <class T>
+// column sums of it: a wavefront takes 64 vectors of VEC columns and every 4
+// gridDim.y-th row.  A last vector of fewer columns moves back to end at the edge;
+// its first columns are counted by the one before.
+template <class T, int VEC>
 __global__ __launch_bounds__(256) void k_linear_dz(const T *__restrict__ dy,
                                                    const T *__restrict__ z,
                                                    const int32_t *n_rows, T *__restrict__ dz,
                                                    float *__restrict__ part, int32_t rows,
                                                    int32_t N, int64_t ld_y, int64_t ld_z, int act)
 {
-    __shared__ float lds[4][64];
+    constexpr int AHEAD = 4;
+    __shared__ float lds[4][64 * VEC];
     const int32_t R = rows_in_use(rows, n_rows);
     const int c = threadIdx.x & 63, r = threadIdx.x >> 6;
-    const int32_t n = blockIdx.x * 64 + c;
-    float sum = 0.f;
-    if (n < N)
-        for (int64_t m = (int64_t)blockIdx.y * 4 + r; m < R; m += (int64_t)gridDim.y * 4) {
-            float v = to_f32(dy[m * ld_y + n]);
-            if (act != TGM_ACT_NONE)
-                v *= act_grad(to_f32(z[m * ld_z + n]), act);
-            if (dz)
-                dz[m * N + n] = from_f32<T>(v);
-            sum += v;
+    const int32_t e = (int32_t)(blockIdx.x * 64 + c) * VEC, n = min(e, N - VEC);
+    float sum[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j)
+        sum[j] = 0.f;
+    const int64_t by = (int64_t)gridDim.y * 4;
+    if (e < N)
+        for (int64_t m0 = (int64_t)blockIdx.y * 4 + r; m0 < R; m0 += AHEAD * by) {
+            Pack<T, VEC> py[AHEAD], pz[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t m = min(m0 + u * by, (int64_t)R - 1);
+                py[u] = load_pack<T, VEC>(dy + m * ld_y + n);
+                if (act != TGM_ACT_NONE)
+                    pz[u] = load_pack<T, VEC>(z + m * ld_z + n);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (m0 + u * by < R) {
+                    Pack<T, VEC> po;
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) {
+                        float v = to_f32(py[u].v[j]);
+                        if (act != TGM_ACT_NONE)
+                            v *= act_grad(to_f32(pz[u].v[j]), act);
+                        po.v[j] = from_f32<T>(v);
+                        sum[j] += v;
+                    }
+                    if (dz)
+                        store_pack(dz + (m0 + u * by) * N + n, po);
+                }
         }
     if (!part)
         return;
-    lds[r][c] = sum;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j)
+        lds[r][c * VEC + j] = sum[j];
     __syncthreads();
-    if (r == 0 && n < N)
-        part[(int64_t)blockIdx.y * N + n] = lds[0][c] + lds[1][c] + lds[2][c] + lds[3][c];
+    for (int i = threadIdx.x; i < 64 * VEC; i += 256) {
+        const int32_t e0 = (int32_t)(blockIdx.x * 64 + i / VEC) * VEC;
+        const int32_t at = min(e0, N - VEC) + i % VEC;
+        if (e0 < N && i % VEC >= e0 - min(e0, N - VEC))
+            part[(int64_t)blockIdx.y * N + at] = lds[0][i] + lds[1][i] + lds[2][i] + lds[3][i];
+    }
 }
 
 template <class T>
@@ -130,6 +181,7 @@ __global__ __launch_bounds__(1024) void k_linear_db(const float *__restrict__ pa
     const int32_t n = blockIdx.x * 32 + c;
     float a = 0.f;
     if (n < N)
+#pragma unroll 8
         for (int p = r; p < P; p += 32)
             a += part[(int64_t)p * N + n];
     lds[r][c] = a;
@@ -142,20 +194,26 @@ __global__ __launch_bounds__(1024) void k_linear_db(const float *__restrict__ pa
 }
 
 // ---------------------------------------------------------------- host
-template <class T, class O, bool PK, bool QK, int MB> tgm_status_t few(const LinearProduct &p)
+template <class T, class O, int MB> tgm_status_t few(const LinearProduct &p)
 {
-    constexpr int W = 4;
-    TGM_LAUNCH((k_linear_few<T, O, PK, QK, MB, W>),
-               dim3((uint32_t)cdiv(p.o.N, 16), (uint32_t)cdiv(p.o.M, 16 * MB)), dim3(64 * W), 0,
-               p.s, (const T *)p.P, (const T *)p.Q, p.ld_p, p.ld_q, p.K, p.o, p.k_rows);
+    constexpr int W = 8;
+    const int64_t tn = cdiv(p.o.N, 16), wg = tn * cdiv(p.o.M, 16 * MB);
+    TGM_LAUNCH((k_linear_few<T, O, MB, W>), dim3((uint32_t)wg), dim3(64 * W), 0, p.s,
+               (const T *)p.P, (const T *)p.Q, p.ld_p, p.ld_q, p.K, p.o, (int32_t)tn);
     return TGM_OK;
 }
+
+// Up to how many rows k_linear_few takes a forward product.
+constexpr int kFewRows = 64;
+
 template <class T, class O, bool PK, bool QK> tgm_status_t product(const LinearProduct &p)
 {
-    if (p.o.M <= 16)
-        return few<T, O, PK, QK, 1>(p);
-    if (p.o.M <= 64)
-        return few<T, O, PK, QK, 4>(p);
+    if constexpr (PK && QK) {
+        if (p.o.M <= 16)
+            return few<T, O, 1>(p);
+        if (p.o.M <= kFewRows)
+            return few<T, O, 4>(p);
+    }
     constexpr int which = PK ? 0 : QK ? 1 : 2, out = TypeCode<O>::code;
     if constexpr (sizeof(T) == 4)
         return linear_tile_f32(p, which, out);
@@ -170,11 +228,13 @@ template <class T, class O, bool PK, bool QK> tgm_status_t product(const LinearP
 // Bytes that the parts of a product need.
 size_t split_bytes(int64_t M, int64_t N, int64_t K, int code)
 {
-    const int parts = M <= 64 ? 1 : linear_splits(M, N, K, code);
+    if (M <= 0 || K <= 0)
+        return 0;
+    const int parts = linear_plan(M, N, K, code).parts;
     return parts == 1 ? 0 : (size_t)parts * M * ((N + 3) / 4 * 4) * 4;
 }
 
-constexpr int kDbParts = 64;
+constexpr int kDbParts = 128;
 
 // The work space of the gradient: dz, the partial sums of db, then those of a product.
 size_t db_bytes(int32_t rows, int32_t N)
@@ -197,9 +257,14 @@ tgm_status_t backward(const tgm_linear_desc *d, const int64_t *ld, const void *x
     float *split = (float *)(work + zb + db_bytes(d->rows, d->N));
     const int32_t parts = (int32_t)std::min<int64_t>(cdiv(d->rows, 4), kDbParts);
     if ((dz || db) && parts) {
-        TGM_LAUNCH((k_linear_dz<T>), dim3((uint32_t)cdiv(d->N, 64), parts), dim3(256), 0, s,
-                   (const T *)dy, (const T *)z, n_rows, dz, db ? part : nullptr, d->rows, d->N,
-                   ld[4], ld[3], d->act);
+        constexpr int VEC = 16 / (int)sizeof(T);
+        const dim3 grid((uint32_t)cdiv(d->N, 64 * (d->N < VEC ? 1 : VEC)), parts);
+        if (d->N < VEC)
+            TGM_LAUNCH((k_linear_dz<T, 1>), grid, dim3(256), 0, s, (const T *)dy, (const T *)z,
+                       n_rows, dz, db ? part : nullptr, d->rows, d->N, ld[4], ld[3], d->act);
+        else
+            TGM_LAUNCH((k_linear_dz<T, VEC>), grid, dim3(256), 0, s, (const T *)dy, (const T *)z,
+                       n_rows, dz, db ? part : nullptr, d->rows, d->N, ld[4], ld[3], d->act);
     }
     if (db)
         TGM_LAUNCH((k_linear_db<T>), dim3((uint32_t)cdiv(d->N, 32)), dim3(1024), 0, s, part, parts,
@@ -244,11 +309,29 @@ tgm_status_t check_work(size_t need, const void *work, size_t bytes)
 
 }  // namespace
 
-int tgm::linear_splits(int64_t M, int64_t N, int64_t K, int code)
+// A sum is split as far as there are CUs for the parts and 8 steps of 128 bytes for
+// each.  Of the two tiles the large one is taken where its busiest CU has no more
+// to multiply than with the small ones, its sums are whole and (16 and 8 bits) at
+// least 32 steps long: a CU holds one of it, so that nothing hides how a tile begins
+// and ends.  Large against small, us, bf16: 16,384 x 4,096 x 8,192: 857, 966; 8,192 x
+// 4,096 x 4,096: 229, 288; 4,096 x 4,096 x 4,096: 130, 140; but 8,192 x 8,192 x 1,024: 169,
+// 161; 2,048 x 2,048 x 2,048 (in 4 parts): 39, 33.  fp32, where the matrix cores
+// take 16 times as long: 4,096 x 2,048 x 1,024: 132, 141; 12,000 x 200 x 472: 47, 34.
+LinearPlan tgm::linear_plan(int64_t M, int64_t N, int64_t K, int code)
 {
-    const int64_t tiles = code == TGM_F32 ? cdiv(M, 64) * cdiv(N, 128) : cdiv(M, 256) * cdiv(N, 256);
+    const bool f32 = code == TGM_F32;
     const int64_t steps = cdiv(K * elem_bytes(code), 128);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, steps / 8));
+    const int64_t side = f32 ? 128 : 256, half = side / 2;
+    const int64_t large = cdiv(M, side) * cdiv(N, side), small = cdiv(M, half) * cdiv(N, half);
+    if (cdiv(large, 256) * 4 <= cdiv(small, 256) && large >= (f32 ? 512 : 192) &&
+        (f32 || steps >= 32))
+        return LinearPlan{true, 1};
+    // half as many large tiles as CUs, and a sum that is long in halves too: the weights'
+    // gradient of 8,192 rows of a 4,096 x 2,048 layer, 147 us against 156
+    if (!f32 && large >= 96 && large <= 128 && steps >= 128)
+        return LinearPlan{true, 2};
+    return LinearPlan{
+        false, (int)std::max<int64_t>(1, std::min<int64_t>({512 / small, steps / 8, 64}))};
 }
 
 extern "C" tgm_status_t tgm_linear_work_bytes(int32_t rows, int32_t N, int32_t K, int32_t dtype,

@@ -1,19 +1,25 @@
 // The tiled product of tgm_linear: C[m, n] = sum_k P(n, k) Q(m, k).
 //
 // A workgroup takes BN columns and BM rows of C.  The sum goes in steps of 128
-// bytes of an operand's row (64 elements of 16 bits), two steps' tiles in LDS:
-// while one is multiplied the next one arrives.  Bound by the matrix cores for
-// large products; a step of a 256 x 256 tile reads LDS for about three quarters
-// of the time that its matrix instructions take.
+// bytes of an operand's row (64 elements of 16 bits), two steps' tiles in LDS.  A
+// step has two halves, each with its fragments in registers: while one half is
+// multiplied the other half's fragments (or the next step's first) are read, and
+// the tile that was read last is refilled, a piece after every few matrix
+// instructions: a wavefront issues in order, and LDS takes all wavefronts' reads of
+// a half at 4 cycles each, so that reads issued at once left the matrix cores idle
+// for half of the time.  Bound by the matrix cores for large products.
 #pragma once
 
 #include <algorithm>
+#include <type_traits>
 
 #include "linear.h"
 
 namespace tgm {
 
 typedef short s4v __attribute__((ext_vector_type(4)));
+typedef int i8v __attribute__((ext_vector_type(8)));
+typedef float f16v __attribute__((ext_vector_type(16)));
 
 // An operand's tile in LDS: X elements along the output, 128 bytes along the sum.
 // KC (contiguous along the sum): X rows of 128 bytes; else a row of X elements for
@@ -41,7 +47,7 @@ template <class T, bool KC, int X> struct LdsTile {
         return row * PITCH + ((chunk ^ turn(row)) << 4);
     }
 
-    // The fragment of rows (columns) x0 .. x0 + 15 and the c-th 64 bytes of the sum.
+    // The fragment of rows (columns) x0 .. x0 + 15 in half c of the step.
     static __device__ __forceinline__ Frag<T> read(const char *lds, int x0, int c)
     {
         const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
@@ -69,6 +75,18 @@ template <class T, bool KC, int X> struct LdsTile {
         }
         return f;
     }
+    // For the 32 x 32 x 64 instruction of 8-bit values: rows x0 .. x0 + 31, 32 bytes a
+    // lane.
+    static __device__ __forceinline__ i8v read32(const char *lds, int x0, int c)
+    {
+        const int lane = threadIdx.x & 63, i = lane & 31, q = lane >> 5;
+        typedef int i4v __attribute__((ext_vector_type(4)));
+        const i4v a = *reinterpret_cast<const i4v *>(
+            __builtin_assume_aligned(lds + at(x0 + i, 4 * c + q), 16));
+        const i4v b = *reinterpret_cast<const i4v *>(
+            __builtin_assume_aligned(lds + at(x0 + i, 4 * c + q + 2), 16));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
 };
 
 // One operand on its way into LDS.  DIRECT: 16 bytes a lane straight into LDS,
@@ -78,14 +96,15 @@ template <class T, bool KC, int X, int TH, bool DIRECT> struct Operand {
     using Lds = LdsTile<T, KC, X>;
     static constexpr int VEC = Lds::VEC, BK = Lds::BK;
     static constexpr int NR = (Lds::ROWS * Lds::CHUNKS + TH - 1) / TH;   // chunks a thread
-    static constexpr int ND = Lds::BYTES / (TH * 16);                    // direct loads a thread
-    static_assert(!DIRECT || Lds::BYTES % (TH * 16) == 0, "");
+    static constexpr int ND = (Lds::BYTES + TH * 16 - 1) / (TH * 16);    // direct loads a thread
+    static_assert(Lds::BYTES % 1024 == 0, "");
 
     const T *base;
     int64_t ld;
     int32_t x0, n;              // the tile's first row (column) and how many the operand has
     uint32_t off[DIRECT ? ND : 1];
-    Pack<T, VEC> v[DIRECT ? 1 : NR];
+    using PackT = Pack<T, VEC>;
+    PackT v[DIRECT ? 1 : NR];
 
     __device__ __forceinline__ void init(const T *p, int64_t ld_, int32_t x0_, int32_t n_)
     {
@@ -102,61 +121,58 @@ template <class T, bool KC, int X, int TH, bool DIRECT> struct Operand {
                                   16u * c
                             : (uint32_t)row * (uint32_t)(ld * sizeof(T)) +
                                   (uint32_t)(min(x0 + c * VEC, n - VEC) - x0) * (uint32_t)sizeof(T);
+                // a register of its own: a product's upper half would stay with it
+                asm volatile("" : "+v"(off[u]));
             }
         }
     }
-    // a whole step from k on into `lds`, without waiting for it
-    __device__ __forceinline__ void direct(char *lds, int64_t k) const
+    // the u-th of the ND loads of a whole step from k on into `lds`, without waiting
+    // for it; `from` as from_k(k)
+    __device__ __forceinline__ const char *from_k(int64_t k) const
     {
-        const char *from = reinterpret_cast<const char *>(KC ? base + (int64_t)x0 * ld + k
-                                                             : base + k * ld + x0);
-#pragma unroll
-        for (int u = 0; u < ND; ++u) {
-            const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds +
-                                1024u * (u * (TH / 64) +
-                                         __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)));
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                         :
-                         : "s"(to), "v"(off[u]), "s"(from)
-                         : "memory", "m0");
-        }
+        return reinterpret_cast<const char *>(KC ? base + (int64_t)x0 * ld + k
+                                                 : base + k * ld + x0);
     }
-    __device__ __forceinline__ Pack<T, VEC> chunk(int row, int c, int64_t k, int64_t K,
-                                                  bool whole) const
+    __device__ __forceinline__ void direct(char *lds, const char *from, int u) const
     {
-        Pack<T, VEC> r;
-        if (KC) {
-            const T *p = base + (int64_t)min(x0 + row, n - 1) * ld + k + c * VEC;
-            if (whole || k + (c + 1) * VEC <= K)
-                return load_pack<T, VEC>(p);
-            __builtin_memset(&r, 0, sizeof(r));
-#pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (k + c * VEC + j < K)
-                    r.v[j] = p[j];
-        } else {
-            const int32_t x = x0 + c * VEC;
-            const T *p = base + (k + row) * ld + x;
-            if ((whole || k + row < K) && x + VEC <= n)
-                return load_pack<T, VEC>(p);
-            __builtin_memset(&r, 0, sizeof(r));
-            if (whole || k + row < K)
-#pragma unroll
-                for (int j = 0; j < VEC; ++j)
-                    if (x + j < n)
-                        r.v[j] = p[j];
-        }
-        return r;
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds +
+                            1024u * (u * (TH / 64) +
+                                     __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)));
+        if (Lds::BYTES % (TH * 16) && u == ND - 1 &&
+            1024 * (u * (TH / 64) + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6))) >=
+                Lds::BYTES)
+            return;   // a wavefront past the tile's end
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                     :
+                     : "s"(to), "v"(off[u]), "s"(from)
+                     : "memory", "m0");
     }
-    // the step from k on (up to K: zeros past it) through registers
-    __device__ __forceinline__ void load(int64_t k, int64_t K)
+    // Whether a step from k on can be loaded by vectors: a whole one, of rows that hold
+    // one.  Others go by elements (tail).
+    __device__ __forceinline__ bool by_vectors(int64_t k, int64_t K) const
     {
-        const bool whole = k + BK <= K;
+        return k + BK <= K && (KC || n >= VEC);
+    }
+    __device__ __forceinline__ void load(int64_t k)
+    {
         if constexpr (!DIRECT) {
 #pragma unroll
             for (int u = 0; u < NR; ++u) {
                 const int e = min(u * TH + (int)threadIdx.x, Lds::ROWS * Lds::CHUNKS - 1);
-                v[u] = chunk(e / Lds::CHUNKS, e % Lds::CHUNKS, k, K, whole);
+                const int row = e / Lds::CHUNKS, x = x0 + e % Lds::CHUNKS * VEC;
+                if (KC) {
+                    v[u] = load_pack<T, VEC>(base + (int64_t)min(x0 + row, n - 1) * ld + k +
+                                             e % Lds::CHUNKS * VEC);
+                } else {
+                    // past the edge: the last vector, moved up to the columns asked for
+                    const int back = max(0, x - (n - VEC));
+                    v[u] = load_pack<T, VEC>(base + (k + row) * ld + (x - back));
+                    if (back)
+                        v[u] = __builtin_bit_cast(PackT, back < VEC
+                                   ? __builtin_bit_cast(unsigned __int128, v[u]) >>
+                                         (8 * (int)sizeof(T) * back)
+                                   : (unsigned __int128)0);
+                }
             }
         }
     }
@@ -172,28 +188,23 @@ template <class T, bool KC, int X, int TH, bool DIRECT> struct Operand {
             }
         }
     }
-    // the last, partial step at once
+    // the last, partial step at once, by elements: zeros past K
     __device__ __forceinline__ void tail(char *lds, int64_t k, int64_t K) const
     {
-        for (int e = threadIdx.x; e < Lds::ROWS * Lds::CHUNKS; e += TH)
-            *reinterpret_cast<Pack<T, VEC> *>(__builtin_assume_aligned(
-                lds + Lds::at(e / Lds::CHUNKS, e % Lds::CHUNKS), 16)) =
-                chunk(e / Lds::CHUNKS, e % Lds::CHUNKS, k, K, false);
+        constexpr int PER = KC ? BK : Lds::CHUNKS * VEC;   // elements of a row
+#pragma unroll 1
+        for (int e = threadIdx.x; e < Lds::ROWS * PER; e += TH) {
+            const int row = e / PER, i = e % PER;
+            const int64_t kk = k + (KC ? i : row);
+            T v;
+            __builtin_memset(&v, 0, sizeof(v));
+            if (kk < K)
+                v = KC ? base[(int64_t)min(x0 + row, n - 1) * ld + kk]
+                       : base[kk * ld + min(x0 + i, n - 1)];
+            *reinterpret_cast<T *>(lds + Lds::at(row, i / VEC) + i % VEC * (int)sizeof(T)) = v;
+        }
     }
 };
-
-__device__ __forceinline__ f4 mfma_e4m3(const Frag<e4m3> &p0, const Frag<e4m3> &p1,
-                                        const Frag<e4m3> &q0, const Frag<e4m3> &q1, f4 c)
-{
-    typedef int i8v __attribute__((ext_vector_type(8)));
-    struct Two {
-        Frag<e4m3> a, b;
-    };
-    // 128 k at once, at twice the rate of 32; block scales of 1 (the exponent 127)
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-        __builtin_bit_cast(i8v, Two{p0, p1}), __builtin_bit_cast(i8v, Two{q0, q1}), c, 0, 0, 0,
-        127, 0, 127);
-}
 
 // Which tile workgroup `id` takes: every XCD (id % 8) a run of neighbouring tiles,
 // 8 rows of tiles deep, so that its L2 holds what they share.
@@ -211,123 +222,292 @@ __device__ __forceinline__ TileAt tile_of(uint32_t id, int32_t tn, int32_t tm, i
     return TileAt{(int32_t)(r / deep), (int32_t)(band * 8 + r % deep), (int32_t)part};
 }
 
+// One half step's fragments of a wavefront, and their products.
+template <class T, class O, class LP, class LQ, int NA, int MA> struct Half {
+    Frag<T> p[NA], q[MA];
+    using Acc = f4;
+    static constexpr int SIDE = 16;
+    // piece a of NA
+    __device__ __forceinline__ void read(const char *lp, const char *lq, int wn, int wm, int c,
+                                         int a)
+    {
+        p[a] = LP::read(lp, wn + 16 * a, c);
+#pragma unroll
+        for (int b = a * MA / NA; b < (a + 1) * MA / NA; ++b)
+            q[b] = LQ::read(lq, wm + 16 * b, c);
+    }
+    // used: blocks of columns that C has (the others' products are left out)
+    __device__ __forceinline__ void multiply(Acc (&acc)[NA][MA], int a, int used) const
+    {
+        if constexpr (sizeof(T) == 4) {
+            // a quarter of the sum for every block: four instructions in a row on one
+            // block would wait for each other
+            static_assert(NA == 4, "");
+#pragma unroll
+            for (int i = 0; i < NA; ++i)
+                if (i < used)
+#pragma unroll
+                    for (int b = 0; b < MA; ++b)
+                        acc[i][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                            p[i].v.v[a], q[b].v.v[a], acc[i][b], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int b = 0; b < MA; ++b)
+                if constexpr (sizeof(T) == 1)
+                    acc[a][b] = mfma_wide(p[a], q[b], acc[a][b]);
+                else
+                    acc[a][b] = mfma(p[a], q[b], acc[a][b]);
+        }
+    }
+};
+// 8-bit operands: blocks of 32 x 32, 64 k an instruction, which runs at twice the rate
+// of those for 32 k.
+template <class T, class O, class LP, class LQ, int NA, int MA> struct Half8 {
+    i8v p[NA], q[MA];
+    using Acc = f16v;
+    static constexpr int SIDE = 32;
+    __device__ __forceinline__ void read(const char *lp, const char *lq, int wn, int wm, int c,
+                                         int a)
+    {
+        p[a] = LP::read32(lp, wn + 32 * a, c);
+#pragma unroll
+        for (int b = a * MA / NA; b < (a + 1) * MA / NA; ++b)
+            q[b] = LQ::read32(lq, wm + 32 * b, c);
+    }
+    __device__ __forceinline__ void multiply(Acc (&acc)[NA][MA], int a, int) const
+    {
+        // block scales of 1 (the exponent 127)
+#pragma unroll
+        for (int b = 0; b < MA; ++b)
+            acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                p[a], q[b], acc[a][b], 0, 0, 0, 127, 0, 127);
+    }
+};
+
 template <class T, class O, bool PK, bool QK, int BN, int BM, int NW, int MW, bool DIRECT>
-__global__ __launch_bounds__(64 * NW * MW) void k_linear_tile(
+__global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
     const T *__restrict__ P, const T *__restrict__ Q, int64_t ld_p, int64_t ld_q, int32_t K_,
     LinearOut o, const int32_t *k_rows, float *work, int32_t tn, int32_t tm, int32_t parts)
 {
-    constexpr int TH = 64 * NW * MW, NA = BN / NW / 16, MA = BM / MW / 16;
+    constexpr int TH = 64 * NW * MW;
+    constexpr bool BIG = sizeof(T) == 1 && sizeof(O) != 4;
+    constexpr int SIDE = BIG ? 32 : 16, NA = BN / NW / SIDE, MA = BM / MW / SIDE;
     using OP = Operand<T, PK, BN, TH, DIRECT>;
     using OQ = Operand<T, QK, BM, TH, DIRECT>;
+    using LP = typename OP::Lds;
+    using LQ = typename OQ::Lds;
+    using H = std::conditional_t<BIG, Half8<T, O, LP, LQ, NA, MA>, Half<T, O, LP, LQ, NA, MA>>;
     constexpr int BK = OP::BK;
-    __shared__ __attribute__((aligned(1024))) char lds[2][OP::Lds::BYTES + OQ::Lds::BYTES];
+    __shared__ __attribute__((aligned(1024))) char lds[2][LP::BYTES + LQ::BYTES];
     const TileAt t = tile_of(blockIdx.x, tn, tm, parts);
     const int32_t M = rows_in_use(o.M, o.n_rows), n0 = t.n * BN, m0 = t.m * BM;
     if (m0 >= M)
         return;
     const int64_t K = rows_in_use(K_, k_rows);
     const int64_t steps = (K + BK - 1) / BK, per = (steps + parts - 1) / parts;
-    const int64_t s0 = t.part * per, ns = max((int64_t)0, min(steps - s0, per));
+    const int64_t s0 = t.part * per;
+    const int32_t ns = (int32_t)max((int64_t)0, min(steps - s0, per));
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int wn = (w % NW) * (BN / NW), wm = (w / NW) * (BM / MW);
 
+    const int used = min(NA, (o.N - n0 - wn + SIDE - 1) / SIDE);
     OP p;
     OQ q;
     p.init(P, ld_p, n0, o.N);
     q.init(Q, ld_q, m0, M);
-    f4 acc[NA][MA];
+    typename H::Acc acc[NA][MA];
 #pragma unroll
     for (int a = 0; a < NA; ++a)
 #pragma unroll
         for (int b = 0; b < MA; ++b)
-            acc[a][b] = f4{0.f, 0.f, 0.f, 0.f};
+            acc[a][b] = typename H::Acc(0.f);
 
-    auto fill = [&](int64_t s) __attribute__((always_inline)) {   // direct
+    // Step s into its tile.  DIRECT: whole ones on their way, the tail at once; else
+    // into registers (fetch) and from there (put).
+    auto fill = [&](int32_t s) __attribute__((always_inline)) {
         const int64_t k = (s0 + s) * BK;
         char *to = lds[s & 1];
         if (k + BK <= K) {
-            p.direct(to, k);
-            q.direct(to + OP::Lds::BYTES, k);
+            const char *fp = p.from_k(k), *fq = q.from_k(k);
+#pragma unroll
+            for (int u = 0; u < OP::ND; ++u)
+                p.direct(to, fp, u);
+#pragma unroll
+            for (int u = 0; u < OQ::ND; ++u)
+                q.direct(to + LP::BYTES, fq, u);
         } else {
             p.tail(to, k, K);
-            q.tail(to + OP::Lds::BYTES, k, K);
+            q.tail(to + LP::BYTES, k, K);
+        }
+    };
+    auto fetch = [&](int32_t s) __attribute__((always_inline)) {
+        const int64_t k = (s0 + s) * BK;
+        if (p.by_vectors(k, K) && q.by_vectors(k, K))
+            p.load(k), q.load(k);
+    };
+    auto put = [&](int32_t s) __attribute__((always_inline)) {
+        const int64_t k = (s0 + s) * BK;
+        char *to = lds[s & 1];
+        if (p.by_vectors(k, K) && q.by_vectors(k, K)) {
+            p.store(to), q.store(to + LP::BYTES);
+        } else {
+            p.tail(to, k, K);
+            q.tail(to + LP::BYTES, k, K);
+        }
+    };
+    auto arrive = [&]() __attribute__((always_inline)) {
+        // by the builtin, which the compiler counts: behind an asm it would wait once
+        // more for what it has itself loaded before
+        if constexpr (DIRECT)
+            __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+        lds_barrier();
+    };
+    H h0, h1;
+    // Step s; NEXT: one follows; REFILL: a whole one follows that.
+    auto step = [&](int32_t s, auto next, auto refill) __attribute__((always_inline)) {
+        const char *lp = lds[s & 1];
+#pragma unroll
+        for (int a = 0; a < NA; ++a) {
+            h1.read(lp, lp + LP::BYTES, wn, wm, 1, a);
+            h0.multiply(acc, a, used);
+            issue_fence();
+        }
+        const char *ln = lds[(s + 1) & 1];
+        if constexpr (next) {
+            // the next step's tile is there, and no one reads this one's any more
+            if constexpr (!DIRECT)
+                put(s + 1);
+            arrive();
+            if constexpr (!refill)
+                if (s + 2 < ns) {
+                    if constexpr (DIRECT)
+                        fill(s + 2);
+                    else
+                        fetch(s + 2);
+                }
+        }
+        const int64_t k = (s0 + s + 2) * BK;
+        const char *fp = p.from_k(k), *fq = q.from_k(k);
+        char *to = lds[s & 1];
+#pragma unroll
+        for (int a = 0; a < NA; ++a) {
+            if constexpr (refill) {
+                constexpr int ND = OP::ND + OQ::ND;
+#pragma unroll
+                for (int u = a * ND / NA; u < (a + 1) * ND / NA; ++u)
+                    if (u < OP::ND)
+                        p.direct(to, fp, u);
+                    else
+                        q.direct(to + LP::BYTES, fq, u - OP::ND);
+            }
+            if constexpr (next)
+                h0.read(ln, ln + LP::BYTES, wn, wm, 0, a);
+            h1.multiply(acc, a, used);
+            issue_fence();
         }
     };
     if (ns > 0) {
         if constexpr (DIRECT) {
             fill(0);
         } else {
-            p.load(s0 * BK, K), q.load(s0 * BK, K);
-            p.store(lds[0]), q.store(lds[0] + OP::Lds::BYTES);
+            fetch(0);
+            put(0);
         }
-    }
-    for (int64_t s = 0; s < ns; ++s) {
-        // this step's tiles are there and no one reads the other ones any more
-        if constexpr (DIRECT)
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        lds_barrier();
-        if (s + 1 < ns) {
+        arrive();
+        if (ns > 1) {
             if constexpr (DIRECT)
-                fill(s + 1);
+                fill(1);
             else
-                p.load((s0 + s + 1) * BK, K), q.load((s0 + s + 1) * BK, K);
+                fetch(1);
         }
-        const char *lp = lds[s & 1], *lq = lp + OP::Lds::BYTES;
-        if constexpr (sizeof(T) == 1 && sizeof(O) != 4) {
-            Frag<T> fq[MA][2];
 #pragma unroll
-            for (int b = 0; b < MA; ++b)
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    fq[b][c] = OQ::Lds::read(lq, wm + 16 * b, c);
-#pragma unroll
-            for (int a = 0; a < NA; ++a) {
-                const Frag<T> f0 = OP::Lds::read(lp, wn + 16 * a, 0);
-                const Frag<T> f1 = OP::Lds::read(lp, wn + 16 * a, 1);
-#pragma unroll
-                for (int b = 0; b < MA; ++b)
-                    acc[a][b] = mfma_e4m3(f0, f1, fq[b][0], fq[b][1], acc[a][b]);
-            }
-        } else {
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                Frag<T> fq[MA];
-#pragma unroll
-                for (int b = 0; b < MA; ++b)
-                    fq[b] = OQ::Lds::read(lq, wm + 16 * b, c);
-#pragma unroll
-                for (int a = 0; a < NA; ++a) {
-                    const Frag<T> f = OP::Lds::read(lp, wn + 16 * a, c);
-#pragma unroll
-                    for (int b = 0; b < MA; ++b)
-                        if constexpr (sizeof(T) == 1)
-                            acc[a][b] = mfma_wide(f, fq[b], acc[a][b]);
-                        else
-                            acc[a][b] = mfma(f, fq[b], acc[a][b]);
-                }
-            }
+        for (int a = 0; a < NA; ++a)
+            h0.read(lds[0], lds[0] + LP::BYTES, wn, wm, 0, a);
+        using yes = std::true_type;
+        using no = std::false_type;
+        int32_t s = 0;
+        if constexpr (DIRECT) {
+            const int32_t whole = (int32_t)min((int64_t)ns, max((int64_t)0, K / BK - s0));
+            for (; s + 2 < whole; ++s)
+                step(s, yes{}, yes{});
         }
-        if constexpr (!DIRECT)
-            if (s + 1 < ns)
-                p.store(lds[(s + 1) & 1]), q.store(lds[(s + 1) & 1] + OP::Lds::BYTES);
+        for (; s + 1 < ns; ++s)
+            step(s, yes{}, no{});
+        step(s, no{}, no{});
     }
 
-    const int32_t wide = (o.N + 3) & ~3;
+    constexpr int LANES = SIDE, QUADS = BIG ? 4 : 1;
+    auto sums = [&](int a, int b, int u) __attribute__((always_inline)) {
+        if constexpr (BIG)
+            return f4{acc[a][b][4 * u], acc[a][b][4 * u + 1], acc[a][b][4 * u + 2],
+                      acc[a][b][4 * u + 3]};
+        else
+            return acc[a][b];
+    };
+    const int32_t n1 = n0 + wn + 4 * (lane / LANES), m1 = m0 + wm + lane % LANES;
+    if (work) {
+        const int32_t wide = (o.N + 3) & ~3;
 #pragma unroll
-    for (int b = 0; b < MA; ++b) {
-        const int32_t m = m0 + wm + 16 * b + (lane & 15);
-        if (m < M)
+        for (int b = 0; b < MA; ++b)
+            if (m1 + SIDE * b < M)
 #pragma unroll
-            for (int a = 0; a < NA; ++a) {
-                const int32_t n = n0 + wn + 16 * a + 4 * (lane >> 4);
-                if (n < o.N) {
-                    if (work)
-                        *reinterpret_cast<f4 *>(work + ((int64_t)t.part * o.M + m) * wide + n) =
-                            acc[a][b];
-                    else
-                        finish<O>(o, m, n, acc[a][b]);
-                }
+                for (int a = 0; a < NA; ++a)
+#pragma unroll
+                    for (int u = 0; u < QUADS; ++u) {
+                        const int32_t n = n1 + SIDE * a + 8 * u;
+                        if (n < o.N)
+                            *reinterpret_cast<f4 *>(
+                                work + ((int64_t)t.part * o.M + m1 + SIDE * b) * wide + n) =
+                                sums(a, b, u);
+                    }
+        return;
+    }
+    // A lane holds four columns of a row; through LDS, a block of SIDE rows and CW
+    // columns at a time, it gets eight of them, and eight lanes a whole 128-byte line (of
+    // 16-bit results) where the wavefront wrote quarters of 16 lines.  A block's residual
+    // is loaded before any of it is stored: the compiler, which cannot tell it from
+    // y, would wait for every load in turn.
+    constexpr int CW = BN / NW < 64 ? BN / NW : 64, PITCH = CW + 4, LPR = CW / 8;
+    constexpr int PASS = 64 / LPR, PASSES = SIDE / PASS;   // rows at a time
+    static_assert(sizeof(lds) >= NW * MW * SIDE * PITCH * sizeof(float), "");
+    lds_barrier();   // no one reads a tile any more
+    float *mine = reinterpret_cast<float *>(&lds[0][0]) + w * (SIDE * PITCH);
+    const int row = lane / LPR, col = lane % LPR * 8;
+#pragma unroll
+    for (int cc = 0; cc < BN / NW / CW; ++cc) {
+        const int32_t n = n0 + wn + cc * CW + col;
+        Columns<O, 8> columns;
+        columns.load(o, n);
+        Pack<O, 8> res[MA][PASSES];
+        float sm[MA][PASSES];
+#pragma unroll
+        for (int b = 0; b < MA; ++b)
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i) {
+                const int32_t m = m0 + wm + SIDE * b + PASS * i + row;
+                sm[b][i] = o.sm && m < M ? o.sm[m] : 1.f;
+                if (o.res && m < M && columns.left > 0)
+                    res[b][i] = columns.residual(o, m, n);
             }
+#pragma unroll
+        for (int b = 0; b < MA; ++b) {
+#pragma unroll
+            for (int a = 0; a < CW / SIDE; ++a)
+#pragma unroll
+                for (int u = 0; u < QUADS; ++u)
+                    *reinterpret_cast<f4 *>(mine + lane % LANES * PITCH + SIDE * a +
+                                            4 * (lane / LANES) + 8 * u) =
+                        sums(cc * (CW / SIDE) + a, b, u);
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i) {
+                const int32_t m = m0 + wm + SIDE * b + PASS * i + row;
+                const f4 *from = reinterpret_cast<const f4 *>(mine + (PASS * i + row) * PITCH + col);
+                const f4 c0 = from[0], c1 = from[1];
+                float v[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+                if (m < M && columns.left > 0)
+                    columns.finish(o, m, n, v, sm[b][i], res[b][i]);
+            }
+        }
     }
 }
 
@@ -356,21 +536,21 @@ template <class T, bool KC> inline bool lies_on_16(const void *X, int64_t ld, in
     return ((uintptr_t)X & 15) == 0 && ld % VEC == 0 && ld * (int64_t)sizeof(T) < (1 << 23) &&
            (KC || n % VEC == 0);
 }
+template <class T, bool PK, bool QK> inline bool direct(const LinearProduct &p)
+{
+    return lies_on_16<T, PK>(p.P, p.ld_p, p.o.N) && lies_on_16<T, QK>(p.Q, p.ld_q, p.o.M);
+}
 
-template <class T, class O, bool PK, bool QK, int BN, int BM, int NW, int MW>
+template <class T, class O, bool PK, bool QK, int BN, int BM, int NW, int MW, bool DIRECT>
 tgm_status_t launch_tile(const LinearProduct &p, int parts)
 {
-    const int32_t tn = (int32_t)cdiv(p.o.N, BN), tm = (int32_t)cdiv(p.o.M, BM);
-    const dim3 grid((uint32_t)((int64_t)tn * tm * parts)), block(64 * NW * MW);
+    const int64_t tn = cdiv(p.o.N, BN), tm = cdiv(p.o.M, BM), wg = tn * tm * parts;
+    if (wg * (64 * NW * MW) >= (int64_t)1 << 32)
+        return TGM_EINVAL;
     float *work = parts > 1 ? p.work : nullptr;
-    if (lies_on_16<T, PK>(p.P, p.ld_p, p.o.N) && lies_on_16<T, QK>(p.Q, p.ld_q, p.o.M))
-        TGM_LAUNCH((k_linear_tile<T, O, PK, QK, BN, BM, NW, MW, true>), grid, block, 0, p.s,
-                   (const T *)p.P, (const T *)p.Q, p.ld_p, p.ld_q, p.K, p.o, p.k_rows, work, tn,
-                   tm, parts);
-    else
-        TGM_LAUNCH((k_linear_tile<T, O, PK, QK, BN, BM, NW, MW, false>), grid, block, 0, p.s,
-                   (const T *)p.P, (const T *)p.Q, p.ld_p, p.ld_q, p.K, p.o, p.k_rows, work, tn,
-                   tm, parts);
+    TGM_LAUNCH((k_linear_tile<T, O, PK, QK, BN, BM, NW, MW, DIRECT>), dim3((uint32_t)wg),
+               dim3(64 * NW * MW), 0, p.s, (const T *)p.P, (const T *)p.Q, p.ld_p, p.ld_q, p.K, p.o,
+               p.k_rows, work, (int32_t)tn, (int32_t)tm, parts);
     if (parts > 1)
         TGM_LAUNCH((k_linear_join<O>),
                    dim3((uint32_t)std::min<int64_t>(cdiv((int64_t)p.o.M * cdiv(p.o.N, 4), 256),

@@ -248,6 +248,7 @@ __global__ __launch_bounds__(1024) void k_norm_dw(const float *__restrict__ part
     const int col = blockIdx.x * 32 + c;
     float a = 0.f;
     if (col < D)
+#pragma unroll 8
         for (int p = r; p < P; p += 32)
             a += part[(int64_t)p * D + col];
     lds[r][c] = a;

@@ -617,69 +617,85 @@ def tgm_embed(m, g, R, nb, root_pos, root_ts, nbr_pos, eid, nts, cnt, mem_new, n
 
 
 # ------------------------------------------------------------------ sequence operators
-def _types():
-    import torch
-    return {torch.float32: TGM_F32, torch.bfloat16: TGM_BF16, torch.float16: TGM_F16,
-            torch.float8_e4m3fn: TGM_E4M3}
+_codes = {}   # torch types to TGM_F32, ...
 
 
 def dtype_code(dtype) -> int:
     """TGM_F32, ... of a torch type."""
-    try:
-        return _types()[dtype]
-    except KeyError:
-        raise ValueError(f"no operator takes {dtype}") from None
+    if not _codes:
+        import torch
+        _codes.update({torch.float32: TGM_F32, torch.bfloat16: TGM_BF16, torch.float16: TGM_F16,
+                       torch.float8_e4m3fn: TGM_E4M3})
+    code = _codes.get(dtype)
+    if code is None:
+        raise ValueError(f"no operator takes {dtype}")
+    return code
 
 
-def _arg(name, t, dtype, shape, device, optional=False):
-    """Check a tensor argument and return (pointer, row stride).  The stride is
-    0 where there is no second row for it to lead to."""
+def _arg(name, t, dtype, shape, gpu):
+    """Check a tensor argument and return (address, row stride).  ``gpu`` is the
+    index of the device of the call's tensors.  The stride is 0 where there is no
+    second row for it to lead to."""
     if t is None:
-        if not optional:
-            raise ValueError(f"{name} is missing")
-        return None, 0
-    if t.dtype != dtype:
+        raise ValueError(f"{name} is missing")
+    if t.dtype is not dtype:
         raise ValueError(f"{name} has type {t.dtype}, not {dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, not {tuple(shape)}")
-    if t.device != device or device.type != "cuda":
-        raise ValueError(f"{name} is on {t.device}: every tensor of a call is on one GPU")
     ld = 0
-    if t.dim() == 2 and t.numel():
-        if shape[1] > 1 and t.stride(1) != 1:
-            raise ValueError(f"{name}'s columns are not contiguous")
-        if shape[0] > 1:
-            ld = t.stride(0)
-            if ld < shape[1]:
+    if len(shape) == 2:
+        ld, step = t.stride()
+        if t.numel():
+            if step != 1 and shape[1] > 1:
+                raise ValueError(f"{name}'s columns are not contiguous")
+            if shape[0] > 1 and ld < shape[1]:
                 raise ValueError(f"{name}'s rows overlap (stride {ld}, width {shape[1]})")
-    elif t.numel() > 1 and not t.is_contiguous():
+        if shape[0] <= 1:
+            ld = 0
+    elif not t.is_contiguous():
         raise ValueError(f"{name} is not contiguous")
-    return C.c_void_p(t.data_ptr()), ld
+    if gpu < 0 or t.get_device() != gpu:
+        raise ValueError(f"{name} is on {t.device}: every tensor of a call is on one GPU")
+    return t.data_ptr(), ld
 
 
-def _work_arg(work, device):
+def _opt(name, t, dtype, shape, gpu):
+    return (None, 0) if t is None else _arg(name, t, dtype, shape, gpu)
+
+
+def _dense(name, t, dtype, shape, gpu):
+    """Address of an optional tensor without gaps between its rows."""
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        raise ValueError(f"{name} is not contiguous")
+    return _arg(name, t, dtype, shape, gpu)[0]
+
+
+def _work_arg(work, gpu):
     import torch
     if work is None:
         return None, 0
-    if work.device != device or work.dtype != torch.uint8 or not work.is_contiguous():
+    if work.get_device() != gpu or work.dtype is not torch.uint8 or not work.is_contiguous():
         raise ValueError("work is a contiguous uint8 tensor on the call's GPU")
-    return C.c_void_p(work.data_ptr()), work.numel()
+    return work.data_ptr(), work.numel()
 
 
-def _call(fn, device, stream, *args):
+def _call(fn, gpu, stream, *args):
     """fn(*args, stream) with the tensors' device current."""
     import torch
-    if device.type != "cuda":
-        raise ValueError(f"{fn}: tensors on {device}; the operators run on a GPU")
-    s = torch.cuda.current_stream(device) if stream is None else stream
-    if s.device != device:
-        raise ValueError(f"{fn}: a stream of {s.device} for tensors on {device}")
+    if gpu < 0:
+        raise ValueError(f"{fn}: the operators run on a GPU")
+    s = torch.cuda.current_stream(gpu) if stream is None else stream
+    if s.device_index != gpu:
+        raise ValueError(f"{fn}: a stream of {s.device} for tensors on cuda:{gpu}")
     f = getattr(lib(), fn)
-    if torch.cuda.current_device() == device.index:
-        _check(fn, f(*args, C.c_void_p(s.cuda_stream)))
+    if torch.cuda.current_device() == gpu:
+        rc = f(*args, s.cuda_stream)
     else:
-        with torch.cuda.device(device):
-            _check(fn, f(*args, C.c_void_p(s.cuda_stream)))
+        with torch.cuda.device(gpu):
+            rc = f(*args, s.cuda_stream)
+    _check(fn, rc)
 
 
 def _bytes(fn, *args) -> int:
@@ -699,17 +715,17 @@ def tgm_norm(x, w, y, eps, res=None, total=None, scale=None, n_rows=None, stream
     with ``scale`` [rows] fp32; ``total`` receives t."""
     import torch
     rows, D = _shape2("x", x)
-    dev, dt = x.device, x.dtype
+    gpu, dt = x.get_device(), x.dtype
     out = y.dtype if y is not None and y.dtype == torch.float8_e4m3fn else dt
-    px, lx = _arg("x", x, dt, (rows, D), dev)
-    pr, lr = _arg("res", res, dt, (rows, D), dev, optional=True)
-    pw, _ = _arg("w", w, dt, (D,), dev)
-    pt, lt = _arg("total", total, dt, (rows, D), dev, optional=True)
-    py, ly = _arg("y", y, out, (rows, D), dev)
-    ps, _ = _arg("scale", scale, torch.float32, (rows,), dev, optional=True)
-    pn, _ = _arg("n_rows", n_rows, torch.int32, (1,), dev, optional=True)
+    px, lx = _arg("x", x, dt, (rows, D), gpu)
+    pr, lr = _opt("res", res, dt, (rows, D), gpu)
+    pw, _ = _arg("w", w, dt, (D,), gpu)
+    pt, lt = _opt("total", total, dt, (rows, D), gpu)
+    py, ly = _arg("y", y, out, (rows, D), gpu)
+    ps, _ = _opt("scale", scale, torch.float32, (rows,), gpu)
+    pn, _ = _opt("n_rows", n_rows, torch.int32, (1,), gpu)
     d = NormDesc(rows, D, dtype_code(dt), dtype_code(out), eps, lx, lr, lt, ly)
-    _call("tgm_norm", dev, stream, C.byref(d), px, pr, pw, pn, pt, py, ps)
+    _call("tgm_norm", gpu, stream, C.byref(d), px, pr, pw, pn, pt, py, ps)
 
 
 def tgm_norm_work_bytes(rows, D) -> int:
@@ -719,17 +735,17 @@ def tgm_norm_work_bytes(rows, D) -> int:
 def tgm_norm_backward(t, w, dy, eps, dx, dw, work, dtotal=None, n_rows=None, stream=None):
     import torch
     rows, D = _shape2("t", t)
-    dev, dt = t.device, t.dtype
-    px, lx = _arg("t", t, dt, (rows, D), dev)
-    pw, _ = _arg("w", w, dt, (D,), dev)
-    py, ly = _arg("dy", dy, dt, (rows, D), dev)
-    pd, ld = _arg("dtotal", dtotal, dt, (rows, D), dev, optional=True)
-    po, lo = _arg("dx", dx, dt, (rows, D), dev)
-    pg, _ = _arg("dw", dw, dt, (D,), dev, optional=True)
-    pn, _ = _arg("n_rows", n_rows, torch.int32, (1,), dev, optional=True)
-    pk, nk = _work_arg(work, dev)
+    gpu, dt = t.get_device(), t.dtype
+    px, lx = _arg("t", t, dt, (rows, D), gpu)
+    pw, _ = _arg("w", w, dt, (D,), gpu)
+    py, ly = _arg("dy", dy, dt, (rows, D), gpu)
+    pd, ld = _opt("dtotal", dtotal, dt, (rows, D), gpu)
+    po, lo = _arg("dx", dx, dt, (rows, D), gpu)
+    pg, _ = _opt("dw", dw, dt, (D,), gpu)
+    pn, _ = _opt("n_rows", n_rows, torch.int32, (1,), gpu)
+    pk, nk = _work_arg(work, gpu)
     d = NormDesc(rows, D, dtype_code(dt), dtype_code(dt), eps, lx, ld, lo, ly)
-    _call("tgm_norm_backward", dev, stream, C.byref(d), px, pw, py, pd, pn, po, pg, pk, nk)
+    _call("tgm_norm_backward", gpu, stream, C.byref(d), px, pw, py, pd, pn, po, pg, pk, nk)
 
 
 def _act(name) -> int:
@@ -749,20 +765,20 @@ def tgm_linear(x, w, y, work, act="none", bias=None, residual=None, z=None, scal
     [rows] and ``scale_w`` [N]; ``z`` receives the pre-activation."""
     import torch
     (rows, K), (N, _), out = _shape2("x", x), _shape2("w", w), None if y is None else y.dtype
-    dev, dt = x.device, x.dtype
-    px, lx = _arg("x", x, dt, (rows, K), dev)
-    pw, lw = _arg("w", w, dt, (N, K), dev)
-    psx, _ = _arg("scale_x", scale_x, torch.float32, (rows,), dev, optional=True)
-    psw, _ = _arg("scale_w", scale_w, torch.float32, (N,), dev, optional=True)
-    pb, _ = _arg("bias", bias, out, (N,), dev, optional=True)
-    pr, lr = _arg("residual", residual, out, (rows, N), dev, optional=True)
-    pz, lz = _arg("z", z, out, (rows, N), dev, optional=True)
-    py, ly = _arg("y", y, out, (rows, N), dev)
-    pn, _ = _arg("n_rows", n_rows, torch.int32, (1,), dev, optional=True)
-    pk, nk = _work_arg(work, dev)
+    gpu, dt = x.get_device(), x.dtype
+    px, lx = _arg("x", x, dt, (rows, K), gpu)
+    pw, lw = _arg("w", w, dt, (N, K), gpu)
+    psx, _ = _opt("scale_x", scale_x, torch.float32, (rows,), gpu)
+    psw, _ = _opt("scale_w", scale_w, torch.float32, (N,), gpu)
+    pb, _ = _opt("bias", bias, out, (N,), gpu)
+    pr, lr = _opt("residual", residual, out, (rows, N), gpu)
+    pz, lz = _opt("z", z, out, (rows, N), gpu)
+    py, ly = _arg("y", y, out, (rows, N), gpu)
+    pn, _ = _opt("n_rows", n_rows, torch.int32, (1,), gpu)
+    pk, nk = _work_arg(work, gpu)
     d = LinearDesc(rows, N, K, dtype_code(dt), dtype_code(out), _act(act), lx, lw, lr, lz, ly, 0,
                    0)
-    _call("tgm_linear", dev, stream, C.byref(d), px, psx, pw, psw, pb, pr, pn, pz, py, pk, nk)
+    _call("tgm_linear", gpu, stream, C.byref(d), px, psx, pw, psw, pb, pr, pn, pz, py, pk, nk)
 
 
 def tgm_linear_backward(x, w, dy, work, act="none", z=None, dx=None, dw=None, db=None,
@@ -771,19 +787,19 @@ def tgm_linear_backward(x, w, dy, work, act="none", z=None, dx=None, dw=None, db
     that tgm_linear wrote."""
     import torch
     (rows, K), (N, _) = _shape2("x", x), _shape2("w", w)
-    dev, dt = x.device, x.dtype
-    px, lx = _arg("x", x, dt, (rows, K), dev)
-    pw, lw = _arg("w", w, dt, (N, K), dev)
-    pz, lz = _arg("z", z, dt, (rows, N), dev, optional=True)
-    py, ly = _arg("dy", dy, dt, (rows, N), dev)
-    pdx, ldx = _arg("dx", dx, dt, (rows, K), dev, optional=True)
-    pdw, ldw = _arg("dw", dw, dt, (N, K), dev, optional=True)
-    pdb, _ = _arg("db", db, dt, (N,), dev, optional=True)
-    pn, _ = _arg("n_rows", n_rows, torch.int32, (1,), dev, optional=True)
-    pk, nk = _work_arg(work, dev)
+    gpu, dt = x.get_device(), x.dtype
+    px, lx = _arg("x", x, dt, (rows, K), gpu)
+    pw, lw = _arg("w", w, dt, (N, K), gpu)
+    pz, lz = _opt("z", z, dt, (rows, N), gpu)
+    py, ly = _arg("dy", dy, dt, (rows, N), gpu)
+    pdx, ldx = _opt("dx", dx, dt, (rows, K), gpu)
+    pdw, ldw = _opt("dw", dw, dt, (N, K), gpu)
+    pdb, _ = _opt("db", db, dt, (N,), gpu)
+    pn, _ = _opt("n_rows", n_rows, torch.int32, (1,), gpu)
+    pk, nk = _work_arg(work, gpu)
     d = LinearDesc(rows, N, K, dtype_code(dt), dtype_code(dt), _act(act), lx, lw, 0, lz, ly, ldx,
                    ldw)
-    _call("tgm_linear_backward", dev, stream, C.byref(d), px, pw, pz, py, pn, pdx, pdw, pdb, pk,
+    _call("tgm_linear_backward", gpu, stream, C.byref(d), px, pw, pz, py, pn, pdx, pdw, pdb, pk,
           nk)
 
 
@@ -801,19 +817,13 @@ def tgm_scan_work_bytes(rows, D, S) -> int:
 def _scan_args(g, x, S, offsets, length, h0):
     import torch
     rows, D = _shape2("g", g)
-    dev, dt = g.device, g.dtype
-    pg, lg = _arg("g", g, dt, (rows, D), dev)
-    px, lx = _arg("x", x, dt, (rows, D), dev)
-    po, _ = _arg("offsets", offsets, torch.int64, (S + 1,), dev, optional=True)
-    pl, _ = _arg("length", length, torch.int32, (S,), dev, optional=True)
-    ph, _ = _arg("h0", _dense("h0", h0), torch.float32, (S, D), dev, optional=True)
-    return rows, D, dev, dt, pg, lg, px, lx, po, pl, ph
-
-
-def _dense(name, t):
-    if t is not None and not t.is_contiguous():
-        raise ValueError(f"{name} is not contiguous")
-    return t
+    gpu, dt = g.get_device(), g.dtype
+    pg, lg = _arg("g", g, dt, (rows, D), gpu)
+    px, lx = _arg("x", x, dt, (rows, D), gpu)
+    po, _ = _opt("offsets", offsets, torch.int64, (S + 1,), gpu)
+    pl, _ = _opt("length", length, torch.int32, (S,), gpu)
+    ph = _dense("h0", h0, torch.float32, (S, D), gpu)
+    return rows, D, gpu, dt, pg, lg, px, lx, po, pl, ph
 
 
 def tgm_scan(g, x, y, S, work, offsets=None, length=None, h0=None, h_last=None, carry=None,
@@ -821,16 +831,16 @@ def tgm_scan(g, x, y, S, work, offsets=None, length=None, h0=None, h_last=None, 
     """h_t = a_t h_(t-1) + (1 - a_t) x_t, a = sigmoid(g), along S sequences:
     packed by ``offsets`` [S + 1], or padded (rows / S rows each)."""
     import torch
-    rows, D, dev, dt, pg, lg, px, lx, po, pl, ph = _scan_args(g, x, S, offsets, length, h0)
-    py, ly = _arg("y", y, dt, (rows, D), dev)
-    pe, _ = _arg("h_last", _dense("h_last", h_last), torch.float32, (S, D), dev, optional=True)
+    rows, D, gpu, dt, pg, lg, px, lx, po, pl, ph = _scan_args(g, x, S, offsets, length, h0)
+    py, ly = _arg("y", y, dt, (rows, D), gpu)
+    pe = _dense("h_last", h_last, torch.float32, (S, D), gpu)
     pc = None
     if carry is not None:
         n = tgm_scan_carry_rows(rows, S, offsets is not None)
-        pc, _ = _arg("carry", _dense("carry", carry), torch.float32, (n, D), dev)
-    pk, nk = _work_arg(work, dev)
+        pc = _dense("carry", carry, torch.float32, (n, D), gpu)
+    pk, nk = _work_arg(work, gpu)
     d = ScanDesc(rows, S, D, dtype_code(dt), 1 if reverse else 0, lg, lx, ly, 0, 0)
-    _call("tgm_scan", dev, stream, C.byref(d), pg, px, po, pl, ph, py, pe, pc, pk, nk)
+    _call("tgm_scan", gpu, stream, C.byref(d), pg, px, po, pl, ph, py, pe, pc, pk, nk)
 
 
 def tgm_scan_backward(g, x, dy, carry, dg, dx, S, work, offsets=None, length=None, h0=None,
@@ -838,17 +848,17 @@ def tgm_scan_backward(g, x, dy, carry, dg, dx, S, work, offsets=None, length=Non
     """Gradients of tgm_scan with the same inputs, sequences and the ``carry``
     that it left."""
     import torch
-    rows, D, dev, dt, pg, lg, px, lx, po, pl, ph = _scan_args(g, x, S, offsets, length, h0)
+    rows, D, gpu, dt, pg, lg, px, lx, po, pl, ph = _scan_args(g, x, S, offsets, length, h0)
     n = tgm_scan_carry_rows(rows, S, offsets is not None)
-    pc, _ = _arg("carry", _dense("carry", carry), torch.float32, (n, D), dev)
-    py, ly = _arg("dy", dy, dt, (rows, D), dev)
-    pe, _ = _arg("dh_last", _dense("dh_last", dh_last), torch.float32, (S, D), dev, optional=True)
-    pdg, ldg = _arg("dg", dg, dt, (rows, D), dev)
-    pdx, ldx = _arg("dx", dx, dt, (rows, D), dev)
-    p0, _ = _arg("dh0", _dense("dh0", dh0), torch.float32, (S, D), dev, optional=True)
-    pk, nk = _work_arg(work, dev)
+    pc = _dense("carry", carry, torch.float32, (n, D), gpu)
+    py, ly = _arg("dy", dy, dt, (rows, D), gpu)
+    pe = _dense("dh_last", dh_last, torch.float32, (S, D), gpu)
+    pdg, ldg = _arg("dg", dg, dt, (rows, D), gpu)
+    pdx, ldx = _arg("dx", dx, dt, (rows, D), gpu)
+    p0 = _dense("dh0", dh0, torch.float32, (S, D), gpu)
+    pk, nk = _work_arg(work, gpu)
     d = ScanDesc(rows, S, D, dtype_code(dt), 1 if reverse else 0, lg, lx, ly, ldg, ldx)
-    _call("tgm_scan_backward", dev, stream, C.byref(d), pg, px, po, pl, ph, pc, py, pe, pdg, pdx,
+    _call("tgm_scan_backward", gpu, stream, C.byref(d), pg, px, po, pl, ph, pc, py, pe, pdg, pdx,
           p0, pk, nk)
 
 
@@ -857,13 +867,13 @@ def tgm_scan_step(g, x, state, y, slots=None, n_rows=None, stream=None):
     in place."""
     import torch
     rows, D = _shape2("g", g)
-    dev, dt = g.device, g.dtype
+    gpu, dt = g.get_device(), g.dtype
     S, _ = _shape2("state", state)
-    pg, lg = _arg("g", g, dt, (rows, D), dev)
-    px, lx = _arg("x", x, dt, (rows, D), dev)
-    ps, _ = _arg("state", _dense("state", state), torch.float32, (S, D), dev)
-    py, ly = _arg("y", y, dt, (rows, D), dev, optional=True)
-    pt, _ = _arg("slots", slots, torch.int32, (rows,), dev, optional=True)
-    pn, _ = _arg("n_rows", n_rows, torch.int32, (1,), dev, optional=True)
+    pg, lg = _arg("g", g, dt, (rows, D), gpu)
+    px, lx = _arg("x", x, dt, (rows, D), gpu)
+    ps = _dense("state", state, torch.float32, (S, D), gpu)
+    py, ly = _opt("y", y, dt, (rows, D), gpu)
+    pt, _ = _opt("slots", slots, torch.int32, (rows,), gpu)
+    pn, _ = _opt("n_rows", n_rows, torch.int32, (1,), gpu)
     d = ScanDesc(rows, S, D, dtype_code(dt), 0, lg, lx, ly, 0, 0)
-    _call("tgm_scan_step", dev, stream, C.byref(d), pg, px, pt, pn, ps, py)
+    _call("tgm_scan_step", gpu, stream, C.byref(d), pg, px, pt, pn, ps, py)

@@ -193,16 +193,20 @@ def test_binding_checks_tensors():
     with pytest.raises(ValueError, match="GPU"):
         tgm.tgm_norm(x, w, torch.empty_like(x), 1e-5)
     with pytest.raises(ValueError, match="type"):
-        tgm._arg("w", w.half(), torch.float32, (8,), x.device)
+        tgm._arg("w", w.half(), torch.float32, (8,), 0)
     with pytest.raises(ValueError, match="no operator takes"):
         tgm.dtype_code(torch.int8)
 
 
 def test_binding_checks_strides():
-    m = tgm._arg
-    dev = torch.device("cpu")
-    for bad in (torch.zeros(8, 4).t(), torch.zeros(1, 8).expand(4, 8)):
-        with pytest.raises(ValueError):
-            m("x", bad, torch.float32, (4, 8), dev)
+    m = lambda t: tgm._arg("x", t, torch.float32, (4, 8), 0)
+    with pytest.raises(ValueError, match="contiguous"):
+        m(torch.zeros(8, 4).t())
+    with pytest.raises(ValueError, match="overlap"):
+        m(torch.zeros(1, 8).expand(4, 8))
     with pytest.raises(ValueError, match="shape"):
-        m("x", torch.zeros(4, 9), torch.float32, (4, 8), dev)
+        m(torch.zeros(4, 9))
+    with pytest.raises(ValueError, match="missing"):
+        m(None)
+    with pytest.raises(ValueError, match="GPU"):
+        m(torch.zeros(4, 8))
