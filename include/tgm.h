@@ -711,7 +711,8 @@ tgm_status_t tgm_norm_backward(const tgm_norm_desc *d, const void *t, const void
  * Products are exact and added in fp32; those of 8-bit values, for a 16-bit
  * result, by the 8-bit matrix instructions, which first add 8 neighbouring
  * columns' products aligned to the largest one and cut below 2^-13 of it.
- * 1 <= N, K <= 2^20.
+ * 1 <= N, K <= 2^20, and fewer than 2^24 tiles of 128 x 128 (fp32: 64 x 64) in any
+ * product.
  * Errors: TGM_EINVAL (null, sizes, types, strides, scales), TGM_ESIZE (work). */
 #define TGM_ACT_NONE 0
 #define TGM_ACT_RELU 1   /* max(z, 0) */
@@ -757,9 +758,9 @@ tgm_status_t tgm_linear_backward(const tgm_linear_desc *d, const void *x, const 
  *   padded: offsets NULL, rows divisible by S: with L = rows / S, rows s L ..
  *     s L + L - 1 (the first min(L, max(0, length[s])) of them where length is
  *     given, as tgm_sample's cnt for its [R x nb] outputs).
- * Rows of no sequence are not read and their y is left as it is.  (Offsets that
- * decrease or leave the range give unspecified values, never an access out of
- * range.)  reverse != 0 runs every sequence from its last row to its first, as
+ * What rows of no sequence hold does not matter, and their y is left as it is.
+ * (Offsets that decrease or leave the range give unspecified values, never an
+ * access out of range.)  reverse != 0 runs every sequence from its last row to its first, as
  * sampled neighbours need, which lie newest first.
  * carry (may be NULL) [tgm_scan_carry_rows x D] fp32 receives the states inside
  * the sequences that tgm_scan_backward starts from.

@@ -290,6 +290,11 @@ tgm_status_t linear_args(const tgm_linear_desc *d, int64_t *ld)
     if (!d || d->rows < 0 || d->N < 1 || d->N > kMaxDim || d->K < 1 || d->K > kMaxDim ||
         d->act < TGM_ACT_NONE || d->act > TGM_ACT_GELU)
         return TGM_EINVAL;
+    // a launch has fewer than 2^32 threads, 256 a tile
+    const int64_t side = d->dtype == TGM_F32 ? 64 : 128, most = (int64_t)1 << 24;
+    const int64_t r = cdiv(d->rows, side), n = cdiv(d->N, side), k = cdiv(d->K, side);
+    if (r * n >= most || r * k >= most || n * k >= most)
+        return TGM_EINVAL;
     const int64_t given[7] = {d->ld_x, d->ld_w, d->ld_res, d->ld_z, d->ld_y, d->ld_dx, d->ld_dw};
     const int32_t width[7] = {d->K, d->K, d->N, d->N, d->N, d->K, d->K};
     for (int k = 0; k < 7; ++k)

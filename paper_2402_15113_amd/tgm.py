@@ -707,6 +707,8 @@ def _bytes(fn, *args) -> int:
 def _shape2(name, t):
     if t is None or t.dim() != 2:
         raise ValueError(f"{name} is a matrix")
+    if max(t.shape) >= 1 << 31:
+        raise ValueError(f"{name} has too many rows or columns: {tuple(t.shape)}")
     return tuple(t.shape)
 
 

@@ -77,7 +77,8 @@ def linear_desc(**kw):
 
 BAD_LINEAR = [dict(rows=-1), dict(N=0), dict(K=0), dict(N=(1 << 20) + 1), dict(K=(1 << 20) + 1),
               dict(act=4), dict(act=-1), dict(dtype=0), dict(out_dtype=2), dict(dtype=5),
-              dict(ld_x=63), dict(ld_w=-64), dict(ld_y=31), dict(ld_z=1 << 24), dict(ld_res=1)]
+              dict(ld_x=63), dict(ld_w=-64), dict(ld_y=31), dict(ld_z=1 << 24), dict(ld_res=1),
+              dict(rows=(1 << 31) - 1, K=129), dict(N=1 << 19, K=1 << 19)]
 
 
 @pytest.mark.parametrize("bad", BAD_LINEAR + [dict(ld_dx=63), dict(ld_dw=1)])
