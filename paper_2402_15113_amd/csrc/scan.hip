@@ -286,6 +286,8 @@ struct ScanArgs {
     Seqs q;
     int32_t D, width, blocks;   // channels, those of a wavefront, wavefronts for a row
     int32_t groups;             // workgroups along the rows
+    int32_t spare;              // workgroups for the sequences without rows
+    bool backward;
     const void *g, *x, *dy;
     const float *h0;      // backward: also the forward's
     const float *last;    // backward: dh_last
@@ -349,19 +351,21 @@ template <int W> __device__ void run_chain(const ScanArgs &A, int b, int part)
     const uint32_t ch = (uint32_t)min(c0 + lane, c1 - 1);
     float base = 0.f;             // the state before the first block not done
     int32_t at = 0, known = 0;    // the first map of that block; how many of it are done
+    uint64_t w[kBlock];
+    auto fetch = [&](uint64_t (&to)[kBlock], int32_t first) __attribute__((always_inline)) {
+        const uint64_t *maps = A.maps + (int64_t)min(first, A.groups - 1) * A.D + ch;
+        const int32_t left = max(1, min(kBlock, A.groups - first));
+#pragma unroll
+        for (int i = 0; i < kBlock; ++i)
+            to[i] = word_load(maps + (uint64_t)((uint32_t)min(i, left - 1) * (uint32_t)A.D));
+    };
     for (int turn = 0; at < A.groups; turn ^= 1) {
         const int32_t first = at + kBlock * u, left = min(kBlock, A.groups - first);
-        const uint64_t *maps = A.maps + (int64_t)first * A.D + ch;
-        uint64_t w[kBlock];
+        fetch(w, first);
         uint32_t absent = 0;   // bit i: word i is not there for every lane
-        if (left > 0) {
 #pragma unroll
-            for (int i = 0; i < kBlock; ++i)
-                w[i] = word_load(maps + (uint64_t)((uint32_t)min(i, left - 1) * (uint32_t)A.D));
-#pragma unroll
-            for (int i = 0; i < kBlock; ++i)
-                absent |= __ballot((uint32_t)(w[i] >> 32) == ~0u) ? 1u << i : 0u;
-        }
+        for (int i = 0; i < kBlock; ++i)
+            absent |= __ballot((uint32_t)(w[i] >> 32) == ~0u) ? 1u << i : 0u;
         const int n = left <= 0 ? 0 : absent ? min(left, __builtin_ctz(absent)) : left;
         if (n == kBlock) {
             float P = 1.f, Q = 0.f;
@@ -372,7 +376,7 @@ template <int W> __device__ void run_chain(const ScanArgs &A, int b, int part)
         }
         if (lane == 0)
             there[turn][u] = n;
-        __syncthreads();   // one a turn: two turns' words are apart
+        lds_barrier();   // one a turn: two turns' words are apart
         f2 m[W];
         int32_t count[W];
 #pragma unroll
@@ -394,15 +398,28 @@ template <int W> __device__ void run_chain(const ScanArgs &A, int b, int part)
         if (u <= whole) {   // the state before this wavefront's block is known
             uint64_t *states = A.states + (int64_t)first * A.D + ch;
             const int done = u ? 0 : known;
+            auto next = [&](int i) __attribute__((always_inline)) {
+                const float p = upper(w[i]), q = lower(w[i]);
+                h = p < 0.f ? q : fmaf(p, h, q);
+            };
+            auto hand = [&](int i) __attribute__((always_inline)) {
+                word_store(states + (uint64_t)((uint32_t)i * (uint32_t)A.D), word_of(-1.f, h));
+            };
+            if (n == kBlock && !done) {
 #pragma unroll
-            for (int i = 0; i < kBlock; ++i)
-                if (i < n) {
-                    if (i >= done)
-                        word_store(states + (uint64_t)((uint32_t)i * (uint32_t)A.D),
-                                   word_of(-1.f, h));
-                    const float p = upper(w[i]), q = lower(w[i]);
-                    h = p < 0.f ? q : fmaf(p, h, q);
+                for (int i = 0; i < kBlock; ++i) {
+                    hand(i);
+                    next(i);
                 }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kBlock; ++i)
+                    if (i < n) {
+                        if (i >= done)
+                            hand(i);
+                        next(i);
+                    }
+            }
         }
         if (!whole && rest <= known)
             __builtin_amdgcn_s_sleep(1);
@@ -413,11 +430,40 @@ template <int W> __device__ void run_chain(const ScanArgs &A, int b, int part)
     }
 }
 
-// This workgroup's place and channel block; false: it was a runner and is done.
+// A sequence without rows ends with the state that it starts from (backward: hands
+// its end's gradient to its start): the workgroups past the tiles', a wavefront
+// for 8 sequences at a time.
+template <int W> __device__ void pass_on(const ScanArgs &A, int64_t wg)
+{
+    constexpr int kSeqs = 8;
+    const float *from = A.backward ? A.last : A.h0;
+    const int lane = threadIdx.x & 63;
+    for (int64_t s0 = (wg * W + wave_id()) * kSeqs; s0 < A.q.S;
+         s0 += (int64_t)A.spare * W * kSeqs) {
+        const int64_t s = s0 + lane;
+        bool none = false;
+        if (lane < kSeqs && s < A.q.S) {
+            none = A.q.offsets ? A.q.offsets[s + 1] <= A.q.offsets[s] : A.q.L == 0;
+            none |= A.q.length && A.q.length[s] <= 0;
+        }
+        for (uint64_t m = __ballot(none); m; m &= m - 1) {
+            const int64_t at = (s0 + __ffsll((unsigned long long)m) - 1) * A.D;
+            for (int32_t c = lane; c < A.D; c += 64)
+                A.h_last[at + c] = from ? from[at + c] : 0.f;
+        }
+    }
+}
+
+// This workgroup's place and channel block; false: it had another task, and is done.
 template <int V, int W, bool ALONE>
 __device__ __forceinline__ bool take_place(const ScanArgs &A, int &place, int &b)
 {
     __shared__ int32_t t;
+    const uint32_t tiles = (uint32_t)(A.groups + (A.ticket ? V : 0)) * (uint32_t)A.blocks;
+    if (blockIdx.x >= tiles) {
+        pass_on<W>(A, blockIdx.x - tiles);
+        return false;
+    }
     b = (int)(blockIdx.x % (uint32_t)A.blocks);
     place = (int)(blockIdx.x / (uint32_t)A.blocks);
     if (ALONE || !A.ticket)
@@ -731,36 +777,15 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_bwd(ScanArgs A)
         rows(std::false_type{});
 }
 
-// Before a pass: no word of the chain is there and no place is taken; and a
-// sequence without rows ends with the state that it starts from (backward:
-// hands its end's gradient to its start), which a wavefront does for 8 of them.
-constexpr int kSeqs = 8;
-__global__ __launch_bounds__(256) void k_scan_begin(Seqs q, int32_t D,
-                                                    const float *__restrict__ from, float *to,
-                                                    uint64_t *words, int64_t n, int32_t *ticket,
+// Before a pass with a chain: none of its words is there and no place is taken.
+__global__ __launch_bounds__(256) void k_scan_begin(uint64_t *words, int64_t n, int32_t *ticket,
                                                     int32_t blocks)
 {
     const int64_t threads = (int64_t)gridDim.x * 256, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     for (int64_t i = id; i < n; i += threads)
         words[i] = kAbsent;
-    if (ticket && id < blocks)
+    if (id < blocks)
         ticket[id] = 0;
-    if (!to)
-        return;
-    const int lane = threadIdx.x & 63;
-    for (int64_t s0 = (id >> 6) * kSeqs; s0 < q.S; s0 += (threads >> 6) * kSeqs) {
-        const int64_t s = s0 + lane;
-        bool none = false;
-        if (lane < kSeqs && s < q.S) {
-            none = q.offsets ? q.offsets[s + 1] <= q.offsets[s] : q.L == 0;
-            none |= q.length && q.length[s] <= 0;
-        }
-        for (uint64_t m = __ballot(none); m; m &= m - 1) {
-            const int64_t at = (s0 + __ffsll((unsigned long long)m) - 1) * D;
-            for (int32_t c = lane; c < D; c += 64)
-                to[at + c] = from ? from[at + c] : 0.f;
-        }
-    }
 }
 
 template <class T, int V>
@@ -857,7 +882,7 @@ template <class T, int V, int W, bool BWD>
 tgm_status_t launch_scan(const ScanArgs &A, hipStream_t s)
 {
     // and the chains' runners
-    const dim3 grid((uint32_t)(((int64_t)A.groups + (A.ticket ? V : 0)) * A.blocks));
+    const dim3 grid((uint32_t)(((int64_t)A.groups + (A.ticket ? V : 0)) * A.blocks + A.spare));
     const dim3 block(64 * W);
     if constexpr (BWD) {
         if (A.q.per)
@@ -884,7 +909,7 @@ tgm_status_t run_scan(ScanArgs A, void *work, size_t work_bytes, hipStream_t s)
     constexpr int W = BWD ? kWavesBwd : kWaves;
     A.blocks = (int32_t)cdiv(A.D, A.width);
     A.groups = (int32_t)cdiv(A.q.tiles, W);
-    if (((int64_t)A.groups + 2) * A.blocks >= kMaxGrid)
+    if (((int64_t)A.groups + 2) * A.blocks + 256 >= kMaxGrid)
         return TGM_EINVAL;
     if (A.q.rows) {
         if (!work || ((uintptr_t)work & 15))
@@ -899,14 +924,13 @@ tgm_status_t run_scan(ScanArgs A, void *work, size_t work_bytes, hipStream_t s)
         A.states = A.maps + words / 2;
         A.ticket = (int32_t *)(A.maps + words);
     }
-    const bool empty = A.h_last && A.q.S && (A.q.offsets || A.q.length || A.q.L == 0);
-    if (words || empty) {
-        const int64_t wg = std::min<int64_t>(cdiv(std::max<int64_t>(words, empty ? A.q.S * (int64_t)(64 / kSeqs) : 0), 256), 2048);
-        TGM_LAUNCH(k_scan_begin, dim3((uint32_t)wg), dim3(256), 0, s, A.q, A.D,
-                   BWD ? A.last : A.h0, empty ? A.h_last : nullptr, A.maps, words, A.ticket,
-                   A.blocks);
-    }
-    if (!A.q.tiles)
+    A.backward = BWD;
+    if (A.h_last && A.q.S && (A.q.offsets || A.q.length || A.q.L == 0))
+        A.spare = (int32_t)std::min<int64_t>(cdiv(A.q.S, 8 * W), 256);
+    if (words)
+        TGM_LAUNCH(k_scan_begin, dim3((uint32_t)std::min<int64_t>(cdiv(words, 256), 1024)),
+                   dim3(256), 0, s, A.maps, words, A.ticket, A.blocks);
+    if (!A.q.tiles && !A.spare)
         return TGM_OK;
     if constexpr (sizeof(T) == 2)
         if (V == 2)
