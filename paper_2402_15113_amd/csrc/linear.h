@@ -69,12 +69,34 @@ __device__ __forceinline__ f4 mfma_wide(const Frag<e4m3> &p, const Frag<e4m3> &q
 }
 
 // ---------------------------------------------------------------- activations
+// The normal distribution function Phi(z) = erfc(-z / sqrt 2) / 2 and e = exp(-z^2/2),
+// by Abramowitz and Stegun's rational approximation 7.1.26 of erfc for x >= 0,
+// erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2) with t = 1 / (1 + 0.3275911 x), within
+// 1.5e-7; Phi of a negative z is that half, so it does not cancel.  About 20
+// instructions, an exponential that the derivative needs as well among them;
+// erff takes three times as many, more than a pass over memory leaves time for.
+struct Normal {
+    float phi, e;
+};
+__device__ __forceinline__ Normal normal_of(float z)
+{
+    const float x = fabsf(z) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    const float e = __expf(-0.5f * z * z);
+    const float tail = 0.5f * p * t * e;
+    return Normal{z > 0.f ? 1.f - tail : tail, e};
+}
+
 __device__ __forceinline__ float act_of(float z, int act)
 {
     switch (act) {
     case TGM_ACT_RELU: return z > 0.f || z != z ? z : 0.f;
-    case TGM_ACT_SILU: return z / (1.f + __expf(-z));
-    case TGM_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case TGM_ACT_SILU: return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));
+    case TGM_ACT_GELU: return z * normal_of(z).phi;
     default: return z;
     }
 }
@@ -83,12 +105,13 @@ __device__ __forceinline__ float act_grad(float z, int act)
     switch (act) {
     case TGM_ACT_RELU: return z > 0.f ? 1.f : 0.f;
     case TGM_ACT_SILU: {
-        const float p = 1.f / (1.f + __expf(-z));
-        return p * (1.f + z * (1.f - p));
+        const float p = __builtin_amdgcn_rcpf(1.f + __expf(-z));
+        return p * fmaf(z, 1.f - p, 1.f);
     }
-    case TGM_ACT_GELU:
-        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) +
-               z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+    case TGM_ACT_GELU: {
+        const Normal n = normal_of(z);
+        return fmaf(z * 0.39894228040143268f, n.e, n.phi);
+    }
     default: return 1.f;
     }
 }
