@@ -103,8 +103,10 @@ template <class T, bool KC, int X, int TH, bool DIRECT> struct Operand {
     int64_t ld;
     int32_t x0, n;              // the tile's first row (column) and how many the operand has
     uint32_t off[DIRECT ? ND : 1];
-    using PackT = Pack<T, VEC>;
-    PackT v[DIRECT ? 1 : NR];
+    // of a vector type, which the compiler loads as one (a Pack it takes apart)
+    typedef unsigned u4v __attribute__((ext_vector_type(4), may_alias));
+    typedef u4v u4v_any __attribute__((aligned(1)));
+    u4v v[DIRECT ? 1 : NR];
 
     __device__ __forceinline__ void init(const T *p, int64_t ld_, int32_t x0_, int32_t n_)
     {
@@ -161,14 +163,14 @@ template <class T, bool KC, int X, int TH, bool DIRECT> struct Operand {
                 const int e = min(u * TH + (int)threadIdx.x, Lds::ROWS * Lds::CHUNKS - 1);
                 const int row = e / Lds::CHUNKS, x = x0 + e % Lds::CHUNKS * VEC;
                 if (KC) {
-                    v[u] = load_pack<T, VEC>(base + (int64_t)min(x0 + row, n - 1) * ld + k +
-                                             e % Lds::CHUNKS * VEC);
+                    v[u] = *reinterpret_cast<const u4v_any *>(
+                        base + (int64_t)min(x0 + row, n - 1) * ld + k + e % Lds::CHUNKS * VEC);
                 } else {
                     // past the edge: the last vector, moved up to the columns asked for
                     const int back = max(0, x - (n - VEC));
-                    v[u] = load_pack<T, VEC>(base + (k + row) * ld + (x - back));
+                    v[u] = *reinterpret_cast<const u4v_any *>(base + (k + row) * ld + (x - back));
                     if (back)
-                        v[u] = __builtin_bit_cast(PackT, back < VEC
+                        v[u] = __builtin_bit_cast(u4v, back < VEC
                                    ? __builtin_bit_cast(unsigned __int128, v[u]) >>
                                          (8 * (int)sizeof(T) * back)
                                    : (unsigned __int128)0);
@@ -183,25 +185,56 @@ template <class T, bool KC, int X, int TH, bool DIRECT> struct Operand {
             for (int u = 0; u < NR; ++u) {
                 const int e = u * TH + (int)threadIdx.x;
                 if (Lds::ROWS * Lds::CHUNKS % TH == 0 || e < Lds::ROWS * Lds::CHUNKS)
-                    *reinterpret_cast<Pack<T, VEC> *>(__builtin_assume_aligned(
-                        lds + Lds::at(e / Lds::CHUNKS, e % Lds::CHUNKS), 16)) = v[u];
+                    *reinterpret_cast<u4v *>(
+                        lds + Lds::at(e / Lds::CHUNKS, e % Lds::CHUNKS)) = v[u];
             }
         }
     }
-    // the last, partial step at once, by elements: zeros past K
+    // The last, partial step at once: zeros past K.  By vectors where none of them
+    // straddles K (or the operand's edge), else by elements, several on their way
+    // together.
     __device__ __forceinline__ void tail(char *lds, int64_t k, int64_t K) const
     {
-        constexpr int PER = KC ? BK : Lds::CHUNKS * VEC;   // elements of a row
+        if (KC ? K % VEC == 0 : n % VEC == 0) {
+#pragma unroll 2
+            for (int u = 0; u < NR; ++u) {
+                const int e = u * TH + (int)threadIdx.x;
+                const int row = min(e / Lds::CHUNKS, Lds::ROWS - 1), c = e % Lds::CHUNKS;
+                const int32_t x = x0 + (KC ? row : c * VEC);
+                const int64_t kk = k + (KC ? c * VEC : row);
+                // past the ends: the last one again
+                const T *from = KC ? base + (int64_t)min(x, n - 1) * ld + min(kk, K - VEC)
+                                   : base + min(kk, K - 1) * ld + min(x, n - VEC);
+                Pack<T, VEC> r = load_pack<T, VEC>(from);
+                if (kk >= K)
+                    __builtin_memset(&r, 0, sizeof(r));
+                if (e < Lds::ROWS * Lds::CHUNKS)
+                    *reinterpret_cast<Pack<T, VEC> *>(
+                        __builtin_assume_aligned(lds + Lds::at(row, c), 16)) = r;
+            }
+            return;
+        }
+        constexpr int PER = KC ? BK : Lds::CHUNKS * VEC, MANY = 8;
+        constexpr int ALL = Lds::ROWS * PER;
 #pragma unroll 1
-        for (int e = threadIdx.x; e < Lds::ROWS * PER; e += TH) {
-            const int row = e / PER, i = e % PER;
-            const int64_t kk = k + (KC ? i : row);
-            T v;
-            __builtin_memset(&v, 0, sizeof(v));
-            if (kk < K)
-                v = KC ? base[(int64_t)min(x0 + row, n - 1) * ld + kk]
-                       : base[kk * ld + min(x0 + i, n - 1)];
-            *reinterpret_cast<T *>(lds + Lds::at(row, i / VEC) + i % VEC * (int)sizeof(T)) = v;
+        for (int e0 = threadIdx.x; e0 < ALL; e0 += MANY * TH) {
+            T v[MANY];
+#pragma unroll
+            for (int j = 0; j < MANY; ++j) {
+                const int e = min(e0 + j * TH, ALL - 1), row = e / PER, i = e % PER;
+                const int64_t kk = min(k + (KC ? i : row), K - 1);
+                v[j] = KC ? base[(int64_t)min(x0 + row, n - 1) * ld + kk]
+                          : base[kk * ld + min(x0 + i, n - 1)];
+            }
+#pragma unroll
+            for (int j = 0; j < MANY; ++j) {
+                const int e = e0 + j * TH, row = e / PER, i = e % PER;
+                if (k + (KC ? i : row) >= K)
+                    __builtin_memset(&v[j], 0, sizeof(T));
+                if (e < ALL)
+                    *reinterpret_cast<T *>(lds + Lds::at(row, i / VEC) +
+                                           i % VEC * (int)sizeof(T)) = v[j];
+            }
         }
     }
 };
@@ -315,45 +348,67 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
     OQ q;
     p.init(P, ld_p, n0, o.N);
     q.init(Q, ld_q, m0, M);
+    // Steps that come whole, by vectors; the others go first, by their elements: behind
+    // the loop their code would take registers from it.
+    const int32_t quick = p.by_vectors(0, BK) && q.by_vectors(0, BK)
+                              ? (int32_t)min((int64_t)ns, max((int64_t)0, K / BK - s0)) : 0;
+    auto slow = [&](int32_t s) __attribute__((always_inline)) {
+        const int64_t k = (s0 + s) * BK;
+        p.tail(lds[0], k, K);
+        q.tail(lds[0] + LP::BYTES, k, K);
+        lds_barrier();
+    };
+    if (quick < ns)
+        slow(quick);
     typename H::Acc acc[NA][MA];
 #pragma unroll
     for (int a = 0; a < NA; ++a)
 #pragma unroll
         for (int b = 0; b < MA; ++b)
             acc[a][b] = typename H::Acc(0.f);
+    if (quick < ns) {
+#pragma unroll 1
+        for (int32_t s = quick;;) {
+            H h;
+#pragma unroll 1
+            for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                for (int a = 0; a < NA; ++a)
+                    h.read(lds[0], lds[0] + LP::BYTES, wn, wm, c, a);
+#pragma unroll
+                for (int a = 0; a < NA; ++a)
+                    h.multiply(acc, a, used);
+            }
+            lds_barrier();
+            if constexpr (DIRECT) {   // one partial step at most
+                break;
+            } else {
+                if (++s >= ns)
+                    break;
+                slow(s);
+            }
+        }
+    }
 
-    // Step s into its tile.  DIRECT: whole ones on their way, the tail at once; else
-    // into registers (fetch) and from there (put).
+    // Step s into its tile.  DIRECT: on its way there; else into registers (fetch) and
+    // from there (put).
     auto fill = [&](int32_t s) __attribute__((always_inline)) {
         const int64_t k = (s0 + s) * BK;
         char *to = lds[s & 1];
-        if (k + BK <= K) {
-            const char *fp = p.from_k(k), *fq = q.from_k(k);
+        const char *fp = p.from_k(k), *fq = q.from_k(k);
 #pragma unroll
-            for (int u = 0; u < OP::ND; ++u)
-                p.direct(to, fp, u);
+        for (int u = 0; u < OP::ND; ++u)
+            p.direct(to, fp, u);
 #pragma unroll
-            for (int u = 0; u < OQ::ND; ++u)
-                q.direct(to + LP::BYTES, fq, u);
-        } else {
-            p.tail(to, k, K);
-            q.tail(to + LP::BYTES, k, K);
-        }
+        for (int u = 0; u < OQ::ND; ++u)
+            q.direct(to + LP::BYTES, fq, u);
     };
     auto fetch = [&](int32_t s) __attribute__((always_inline)) {
-        const int64_t k = (s0 + s) * BK;
-        if (p.by_vectors(k, K) && q.by_vectors(k, K))
-            p.load(k), q.load(k);
+        p.load((s0 + s) * BK), q.load((s0 + s) * BK);
     };
     auto put = [&](int32_t s) __attribute__((always_inline)) {
-        const int64_t k = (s0 + s) * BK;
         char *to = lds[s & 1];
-        if (p.by_vectors(k, K) && q.by_vectors(k, K)) {
-            p.store(to), q.store(to + LP::BYTES);
-        } else {
-            p.tail(to, k, K);
-            q.tail(to + LP::BYTES, k, K);
-        }
+        p.store(to), q.store(to + LP::BYTES);
     };
     auto arrive = [&]() __attribute__((always_inline)) {
         // by the builtin, which the compiler counts: behind an asm it would wait once
@@ -363,8 +418,8 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
         lds_barrier();
     };
     H h0, h1;
-    // Step s; NEXT: one follows; REFILL: a whole one follows that.
-    auto step = [&](int32_t s, auto next, auto refill) __attribute__((always_inline)) {
+    // Step s; NEXT: one follows; MORE: another one follows that, and is called for.
+    auto step = [&](int32_t s, auto next, auto more) __attribute__((always_inline)) {
         const char *lp = lds[s & 1];
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
@@ -378,20 +433,15 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
             if constexpr (!DIRECT)
                 put(s + 1);
             arrive();
-            if constexpr (!refill)
-                if (s + 2 < ns) {
-                    if constexpr (DIRECT)
-                        fill(s + 2);
-                    else
-                        fetch(s + 2);
-                }
+            if constexpr (!DIRECT && more)
+                fetch(s + 2);
         }
         const int64_t k = (s0 + s + 2) * BK;
         const char *fp = p.from_k(k), *fq = q.from_k(k);
         char *to = lds[s & 1];
 #pragma unroll
         for (int a = 0; a < NA; ++a) {
-            if constexpr (refill) {
+            if constexpr (DIRECT && more) {
                 constexpr int ND = OP::ND + OQ::ND;
 #pragma unroll
                 for (int u = a * ND / NA; u < (a + 1) * ND / NA; ++u)
@@ -406,7 +456,7 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
             issue_fence();
         }
     };
-    if (ns > 0) {
+    if (quick > 0) {
         if constexpr (DIRECT) {
             fill(0);
         } else {
@@ -414,7 +464,7 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
             put(0);
         }
         arrive();
-        if (ns > 1) {
+        if (quick > 1) {
             if constexpr (DIRECT)
                 fill(1);
             else
@@ -426,13 +476,10 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
         using yes = std::true_type;
         using no = std::false_type;
         int32_t s = 0;
-        if constexpr (DIRECT) {
-            const int32_t whole = (int32_t)min((int64_t)ns, max((int64_t)0, K / BK - s0));
-            for (; s + 2 < whole; ++s)
-                step(s, yes{}, yes{});
-        }
-        for (; s + 1 < ns; ++s)
-            step(s, yes{}, no{});
+        for (; s + 2 < quick; ++s)
+            step(s, yes{}, yes{});
+        if (s + 1 < quick)
+            step(s++, yes{}, no{});
         step(s, no{}, no{});
     }
 
