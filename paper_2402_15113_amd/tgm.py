@@ -636,6 +636,10 @@ def _arg(name, t, dtype, shape, gpu):
     """Check a tensor argument and return (address, row stride).  ``gpu`` is the
     index of the device of the call's tensors.  The stride is 0 where there is no
     second row for it to lead to."""
+    # a call costs a few us in all: the usual argument by one test
+    if t is not None and t.dtype is dtype and t.shape == shape and t.get_device() == gpu >= 0 \
+            and t.is_contiguous():
+        return t.data_ptr(), shape[1] if len(shape) == 2 and shape[0] > 1 else 0
     if t is None:
         raise ValueError(f"{name} is missing")
     if t.dtype is not dtype:
@@ -686,16 +690,21 @@ def _call(fn, gpu, stream, *args):
     import torch
     if gpu < 0:
         raise ValueError(f"{fn}: the operators run on a GPU")
-    s = torch.cuda.current_stream(gpu) if stream is None else stream
-    if s.device_index != gpu:
-        raise ValueError(f"{fn}: a stream of {s.device} for tensors on cuda:{gpu}")
+    if stream is None:
+        # the address alone: a Stream object takes ten times as long to make
+        s = torch._C._cuda_getCurrentRawStream(gpu)
+    elif stream.device_index != gpu:
+        raise ValueError(f"{fn}: a stream of {stream.device} for tensors on cuda:{gpu}")
+    else:
+        s = stream.cuda_stream
     f = getattr(lib(), fn)
     if torch.cuda.current_device() == gpu:
-        rc = f(*args, s.cuda_stream)
+        rc = f(*args, s)
     else:
         with torch.cuda.device(gpu):
-            rc = f(*args, s.cuda_stream)
-    _check(fn, rc)
+            rc = f(*args, s)
+    if rc:
+        _check(fn, rc)
 
 
 def _bytes(fn, *args) -> int:
@@ -707,9 +716,10 @@ def _bytes(fn, *args) -> int:
 def _shape2(name, t):
     if t is None or t.dim() != 2:
         raise ValueError(f"{name} is a matrix")
-    if max(t.shape) >= 1 << 31:
-        raise ValueError(f"{name} has too many rows or columns: {tuple(t.shape)}")
-    return tuple(t.shape)
+    shape = rows, columns = tuple(t.shape)
+    if rows >= 1 << 31 or columns >= 1 << 31:
+        raise ValueError(f"{name} has too many rows or columns: {shape}")
+    return shape
 
 
 def tgm_norm(x, w, y, eps, res=None, total=None, scale=None, n_rows=None, stream=None):
