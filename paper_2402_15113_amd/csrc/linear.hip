@@ -38,10 +38,12 @@ template <class T> __device__ __forceinline__ Frag<T> load_frag(const T *row, in
     return f;
 }
 
-// Few rows: bound by reading W once.  A workgroup takes 16 columns and 16 MB rows of
-// C; its wavefronts share the sum, each a run of it, and add up through LDS.
+// Few rows, or a small product: bound by reading W once, or by what a launch takes.  A
+// workgroup takes 16 columns and 16 MB rows of C; its wavefronts share the sum, each a
+// run of it, and add up through LDS, so that a short sum needs no second launch.
 // Operands come straight from memory into the matrix instructions, eight loads of
-// a row of W at a time.
+// a row of W at a time.  fp16, 4 and 16 rows, 4,096 x 2,048 (W of 16.8 MB): 5.4 and 6.5 us,
+// 2.6 TB/s; fp32, 16 rows, 8,192 x 2,048: 18.3 us, 3.7 TB/s.
 template <class T, class O, int MB, int W>
 __global__ __launch_bounds__(64 * W) void k_linear_few(const T *__restrict__ P,
                                                        const T *__restrict__ Q, int64_t ld_p,
@@ -203,16 +205,31 @@ template <class T, class O, int MB> tgm_status_t few(const LinearProduct &p)
     return TGM_OK;
 }
 
-// Up to how many rows k_linear_few takes a forward product.
-constexpr int kFewRows = 64;
+// Blocks of 16 rows a workgroup of k_linear_few has for a forward product, 0 where the
+// tiles take it.  Its time grows with the length of a sum (each wavefront has an eighth)
+// and with the workgroups past one a CU; the tiles' is 9 to 10 us until they fill
+// the chip.  One block against four against tiles, us, fp16 (rows x columns x sum): 40 x 1,024 x
+// 512: 3.4, 4.6, 8.1; 512 x 512 x 1,024: 10.0, 7.4, 10.3; 128 x 1,024 x 2,048: 9.4, 11.5, 10.8;
+// 64 x 4,096 x 2,048: 17.2, 12.6, 11.1; 1,000 x 1,024 x 512: 18.2, 12.7, 9.8; 16 x 1,024 x 8,192: 16.1,
+// 22.9, 12.1.  Up to 16 rows the tiles multiply four times as many, which shows in fp32:
+// 16 x 8,192 x 8,192: 67, 102, 78 (fp16: 31, 45, 26; 8 bit: 17.6, 24.0, 17.1).
+int few_blocks(int64_t M, int64_t N, int64_t K, int code)
+{
+    const int64_t bytes = K * elem_bytes(code);
+    const int64_t one = cdiv(N, 16) * cdiv(M, 16), four = cdiv(N, 16) * cdiv(M, 64);
+    if (M <= 16)
+        return bytes <= 8192 || (code == TGM_F32 && one >= 256) ? 1 : 0;
+    if (one <= 768)
+        return bytes * std::max<int64_t>(one, 256) <= 8192 * 256 ? 1 : 0;
+    return four <= 512 && bytes * std::max<int64_t>(four, 256) < 4096 * 256 ? 4 : 0;
+}
 
 template <class T, class O, bool PK, bool QK> tgm_status_t product(const LinearProduct &p)
 {
     if constexpr (PK && QK) {
-        if (p.o.M <= 16)
-            return few<T, O, 1>(p);
-        if (p.o.M <= kFewRows)
-            return few<T, O, 4>(p);
+        const int blocks = few_blocks(p.o.M, p.o.N, p.K, TypeCode<T>::code);
+        if (blocks)
+            return blocks == 1 ? few<T, O, 1>(p) : few<T, O, 4>(p);
     }
     constexpr int which = PK ? 0 : QK ? 1 : 2, out = TypeCode<O>::code;
     if constexpr (sizeof(T) == 4)
@@ -317,11 +334,13 @@ tgm_status_t check_work(size_t need, const void *work, size_t bytes)
 // A sum is split as far as there are CUs for the parts and 8 steps of 128 bytes for
 // each.  Of the two tiles the large one is taken where its busiest CU has no more
 // to multiply than with the small ones, its sums are whole and (16 and 8 bits) at
-// least 32 steps long: a CU holds one of it, so that nothing hides how a tile begins
-// and ends.  Large against small, us, bf16: 16,384 x 4,096 x 8,192: 857, 966; 8,192 x
-// 4,096 x 4,096: 229, 288; 4,096 x 4,096 x 4,096: 130, 140; but 8,192 x 8,192 x 1,024: 169,
-// 161; 2,048 x 2,048 x 2,048 (in 4 parts): 39, 33.  fp32, where the matrix cores
-// take 16 times as long: 4,096 x 2,048 x 1,024: 132, 141; 12,000 x 200 x 472: 47, 34.
+// least 16 steps long: a CU holds one of it, so that nothing hides how a tile begins
+// and ends.  Large against small, us, bf16: 16,384 x 4,096 x 8,192: 865, 974; 8,192 x
+// 4,096 x 4,096: 231, 290; 4,096 x 4,096 x 4,096: 134, 145; 8,192 x 8,192 x 1,024: 159,
+// 166; but 16,384 x 4,096 x 512: 118, 110; 2,048 x 2,048 x 2,048 (in 4 parts): 51, 32.  8 bit:
+// 16,384 x 4,096 x 8,192: 427, 492; 8,192 x 8,192 x 1,024 (8 steps): 112, 107.  fp32, where the
+// matrix cores take 16 times as long: 4,096 x 2,048 x 1,024: 135, 143; 12,000 x 200 x 472:
+// 43, 31.
 LinearPlan tgm::linear_plan(int64_t M, int64_t N, int64_t K, int code)
 {
     const bool f32 = code == TGM_F32;
@@ -329,7 +348,7 @@ LinearPlan tgm::linear_plan(int64_t M, int64_t N, int64_t K, int code)
     const int64_t side = f32 ? 128 : 256, half = side / 2;
     const int64_t large = cdiv(M, side) * cdiv(N, side), small = cdiv(M, half) * cdiv(N, half);
     if (cdiv(large, 256) * 4 <= cdiv(small, 256) && large >= (f32 ? 512 : 192) &&
-        (f32 || steps >= 32))
+        (f32 || steps >= 16))
         return LinearPlan{true, 1};
     // half as many large tiles as CUs, and a sum that is long in halves too: the weights'
     // gradient of 8,192 rows of a 4,096 x 2,048 layer, 147 us against 156
@@ -347,7 +366,7 @@ extern "C" tgm_status_t tgm_linear_work_bytes(int32_t rows, int32_t N, int32_t K
         return TGM_EINVAL;
     *bytes = backward ? dz_bytes(rows, N, dtype, act) + db_bytes(rows, N) +
                             std::max(split_bytes(rows, K, N, dtype), split_bytes(N, K, rows, dtype))
-                      : split_bytes(rows, N, K, dtype);
+                      : few_blocks(rows, N, K, dtype) ? 0 : split_bytes(rows, N, K, dtype);
     return TGM_OK;
 }
 
