@@ -137,6 +137,55 @@ def test_many_tiles(tgm, size):
     forward(tgm, *size, torch.float16, "silu", pad=1)
 
 
+@pytest.mark.parametrize("K", [1, 37, 64, 75, 129, 300])
+@pytest.mark.parametrize("dtype", list(TYPES) + ["e4m3"])
+def test_ragged_tiles(tgm, dtype, K):
+    """More workgroups than a product without tiles takes; the sums end inside a step,
+    rows and columns inside a tile."""
+    dt = TYPES.get(dtype, E4M3)
+    out = torch.float16 if dt == E4M3 else None
+    forward(tgm, 601, 1101, K, dt, ACTS[K % 4], pad=K % 3, out=out)
+    forward(tgm, 513, 1160, K, dt, "none", pad=0, bias=False, res=True, z=False, out=out)
+
+
+@pytest.mark.parametrize("rows,N,K", [(601, 1101, 75), (130, 96, 2100), (17, 64, 9000)])
+def test_tiles_beside_what_is_not_read(tgm, rows, N, K):
+    """A row count on the device, infinities in one row and NaN in one column, and a
+    residual in place, where tiles (in one part or several) take the product."""
+    for dt in TYPES.values():
+        x, w, r = (randn(s, *shape).to(dt).cuda() for s, shape in
+                   ((1, (rows, K)), (2, (N, K)), (3, (rows, N))))
+        k = work(tgm, rows, N, K, dt)
+        y = torch.full_like(r, 7.0)
+        m = rows - 9
+        bad = x.clone()
+        bad[m:] = float("nan")
+        nr = torch.tensor([m], dtype=torch.int32, device="cuda")
+        tgm.tgm_linear(bad, w, y, k, n_rows=nr)
+        ref, _, _, e = linear(x[:m], w, "none")
+        check("y", y[:m], ref, e + rounded(ref.abs() + e, dt))
+        assert (y[m:] == 7).all()
+        tgm.tgm_linear(x, w, y, k, residual=r)
+        own = r.clone()
+        tgm.tgm_linear(x, w, own, k, residual=own)
+        assert torch.equal(y, own)
+        x[3, K - 1], w[5, 0] = float("inf"), float("nan")
+        tgm.tgm_linear(x, w, y, k)
+        assert torch.isnan(y[:, 5]).all()
+        rest = torch.isfinite(y)
+        rest[3], rest[:, 5] = True, True
+        assert rest.all() and not torch.isfinite(y[3]).any()
+
+
+@pytest.mark.parametrize("size", [(17, 64, 512), (700, 40, 300), (512, 512, 700), (768, 256, 1),
+                                  (100, 4096, 65), (16, 8200, 130)])
+def test_without_tiles(tgm, size):
+    for dt in list(TYPES.values()) + [E4M3]:
+        out = torch.bfloat16 if dt == E4M3 else None
+        forward(tgm, *size, dt, "gelu", pad=1, out=out)
+        forward(tgm, *size, dt, "none", pad=0, z=False, out=out)
+
+
 @pytest.mark.parametrize("n", [-3, 0, 1, 16, 63, 64, 100, 300])
 def test_row_count_on_the_device(tgm, n):
     rows, N, K = 200, 72, 40
