@@ -306,11 +306,15 @@ struct ScanArgs {
 // word that is not there yet (a computed NaN never has them all set).
 //
 // Workgroups take their places in the rows' order by a counter as they start.
-// The first of each channel block's chain is its runner: it composes the
-// others' maps in order and hands every workgroup the state before its rows.  A workgroup writes its map without waiting for anyone, and
-// the runner waits only for the lowest place whose map is missing, which a
+// The first of each channel block's chain (one for every 64 channels) are its runners:
+// they compose the others' maps in order and hand every workgroup the state
+// before its rows.  A workgroup writes its map without waiting for anyone, and
+// a runner waits only for the lowest place whose map is missing, which a
 // workgroup that has started holds or the next one to start will hold; so
 // every wait ends, however few workgroups run at once.
+//
+// A product of gates may fall below the smallest number: what it would leave of a state is
+// below 2^-149 of it, except that zero times an infinite state is NaN.
 constexpr uint64_t kAbsent = ~(uint64_t)0;
 
 __device__ __forceinline__ uint64_t word_of(float P, float Q)
