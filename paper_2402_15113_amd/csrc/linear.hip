@@ -213,8 +213,8 @@ template <class T, class O, int MB> tgm_status_t few(const LinearProduct &p)
 // and with the workgroups past one a CU; the tiles' is 9 to 10 us until they fill
 // the chip.  One block against four against tiles, us, fp16 (rows x columns x sum): 40 x 1,024 x
 // 512: 3.4, 4.6, 8.1; 512 x 512 x 1,024: 10.0, 7.4, 10.3; 128 x 1,024 x 2,048: 9.4, 11.5, 10.8;
-// 64 x 4,096 x 2,048: 17.2, 12.6, 11.1; 1,000 x 1,024 x 512: 18.2, 12.7, 9.8; 16 x 1,024 x 8,192: 16.1,
-// 22.9, 12.1.  Up to 16 rows the tiles multiply four times as many, which shows in fp32:
+// 64 x 4,096 x 2,048: 17.2, 12.6, 11.1; 1,000 x 1,024 x 512: 18.2, 12.7, 9.8; 16 x 1,024 x
+// 8,192: 16.1, 22.9, 12.1.  Up to 16 rows the tiles multiply four times as many, which shows in fp32:
 // 16 x 8,192 x 8,192: 67, 102, 78 (fp16: 31, 45, 26; 8 bit: 17.6, 24.0, 17.1).
 int few_blocks(int64_t M, int64_t N, int64_t K, int code)
 {

@@ -550,7 +550,8 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
                 const int32_t m = m0 + wm + SIDE * b + PASS * i + row;
-                const f4 *from = reinterpret_cast<const f4 *>(mine + (PASS * i + row) * PITCH + col);
+                const float *sum = mine + (PASS * i + row) * PITCH + col;
+                const f4 *from = reinterpret_cast<const f4 *>(sum);
                 const f4 c0 = from[0], c1 = from[1];
                 float v[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
                 if (m < M && columns.left > 0)
