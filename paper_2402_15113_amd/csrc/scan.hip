@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "scan_places.h"
 #include "seq.h"
 
 using namespace tgm;
@@ -286,6 +287,7 @@ struct ScanArgs {
     Seqs q;
     int32_t D, width, blocks;   // channels, those of a wavefront, wavefronts for a row
     int32_t groups;             // workgroups along the rows
+    uint32_t tasks;             // workgroups for those and for the chains
     int32_t spare;              // workgroups for the sequences without rows
     bool backward;
     const void *g, *x, *dy;
@@ -295,7 +297,7 @@ struct ScanArgs {
     float *h_last;        // backward: dh0
     float *carry;         // states entering the tiles (may be null in the forward)
     uint64_t *maps, *states;    // [groups x D]: the chain's words
-    int32_t *ticket;            // [blocks]
+    int32_t *ticket;            // [kMaxRunners] tasks taken; null without a chain
     int64_t ld_g, ld_x, ld_y, ld_dg, ld_dx;
 };
 
@@ -305,13 +307,13 @@ struct ScanArgs {
 // ignores the state before (a sequence begins inside it), all bits set for a
 // word that is not there yet (a computed NaN never has them all set).
 //
-// Workgroups take their places in the rows' order by a counter as they start.
-// The first of each channel block's chain (one for every 64 channels) are its runners:
-// they compose the others' maps in order and hand every workgroup the state
-// before its rows.  A workgroup writes its map without waiting for anyone, and
-// a runner waits only for the lowest place whose map is missing, which a
-// workgroup that has started holds or the next one to start will hold; so
-// every wait ends, however few workgroups run at once.
+// Workgroups take their tasks in the rows' order by a counter as they start.  The
+// first are runners: each composes the maps of a chain (64 channels') in order and hands
+// every workgroup the state before its rows.  A workgroup writes its map without
+// waiting for anyone, and what it waits for itself comes from places below its own
+// and from its runner, which have all started.  A runner waits for places that may not
+// have; the order of the tasks (scan_places.h) bounds how many do so at once, and so
+// every wait ends.
 //
 // A product of gates may fall below the smallest number: what it would leave of a state is
 // below 2^-149 of it, except that zero times an infinite state is NaN.
@@ -340,17 +342,17 @@ __device__ __forceinline__ void compose(float &P, float &Q, float p, float q)
     P = p < 0.f || P < 0.f ? -1.f : P * p;
 }
 
-// A runner takes 64 channels.  Its wavefronts take a block of 16 maps each at a
-// time: a block that is there is composed on its own, the state before each
-// block comes from the maps of the blocks before it, and the states inside
-// follow one by one: the same operations whichever words were there at which
-// look, so results do not depend on timing.
-template <int W> __device__ void run_chain(const ScanArgs &A, int b, int part)
+// A runner takes 64 channels, `part` of block b.  Its wavefronts take a block of 16 maps
+// each at a time: a block that is there is composed on its own, the state before each
+// block comes from the maps of the blocks before it, and the states inside follow one
+// by one: the same operations whichever words were there at which look, so results do
+// not depend on timing.  With W = 1 a wavefront is a runner by itself.
+template <int W> __device__ __forceinline__ void run_chain(const ScanArgs &A, int b, int part)
 {
     constexpr int kBlock = 16;
     __shared__ f2 block[2][W][64];
     __shared__ int32_t there[2][W];
-    const int lane = threadIdx.x & 63, u = wave_id();
+    const int lane = threadIdx.x & 63, u = W > 1 ? wave_id() : 0;
     const int32_t c0 = b * A.width + 64 * part, c1 = min(A.D, (b + 1) * A.width);
     const uint32_t ch = (uint32_t)min(c0 + lane, c1 - 1);
     float base = 0.f;             // the state before the first block not done
@@ -371,21 +373,24 @@ template <int W> __device__ void run_chain(const ScanArgs &A, int b, int part)
         for (int i = 0; i < kBlock; ++i)
             absent |= __ballot((uint32_t)(w[i] >> 32) == ~0u) ? 1u << i : 0u;
         const int n = left <= 0 ? 0 : absent ? min(left, __builtin_ctz(absent)) : left;
-        if (n == kBlock) {
-            float P = 1.f, Q = 0.f;
+        f2 m[W];
+        int32_t count[W];
+        float P = 1.f, Q = 0.f;
+        if (n == kBlock)
 #pragma unroll
             for (int i = 0; i < kBlock; ++i)
                 compose(P, Q, upper(w[i]), lower(w[i]));
+        if constexpr (W == 1) {
+            m[0] = f2{P, Q}, count[0] = n;
+        } else {
             block[turn][u][lane] = f2{P, Q};
-        }
-        if (lane == 0)
-            there[turn][u] = n;
-        lds_barrier();   // one a turn: two turns' words are apart
-        f2 m[W];
-        int32_t count[W];
+            if (lane == 0)
+                there[turn][u] = n;
+            lds_barrier();   // one a turn: two turns' words are apart
 #pragma unroll
-        for (int k = 0; k < W; ++k)
-            m[k] = block[turn][k][lane], count[k] = there[turn][k];
+            for (int k = 0; k < W; ++k)
+                m[k] = block[turn][k][lane], count[k] = there[turn][k];
+        }
         float h = base;
         int32_t whole = 0, rest = 0;   // blocks there from the first on; of the one after
 #pragma unroll
@@ -463,21 +468,33 @@ template <int V, int W, bool ALONE>
 __device__ __forceinline__ bool take_place(const ScanArgs &A, int &place, int &b)
 {
     __shared__ int32_t t;
-    const uint32_t tiles = (uint32_t)(A.groups + (A.ticket ? V : 0)) * (uint32_t)A.blocks;
-    if (blockIdx.x >= tiles) {
-        pass_on<W>(A, blockIdx.x - tiles);
+    if (blockIdx.x >= A.tasks) {
+        pass_on<W>(A, blockIdx.x - A.tasks);
         return false;
     }
     b = (int)(blockIdx.x % (uint32_t)A.blocks);
     place = (int)(blockIdx.x / (uint32_t)A.blocks);
     if (ALONE || !A.ticket)
         return true;
+    const ScanTasks all{A.blocks, A.groups, V, W};
     if (threadIdx.x == 0)
-        t = __hip_atomic_fetch_add(A.ticket + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        t = __hip_atomic_fetch_add(A.ticket + (all.narrow() ? b : 0), 1, __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    place = __builtin_amdgcn_readfirstlane(t) - V;   // V runners
+    place = __builtin_amdgcn_readfirstlane(t) - V;
+    if (all.narrow()) {
+        if (place < 0)   // V runners
+            run_chain<W>(A, b, place + V);
+        return place >= 0;
+    }
+    const ScanTask task = wide_task(all, (uint32_t)(place + V));
+    b = task.block, place = task.place;
     if (place < 0) {
-        run_chain<W>(A, b, place + V);
+        const int chain = (-1 - place) * W + wave_id();
+        b += chain / V;
+        if (b < min(A.blocks, task.block + all.deep()) &&
+            b * A.width + 64 * (chain % V) < min(A.D, (b + 1) * A.width))
+            run_chain<1>(A, b, chain % V);
         return false;
     }
     return true;
@@ -818,14 +835,13 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_bwd(ScanArgs A)
         rows(std::false_type{});
 }
 
-// Before a pass with a chain: none of its words is there and no place is taken (4 us).
-__global__ __launch_bounds__(256) void k_scan_begin(uint64_t *words, int64_t n, int32_t *ticket,
-                                                    int32_t blocks)
+// Before a pass with a chain: none of its words is there and no task is taken (4 us).
+__global__ __launch_bounds__(256) void k_scan_begin(uint64_t *words, int64_t n, int32_t *ticket)
 {
     const int64_t threads = (int64_t)gridDim.x * 256, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     for (int64_t i = id; i < n; i += threads)
         words[i] = kAbsent;
-    if (id < blocks)
+    if (id < kMaxRunners)
         ticket[id] = 0;
 }
 
@@ -925,9 +941,7 @@ int pick_width(int32_t D, int want, int32_t *width)
 template <class T, int V, int W, bool BWD>
 tgm_status_t launch_scan(const ScanArgs &A, hipStream_t s)
 {
-    // and the chains' runners
-    const dim3 grid((uint32_t)(((int64_t)A.groups + (A.ticket ? V : 0)) * A.blocks + A.spare));
-    const dim3 block(64 * W);
+    const dim3 grid(A.tasks + (uint32_t)A.spare), block(64 * W);
     if constexpr (BWD) {
         if (A.q.per)
             TGM_LAUNCH((k_scan_bwd<T, V, W, true>), grid, block, 0, s, A);
@@ -942,9 +956,12 @@ tgm_status_t launch_scan(const ScanArgs &A, hipStream_t s)
     return TGM_OK;
 }
 
-// Lays the chain out in the work space: maps and states, [groups x D] words
-// each, and the places' counters.
-size_t chain_bytes(int64_t groups, int64_t D) { return (size_t)groups * D * 16 + 2048 * 4; }
+// The chain in the work space: maps and states, [groups x D] words each, and the
+// counters of tasks.
+size_t chain_bytes(int64_t groups, int64_t D)
+{
+    return (size_t)groups * D * 16 + kMaxRunners * sizeof(int32_t);
+}
 
 template <class T, bool BWD>
 tgm_status_t run_scan(ScanArgs A, void *work, size_t work_bytes, hipStream_t s)
@@ -969,11 +986,13 @@ tgm_status_t run_scan(ScanArgs A, void *work, size_t work_bytes, hipStream_t s)
         A.ticket = (int32_t *)(A.maps + words);
     }
     A.backward = BWD;
+    A.tasks = (uint32_t)(words ? ScanTasks{A.blocks, A.groups, V, W}.all()
+                               : (int64_t)A.groups * A.blocks);
     if (A.h_last && A.q.S && (A.q.offsets || A.q.length || A.q.L == 0))
         A.spare = (int32_t)std::min<int64_t>(cdiv(A.q.S, 8 * W), 256);
     if (words)
         TGM_LAUNCH(k_scan_begin, dim3((uint32_t)std::min<int64_t>(cdiv(words, 256), 1024)),
-                   dim3(256), 0, s, A.maps, words, A.ticket, A.blocks);
+                   dim3(256), 0, s, A.maps, words, A.ticket);
     if (!A.q.tiles && !A.spare)
         return TGM_OK;
     if constexpr (sizeof(T) == 2)
