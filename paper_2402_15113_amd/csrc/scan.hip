@@ -957,11 +957,8 @@ tgm_status_t launch_scan(const ScanArgs &A, hipStream_t s)
 }
 
 // The chain in the work space: maps and states, [groups x D] words each, and the
-// counters of tasks.
-size_t chain_bytes(int64_t groups, int64_t D)
-{
-    return (size_t)groups * D * 16 + kMaxRunners * sizeof(int32_t);
-}
+// counters of tasks, with room to 8 KiB.
+size_t chain_bytes(int64_t groups, int64_t D) { return (size_t)groups * D * 16 + 8192; }
 
 template <class T, bool BWD>
 tgm_status_t run_scan(ScanArgs A, void *work, size_t work_bytes, hipStream_t s)
