@@ -879,7 +879,6 @@ __global__ __launch_bounds__(256) void k_scan_step(const T *g, const T *x,
 }
 
 constexpr int64_t kMaxRows = ((int64_t)1 << 30) + 1;
-constexpr int64_t kMaxGrid = ((int64_t)1 << 32) / (64 * kWaves);   // threads of a launch: 32 bits
 constexpr int kMaxD = 65536;
 
 // Fills q's division into tiles; false where the sequences cannot be.
@@ -908,6 +907,15 @@ bool divide(Seqs *q, bool packed)
     }
     return true;
 }
+
+// Whether a launch has fewer than 2^32 threads: forward, with the runners and the workgroups
+// for sequences without rows, and so in the gradient, whose workgroups are half as wide
+// and at most twice as many.  T ceil(D / 64) <= 2^26 - 2^15 does in every type.
+bool fits(int64_t tiles, int32_t blocks)
+{
+    return (cdiv(tiles, kWaves) + 2) * blocks + 256 < ((int64_t)1 << 32) / (64 * kWaves);
+}
+static_assert(kWaves == 2 * kWavesBwd, "");
 
 int64_t most_tiles(int64_t rows, int32_t S)
 {
@@ -967,7 +975,7 @@ tgm_status_t run_scan(ScanArgs A, void *work, size_t work_bytes, hipStream_t s)
     constexpr int W = BWD ? kWavesBwd : kWaves;
     A.blocks = (int32_t)cdiv(A.D, A.width);
     A.groups = (int32_t)cdiv(A.q.tiles, W);
-    if (((int64_t)A.groups + 2) * A.blocks + 256 >= kMaxGrid)
+    if (!fits(A.q.tiles, A.blocks))
         return TGM_EINVAL;
     if (A.q.rows) {
         if (!work || ((uintptr_t)work & 15))
@@ -1037,7 +1045,9 @@ extern "C" tgm_status_t tgm_scan_carry_rows(int64_t rows, int32_t S, int32_t pac
 extern "C" tgm_status_t tgm_scan_work_bytes(int64_t rows, int32_t D, int32_t S, size_t *bytes)
 {
     const int64_t n = most_tiles(rows, S);
-    if (!bytes || n < 0 || D < 1 || D > kMaxD)
+    // the fewest tiles and channel blocks of any call of this size
+    if (!bytes || n < 0 || D < 1 || D > kMaxD ||
+        !fits(cdiv(rows, kRows), (int32_t)cdiv(D, 128)))
         return TGM_EINVAL;
     *bytes = n ? chain_bytes(cdiv(n, kWavesBwd), D) : 0;
     return TGM_OK;
