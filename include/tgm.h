@@ -759,8 +759,8 @@ tgm_status_t tgm_linear_backward(const tgm_linear_desc *d, const void *x, const 
  *     s L + L - 1 (the first min(L, max(0, length[s])) of them where length is
  *     given, as tgm_sample's cnt for its [R x nb] outputs).
  * What rows of no sequence hold does not matter, and their y is left as it is.
- * An infinite state goes on as one until the gates' product since a multiple of
- * 32 rows before it has fallen to zero in fp32, and as NaN from there on.
+ * A gate below 2^-126 (a where g < -87.3, 1 - a where g > 87.3) is zero, which
+ * makes NaN of an infinite state, x or gradient; any other gate leaves it infinite.
  * (Offsets that decrease or leave the range give unspecified values, never an
  * access out of range.)  reverse != 0 runs every sequence from its last row to its first, as
  * sampled neighbours need, which lie newest first.

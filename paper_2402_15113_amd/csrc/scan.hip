@@ -160,7 +160,7 @@ __device__ __forceinline__ RowInfo rows_packed(const Seqs &q, const Tile &t)
 }
 
 // The gates.  exp(-|g|) lies in (0, 1], so neither gate loses its small values
-// and infinite g gives 0 and 1.
+// and infinite g gives 0 and 1.  A gate below 2^-126, where the exponential ends, is 0.
 struct Gate {
     float a, i;   // sigmoid(g), sigmoid(-g)
 };
@@ -315,8 +315,10 @@ struct ScanArgs {
 // have; the order of the tasks (scan_places.h) bounds how many do so at once, and so
 // every wait ends.
 //
-// A product of gates may fall below the smallest number: what it would leave of a state is
-// below 2^-149 of it, except that zero times an infinite state is NaN.
+// P is zero where a gate is, and nowhere else: a product that falls below the smallest
+// number is kLeast instead, so that an infinite state stays infinite (zero times it is
+// NaN) wherever its rows fall into tiles.
+constexpr float kLeast = 0x1p-149f;
 constexpr uint64_t kAbsent = ~(uint64_t)0;
 
 __device__ __forceinline__ uint64_t word_of(float P, float Q)
@@ -335,11 +337,40 @@ __device__ __forceinline__ void word_store(uint64_t *p, uint64_t w)
 __device__ __forceinline__ float upper(uint64_t w) { return __uint_as_float((uint32_t)(w >> 32)); }
 __device__ __forceinline__ float lower(uint64_t w) { return __uint_as_float((uint32_t)w); }
 
-// (P, Q) after (p, q): the map of both.
-__device__ __forceinline__ void compose(float &P, float &Q, float p, float q)
+// (P, Q) after (p, q): the map of both, but for the product, which lift() makes kLeast
+// where it is zero and `low`, the lowest p of all (1 before the first), is not.
+__device__ __forceinline__ void compose(float &P, float &Q, float &low, float p, float q)
 {
     Q = p < 0.f ? q : fmaf(p, Q, q);
     P = p < 0.f || P < 0.f ? -1.f : P * p;
+    low = fminf(low, p);
+}
+__device__ __forceinline__ float lift(float P, float low)
+{
+    return P == 0.f && low > 0.f ? kLeast : P;
+}
+// P of a tile, which the pass over its rows has only multiplied: where it is zero and
+// no gate of the rows in `valid` is.  lowest(r, v): row r's gate, or what it grows with;
+// is_zero(its lowest one): whether that gate is zero.
+template <int V, class L, class Z>
+__device__ __forceinline__ void raise(float (&P)[V], uint32_t valid, L lowest, Z is_zero)
+{
+    if (__builtin_expect(!__any(P[0] == 0.f || P[V - 1] == 0.f), 1))
+        return;
+    float least[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        least[v] = INFINITY;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+        if ((valid >> r) & 1)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                least[v] = fminf(least[v], lowest(r, v));
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (P[v] == 0.f && !is_zero(least[v]))
+            P[v] = kLeast;
 }
 
 // A runner takes 64 channels, `part` of block b.  Its wavefronts take a block of 16 maps
@@ -375,11 +406,12 @@ template <int W> __device__ __forceinline__ void run_chain(const ScanArgs &A, in
         const int n = left <= 0 ? 0 : absent ? min(left, __builtin_ctz(absent)) : left;
         f2 m[W];
         int32_t count[W];
-        float P = 1.f, Q = 0.f;
+        float P = 1.f, Q = 0.f, low = 1.f;
         if (n == kBlock)
 #pragma unroll
             for (int i = 0; i < kBlock; ++i)
-                compose(P, Q, upper(w[i]), lower(w[i]));
+                compose(P, Q, low, upper(w[i]), lower(w[i]));
+        P = lift(P, low);
         if constexpr (W == 1) {
             m[0] = f2{P, Q}, count[0] = n;
         } else {
@@ -516,22 +548,22 @@ __device__ __forceinline__ void enter(const ScanArgs &A, int place, const Lane &
     if (threadIdx.x == 0)
         wanted = need && A.ticket && place > 0;
     __syncthreads();
-    float p[V], q[V];
+    float p[V], q[V], low[V];
 #pragma unroll
     for (int v = 0; v < V; ++v)
-        p[v] = 1.f, q[v] = 0.f;
+        p[v] = 1.f, q[v] = 0.f, low[v] = 1.f;
     for (int u = 0; u < w; ++u)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const f2 m = maps[u][lane * V + v];
-            compose(p[v], q[v], m.x, m.y);
+            compose(p[v], q[v], low[v], m.x, m.y);
         }
     if (A.ticket && w == W - 1 && c.on) {   // the workgroup's map, as soon as it is known
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            float ap = p[v], aq = q[v];
-            compose(ap, aq, P[v], Q[v]);
-            word_store(A.maps + (int64_t)place * A.D + c.ch + v, word_of(ap, aq));
+            float ap = p[v], aq = q[v], al = low[v];
+            compose(ap, aq, al, P[v], Q[v]);
+            word_store(A.maps + (int64_t)place * A.D + c.ch + v, word_of(lift(ap, al), aq));
         }
     }
     if (__builtin_amdgcn_readfirstlane((int)wanted)) {
@@ -564,7 +596,7 @@ __device__ __forceinline__ void enter(const ScanArgs &A, int place, const Lane &
     if (need)
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            h[v] = p[v] < 0.f ? q[v] : fmaf(p[v], h[v], q[v]);
+            h[v] = p[v] < 0.f ? q[v] : fmaf(lift(p[v], low[v]), h[v], q[v]);
 }
 
 // ---------------------------------------------------------------- the passes
@@ -661,6 +693,9 @@ __global__ __launch_bounds__(64 * W, 4) void k_scan(ScanArgs A)
 #pragma unroll
             for (int v = 0; v < V; ++v)
                 P[v] = -1.f;
+        else
+            raise<V>(P, in.valid, [&](int r, int v) { return pg[r].at(v); },
+                     [](float a) { return (KEEP ? a : gate_of(a).a) == 0.f; });
         const bool need = in.valid & ~in.first & 1;
         enter<V, W>(A, place, c, need, P, Q, h);
         if (need && A.carry && c.on) {
@@ -793,10 +828,37 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_bwd(ScanArgs A)
     else
         map(std::false_type{});
     if constexpr (!ALONE) {
+        // an infinite dy times a product that fell to zero
+        if (__builtin_expect(__any((P[0] == 0.f && Q[0] != Q[0]) ||
+                                   (P[V - 1] == 0.f && Q[V - 1] != Q[V - 1])), 0)) {
+            const uint32_t open = in.valid & (in.last ^ (in.last - 1));   // up to the first end
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                P[v] = 1.f, Q[v] = 0.f;
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+                if ((open >> r) & 1) {
+                    float end[V];
+#pragma unroll
+                    for (int v = 0; v < V; ++v)
+                        end[v] = 0.f;
+                    if ((in.last >> r) & 1)
+                        ends.get(end, A.last, in.last, r, in.seq, A.D, c.ch);
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const float a = gate_of(pg[r].at(v)).a;
+                        P[v] = fmaf(P[v], a, P[v] > 0.f && a > 0.f ? kLeast : 0.f);
+                        Q[v] = fmaf(P[v], py[r].at(v) + end[v], Q[v]);
+                    }
+                }
+        }
         if (in.last)
 #pragma unroll
             for (int v = 0; v < V; ++v)
                 P[v] = -1.f;
+        else
+            raise<V>(P, in.valid, [&](int r, int v) { return pg[r].at(v); },
+                     [](float g) { return gate_of(g).a == 0.f; });
         const bool need = ((in.valid & ~in.last) >> (t.n - 1)) & 1;
         enter<V, W>(A, place, c, need, P, Q, e);
     }
