@@ -711,6 +711,9 @@ tgm_status_t tgm_norm_backward(const tgm_norm_desc *d, const void *t, const void
  * Products are exact and added in fp32; those of 8-bit values, for a 16-bit
  * result, by the 8-bit matrix instructions, which first add 8 neighbouring
  * columns' products aligned to the largest one and cut below 2^-13 of it.
+ * Activations and their derivatives are formed in fp32 from z before its rounding; the
+ * factor of z (sigmoid, normal distribution) is within 2^-19 of itself for fp32 results and
+ * 2^-18 + 2^-23 (z^2 or |z|) for 16 bits, small values too (below 2^-126 it may be zero).
  * 1 <= N, K <= 2^20, and fewer than 2^24 tiles of 128 x 128 (fp32: 64 x 64) in any
  * product.
  * Errors: TGM_EINVAL (null, sizes, types, strides, scales), TGM_ESIZE (work). */

@@ -69,47 +69,90 @@ __device__ __forceinline__ f4 mfma_wide(const Frag<e4m3> &p, const Frag<e4m3> &q
 }
 
 // ---------------------------------------------------------------- activations
-// The normal distribution function Phi(z) = erfc(-z / sqrt 2) / 2 and e = exp(-z^2/2),
-// by Abramowitz and Stegun's rational approximation 7.1.26 of erfc for x >= 0,
-// erfc(x) = (a1 t + ... + a5 t^5) exp(-x^2) with t = 1 / (1 + 0.3275911 x), within
-// 1.5e-7; Phi of a negative z is that half, so it does not cancel.  About 20
-// instructions, an exponential that the derivative needs as well among them;
-// erff takes three times as many, more than a pass over memory leaves time for.
+// FULL: for results of 32 bits, to a few units of the last place, of small values too; else
+// for 16 bits, with the exponent's rounding (2^-24 times its size) besides.
+//
+// The normal distribution function Phi(z) = erfc(-z / sqrt 2) / 2 and e = exp(-z^2 / 2).
+// For x >= 0, erfc(x) = exp(-x^2) t p(t) with t = 1 / (1 + c x); Phi of a negative z is half
+// of that, so it does not cancel.  p is fitted to the scaled function exp(x^2) erfc(x) by
+// least squares in relative error, reweighted towards the smallest maximum, over every x
+// whose exp(-x^2) is not zero: FULL 9 coefficients, within 4.4e-8 (evaluated in fp32 8e-8
+// rms and 3.5e-7 at most), else 8, within 1.3e-7 (5.1e-7).  About 22 instructions, with an
+// exponential that the derivative needs as well (FULL 32).
 struct Normal {
     float phi, e;
 };
-__device__ __forceinline__ Normal normal_of(float z)
+template <bool FULL> __device__ __forceinline__ Normal normal_of(float z)
 {
-    const float x = fabsf(z) * 0.70710678118654752f;
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
-    float p = fmaf(1.061405429f, t, -1.453152027f);
-    p = fmaf(p, t, 1.421413741f);
-    p = fmaf(p, t, -0.284496736f);
-    p = fmaf(p, t, 0.254829592f);
-    const float e = __expf(-0.5f * z * z);
+    constexpr float k = -0.72134752f;   // -log2(e) / 2, and what is left of it
+    constexpr float k_lo = -9.6298149e-09f;
+    float p, e, t;
+    if constexpr (FULL) {
+        const float a = fabsf(z) > 16.f ? 16.f : fabsf(z);   // exp(-128) is zero
+        t = __builtin_amdgcn_rcpf(fmaf(0.5f * 0.70710678118654752f, a, 1.f));
+        p = fmaf(-0.05926307663321495f, t, 0.2855231761932373f);
+        p = fmaf(p, t, -0.4891655147075653f);
+        p = fmaf(p, t, 0.28031840920448303f);
+        p = fmaf(p, t, -0.028178079053759575f);
+        p = fmaf(p, t, 0.20334427058696747f);
+        p = fmaf(p, t, 0.24293752014636993f);
+        p = fmaf(p, t, 0.28239816427230835f);
+        p = fmaf(p, t, 0.282085120677948f);
+        // the exponent and what its roundings have left out
+        const float s = a * a, v = s * k;
+        const float rest = fmaf(fmaf(a, a, -s), k, fmaf(s, k_lo, fmaf(s, k, -v)));
+        e = __builtin_amdgcn_exp2f(v);
+        e = fmaf(e, rest * 0.69314718f, e);
+    } else {
+        t = __builtin_amdgcn_rcpf(fmaf(0.33f * 0.70710678118654752f, fabsf(z), 1.f));
+        p = fmaf(-0.13381193578243256f, t, 0.4537965655326843f);
+        p = fmaf(p, t, -0.33991068601608276f);
+        p = fmaf(p, t, 0.3979606032371521f);
+        p = fmaf(p, t, 0.052942752838134766f);
+        p = fmaf(p, t, 0.1994291990995407f);
+        p = fmaf(p, t, 0.18325647711753845f);
+        p = fmaf(p, t, 0.18633709847927094f);
+        e = __builtin_amdgcn_exp2f(k * z * z);
+    }
     const float tail = 0.5f * p * t * e;
     return Normal{z > 0.f ? 1.f - tail : tail, e};
 }
+// sigmoid(z) and sigmoid(-z)
+struct Sigmoid {
+    float p, q;
+};
+template <bool FULL> __device__ __forceinline__ Sigmoid sigmoid_of(float z)
+{
+    if constexpr (FULL) {
+        // neither loses its small values, and a step of Newton's for the reciprocal
+        const float e = expf(-fabsf(z)), d = 1.f + e, r0 = __builtin_amdgcn_rcpf(d);
+        const float r = fmaf(r0, fmaf(-d, r0, 1.f), r0), s = e * r;
+        return z > 0.f ? Sigmoid{r, s} : Sigmoid{s, r};
+    } else {
+        const float p = __builtin_amdgcn_rcpf(1.f + __expf(-z));
+        return Sigmoid{p, 1.f - p};
+    }
+}
 
-__device__ __forceinline__ float act_of(float z, int act)
+template <bool FULL> __device__ __forceinline__ float act_of(float z, int act)
 {
     switch (act) {
     case TGM_ACT_RELU: return z > 0.f || z != z ? z : 0.f;
-    case TGM_ACT_SILU: return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));
-    case TGM_ACT_GELU: return z * normal_of(z).phi;
+    case TGM_ACT_SILU: return z * sigmoid_of<FULL>(z).p;
+    case TGM_ACT_GELU: return z * normal_of<FULL>(z).phi;
     default: return z;
     }
 }
-__device__ __forceinline__ float act_grad(float z, int act)
+template <bool FULL> __device__ __forceinline__ float act_grad(float z, int act)
 {
     switch (act) {
     case TGM_ACT_RELU: return z > 0.f ? 1.f : 0.f;
     case TGM_ACT_SILU: {
-        const float p = __builtin_amdgcn_rcpf(1.f + __expf(-z));
-        return p * fmaf(z, 1.f - p, 1.f);
+        const Sigmoid s = sigmoid_of<FULL>(z);
+        return s.p * fmaf(z, s.q, 1.f);
     }
     case TGM_ACT_GELU: {
-        const Normal n = normal_of(z);
+        const Normal n = normal_of<FULL>(z);
         return fmaf(z * 0.39894228040143268f, n.e, n.phi);
     }
     default: return 1.f;
@@ -193,7 +236,7 @@ template <class O, int W> struct Columns {
         if (o.act != TGM_ACT_NONE)
 #pragma unroll
             for (int j = 0; j < W; ++j)
-                v[j] = act_of(v[j], o.act);
+                v[j] = act_of<sizeof(O) == 4>(v[j], o.act);
 #pragma unroll
         for (int j = 0; j < W; ++j)
             p.v[j] = from_f32<O>(o.res ? v[j] + to_f32(res.v[j]) : v[j]);

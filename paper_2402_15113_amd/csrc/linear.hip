@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256) void k_linear_dz(const T *__restrict__ dy,
                     for (int j = 0; j < VEC; ++j) {
                         float v = to_f32(py[u].v[j]);
                         if (act != TGM_ACT_NONE)
-                            v *= act_grad(to_f32(pz[u].v[j]), act);
+                            v *= act_grad<sizeof(T) == 4>(to_f32(pz[u].v[j]), act);
                         po.v[j] = from_f32<T>(v);
                         sum[j] += v;
                     }
