@@ -712,8 +712,8 @@ tgm_status_t tgm_norm_backward(const tgm_norm_desc *d, const void *t, const void
  * result, by the 8-bit matrix instructions, which first add 8 neighbouring
  * columns' products aligned to the largest one and cut below 2^-13 of it.
  * Activations and their derivatives are formed in fp32 from z before its rounding; the
- * factor of z (sigmoid, normal distribution) is within 2^-19 of itself for fp32 results and
- * 2^-18 + 2^-23 (z^2 or |z|) for 16 bits, small values too (below 2^-126 it may be zero).
+ * factor of z (sigmoid, normal distribution) is within 2^-18 of itself, and for 16-bit
+ * results 2^-23 (z^2 or |z|) more, small values too (below 2^-126 it may be zero).
  * 1 <= N, K <= 2^20, and fewer than 2^24 tiles of 128 x 128 (fp32: 64 x 64) in any
  * product.
  * Errors: TGM_EINVAL (null, sizes, types, strides, scales), TGM_ESIZE (work). */
@@ -740,8 +740,11 @@ tgm_status_t tgm_linear(const tgm_linear_desc *d, const void *x, const float *sc
  * as the forward call wrote it:
  *   dz = dy act'(z),  dx = dz W,  dW = dz^T x,  db = sum_rows dz.
  * dx [rows x K], dW [N x K], db [N]; each may be NULL.  act' of ReLU is 0 at 0.
- * dz is rounded to dtype for the products, which take operands of that type;
- * db adds it unrounded.  With no rows dW and db are zero. */
+ * dz is rounded to dtype for the products, which take operands of that type (one
+ * rounding of 16 bits besides the result's: about 1.4 times the error of dx and dW);
+ * db adds it unrounded.  f16, SiLU and GELU: dz is held times a power of two that puts
+ * the largest finite dy near f16's largest value, so no dz becomes infinite or, above
+ * 2^-40 of that dy, zero by its rounding.  With no rows dW and db are zero. */
 tgm_status_t tgm_linear_backward(const tgm_linear_desc *d, const void *x, const void *W,
                                  const void *z, const void *dy, const int32_t *n_rows, void *dx,
                                  void *dW, void *db, void *work, size_t work_bytes, void *stream);

@@ -163,7 +163,7 @@ template <bool FULL> __device__ __forceinline__ float act_grad(float z, int act)
 struct LinearOut {
     void *y, *z;
     const void *bias, *res;
-    const float *sm, *sn;   // scales of the rows and columns of C
+    const float *sm, *sn;   // scales of the rows (1 where null) and columns of C
     int64_t ld_y, ld_z, ld_res;
     int32_t M, N, act;
     const int32_t *n_rows;  // bounds M where given
@@ -226,7 +226,7 @@ template <class O, int W> struct Columns {
         Pack<O, W> p;
 #pragma unroll
         for (int j = 0; j < W; ++j) {
-            if (o.sm)
+            if (o.sn)
                 v[j] *= sm * scale[j];
             v[j] += bias[j];
             p.v[j] = from_f32<O>(v[j]);

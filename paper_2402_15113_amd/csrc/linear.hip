@@ -11,6 +11,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "linear.h"
 
@@ -113,20 +114,74 @@ __global__ __launch_bounds__(64 * W) void k_linear_few(const T *__restrict__ P,
 }
 
 // ---------------------------------------------------------------- dz and db
-// dz = dy act'(z) (stored where `dz` is given) and, with `part`, partial
-// column sums of it: a wavefront takes 64 vectors of VEC columns and every 4
-// gridDim.y-th row.  A last vector of fewer columns moves back to end at the edge;
-// its first columns are counted by the one before.  Bound by memory: 8,192 x 4,096
-// bf16, GELU (201 MB): 47 us, 4.3 TB/s.
+// The largest finite |dy| of each workgroup's rows, a wavefront a row.  Bound by memory: 8,192
+// x 4,096 fp16 (67 MB): 24 us of a gradient of 323, with its launch.
+constexpr int kTops = 512;
 template <class T, int VEC>
+__global__ __launch_bounds__(256) void k_linear_top(const T *__restrict__ dy,
+                                                    const int32_t *n_rows,
+                                                    float *__restrict__ tops, int32_t rows,
+                                                    int32_t N, int64_t ld_y)
+{
+    __shared__ float lds[4];
+    const int32_t R = rows_in_use(rows, n_rows);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    float top = 0.f;
+    for (int64_t m = (int64_t)blockIdx.x * 4 + w; m < R; m += 4 * kTops)
+#pragma unroll 4
+        for (int32_t e = lane * VEC; e < N; e += 64 * VEC) {
+            const Pack<T, VEC> p = load_pack<T, VEC>(dy + m * ld_y + min(e, N - VEC));
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float v = fabsf(to_f32(p.v[j]));
+                top = v < INFINITY && v > top ? v : top;
+            }
+        }
+    top = group_max<64>(top);
+    if (lane == 0)
+        lds[w] = top;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        tops[blockIdx.x] = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+}
+// The power of two that dz is held times: |act'| <= 1.13 keeps it within 65,504.
+__device__ __forceinline__ float dz_scale(const float *__restrict__ tops, float *lds)
+{
+    const int t = threadIdx.x;
+    const float top = group_max<64>(fmaxf(tops[t], tops[t + 256]));
+    static_assert(kTops == 512, "");
+    if ((t & 63) == 0)
+        lds[t >> 6] = top;
+    __syncthreads();
+    const float most = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+    __syncthreads();   // lds has other uses
+    return most > 0.f ? ldexpf(1.f, ilogbf(65504.f / 1.13f / most)) : 1.f;
+}
+
+// dz = dy act'(z) (stored where `dz` is given) and, with `part`, partial column sums of it;
+// SCALED: dz is stored times a power of two, whose reciprocal goes to `unscale` as the
+// scale of the products' K columns.  A wavefront takes 64 vectors of VEC columns and every
+// 4 gridDim.y-th row.  A last vector of fewer columns moves back to end at the edge; its
+// first columns are counted by the one before.  Bound by memory: 8,192 x 4,096
+// bf16, GELU (201 MB): 47 us, 4.3 TB/s.
+template <class T, int VEC, bool SCALED>
 __global__ __launch_bounds__(256) void k_linear_dz(const T *__restrict__ dy,
                                                    const T *__restrict__ z,
                                                    const int32_t *n_rows, T *__restrict__ dz,
                                                    float *__restrict__ part, int32_t rows,
-                                                   int32_t N, int64_t ld_y, int64_t ld_z, int act)
+                                                   int32_t N, int64_t ld_y, int64_t ld_z, int act,
+                                                   const float *__restrict__ tops,
+                                                   float *__restrict__ unscale, int32_t K)
 {
     constexpr int AHEAD = 4;
     __shared__ float lds[4][64 * VEC];
+    float scale = 1.f;
+    if (SCALED) {
+        scale = dz_scale(tops, &lds[0][0]);
+        const int32_t at = (int32_t)(blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
+        for (int32_t k = at; k < K; k += (int32_t)(gridDim.x * gridDim.y) * 256)
+            unscale[k] = 1.f / scale;
+    }
     const int32_t R = rows_in_use(rows, n_rows);
     const int c = threadIdx.x & 63, r = threadIdx.x >> 6;
     const int32_t e = (int32_t)(blockIdx.x * 64 + c) * VEC, n = min(e, N - VEC);
@@ -154,7 +209,7 @@ __global__ __launch_bounds__(256) void k_linear_dz(const T *__restrict__ dy,
                         float v = to_f32(py[u].v[j]);
                         if (act != TGM_ACT_NONE)
                             v *= act_grad<sizeof(T) == 4>(to_f32(pz[u].v[j]), act);
-                        po.v[j] = from_f32<T>(v);
+                        po.v[j] = from_f32<T>(SCALED ? v * scale : v);
                         sum[j] += v;
                     }
                     if (dz)
@@ -256,7 +311,8 @@ size_t split_bytes(int64_t M, int64_t N, int64_t K, int code)
 
 constexpr int kDbParts = 128;
 
-// The work space of the gradient: dz, the partial sums of db, then those of a product.
+// The work space of the gradient: dz, the partial sums of db, dz's scale, then the partial
+// sums of a product.
 size_t db_bytes(int32_t rows, int32_t N)
 {
     return ((size_t)std::min<int64_t>(cdiv(rows, 4), kDbParts) * N * 4 + 15) / 16 * 16;
@@ -264,6 +320,15 @@ size_t db_bytes(int32_t rows, int32_t N)
 size_t dz_bytes(int32_t rows, int32_t N, int32_t dtype, int32_t act)
 {
     return act == TGM_ACT_NONE ? 0 : ((size_t)rows * N * elem_bytes(dtype) + 15) / 16 * 16;
+}
+// fp16's range is narrower than that of dy times a derivative
+bool scales_dz(int32_t dtype, int32_t act)
+{
+    return dtype == TGM_F16 && (act == TGM_ACT_SILU || act == TGM_ACT_GELU);
+}
+size_t scale_bytes(int32_t rows, int32_t K, int32_t dtype, int32_t act)
+{
+    return rows && scales_dz(dtype, act) ? (kTops + (size_t)round_up(K, 4)) * sizeof(float) : 0;
 }
 
 template <class T>
@@ -274,17 +339,32 @@ tgm_status_t backward(const tgm_linear_desc *d, const int64_t *ld, const void *x
     const size_t zb = dz_bytes(d->rows, d->N, d->dtype, d->act);
     T *dz = zb && (dx || dW) ? (T *)work : nullptr;
     float *part = (float *)(work + zb);
-    float *split = (float *)(work + zb + db_bytes(d->rows, d->N));
+    const size_t sb = scale_bytes(d->rows, d->K, d->dtype, d->act);
+    float *tops = dz && sb ? (float *)(work + zb + db_bytes(d->rows, d->N)) : nullptr;
+    float *unscale = tops ? tops + kTops : nullptr;
+    float *split = (float *)(work + zb + db_bytes(d->rows, d->N) + sb);
     const int32_t parts = (int32_t)std::min<int64_t>(cdiv(d->rows, 4), kDbParts);
     if ((dz || db) && parts) {
+        auto go = [&](auto vec) -> tgm_status_t {
+            constexpr int VEC = decltype(vec)::value;
+            const dim3 grid((uint32_t)cdiv(d->N, 64 * VEC), parts);
+            if constexpr (TypeCode<T>::code == TGM_F16)
+                if (tops) {
+                    TGM_LAUNCH((k_linear_top<T, VEC>), dim3(kTops), dim3(256), 0, s,
+                               (const T *)dy, n_rows, tops, d->rows, d->N, ld[4]);
+                    TGM_LAUNCH((k_linear_dz<T, VEC, true>), grid, dim3(256), 0, s, (const T *)dy,
+                               (const T *)z, n_rows, dz, db ? part : nullptr, d->rows, d->N,
+                               ld[4], ld[3], d->act, tops, unscale, d->K);
+                    return TGM_OK;
+                }
+            TGM_LAUNCH((k_linear_dz<T, VEC, false>), grid, dim3(256), 0, s, (const T *)dy,
+                       (const T *)z, n_rows, dz, db ? part : nullptr, d->rows, d->N, ld[4], ld[3],
+                       d->act, tops, unscale, d->K);
+            return TGM_OK;
+        };
         constexpr int VEC = 16 / (int)sizeof(T);
-        const dim3 grid((uint32_t)cdiv(d->N, 64 * (d->N < VEC ? 1 : VEC)), parts);
-        if (d->N < VEC)
-            TGM_LAUNCH((k_linear_dz<T, 1>), grid, dim3(256), 0, s, (const T *)dy, (const T *)z,
-                       n_rows, dz, db ? part : nullptr, d->rows, d->N, ld[4], ld[3], d->act);
-        else
-            TGM_LAUNCH((k_linear_dz<T, VEC>), grid, dim3(256), 0, s, (const T *)dy, (const T *)z,
-                       n_rows, dz, db ? part : nullptr, d->rows, d->N, ld[4], ld[3], d->act);
+        TGM_TRY_STATUS(d->N < VEC ? go(std::integral_constant<int, 1>{})
+                                  : go(std::integral_constant<int, VEC>{}));
     }
     if (db)
         TGM_LAUNCH((k_linear_db<T>), dim3((uint32_t)cdiv(d->N, 32)), dim3(1024), 0, s, part, parts,
@@ -294,11 +374,12 @@ tgm_status_t backward(const tgm_linear_desc *d, const int64_t *ld, const void *x
     if (dx && d->rows) {
         LinearProduct p{W, g, ld[1], ld_g, d->N, nullptr, {}, split, s};
         p.o.y = dx, p.o.ld_y = ld[5], p.o.M = d->rows, p.o.N = d->K, p.o.n_rows = n_rows;
+        p.o.sn = unscale;
         TGM_TRY_STATUS((product<T, T, false, true>(p)));
     }
     if (dW) {
         LinearProduct p{x, g, ld[0], ld_g, d->rows, n_rows, {}, split, s};
-        p.o.y = dW, p.o.ld_y = ld[6], p.o.M = d->N, p.o.N = d->K;
+        p.o.y = dW, p.o.ld_y = ld[6], p.o.M = d->N, p.o.N = d->K, p.o.sn = unscale;
         TGM_TRY_STATUS((product<T, T, false, false>(p)));
     }
     return TGM_OK;
@@ -368,6 +449,7 @@ extern "C" tgm_status_t tgm_linear_work_bytes(int32_t rows, int32_t N, int32_t K
         act > TGM_ACT_GELU || !(wide_type(dtype) || (dtype == TGM_E4M3 && !backward)))
         return TGM_EINVAL;
     *bytes = backward ? dz_bytes(rows, N, dtype, act) + db_bytes(rows, N) +
+                            scale_bytes(rows, K, dtype, act) +
                             std::max(split_bytes(rows, K, N, dtype), split_bytes(N, K, rows, dtype))
                       : few_blocks(rows, N, K, dtype) ? 0 : split_bytes(rows, N, K, dtype);
     return TGM_OK;
