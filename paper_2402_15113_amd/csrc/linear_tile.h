@@ -241,6 +241,16 @@ template <class T, bool KC, int X, int TH, bool DIRECT> struct Operand {
     }
 };
 
+// Between a wavefront's lanes' writes to LDS and its other lanes' reads of them, and back:
+// LDS serves a wavefront in order, so that only the compiler has to be kept from moving
+// them (no instruction).
+__device__ __forceinline__ void lanes_exchange()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // Which tile workgroup `id` takes: every XCD (id % 8) a run of neighbouring tiles,
 // 8 rows of tiles deep, so that its L2 holds what they share.
 struct TileAt {
@@ -547,6 +557,7 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
                     *reinterpret_cast<f4 *>(mine + lane % LANES * PITCH + SIDE * a +
                                             4 * (lane / LANES) + 8 * u) =
                         sums(cc * (CW / SIDE) + a, b, u);
+            lanes_exchange();
 #pragma unroll
             for (int i = 0; i < PASSES; ++i) {
                 const int32_t m = m0 + wm + SIDE * b + PASS * i + row;
@@ -557,6 +568,7 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
                 if (m < M && columns.left > 0)
                     columns.finish(o, m, n, v, sm[b][i], res[b][i]);
             }
+            lanes_exchange();
         }
     }
 }
