@@ -226,8 +226,8 @@ template <class O, int W> struct Columns {
         Pack<O, W> p;
 #pragma unroll
         for (int j = 0; j < W; ++j) {
-            if (o.sn)
-                v[j] *= sm * scale[j];
+            if (o.sn)   // one after the other: the scales' product may leave fp32
+                v[j] = v[j] * sm * scale[j];
             v[j] += bias[j];
             p.v[j] = from_f32<O>(v[j]);
         }

@@ -1,4 +1,5 @@
-"""tgm_linear_backward in fp16 where dy times the activation's derivative leaves fp16's range
+"""Products past the range of their types: 8-bit scales whose product leaves fp32, and
+tgm_linear_backward in fp16 where dy times the activation's derivative leaves fp16's range
 and the gradients do not: large and small dy, both in one call, infinities and row counts.
 Against fp64; tolerances (opref): the rounding of dz, held times a power of two of at least
 65,504 / (2.26 max|dy|), the sums' error in any order, one rounding of the result."""
@@ -8,7 +9,7 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-from opref import F64, STEP, U, act, act_grad_err, check, half_step, rounded  # noqa: E402
+from opref import F64, STEP, U, act, act_grad_err, check, cut, half_step, rounded  # noqa: E402
 
 F16 = torch.float16
 
@@ -101,3 +102,27 @@ def test_zeros_and_infinities(tgm):
     assert torch.equal(dw[rest], want[1][rest]) and torch.equal(db[rest], want[2][rest])
     dy[5, 7] = float("nan")
     assert torch.isnan(run(tgm, x, w, z, dy, "silu")[2][7])
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,N,K", [(20, 24, 64), (700, 264, 128)])
+def test_scales_whose_product_leaves_fp32(tgm, rows, N, K, out):
+    """8-bit products with scales of 2^-126 and 2^-24, and of 2^100 each where the sum is
+    zero: the results are ordinary fp32 values, their scales' product is not."""
+    E4M3, ot = torch.float8_e4m3fn, dict(f32=torch.float32, bf16=torch.bfloat16)[out]
+    x, w = (256 * randn(1, rows, K)).clamp(-448, 448).to(E4M3), torch.full((N, K), 448.0).to(E4M3)
+    x.view(torch.uint8)[rows // 2:] = 0
+    sx, sw = torch.full((rows,), 2.0 ** -126), torch.full((N,), 2.0 ** -24)
+    sx[rows // 2:], sw[N // 2:] = 2.0 ** 100, 2.0 ** 100
+    y = torch.empty(rows, N, device="cuda", dtype=ot)
+    k = torch.empty(max(16, tgm.tgm_linear_work_bytes(rows, N, K, E4M3)), dtype=torch.uint8,
+                    device="cuda")
+    tgm.tgm_linear(x.cuda(), w.cuda(), y, k, scale_x=sx.cuda(), scale_w=sw.cuda())
+    x, w = x.to(F64), w.to(F64)
+    s = sx.to(F64)[:, None] * sw.to(F64)[None]
+    ref, size = (x @ w.t()) * s, (x.abs() @ w.abs().t()) * s
+    lost = 0 if ot == torch.float32 else cut(x, w) * s
+    # the sum, and a product below 2^-126, which keeps no more than steps of 2^-149
+    err = (K + 8) * U * size + lost + 2.0 ** -149
+    check("y", y, ref, err + rounded(ref.abs() + err, ot))
+    assert (y[rows // 2:] == 0).all() and (y[:rows // 2, :N // 2] != 0).any()
