@@ -707,7 +707,15 @@ def _call(fn, gpu, stream, *args):
         _check(fn, rc)
 
 
+def _sizes(fn, args, types):
+    """Refuse whole numbers that the C types would cut short."""
+    for v, t in zip(args, types):
+        if t(v).value != v:
+            raise ValueError(f"{fn}: {v} is out of range")
+
+
 def _bytes(fn, *args) -> int:
+    _sizes(fn, args, getattr(lib(), fn).argtypes)
     n = C.c_size_t(0)
     _check(fn, getattr(lib(), fn)(*args, C.byref(n)))
     return int(n.value)
@@ -816,6 +824,7 @@ def tgm_linear_backward(x, w, dy, work, act="none", z=None, dx=None, dw=None, db
 
 
 def tgm_scan_carry_rows(rows, S, packed) -> int:
+    _sizes("tgm_scan_carry_rows", (rows, S), (I64, I32))
     n = I64()
     _check("tgm_scan_carry_rows", lib().tgm_scan_carry_rows(rows, S, 1 if packed else 0,
                                                             C.byref(n)))
@@ -829,6 +838,8 @@ def tgm_scan_work_bytes(rows, D, S) -> int:
 def _scan_args(g, x, S, offsets, length, h0):
     import torch
     rows, D = _shape2("g", g)
+    if not 0 <= S < 1 << 31:
+        raise ValueError(f"S is {S}")
     gpu, dt = g.get_device(), g.dtype
     pg, lg = _arg("g", g, dt, (rows, D), gpu)
     px, lx = _arg("x", x, dt, (rows, D), gpu)

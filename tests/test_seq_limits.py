@@ -34,3 +34,23 @@ def test_scan_refuses_forward_and_back(L, rows, S, D, packed):
     if packed:
         with pytest.raises(tgm.TgmError):
             tgm.tgm_scan_work_bytes(rows, D, S)
+
+
+@pytest.mark.parametrize("wide", [1 << 31, (1 << 32) + 3, -(1 << 32) + 3])
+def test_binding_cuts_no_size_short(wide):
+    """3 plus a multiple of 2^32 is not 3."""
+    f32 = torch.float32
+    for call in (lambda: tgm.tgm_norm_work_bytes(wide, 64), lambda: tgm.tgm_norm_work_bytes(3, wide),
+                 lambda: tgm.tgm_linear_work_bytes(wide, 3, 3, f32),
+                 lambda: tgm.tgm_linear_work_bytes(3, wide, 3, f32, backward=True),
+                 lambda: tgm.tgm_linear_work_bytes(3, 3, wide, f32),
+                 lambda: tgm.tgm_scan_work_bytes(96, 64, wide),
+                 lambda: tgm.tgm_scan_work_bytes(96, wide, 3),
+                 lambda: tgm.tgm_scan_carry_rows(96, wide, False)):
+        with pytest.raises(ValueError, match="out of range"):
+            call()
+    g = torch.zeros(96, 64)
+    for call in (lambda: tgm.tgm_scan(g, g, g, wide, None),
+                 lambda: tgm.tgm_scan_backward(g, g, g, None, g, g, wide, None)):
+        with pytest.raises(ValueError, match="S is"):
+            call()
