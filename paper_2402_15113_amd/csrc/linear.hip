@@ -434,8 +434,12 @@ LinearPlan tgm::linear_plan(int64_t M, int64_t N, int64_t K, int code)
     if (cdiv(large, 256) * 4 <= cdiv(small, 256) && large >= (f32 ? 512 : 192) &&
         (f32 || steps >= 16))
         return LinearPlan{true, 1};
-    // half as many large tiles as CUs, and a sum that is long in halves too: the weights'
-    // gradient of 8,192 rows of a 4,096 x 2,048 layer, 147 us against 156
+    // half as many large tiles as CUs or a little less, and a sum that is long in halves too.
+    // us, bf16, two parts of the large tile against the small one's, rows x columns x sum:
+    // 4,096 x 2,048 x 8,192: 123, 130 (x 4,096: 72, 65; x 2,048: 50, 37); 2,560 x 2,560 x 16,384: 178,
+    // 204; 6,144 x 1,024 x 8,192: 98, 102; but 2,048 x 2,048 (64 tiles) x 8,192: 85, 72; weights'
+    // gradients: 4,096 x 2,048 x 8,192: 124, 129 (x 4,096: 76, 70); 2,560 x 2,560 x 8,192: 108, 115;
+    // 2,048 x 2,048 x 8,192: 95, 76.
     if (!f32 && large >= 96 && large <= 128 && steps >= 128)
         return LinearPlan{true, 2};
     return LinearPlan{
