@@ -43,8 +43,8 @@ template <class T> __device__ __forceinline__ Frag<T> load_frag(const T *row, in
 // workgroup takes 16 columns and 16 MB rows of C; its wavefronts share the sum, each a
 // run of it, and add up through LDS, so that a short sum needs no second launch.
 // Operands come straight from memory into the matrix instructions, eight loads of
-// a row of W at a time.  fp16, 4 and 16 rows, 4,096 x 2,048 (W of 16.8 MB): 5.4 and 6.5 us,
-// 2.6 TB/s; fp32, 16 rows, 8,192 x 2,048: 18.3 us, 3.7 TB/s.
+// a row of W at a time.  fp16, 4 rows, 4,096 x 2,048 (W of 16.8 MB): 6.8 us, 2.5
+// TB/s; fp32, 16 rows, 8,192 x 2,048: 18.3 us, 3.7 TB/s.
 template <class T, class O, int MB, int W>
 __global__ __launch_bounds__(64 * W) void k_linear_few(const T *__restrict__ P,
                                                        const T *__restrict__ Q, int64_t ld_p,
@@ -115,19 +115,20 @@ __global__ __launch_bounds__(64 * W) void k_linear_few(const T *__restrict__ P,
 
 // ---------------------------------------------------------------- dz and db
 // The largest finite |dy| of each workgroup's rows, a wavefront a row.  Bound by memory: 8,192
-// x 4,096 fp16 (67 MB): 24 us of a gradient of 323, with its launch.
+// x 4,096 fp16 (67 MB): 19 us, 3.6 TB/s, of a gradient of 320.
 constexpr int kTops = 512;
 template <class T, int VEC>
-__global__ __launch_bounds__(256) void k_linear_top(const T *__restrict__ dy,
-                                                    const int32_t *n_rows,
-                                                    float *__restrict__ tops, int32_t rows,
-                                                    int32_t N, int64_t ld_y)
+__global__ __launch_bounds__(1024) void k_linear_top(const T *__restrict__ dy,
+                                                     const int32_t *n_rows,
+                                                     float *__restrict__ tops, int32_t rows,
+                                                     int32_t N, int64_t ld_y)
 {
-    __shared__ float lds[4];
+    constexpr int W = 16;
+    __shared__ float lds[W];
     const int32_t R = rows_in_use(rows, n_rows);
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     float top = 0.f;
-    for (int64_t m = (int64_t)blockIdx.x * 4 + w; m < R; m += 4 * kTops)
+    for (int64_t m = (int64_t)blockIdx.x * W + w; m < R; m += W * kTops)
 #pragma unroll 4
         for (int32_t e = lane * VEC; e < N; e += 64 * VEC) {
             const Pack<T, VEC> p = load_pack<T, VEC>(dy + m * ld_y + min(e, N - VEC));
@@ -141,8 +142,11 @@ __global__ __launch_bounds__(256) void k_linear_top(const T *__restrict__ dy,
     if (lane == 0)
         lds[w] = top;
     __syncthreads();
-    if (threadIdx.x == 0)
-        tops[blockIdx.x] = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+    if (threadIdx.x == 0) {
+        for (int k = 1; k < W; ++k)
+            top = fmaxf(top, lds[k]);
+        tops[blockIdx.x] = top;
+    }
 }
 // The power of two that dz is held times: |act'| <= 1.13 keeps it within 65,504.
 __device__ __forceinline__ float dz_scale(const float *__restrict__ tops, float *lds)
@@ -163,7 +167,7 @@ __device__ __forceinline__ float dz_scale(const float *__restrict__ tops, float 
 // scale of the products' K columns.  A wavefront takes 64 vectors of VEC columns and every
 // 4 gridDim.y-th row.  A last vector of fewer columns moves back to end at the edge; its
 // first columns are counted by the one before.  Bound by memory: 8,192 x 4,096
-// bf16, GELU (201 MB): 47 us, 4.3 TB/s.
+// bf16, GELU (201 MB): 49 us, 4.1 TB/s.
 template <class T, int VEC, bool SCALED>
 __global__ __launch_bounds__(256) void k_linear_dz(const T *__restrict__ dy,
                                                    const T *__restrict__ z,
@@ -231,7 +235,7 @@ __global__ __launch_bounds__(256) void k_linear_dz(const T *__restrict__ dy,
 }
 
 // db = the P partial sums added up in order: 32 columns a workgroup, 32 threads each (128
-// partial rows of 4,096: 4 us, most of it the launch).
+// partial rows of 4,096: 5.5 us, most of it the launch).
 template <class T>
 __global__ __launch_bounds__(1024) void k_linear_db(const float *__restrict__ part, int32_t P,
                                                     int32_t N, T *__restrict__ db)
@@ -350,7 +354,7 @@ tgm_status_t backward(const tgm_linear_desc *d, const int64_t *ld, const void *x
             const dim3 grid((uint32_t)cdiv(d->N, 64 * VEC), parts);
             if constexpr (TypeCode<T>::code == TGM_F16)
                 if (tops) {
-                    TGM_LAUNCH((k_linear_top<T, VEC>), dim3(kTops), dim3(256), 0, s,
+                    TGM_LAUNCH((k_linear_top<T, VEC>), dim3(kTops), dim3(1024), 0, s,
                                (const T *)dy, n_rows, tops, d->rows, d->N, ld[4]);
                     TGM_LAUNCH((k_linear_dz<T, VEC, true>), grid, dim3(256), 0, s, (const T *)dy,
                                (const T *)z, n_rows, dz, db ? part : nullptr, d->rows, d->N,
