@@ -574,7 +574,7 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
 }
 
 // The parts' sums added in order.  Bound by memory: two parts of 4,096 x 2,048, to bf16
-// (84 MB): 15 us, 5.6 TB/s.
+// (84 MB): 16 us, 5.2 TB/s.
 template <class O>
 __global__ __launch_bounds__(256) void k_linear_join(const float *__restrict__ work, LinearOut o,
                                                      int32_t parts)

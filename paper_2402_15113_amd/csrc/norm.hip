@@ -48,7 +48,7 @@ template <int G, bool MAX> __device__ __forceinline__ float row_all(float v, flo
     return v;
 }
 
-// 8,192 rows of 4,096 bf16, added to a residual and out in 8 bits (235 MB): 49.6 us, 4.7 TB/s.
+// 8,192 rows of 4,096 bf16, added to a residual and out in 8 bits (235 MB): 50.8 us, 4.6 TB/s.
 template <class T, class O, int VEC, int G, int NV>
 __global__ __launch_bounds__((G > 256 ? G : 256)) void k_norm(
     const T *x, const T *res, const T *__restrict__ w, const int32_t *__restrict__ n_rows,
@@ -138,7 +138,7 @@ __global__ __launch_bounds__((G > 256 ? G : 256)) void k_norm(
 // lanes' part of dw in registers over all of them and leaves one partial row
 // of dw in `part`; k_norm_dw adds the partial rows in order.  Bound by memory: 8,192
 // bf16 rows of 8,192 (403 MB), both: 87 us, 4.6 TB/s; 12,000 fp32 rows of 100 (14 MB): 5.4
-// and 2.9 us, of which a launch that does nothing would take half.
+// and 2.8 us, of which a launch that does nothing would take half.
 template <class T, int VEC, int G, int NV>
 __global__ __launch_bounds__((G > 256 ? G : 256)) void k_norm_bwd(
     const T *t_, const T *__restrict__ w, const T *dy, const T *dtotal,

@@ -353,7 +353,7 @@ __device__ __forceinline__ float lift(float P, float low)
 // no gate of the rows in `valid` is.  lowest(r, v): row r's gate, or what it grows with;
 // is_zero(its lowest one): whether that gate is zero.
 template <int V, class L, class Z>
-__device__ __forceinline__ void raise(float (&P)[V], uint32_t valid, L lowest, Z is_zero)
+__device__ __forceinline__ void lift_tile(float (&P)[V], uint32_t valid, L lowest, Z is_zero)
 {
     if (__builtin_expect(!__any(P[0] == 0.f || P[V - 1] == 0.f), 1))
         return;
@@ -602,8 +602,8 @@ __device__ __forceinline__ void enter(const ScanArgs &A, int place, const Lane &
 // ---------------------------------------------------------------- the passes
 // ALONE: no sequence leaves its tile (short padded ones).  Bound by memory: 12,000 padded
 // sequences of 10 rows, 100 fp32 channels (144 MB): 31 us, 4.6 TB/s; by the chain's hand-over
-// besides where there is one: 1,000,003 rows of 128 bf16 (768 MB): 210 us, 3.7 TB/s;
-// 131,072 of 512 (403 MB, and the carries): 125 us, 3.2 TB/s.
+// besides where there is one: 1,000,003 rows of 128 bf16 (768 MB): 216 to 228 us, 3.4 TB/s;
+// 131,072 of 512 (403 MB, and the carries): 126 us, 3.2 TB/s.
 template <class T, int V, int W, bool ALONE>
 __global__ __launch_bounds__(64 * W, 4) void k_scan(ScanArgs A)
 {
@@ -694,7 +694,7 @@ __global__ __launch_bounds__(64 * W, 4) void k_scan(ScanArgs A)
             for (int v = 0; v < V; ++v)
                 P[v] = -1.f;
         else
-            raise<V>(P, in.valid, [&](int r, int v) { return pg[r].at(v); },
+            lift_tile<V>(P, in.valid, [&](int r, int v) { return pg[r].at(v); },
                      [](float a) { return (KEEP ? a : gate_of(a).a) == 0.f; });
         const bool need = in.valid & ~in.first & 1;
         enter<V, W>(A, place, c, need, P, Q, h);
@@ -741,7 +741,7 @@ __global__ __launch_bounds__(64 * W, 4) void k_scan(ScanArgs A)
 // The gradient's pass, tiles in the other order: a row hands a e back to the
 // one before it, with e = dy + what it was handed itself.  Five rows a row where the
 // pass forward has three, so half as many wavefronts fit a CU: 131,072 rows of 512 bf16
-// (671 MB): 197 us, 3.4 TB/s.
+// (671 MB): 203 us, 3.3 TB/s.
 template <class T, int V, int W, bool ALONE>
 __global__ __launch_bounds__(64 * W, 2) void k_scan_bwd(ScanArgs A)
 {
@@ -857,7 +857,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_bwd(ScanArgs A)
             for (int v = 0; v < V; ++v)
                 P[v] = -1.f;
         else
-            raise<V>(P, in.valid, [&](int r, int v) { return pg[r].at(v); },
+            lift_tile<V>(P, in.valid, [&](int r, int v) { return pg[r].at(v); },
                      [](float g) { return gate_of(g).a == 0.f; });
         const bool need = ((in.valid & ~in.last) >> (t.n - 1)) & 1;
         enter<V, W>(A, place, c, need, P, Q, e);
@@ -897,7 +897,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_bwd(ScanArgs A)
         rows(std::false_type{});
 }
 
-// Before a pass with a chain: none of its words is there and no task is taken (4 us).
+// Before a pass with a chain: none of its words is there and no task is taken (5 us).
 __global__ __launch_bounds__(256) void k_scan_begin(uint64_t *words, int64_t n, int32_t *ticket)
 {
     const int64_t threads = (int64_t)gridDim.x * 256, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
