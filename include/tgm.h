@@ -674,6 +674,8 @@ tgm_status_t tgm_min_staleness(const double *tau, int64_t n, int32_t k_max, int3
  *   scale = max(max_j |y_j| / 448, 2^-126), stored y = y / scale to the nearest
  *   8-bit value (ties to even).  The maximum passes over NaN; a row with an
  *   infinite y has an infinite scale, and NaN or 0 for values.
+ * Squares and their sum are fp32: where they leave its range (|t| above 2^64 / sqrt(D) or
+ * so) y is 0, and where they vanish (|t| below 2^-75) eps alone is left.
  * total may be x or res, and y (of out_dtype == dtype) may be x or res unless
  * total is that one, each with the same stride.  1 <= D <= 32768.
  * Errors: TGM_EINVAL (null, sizes, types, strides, eps negative or NaN). */
