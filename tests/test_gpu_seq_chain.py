@@ -211,3 +211,42 @@ def test_a_long_history_past_32_bit_offsets(tgm):
     e = 2 * recurrence(a, (gate + 6 * U) * ((a * ref.roll(1, 0)).abs() + (i * X).abs()))
     k = 3000
     check("y", y[-k:], ref[-k:].cpu(), (e + rounded(ref.abs() + e, y.dtype))[-k:].cpu())
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype,D", [("f32", 600), ("f16", 1030)])
+def test_wide_padded(tgm, dtype, D, reverse):
+    """Long padded sequences with lengths, short ones that share a tile, and ones without
+    rows, more channels than one counter a block serves."""
+    for kw in (dict(S=3, L=700, length=[700, 0, 431]), dict(S=40, L=10, length=[7] * 39 + [0]),
+               dict(S=5, L=33), dict(lengths=[0] * 30 + [600] + [0] * 30)):
+        Batch(tgm, D, TYPES[dtype], reverse=reverse, **kw).run()
+
+
+def test_wide_calls_captured(tgm):
+    """A wide call and its gradient in a graph, replayed on new inputs with eager calls
+    between the replays."""
+    kw = dict(lengths=[1500, 0, 900], extra=3)
+    b, eager = (Batch(tgm, 1100, torch.bfloat16, **kw) for _ in range(2))
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        b.forward()
+        b.backward()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        b.forward()
+        b.backward()
+    for k in range(4):
+        for v, e in ((b.x, eager.x), (b.dy, eager.dy), (b.h0, eager.h0)):
+            v.copy_(torch.randn(v.shape, generator=torch.Generator().manual_seed(k)))
+            e.copy_(v)
+        eager.forward()
+        eager.backward()
+        if k % 2:
+            torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in ("y", "h_last", "dg", "dx", "dh0"):
+            assert torch.equal(getattr(b, n), getattr(eager, n)), (k, n)

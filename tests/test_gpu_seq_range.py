@@ -126,3 +126,37 @@ def test_scales_whose_product_leaves_fp32(tgm, rows, N, K, out):
     err = (K + 8) * U * size + lost + 2.0 ** -149
     check("y", y, ref, err + rounded(ref.abs() + err, ot))
     assert (y[rows // 2:] == 0).all() and (y[:rows // 2, :N // 2] != 0).any()
+
+
+def test_captured_with_other_sizes_of_dy(tgm):
+    """The scale of dz and the row count are the replay's, not the capture's."""
+    rows, N, K = 150, 64, 40
+    x, w, z, dy = (v.to(F16).cuda() for v in (randn(3, rows, K), randn(4, N, K) / 8,
+                                              randn(1, rows, N), randn(2, rows, N)))
+    nr = torch.tensor([rows], dtype=torch.int32, device="cuda")
+    size = tgm.tgm_linear_work_bytes(rows, N, K, F16, act="gelu", backward=True)
+    out, want = ([torch.zeros(rows, K), torch.zeros(N, K), torch.zeros(N)] for _ in range(2))
+    out, want = ([v.to(F16).cuda() for v in o] for o in (out, want))
+    works = [torch.empty(size, dtype=torch.uint8, device="cuda").fill_(255) for _ in range(2)]
+
+    def call(o, k):
+        tgm.tgm_linear_backward(x, w, dy, k, act="gelu", z=z, dx=o[0], dw=o[1], db=o[2], n_rows=nr)
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        call(out, works[0])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        call(out, works[0])
+    for k, (scale, n) in enumerate(((1e-6, rows), (1.0, 77), (9000.0, rows), (0.0, 5), (1e-3, 0))):
+        dy.copy_((randn(20 + k, rows, N) * scale).clamp(-60000, 60000))
+        nr.fill_(n)
+        for o in (out, want):
+            o[0].zero_()
+        call(want, works[1])
+        graph.replay()
+        torch.cuda.synchronize()
+        for u, v in zip(out, want):
+            assert torch.equal(u, v), k
