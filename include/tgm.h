@@ -774,6 +774,7 @@ tgm_status_t tgm_linear_backward(const tgm_linear_desc *d, const void *x, const 
  * sampled neighbours need, which lie newest first.
  * carry (may be NULL) [tgm_scan_carry_rows x D] fp32 receives the states inside
  * the sequences that tgm_scan_backward starts from.
+ * Up to 63 calls (this one and its gradient together) may run on a GPU at the same time.
  * y may be g or x, with the same stride.  rows <= 2^30, D <= 65536, and with T =
  * tgm_scan_carry_rows, T ceil(D / 64) <= 2^26 - 2^15 (with 16-bit elements up to about
  * twice that is taken), here and in tgm_scan_backward alike.
