@@ -635,6 +635,7 @@ tgm_status_t tgm_min_staleness(const double *tau, int64_t n, int32_t k_max, int3
  *   tgm_linear         matrix product with bias, activation and residual
  *   tgm_scan           gated linear recurrence along packed or padded histories
  *   tgm_scan_step      one row of it for each of n slots of a state table
+ *   tgm_rotary         rotary positions, by place or event time; its own gradient
  *   tgm_..._backward   their gradients
  *
  * Conventions, besides those at the top of this file:
@@ -819,6 +820,52 @@ tgm_status_t tgm_scan_backward(const tgm_scan_desc *d, const void *g, const void
 tgm_status_t tgm_scan_step(const tgm_scan_desc *d, const void *g, const void *x,
                            const int32_t *slots, const int32_t *n_rows, float *state, void *y,
                            void *stream);
+
+/* Rotary positions: in each of H heads of d columns, the first rot columns are pairs
+ * (x_a, x_b) that are turned by the angle p omega_j, p the row's position:
+ *   y_a = A (x_a cos - x_b sin),  y_b = A (x_b cos + x_a sin),  j = 0 .. rot / 2 - 1,
+ * a = j, b = j + rot / 2 (TGM_ROTARY_HALF) or a = 2 j, b = 2 j + 1
+ * (TGM_ROTARY_INTERLEAVED), A = amplitude; the other columns are copied.  inverse != 0
+ * turns by -p omega_j: with the forward call's arguments that is the gradient in x from the
+ * one in y.  x, y [rows x H d] have type dtype (f32, bf16 or f16); q and k that lie side
+ * by side in one matrix are one call.  omega [rot / 2] fp64 on the device (as
+ * tgm_rotary_frequencies gives them), pos [rows] of pos_type: places (int32, int64) or event
+ * times (fp64); NULL: the row's number.  Angles are formed and reduced in fp64: their error
+ * is 2^-24 and 2^-52 of the angle (|p omega_j| up to 2^40; what is turned by more has no
+ * meaning, an infinite or NaN angle gives NaN).  y may be x, with the same stride; the
+ * columns that are not turned are then left alone.  1 <= H <= 4096, 2 <= rot <= d <= 1024,
+ * rot even.  Errors: TGM_EINVAL (null, sizes, types, strides). */
+#define TGM_ROTARY_HALF 0
+#define TGM_ROTARY_INTERLEAVED 1
+#define TGM_POS_I32 0
+#define TGM_POS_I64 1
+#define TGM_POS_F64 2
+typedef struct {
+    int32_t rows, H, d, rot;
+    int32_t dtype, pos_type, layout, inverse;
+    float amplitude;
+    int64_t ld_x, ld_y;
+} tgm_rotary_desc;
+tgm_status_t tgm_rotary(const tgm_rotary_desc *d, const void *x, const double *omega,
+                        const void *pos, const int32_t *n_rows, void *y, void *stream);
+
+/* The frequencies of rot / 2 pairs, omega_j = base^(-2 j / rot), and the amplitude of
+ * cos and sin, for histories `factor` >= 1 times as long as those that a model has seen:
+ *   TGM_ROTARY_PLAIN   as they are;
+ *   TGM_ROTARY_LINEAR  omega_j / factor;
+ *   TGM_ROTARY_BASE    base factor^(rot / (rot - 2)) for base, which divides the lowest
+ *                      frequency by factor and leaves the highest;
+ *   TGM_ROTARY_PARTS   pairs that turn at least `often` times within `original` positions
+ *                      keep theirs, those that turn at most `seldom` times have it divided,
+ *                      a line between; amplitude 0.1 ln(factor) + 1 (else 1).
+ * HOST arrays omega [rot / 2] and amplitude [1]; touches no device.  Errors: TGM_EINVAL. */
+#define TGM_ROTARY_PLAIN 0
+#define TGM_ROTARY_LINEAR 1
+#define TGM_ROTARY_BASE 2
+#define TGM_ROTARY_PARTS 3
+tgm_status_t tgm_rotary_frequencies(int32_t rot, int32_t scaling, double base, double factor,
+                                    double original, double often, double seldom, double *omega,
+                                    float *amplitude);
 
 /* ------------------------------------------------------------------------
  * Per-kernel timing.  When enabled, every kernel the library launches is

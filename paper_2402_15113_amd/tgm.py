@@ -38,7 +38,7 @@ SYMBOLS = ["tgm_status_str", "tgm_last_device_error", "tgm_version", "tgm_alloc_
            "tgm_norm", "tgm_norm_work_bytes", "tgm_norm_backward",
            "tgm_linear", "tgm_linear_work_bytes", "tgm_linear_backward",
            "tgm_scan", "tgm_scan_carry_rows", "tgm_scan_work_bytes", "tgm_scan_backward",
-           "tgm_scan_step",
+           "tgm_scan_step", "tgm_rotary", "tgm_rotary_frequencies",
            "tgm_profile_enable", "tgm_profile_reset", "tgm_profile_count", "tgm_profile_get"]
 
 
@@ -117,9 +117,22 @@ class ScanDesc(C.Structure):
                 ("ld_y", C.c_int64), ("ld_dg", C.c_int64), ("ld_dx", C.c_int64)]
 
 
+class RotaryDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("H", C.c_int32), ("d", C.c_int32), ("rot", C.c_int32),
+                ("dtype", C.c_int32), ("pos_type", C.c_int32), ("layout", C.c_int32),
+                ("inverse", C.c_int32), ("amplitude", C.c_float), ("ld_x", C.c_int64),
+                ("ld_y", C.c_int64)]
+
+
 TGM_F32, TGM_BF16, TGM_F16, TGM_E4M3 = 0, 1, 2, 3
 TGM_ACT_NONE, TGM_ACT_RELU, TGM_ACT_SILU, TGM_ACT_GELU = 0, 1, 2, 3
 ACTS = {"none": TGM_ACT_NONE, "relu": TGM_ACT_RELU, "silu": TGM_ACT_SILU, "gelu": TGM_ACT_GELU}
+TGM_ROTARY_HALF, TGM_ROTARY_INTERLEAVED = 0, 1
+ROTARY_LAYOUTS = {"half": TGM_ROTARY_HALF, "interleaved": TGM_ROTARY_INTERLEAVED}
+TGM_POS_I32, TGM_POS_I64, TGM_POS_F64 = 0, 1, 2
+TGM_ROTARY_PLAIN, TGM_ROTARY_LINEAR, TGM_ROTARY_BASE, TGM_ROTARY_PARTS = 0, 1, 2, 3
+ROTARY_SCALINGS = {"none": TGM_ROTARY_PLAIN, "linear": TGM_ROTARY_LINEAR,
+                   "base": TGM_ROTARY_BASE, "parts": TGM_ROTARY_PARTS}
 
 _lib = None
 V, I32, I64, P = C.c_void_p, C.c_int32, C.c_int64, C.c_void_p
@@ -202,6 +215,9 @@ def lib():
             "tgm_norm": [C.POINTER(NormDesc), P, P, P, P, P, P, P, V],
             "tgm_norm_work_bytes": [I32, I32, C.POINTER(C.c_size_t)],
             "tgm_norm_backward": [C.POINTER(NormDesc), P, P, P, P, P, P, P, P, C.c_size_t, V],
+            "tgm_rotary": [C.POINTER(RotaryDesc), P, P, P, P, P, V],
+            "tgm_rotary_frequencies": [I32, I32, C.c_double, C.c_double, C.c_double, C.c_double,
+                                       C.c_double, P, C.POINTER(C.c_float)],
         }
         sig["tgm_profile_enable"] = [I32]
         sig["tgm_profile_reset"] = []
@@ -900,3 +916,58 @@ def tgm_scan_step(g, x, state, y, slots=None, n_rows=None, stream=None):
     pn, _ = _opt("n_rows", n_rows, torch.int32, (1,), gpu)
     d = ScanDesc(rows, S, D, dtype_code(dt), 0, lg, lx, ly, 0, 0)
     _call("tgm_scan_step", gpu, stream, C.byref(d), pg, px, pt, pn, ps, py)
+
+
+def _choice(what, name, choices) -> int:
+    if name not in choices:
+        raise ValueError(f"{what} is one of {sorted(choices)}, not {name!r}")
+    return choices[name]
+
+
+_pos_codes = {}   # torch types to TGM_POS_I32, ...
+
+
+def tgm_rotary(x, y, heads, omega, pos=None, layout="half", amplitude=1.0, inverse=False,
+               n_rows=None, stream=None):
+    """y = x [rows x heads d] with the first 2 len(omega) columns of each head turned by
+    ``pos`` (int32, int64 or float64; the row's number without) times ``omega`` (float64, on
+    the GPU); ``inverse`` turns back, which is the gradient."""
+    import torch
+    if not _pos_codes:
+        _pos_codes.update({torch.int32: TGM_POS_I32, torch.int64: TGM_POS_I64,
+                           torch.float64: TGM_POS_F64})
+    rows, W = _shape2("x", x)
+    gpu, dt = x.get_device(), x.dtype
+    if not 0 < heads <= W or W % heads:
+        raise ValueError(f"x's {W} columns are no {heads} heads")
+    if omega is None or omega.dim() != 1:
+        raise ValueError("omega is a vector")
+    pairs = omega.shape[0]
+    if 2 * pairs > W // heads:
+        raise ValueError(f"{pairs} pairs in heads of {W // heads} columns")
+    kind = TGM_POS_I32
+    if pos is not None:
+        kind = _pos_codes.get(pos.dtype)
+        if kind is None:
+            raise ValueError(f"pos has type {pos.dtype}")
+    px, lx = _arg("x", x, dt, (rows, W), gpu)
+    py, ly = _arg("y", y, dt, (rows, W), gpu)
+    pw, _ = _arg("omega", omega, torch.float64, (pairs,), gpu)
+    pp, _ = _opt("pos", pos, pos.dtype if pos is not None else None, (rows,), gpu)
+    pn, _ = _opt("n_rows", n_rows, torch.int32, (1,), gpu)
+    d = RotaryDesc(rows, heads, W // heads, 2 * pairs, dtype_code(dt), kind,
+                   _choice("layout", layout, ROTARY_LAYOUTS), 1 if inverse else 0, amplitude, lx,
+                   ly)
+    _call("tgm_rotary", gpu, stream, C.byref(d), px, pw, pp, pn, py)
+
+
+def tgm_rotary_frequencies(rot, scaling="none", base=10000.0, factor=1.0, original=0.0,
+                           often=32.0, seldom=1.0):
+    """(omega, amplitude): a float64 numpy array of rot / 2 frequencies, for histories
+    ``factor`` times as long as the ``original`` positions, and the factor of cos and sin."""
+    code = _choice("scaling", scaling, ROTARY_SCALINGS)
+    _sizes("tgm_rotary_frequencies", (rot,), (I32,))
+    omega, a = np.zeros(max(1, rot // 2)), C.c_float(0)
+    _check("tgm_rotary_frequencies", lib().tgm_rotary_frequencies(
+        rot, code, base, factor, original, often, seldom, omega.ctypes.data, C.byref(a)))
+    return omega, float(a.value)
