@@ -636,6 +636,7 @@ tgm_status_t tgm_min_staleness(const double *tau, int64_t n, int32_t k_max, int3
  *   tgm_scan           gated linear recurrence along packed or padded histories
  *   tgm_scan_step      one row of it for each of n slots of a state table
  *   tgm_rotary         rotary positions, by place or event time; its own gradient
+ *   tgm_xent           softmax cross entropy over the nodes of a table
  *   tgm_..._backward   their gradients
  *
  * Conventions, besides those at the top of this file:
@@ -866,6 +867,47 @@ tgm_status_t tgm_rotary(const tgm_rotary_desc *d, const void *x, const double *o
 tgm_status_t tgm_rotary_frequencies(int32_t rot, int32_t scaling, double base, double factor,
                                     double original, double often, double seldom, double *omega,
                                     float *amplitude);
+
+/* Softmax cross entropy over N classes, such as the nodes of a table that may come next,
+ * without keeping the logits:
+ *   z = x W^T + bias,  lse_r = log sum_n exp z_rn,  loss_r = lse_r - z_(r, target_r).
+ * x [rows x K], W [N x K] and bias [N] (may be NULL: zero) have type dtype (f32, bf16 or
+ * f16), target [rows] int32, loss and lse [rows] fp32 (one of them may be NULL).  A row whose
+ * target is outside [0, N) has no part in the loss: loss 0, no gradient, an lse all the same.
+ * Products are exact and added in fp32, logits and exponentials fp32.  A bias of -infinity leaves
+ * a class out: probability 0, loss +infinity where it is the target.  Where every logit of a
+ * row is -infinity, lse is -infinity, the loss +infinity and the row has no gradient.
+ * Other infinities and NaN go through as the formulas have them.  1 <= N, K <= 2^20, and
+ * fewer than 2^24 tiles of 128 x 128 (fp32: 64 x 64) in any product.
+ * Errors: TGM_EINVAL (null, sizes, types, strides), TGM_ESIZE (work). */
+typedef struct {
+    int32_t rows, N, K;
+    int32_t dtype;
+    int64_t ld_x, ld_w;
+    int64_t ld_dx, ld_dw;   /* tgm_xent_backward only */
+} tgm_xent_desc;
+/* For tgm_xent (backward 0) and tgm_xent_backward (1: a piece of the classes' gradients in
+ * dtype, 256 MB or 1,024 classes, whichever is more, and fp32 sums of dx). */
+tgm_status_t tgm_xent_work_bytes(int32_t rows, int32_t N, int32_t K, int32_t dtype,
+                                 int32_t backward, size_t *bytes);
+tgm_status_t tgm_xent(const tgm_xent_desc *d, const void *x, const void *W, const void *bias,
+                      const int32_t *target, const int32_t *n_rows, float *loss, float *lse,
+                      void *work, size_t work_bytes, void *stream);
+
+/* Gradients of sum_r dloss_r loss_r in x, W and bias, with the lse of the forward call and
+ * dloss [rows] fp32:
+ *   dz_rn = dloss_r (exp(z_rn - lse_r) - [n = target_r]),
+ *   dx = dz W,  dW = dz^T x,  db = sum_rows dz.
+ * The logits are formed again, a piece of the classes at a time; dz is rounded to dtype for
+ * the products that read it (one rounding of 16 bits besides the result's: about 1.4 times the
+ * error of dx and dW), db adds it unrounded, and dx adds the pieces in fp32.  f16: dz is held times
+ * a power of two that puts the largest finite dloss near f16's largest value, so what is
+ * above 2^-39 of it is not lost by rounding.  dx [rows x K], dW [N x K], db [N] of type
+ * dtype; each may be NULL.  With no rows dW and db are zero. */
+tgm_status_t tgm_xent_backward(const tgm_xent_desc *d, const void *x, const void *W,
+                               const void *bias, const int32_t *target, const float *lse,
+                               const float *dloss, const int32_t *n_rows, void *dx, void *dW,
+                               void *db, void *work, size_t work_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
  * Per-kernel timing.  When enabled, every kernel the library launches is

@@ -167,6 +167,7 @@ struct LinearOut {
     int64_t ld_y, ld_z, ld_res;
     int32_t M, N, act;
     const int32_t *n_rows;  // bounds M where given
+    int32_t pad_m = 0;      // rows that Q has behind M: they may be read, and come to nothing
 };
 
 // W neighbouring columns of C, from n on: what they share in every row, and their
@@ -316,5 +317,7 @@ struct LinearPlan {
     int parts;
 };
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int code);
+// Bytes that the parts of a product need.
+size_t linear_split_bytes(int64_t M, int64_t N, int64_t K, int code);
 
 }  // namespace tgm

@@ -304,15 +304,6 @@ template <class T, class O, bool PK, bool QK> tgm_status_t product(const LinearP
         return linear_tile_f16(p, which, out);
 }
 
-// Bytes that the parts of a product need.
-size_t split_bytes(int64_t M, int64_t N, int64_t K, int code)
-{
-    if (M <= 0 || K <= 0)
-        return 0;
-    const int parts = linear_plan(M, N, K, code).parts;
-    return parts == 1 ? 0 : (size_t)parts * M * ((N + 3) / 4 * 4) * 4;
-}
-
 constexpr int kDbParts = 128;
 
 // The work space of the gradient: dz, the partial sums of db, dz's scale, then the partial
@@ -450,6 +441,14 @@ LinearPlan tgm::linear_plan(int64_t M, int64_t N, int64_t K, int code)
         false, (int)std::max<int64_t>(1, std::min<int64_t>({512 / small, steps / 8, 64}))};
 }
 
+size_t tgm::linear_split_bytes(int64_t M, int64_t N, int64_t K, int code)
+{
+    if (M <= 0 || K <= 0)
+        return 0;
+    const int parts = linear_plan(M, N, K, code).parts;
+    return parts == 1 ? 0 : (size_t)parts * M * ((N + 3) / 4 * 4) * 4;
+}
+
 extern "C" tgm_status_t tgm_linear_work_bytes(int32_t rows, int32_t N, int32_t K, int32_t dtype,
                                               int32_t act, int32_t backward, size_t *bytes)
 {
@@ -458,8 +457,9 @@ extern "C" tgm_status_t tgm_linear_work_bytes(int32_t rows, int32_t N, int32_t K
         return TGM_EINVAL;
     *bytes = backward ? dz_bytes(rows, N, dtype, act) + db_bytes(rows, N) +
                             scale_bytes(rows, K, dtype, act) +
-                            std::max(split_bytes(rows, K, N, dtype), split_bytes(N, K, rows, dtype))
-                      : few_blocks(rows, N, K, dtype) ? 0 : split_bytes(rows, N, K, dtype);
+                            std::max(linear_split_bytes(rows, K, N, dtype),
+                                     linear_split_bytes(N, K, rows, dtype))
+                      : few_blocks(rows, N, K, dtype) ? 0 : linear_split_bytes(rows, N, K, dtype);
     return TGM_OK;
 }
 

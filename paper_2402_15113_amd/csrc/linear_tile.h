@@ -329,10 +329,18 @@ template <class T, class O, class LP, class LQ, int NA, int MA> struct Half8 {
     }
 };
 
-template <class T, class O, bool PK, bool QK, int BN, int BM, int NW, int MW, bool DIRECT>
+// What becomes of a tile's sums: C itself (with bias, activation and residual), or what
+// another type's `finish` makes of them where they lie (csrc/xent_tile.h).
+struct LinearEnd {
+    struct Args {};
+};
+
+template <class T, class O, bool PK, bool QK, int BN, int BM, int NW, int MW, bool DIRECT,
+          class End = LinearEnd>
 __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
     const T *__restrict__ P, const T *__restrict__ Q, int64_t ld_p, int64_t ld_q, int32_t K_,
-    LinearOut o, const int32_t *k_rows, float *work, int32_t tn, int32_t tm, int32_t parts)
+    LinearOut o, const int32_t *k_rows, float *work, int32_t tn, int32_t tm, int32_t parts,
+    typename End::Args end)
 {
     constexpr int TH = 64 * NW * MW;
     constexpr bool BIG = sizeof(T) == 1 && sizeof(O) != 4;
@@ -359,7 +367,7 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
     OP p;
     OQ q;
     p.init(P, ld_p, n0, o.N);
-    q.init(Q, ld_q, m0, M);
+    q.init(Q, ld_q, m0, M + o.pad_m);
     // Steps that come whole, by vectors; the others go first, by their elements: behind
     // the loop their code would take registers from it.
     const int32_t quick = p.by_vectors(0, BK) && q.by_vectors(0, BK)
@@ -495,6 +503,11 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
         step(s, no{}, no{});
     }
 
+    if constexpr (!std::is_same_v<End, LinearEnd>) {
+        End::template finish<T, NA, MA>(end, o, acc, n0 + wn, m0 + wm, t.n * NW + w % NW,
+                                        t.m * MW + w / NW, M);
+        return;
+    }
     constexpr int LANES = SIDE, QUADS = BIG ? 4 : 1;
     auto sums = [&](int a, int b, int u) __attribute__((always_inline)) {
         if constexpr (BIG)
@@ -601,19 +614,21 @@ template <class T, bool KC> inline bool lies_on_16(const void *X, int64_t ld, in
 }
 template <class T, bool PK, bool QK> inline bool direct(const LinearProduct &p)
 {
-    return lies_on_16<T, PK>(p.P, p.ld_p, p.o.N) && lies_on_16<T, QK>(p.Q, p.ld_q, p.o.M);
+    return lies_on_16<T, PK>(p.P, p.ld_p, p.o.N) &&
+           lies_on_16<T, QK>(p.Q, p.ld_q, p.o.M + p.o.pad_m);
 }
 
-template <class T, class O, bool PK, bool QK, int BN, int BM, int NW, int MW, bool DIRECT>
-tgm_status_t launch_tile(const LinearProduct &p, int parts)
+template <class T, class O, bool PK, bool QK, int BN, int BM, int NW, int MW, bool DIRECT,
+          class End = LinearEnd>
+tgm_status_t launch_tile(const LinearProduct &p, int parts, typename End::Args end = {})
 {
     const int64_t tn = cdiv(p.o.N, BN), tm = cdiv(p.o.M, BM), wg = tn * tm * parts;
     if (wg * (64 * NW * MW) >= (int64_t)1 << 32)
         return TGM_EINVAL;
     float *work = parts > 1 ? p.work : nullptr;
-    TGM_LAUNCH((k_linear_tile<T, O, PK, QK, BN, BM, NW, MW, DIRECT>), dim3((uint32_t)wg),
+    TGM_LAUNCH((k_linear_tile<T, O, PK, QK, BN, BM, NW, MW, DIRECT, End>), dim3((uint32_t)wg),
                dim3(64 * NW * MW), 0, p.s, (const T *)p.P, (const T *)p.Q, p.ld_p, p.ld_q, p.K, p.o,
-               p.k_rows, work, (int32_t)tn, (int32_t)tm, parts);
+               p.k_rows, work, (int32_t)tn, (int32_t)tm, parts, end);
     if (parts > 1)
         TGM_LAUNCH((k_linear_join<O>),
                    dim3((uint32_t)std::min<int64_t>(cdiv((int64_t)p.o.M * cdiv(p.o.N, 4), 256),

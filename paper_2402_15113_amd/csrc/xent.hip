@@ -1,0 +1,374 @@
+// Softmax cross entropy of x W^T + bias over many classes, the nodes of a table (tgm_xent),
+// and its gradient (tgm_xent_backward), without keeping the logits.
+//
+// Forward: the logits' product ends in each tile's largest value and sum of exponentials a
+// row (XentSums); k_xent_loss joins them.  Backward, for a piece of the classes at a time:
+// the same product ends in dz = (softmax - onehot) dloss (XentGrad), rounded to the operands'
+// type for the two products that read it, dx += dz W (fp32 between the pieces) and dW = dz^T
+// x.  Bound by the matrix cores: 2 rows N K operations forward, 6 back.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "xent.h"
+
+using namespace tgm;
+
+namespace {
+
+constexpr int kMaxDim = 1 << 20;
+
+// lse and loss of 64 rows a workgroup; its 16 wavefronts share the runs of columns.
+__global__ __launch_bounds__(1024) void k_xent_loss(const f2 *__restrict__ part, int32_t runs,
+                                                    int32_t rows, int32_t classes,
+                                                    const int32_t *__restrict__ n_rows,
+                                                    const int32_t *__restrict__ target,
+                                                    const float *__restrict__ at_target,
+                                                    float *__restrict__ loss,
+                                                    float *__restrict__ lse)
+{
+    __shared__ f2 lds[16][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t m = (int64_t)blockIdx.x * 64 + lane;
+    const bool on = m < rows_in_use(rows, n_rows);
+    // the sum relative to the largest so far; -infinity: nothing yet (or no more than NaN)
+    float top = -INFINITY, sum = 0.f;
+    auto join = [&](f2 p) __attribute__((always_inline)) {
+        const float t = fmaxf(top, p.x);
+        if (t == -INFINITY) {
+            sum += p.y;
+        } else {
+            sum = sum * expf(top - t) + p.y * expf(p.x - t);
+            top = t;
+        }
+    };
+    if (on)
+#pragma unroll 4
+        for (int r = w; r < runs; r += 16)
+            join(part[(int64_t)r * rows + m]);
+    lds[w][lane] = f2{top, sum};
+    __syncthreads();
+    if (w || !on)
+        return;
+    for (int k = 1; k < 16; ++k)
+        join(lds[k][lane]);
+    const float l = top == -INFINITY ? (sum == 0.f ? top : sum) : top + logf(sum);
+    const int32_t t = target[m];
+    if (lse)
+        lse[m] = l;
+    if (loss) {
+        const float z = t >= 0 && t < classes ? at_target[m] : 0.f;
+        // a class that is left out has probability 0, wherever the others are
+        loss[m] = t < 0 || t >= classes ? 0.f : z == -INFINITY && l == l ? INFINITY : l - z;
+    }
+}
+
+// The power of two that dz is held times in fp16, whose range is narrower than that of
+// dloss: the largest finite |dloss| comes to between 2^14 and 2^15; and its reciprocal for the
+// products' K columns.  One workgroup: 8,192 rows take it 5 us.
+__global__ __launch_bounds__(1024) void k_xent_scale(const float *__restrict__ dloss,
+                                                     const int32_t *__restrict__ target,
+                                                     const int32_t *__restrict__ n_rows,
+                                                     int32_t rows, int32_t classes, int32_t K,
+                                                     float *__restrict__ scale,
+                                                     float *__restrict__ unscale)
+{
+    __shared__ float lds[16];
+    const int32_t R = rows_in_use(rows, n_rows);
+    float top = 0.f;
+#pragma unroll 4
+    for (int64_t m = threadIdx.x; m < R; m += 1024) {
+        const float v = fabsf(dloss[m]);
+        const int32_t t = target[m];
+        top = v < INFINITY && v > top && t >= 0 && t < classes ? v : top;
+    }
+    top = group_max<64>(top);
+    if ((threadIdx.x & 63) == 0)
+        lds[threadIdx.x >> 6] = top;
+    __syncthreads();
+    for (int k = 0; k < 16; ++k)
+        top = fmaxf(top, lds[k]);
+    const float s = top > 0.f ? ldexpf(1.f, min(max(14 - ilogbf(top), -126), 126)) : 1.f;
+    if (threadIdx.x == 0)
+        scale[0] = s;
+    for (int32_t k = threadIdx.x; k < K; k += 1024)
+        unscale[k] = 1.f / s;
+}
+
+// db = the runs' partial sums added in order: 32 columns a workgroup, 32 threads each.
+template <class T>
+__global__ __launch_bounds__(1024) void k_xent_db(const float *__restrict__ part, XentRuns r,
+                                                  int32_t rows, const int32_t *n_rows, int32_t N,
+                                                  const float *scale, T *__restrict__ db)
+{
+    __shared__ float lds[32][33];
+    const int c = threadIdx.x & 31, k0 = threadIdx.x >> 5;
+    const int64_t n = (int64_t)blockIdx.x * 32 + c;
+    const int32_t tiles = (int32_t)(((int64_t)rows_in_use(rows, n_rows) + r.tile_rows - 1) /
+                                    r.tile_rows);
+    float a = 0.f;
+    if (n < N)
+#pragma unroll 4
+        for (int k = k0; k < tiles * r.tile_runs; k += 32)
+            a += part[(int64_t)k * N + n];
+    lds[k0][c] = a;
+    __syncthreads();
+    if (k0 == 0 && n < N) {
+        for (int k = 1; k < 32; ++k)
+            a += lds[k][c];
+        db[n] = from_f32<T>(scale ? a / scale[0] : a);
+    }
+}
+
+// dx from its fp32 sums over the pieces.  Bound by memory.
+template <class T>
+__global__ __launch_bounds__(256) void k_xent_dx(const float *__restrict__ sum, int32_t rows,
+                                                 const int32_t *n_rows, int32_t K, int64_t wide,
+                                                 int64_t ld, T *__restrict__ dx)
+{
+    const int32_t R = rows_in_use(rows, n_rows);
+    const int64_t quads = wide / 4, n = R * quads;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n;
+         i += (int64_t)gridDim.x * 256) {
+        const int64_t m = i / quads;
+        const int32_t k = 4 * (int32_t)(i - m * quads);
+        const f4 v = *reinterpret_cast<const f4 *>(sum + m * wide + k);
+        Pack<T, 4> p;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            p.v[j] = from_f32<T>(v[j]);
+        T *to = dx + m * ld + k;
+        if (k + 4 <= K)
+            store_pack(to, p);
+        else
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (k + j < K)
+                    to[j] = p.v[j];
+    }
+}
+
+// ---------------------------------------------------------------- host
+// Classes of a piece: dz of one takes 256 MB or so, of which the caches hold most between
+// the product that writes it and the two that read it.
+struct XentPlan {
+    int32_t piece, last;      // classes of every piece, and of the last one
+    int64_t pieces, ld_dz;
+    size_t dz, sum, scale, db, split, all;   // bytes of the parts of the work space
+};
+size_t whole(size_t n) { return (n + 255) / 256 * 256; }
+XentPlan xent_plan(int32_t rows, int32_t N, int32_t K, int code)
+{
+    XentPlan p{};
+    const int64_t eb = elem_bytes(code), R = std::max(rows, 1);
+    int64_t most = ((int64_t)256 << 20) / (R * eb) / 256 * 256;
+    most = std::max<int64_t>(most, 1024);
+    p.pieces = cdiv(N, most);
+    p.piece = p.pieces == 1 ? N : (int32_t)(cdiv(cdiv(N, p.pieces), 256) * 256);
+    p.pieces = cdiv(N, p.piece);
+    p.last = (int32_t)(N - (p.pieces - 1) * p.piece);
+    p.ld_dz = cdiv(p.piece, 16) * 16;
+    p.dz = whole((size_t)rows * p.ld_dz * eb);
+    p.sum = p.pieces > 1 ? whole((size_t)rows * round_up(K, 4) * 4) : 0;
+    p.scale = code == TGM_F16 ? whole((size_t)(64 + round_up(K, 4)) * 4) : 0;
+    p.db = whole((size_t)xent_db_parts(rows, code) * p.piece * 4);
+    for (int32_t n : {p.piece, p.last})
+        p.split = std::max({p.split, linear_split_bytes(rows, K, n, code),
+                            linear_split_bytes(n, K, rows, code)});
+    p.all = p.dz + p.sum + p.scale + p.db + p.split;
+    return p;
+}
+size_t sums_bytes(int32_t rows, int32_t N)
+{
+    return whole((size_t)xent_parts(N) * rows * sizeof(f2)) + whole((size_t)rows * 4);
+}
+
+tgm_status_t xent_args(const tgm_xent_desc *d, int64_t *ld)
+{
+    if (!d || d->rows < 0 || d->N < 1 || d->N > kMaxDim || d->K < 1 || d->K > kMaxDim ||
+        !wide_type(d->dtype))
+        return TGM_EINVAL;
+    // a launch has fewer than 2^32 threads, 256 a tile
+    const int64_t side = d->dtype == TGM_F32 ? 64 : 128, most = (int64_t)1 << 24;
+    const int64_t r = cdiv(d->rows, side), n = cdiv(d->N, side), k = cdiv(d->K, side);
+    if (r * n >= most || r * k >= most || n * k >= most)
+        return TGM_EINVAL;
+    const int64_t given[4] = {d->ld_x, d->ld_w, d->ld_dx, d->ld_dw};
+    for (int i = 0; i < 4; ++i)
+        if ((ld[i] = stride_of(given[i], d->K)) < 0)
+            return TGM_EINVAL;
+    return TGM_OK;
+}
+
+tgm_status_t check_work(size_t need, const void *work, size_t bytes)
+{
+    if (!need)
+        return TGM_OK;
+    if (!work || ((uintptr_t)work & 15))
+        return TGM_EINVAL;
+    return bytes < need ? TGM_ESIZE : TGM_OK;
+}
+
+template <class T> constexpr auto sums_of = std::is_same_v<T, float> ? xent_sums_f32
+                                            : std::is_same_v<T, bf16> ? xent_sums_bf16
+                                                                      : xent_sums_f16;
+template <class T> constexpr auto grad_of = std::is_same_v<T, float> ? xent_grad_f32
+                                            : std::is_same_v<T, bf16> ? xent_grad_bf16
+                                                                      : xent_grad_f16;
+template <class T> constexpr auto tile_of_type = std::is_same_v<T, float> ? linear_tile_f32
+                                                 : std::is_same_v<T, bf16> ? linear_tile_bf16
+                                                                           : linear_tile_f16;
+
+template <class T>
+tgm_status_t forward(const tgm_xent_desc *d, const int64_t *ld, const void *x, const void *W,
+                     const void *bias, const int32_t *target, const int32_t *n_rows, float *loss,
+                     float *lse, char *work, hipStream_t s)
+{
+    LinearProduct p{W, x, ld[1], ld[0], d->K, nullptr, {}, nullptr, s};
+    p.o.M = d->rows, p.o.N = d->N, p.o.n_rows = n_rows;
+    XentArgs e{};
+    e.bias = bias, e.target = target, e.rows = d->rows, e.classes = d->N;
+    e.part = (f2 *)work;
+    e.at_target = (float *)(work + whole((size_t)xent_parts(d->N) * d->rows * sizeof(f2)));
+    XentRuns r;
+    TGM_TRY_STATUS(sums_of<T>(p, e, &r));
+    TGM_LAUNCH(k_xent_loss, dim3((uint32_t)cdiv(d->rows, 64)), dim3(1024), 0, s, e.part,
+               r.columns, d->rows, d->N, n_rows, target, e.at_target, loss, lse);
+    return TGM_OK;
+}
+
+template <class T>
+tgm_status_t backward(const tgm_xent_desc *d, const int64_t *ld, const void *x, const void *W,
+                      const void *bias, const int32_t *target, const float *lse,
+                      const float *dloss, const int32_t *n_rows, void *dx, void *dW, void *db,
+                      char *work, hipStream_t s)
+{
+    constexpr int code = TypeCode<T>::code;
+    const XentPlan plan = xent_plan(d->rows, d->N, d->K, code);
+    T *dz = (T *)work;
+    float *sum = (float *)(work + plan.dz);
+    float *scale = plan.scale ? (float *)(work + plan.dz + plan.sum) : nullptr;
+    float *unscale = scale ? scale + 64 : nullptr;
+    float *part = (float *)(work + plan.dz + plan.sum + plan.scale);
+    float *split = (float *)(work + plan.dz + plan.sum + plan.scale + plan.db);
+    const int64_t wide = round_up(d->K, 4);
+    if (scale)
+        TGM_LAUNCH(k_xent_scale, dim3(1), dim3(1024), 0, s, dloss, target, n_rows, d->rows, d->N,
+                   d->K, scale, unscale);
+    for (int64_t i = 0; i < plan.pieces; ++i) {
+        const int64_t n0 = i * plan.piece;
+        const int32_t n = i + 1 < plan.pieces ? plan.piece : plan.last;
+        const T *w = (const T *)W + n0 * ld[1];
+        XentRuns r{0, 1, 0};
+        if (d->rows) {
+            LinearProduct p{w, x, ld[1], ld[0], d->K, nullptr, {}, nullptr, s};
+            p.o.M = d->rows, p.o.N = n, p.o.n_rows = n_rows;
+            XentArgs e{};
+            e.bias = bias ? (const T *)bias + n0 : nullptr;
+            e.target = target, e.rows = d->rows, e.classes = d->N, e.n_first = (int32_t)n0;
+            e.lse = lse, e.dloss = dloss, e.scale = scale, e.dz = dz, e.ld_dz = plan.ld_dz;
+            e.db = db ? part : nullptr;
+            TGM_TRY_STATUS(grad_of<T>(p, e, &r));
+        }
+        if (db)
+            TGM_LAUNCH((k_xent_db<T>), dim3((uint32_t)cdiv(n, 32)), dim3(1024), 0, s, part, r,
+                       d->rows, n_rows, n, scale, (T *)db + n0);
+        if (dx && d->rows) {
+            LinearProduct p{w, dz, ld[1], plan.ld_dz, n, nullptr, {}, split, s};
+            p.o.M = d->rows, p.o.N = d->K, p.o.n_rows = n_rows, p.o.sn = unscale;
+            if (plan.pieces == 1) {
+                p.o.y = dx, p.o.ld_y = ld[2];
+                TGM_TRY_STATUS(tile_of_type<T>(p, 1, code));
+            } else {
+                // the pieces' sums in fp32, rounded once at the end
+                p.o.y = sum, p.o.ld_y = wide;
+                p.o.res = i ? sum : nullptr, p.o.ld_res = wide;
+                if constexpr (code == TGM_F32)
+                    TGM_TRY_STATUS(linear_tile_f32(p, 1, code));
+                else if constexpr (code == TGM_BF16)
+                    TGM_TRY_STATUS(xent_dx_bf16(p));
+                else
+                    TGM_TRY_STATUS(xent_dx_f16(p));
+                if (i + 1 == plan.pieces)
+                    TGM_LAUNCH((k_xent_dx<T>),
+                               dim3((uint32_t)std::min<int64_t>(
+                                   cdiv((int64_t)d->rows * (wide / 4), 256), 1 << 14)),
+                               dim3(256), 0, s, sum, d->rows, n_rows, d->K, wide, ld[2], (T *)dx);
+            }
+        }
+        if (dW) {
+            LinearProduct p{x, dz, ld[0], plan.ld_dz, d->rows, n_rows, {}, split, s};
+            p.o.M = n, p.o.N = d->K, p.o.sn = unscale;
+            // dz's rows have whole vectors
+            p.o.pad_m = round_up(n, 16 / (int)sizeof(T)) - n;
+            p.o.y = (T *)dW + n0 * ld[3], p.o.ld_y = ld[3];
+            TGM_TRY_STATUS(tile_of_type<T>(p, 2, code));
+        }
+    }
+    return TGM_OK;
+}
+
+}  // namespace
+
+extern "C" tgm_status_t tgm_xent_work_bytes(int32_t rows, int32_t N, int32_t K, int32_t dtype,
+                                            int32_t backward, size_t *bytes)
+{
+    if (!bytes)
+        return TGM_EINVAL;
+    int64_t ld[4];
+    tgm_xent_desc d{rows, N, K, dtype, 0, 0, 0, 0};
+    TGM_TRY_STATUS(xent_args(&d, ld));
+    *bytes = backward ? xent_plan(rows, N, K, dtype).all : rows ? sums_bytes(rows, N) : 0;
+    return TGM_OK;
+}
+
+extern "C" tgm_status_t tgm_xent(const tgm_xent_desc *d, const void *x, const void *W,
+                                 const void *bias, const int32_t *target, const int32_t *n_rows,
+                                 float *loss, float *lse, void *work, size_t work_bytes,
+                                 void *stream)
+{
+    int64_t ld[4];
+    TGM_TRY_STATUS(xent_args(d, ld));
+    if (!W || (d->rows && (!x || !target)) || (!loss && !lse && d->rows))
+        return TGM_EINVAL;
+    size_t need = 0;
+    TGM_TRY_STATUS(tgm_xent_work_bytes(d->rows, d->N, d->K, d->dtype, 0, &need));
+    TGM_TRY_STATUS(check_work(need, work, work_bytes));
+    if (d->rows == 0)
+        return TGM_OK;
+    char *w = (char *)work;
+    const hipStream_t s = as_stream(stream);
+    switch (d->dtype) {
+    case TGM_F32: return forward<float>(d, ld, x, W, bias, target, n_rows, loss, lse, w, s);
+    case TGM_BF16: return forward<bf16>(d, ld, x, W, bias, target, n_rows, loss, lse, w, s);
+    default: return forward<f16>(d, ld, x, W, bias, target, n_rows, loss, lse, w, s);
+    }
+}
+
+extern "C" tgm_status_t tgm_xent_backward(const tgm_xent_desc *d, const void *x, const void *W,
+                                          const void *bias, const int32_t *target,
+                                          const float *lse, const float *dloss,
+                                          const int32_t *n_rows, void *dx, void *dW, void *db,
+                                          void *work, size_t work_bytes, void *stream)
+{
+    int64_t ld[4];
+    TGM_TRY_STATUS(xent_args(d, ld));
+    if (!W || (d->rows && (!x || !target || !lse || !dloss)))
+        return TGM_EINVAL;
+    size_t need = 0;
+    TGM_TRY_STATUS(tgm_xent_work_bytes(d->rows, d->N, d->K, d->dtype, 1, &need));
+    TGM_TRY_STATUS(check_work(need, work, work_bytes));
+    if ((!dx || !d->rows) && !dW && !db)
+        return TGM_OK;
+    char *w = (char *)work;
+    const hipStream_t s = as_stream(stream);
+    switch (d->dtype) {
+    case TGM_F32:
+        return backward<float>(d, ld, x, W, bias, target, lse, dloss, n_rows, dx, dW, db, w, s);
+    case TGM_BF16:
+        return backward<bf16>(d, ld, x, W, bias, target, lse, dloss, n_rows, dx, dW, db, w, s);
+    default:
+        return backward<f16>(d, ld, x, W, bias, target, lse, dloss, n_rows, dx, dW, db, w, s);
+    }
+}

@@ -1,0 +1,15 @@
+// The cross entropy's products of f32 operands.
+#include "xent_tile.h"
+
+namespace tgm {
+
+tgm_status_t xent_sums_f32(const LinearProduct &p, const XentArgs &e, XentRuns *r)
+{
+    return xent_product<float, XentSums>(p, e, r);
+}
+tgm_status_t xent_grad_f32(const LinearProduct &p, const XentArgs &e, XentRuns *r)
+{
+    return xent_product<float, XentGrad>(p, e, r);
+}
+
+}  // namespace tgm

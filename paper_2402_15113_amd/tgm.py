@@ -38,7 +38,8 @@ SYMBOLS = ["tgm_status_str", "tgm_last_device_error", "tgm_version", "tgm_alloc_
            "tgm_norm", "tgm_norm_work_bytes", "tgm_norm_backward",
            "tgm_linear", "tgm_linear_work_bytes", "tgm_linear_backward",
            "tgm_scan", "tgm_scan_carry_rows", "tgm_scan_work_bytes", "tgm_scan_backward",
-           "tgm_scan_step", "tgm_rotary", "tgm_rotary_frequencies",
+           "tgm_scan_step", "tgm_rotary", "tgm_rotary_frequencies", "tgm_xent",
+           "tgm_xent_work_bytes", "tgm_xent_backward",
            "tgm_profile_enable", "tgm_profile_reset", "tgm_profile_count", "tgm_profile_get"]
 
 
@@ -122,6 +123,12 @@ class RotaryDesc(C.Structure):
                 ("dtype", C.c_int32), ("pos_type", C.c_int32), ("layout", C.c_int32),
                 ("inverse", C.c_int32), ("amplitude", C.c_float), ("ld_x", C.c_int64),
                 ("ld_y", C.c_int64)]
+
+
+class XentDesc(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("dtype", C.c_int32),
+                ("ld_x", C.c_int64), ("ld_w", C.c_int64), ("ld_dx", C.c_int64),
+                ("ld_dw", C.c_int64)]
 
 
 TGM_F32, TGM_BF16, TGM_F16, TGM_E4M3 = 0, 1, 2, 3
@@ -218,6 +225,10 @@ def lib():
             "tgm_rotary": [C.POINTER(RotaryDesc), P, P, P, P, P, V],
             "tgm_rotary_frequencies": [I32, I32, C.c_double, C.c_double, C.c_double, C.c_double,
                                        C.c_double, P, C.POINTER(C.c_float)],
+            "tgm_xent_work_bytes": [I32, I32, I32, I32, I32, C.POINTER(C.c_size_t)],
+            "tgm_xent": [C.POINTER(XentDesc), P, P, P, P, P, P, P, P, C.c_size_t, V],
+            "tgm_xent_backward": [C.POINTER(XentDesc), P, P, P, P, P, P, P, P, P, P, P,
+                                  C.c_size_t, V],
         }
         sig["tgm_profile_enable"] = [I32]
         sig["tgm_profile_reset"] = []
@@ -971,3 +982,48 @@ def tgm_rotary_frequencies(rot, scaling="none", base=10000.0, factor=1.0, origin
     _check("tgm_rotary_frequencies", lib().tgm_rotary_frequencies(
         rot, code, base, factor, original, often, seldom, omega.ctypes.data, C.byref(a)))
     return omega, float(a.value)
+
+
+def tgm_xent_work_bytes(rows, N, K, dtype, backward=False) -> int:
+    return _bytes("tgm_xent_work_bytes", rows, N, K, dtype_code(dtype), 1 if backward else 0)
+
+
+def _xent_args(x, w, target, bias, n_rows):
+    import torch
+    (rows, K), (N, _) = _shape2("x", x), _shape2("w", w)
+    gpu, dt = x.get_device(), x.dtype
+    px, lx = _arg("x", x, dt, (rows, K), gpu)
+    pw, lw = _arg("w", w, dt, (N, K), gpu)
+    pb, _ = _opt("bias", bias, dt, (N,), gpu)
+    pt, _ = _arg("target", target, torch.int32, (rows,), gpu)
+    pn, _ = _opt("n_rows", n_rows, torch.int32, (1,), gpu)
+    return rows, N, K, gpu, dt, px, lx, pw, lw, pb, pt, pn
+
+
+def tgm_xent(x, w, target, loss, work, lse=None, bias=None, n_rows=None, stream=None):
+    """loss = log sum exp(x w^T + bias) - (x w^T + bias)[target] a row, and ``lse``, the
+    first term (each optional, fp32); rows whose target is outside the classes lose 0."""
+    import torch
+    rows, N, K, gpu, dt, px, lx, pw, lw, pb, pt, pn = _xent_args(x, w, target, bias, n_rows)
+    pl, _ = _opt("loss", loss, torch.float32, (rows,), gpu)
+    pe, _ = _opt("lse", lse, torch.float32, (rows,), gpu)
+    pk, nk = _work_arg(work, gpu)
+    d = XentDesc(rows, N, K, dtype_code(dt), lx, lw, 0, 0)
+    _call("tgm_xent", gpu, stream, C.byref(d), px, pw, pb, pt, pn, pl, pe, pk, nk)
+
+
+def tgm_xent_backward(x, w, target, lse, dloss, work, bias=None, dx=None, dw=None, db=None,
+                      n_rows=None, stream=None):
+    """dx, dw and db (each optional) of sum(dloss * loss), with the ``lse`` that tgm_xent
+    wrote."""
+    import torch
+    rows, N, K, gpu, dt, px, lx, pw, lw, pb, pt, pn = _xent_args(x, w, target, bias, n_rows)
+    pe, _ = _arg("lse", lse, torch.float32, (rows,), gpu)
+    pd, _ = _arg("dloss", dloss, torch.float32, (rows,), gpu)
+    pdx, ldx = _opt("dx", dx, dt, (rows, K), gpu)
+    pdw, ldw = _opt("dw", dw, dt, (N, K), gpu)
+    pdb, _ = _opt("db", db, dt, (N,), gpu)
+    pk, nk = _work_arg(work, gpu)
+    d = XentDesc(rows, N, K, dtype_code(dt), lx, lw, ldx, ldw)
+    _call("tgm_xent_backward", gpu, stream, C.byref(d), px, pw, pb, pt, pe, pd, pn, pdx, pdw, pdb,
+          pk, nk)
