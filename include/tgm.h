@@ -635,6 +635,8 @@ tgm_status_t tgm_min_staleness(const double *tau, int64_t n, int32_t k_max, int3
  *   tgm_linear         matrix product with bias, activation and residual
  *   tgm_scan           gated linear recurrence along packed or padded histories
  *   tgm_scan_step      one row of it for each of n slots of a state table
+ *   tgm_decay_attn     linear attention with a decay for each head along histories
+ *   tgm_decay_attn_step  one row of it for each of n slots of a state table
  *   tgm_rotary         rotary positions, by place or event time; its own gradient
  *   tgm_xent           softmax cross entropy over the nodes of a table
  *   tgm_..._backward   their gradients
@@ -867,6 +869,73 @@ tgm_status_t tgm_rotary(const tgm_rotary_desc *d, const void *x, const double *o
 tgm_status_t tgm_rotary_frequencies(int32_t rot, int32_t scaling, double base, double factor,
                                     double original, double often, double seldom, double *omega,
                                     float *amplitude);
+
+/* Linear attention with a decay for each head, along sequences (histories) of rows: per
+ * head, with a = exp(decay[h]),
+ *   S_t = a S_(t-1) + k_t v_t^T,  o_t = scale q_t S_t,
+ * from S_(before the first row) = state (zero where state is NULL).  Where tgm_scan's state
+ * is a number a channel, this one's is a matrix [d_k x d_v] a head, which a row reads by its
+ * content.
+ *
+ * q [rows x H d_k], k [rows x H_kv d_k], v [rows x H_kv d_v] and o [rows x H d_v] have type
+ * dtype (f32, bf16 or f16), heads side by side; H is a multiple of H_kv, and head h reads
+ * head h / (H / H_kv) of k and v.  decay [H] fp32 on the device holds log a: 0 forgets
+ * nothing, -infinity everything but the row itself (positive ones grow).  state and
+ * state_last [S x H x d_k x d_v] are dense fp32 (state_last may be NULL): what each sequence
+ * starts from and ends with (state's for a sequence without rows).  The sequences are packed by
+ * offsets or padded, and shortened by length, as for tgm_scan; what rows of no sequence
+ * hold does not matter, and their o is left as it is.  reverse != 0 runs every sequence
+ * from its last row to its first.
+ * Products are added in fp32, and states are fp32 and lose nothing to 16 bits; with 16-bit
+ * inputs the weights a^(t-s) scale q_t k_s within some rows, and the state that q_t reads
+ * there, are rounded to 16 bits (f16: times a power of two that keeps them in range), about
+ * 1.4 times the error that rounding o has.  A row that is not finite reaches its own and
+ * later rows only; where the formula has an infinity there may be NaN.
+ * rows <= 2^30, H <= 4096, 1 <= d_k, d_v <= 128.
+ * Errors: TGM_EINVAL (null, sizes, types, strides, S < 0, S = 0 with rows in the padded form
+ * or rows not divisible by it), TGM_ESIZE (work). */
+typedef struct {
+    int64_t rows;
+    int32_t S, H, H_kv, d_k, d_v;
+    int32_t dtype, reverse;
+    float scale;
+    int64_t ld_q, ld_k, ld_v, ld_o;     /* o; in tgm_decay_attn_backward do */
+    int64_t ld_dq, ld_dk, ld_dv;        /* tgm_decay_attn_backward only */
+} tgm_decay_attn_desc;
+/* For tgm_decay_attn (backward 0) and tgm_decay_attn_backward (1). */
+tgm_status_t tgm_decay_attn_work_bytes(int64_t rows, int32_t S, int32_t H, int32_t H_kv,
+                                       int32_t d_k, int32_t d_v, int32_t dtype, int32_t backward,
+                                       size_t *bytes);
+tgm_status_t tgm_decay_attn(const tgm_decay_attn_desc *d, const void *q, const void *k,
+                            const void *v, const float *decay, const int64_t *offsets,
+                            const int32_t *length, const float *state, void *o,
+                            float *state_last, void *work, size_t work_bytes, void *stream);
+
+/* Gradients of tgm_decay_attn in q, k, v and state, from dO [rows x H d_v] of type dtype
+ * and dstate_last [S x H x d_k x d_v] (fp32, may be NULL: zero), with the forward call's
+ * desc, inputs and sequences; o is not read and nothing has to be kept for it:
+ *   G_t = a G_(t+1) + scale q_t do_t^T  (dstate_last for the first term at the last row),
+ *   dq_t = scale S_t do_t,  dk_t = G_t v_t,  dv_t = G_t^T k_t,
+ *   dstate = a G_1  (dstate_last for a sequence without rows).
+ * dq, dk, dv of type dtype, laid out as q, k, v (rows of no sequence are left as they are):
+ * dk and dv of a head of k and v are added over the heads that share it, in fp32.  dstate
+ * fp32.  Each may be NULL.  The decays are constants: they have no gradient.  Errors as
+ * tgm_decay_attn. */
+tgm_status_t tgm_decay_attn_backward(const tgm_decay_attn_desc *d, const void *q, const void *k,
+                                     const void *v, const float *decay, const int64_t *offsets,
+                                     const int32_t *length, const float *state, const void *dO,
+                                     const float *dstate_last, void *dq, void *dk, void *dv,
+                                     float *dstate, void *work, size_t work_bytes, void *stream);
+
+/* One row for each of n = d->rows sequences whose states are rows of a table (node
+ * states): with S = state[slots[p]] (row p where slots is NULL),
+ *   S <- a S + k_p v_p^T,  o_p = scale q_p S,  state[slots[p]] = S,
+ * for the rows p < *n_rows.  state [d->S x H x d_k x d_v] dense fp32, updated in place; slots
+ * [n] int32 are distinct among the rows in use; a slot outside [0, S) stands for a state
+ * of zeros that is not kept.  o may be NULL.  reverse is not read. */
+tgm_status_t tgm_decay_attn_step(const tgm_decay_attn_desc *d, const void *q, const void *k,
+                                 const void *v, const float *decay, const int32_t *slots,
+                                 const int32_t *n_rows, float *state, void *o, void *stream);
 
 /* Softmax cross entropy over N classes, such as the nodes of a table that may come next,
  * without keeping the logits:

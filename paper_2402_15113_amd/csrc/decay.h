@@ -1,0 +1,109 @@
+// What the kernels of the linear attention with a decay for each head (tgm_decay_attn)
+// share.
+//
+// The operator and each of its gradients is one recurrence over three matrices' rows,
+//   S_t = a S_(t-1) + c_y y_t z_t^T,   out_t = c_out x_t S_t,
+// along every sequence or against it:
+//   o:   x, y, z = q, k, v            from the first state
+//   dq:  x, y, z = do, v, k           from its transpose
+//   dk:  x, y, z = v, do, q           backwards, from the transpose of the last state's gradient
+//   dv:  x, y, z = k, q, do           backwards, from the last state's gradient
+#pragma once
+
+#include "seq.h"
+
+namespace tgm {
+
+constexpr int kDecayMaxD = 128;
+
+// A matrix of rows and the head that head h of the recurrence reads: h / share.
+struct DecayIn {
+    const void *p;
+    int64_t ld;
+    int32_t share;
+};
+
+struct DecayArgs {
+    DecayIn x, y, z;         // p, p and r columns a head
+    void *out;               // null: states only
+    int64_t ld_out;
+    const float *decay;      // [H]: log a
+    const int64_t *offsets;  // null: sequences of L rows
+    const int32_t *length;
+    const float *first;      // states [S x H x dk x dv] before the first rows; may be null
+    float *last;             // states after the last ones; may be null
+    int64_t rows, L;
+    int32_t S, H, p, r;
+    int32_t turned;          // the states in memory are S^T, [r x p]
+    int32_t rev;             // from each sequence's last row to its first
+    int32_t lag0;            // the first state's weight at the first row: a^lag0 (0 or 1)
+    int32_t lag1;            // the last state is a^lag1 S (0 or 1)
+    float c_y, c_out;
+};
+
+// Rows b .. e - 1 of sequence s; empty where its offsets make no sense.
+struct DecaySeq {
+    int64_t b, e;
+};
+__device__ __forceinline__ DecaySeq decay_seq(const DecayArgs &a, int32_t s)
+{
+    int64_t b, e;
+    if (a.offsets) {
+        b = min(max(a.offsets[s], (int64_t)0), a.rows);
+        e = min(max(a.offsets[s + 1], b), a.rows);
+    } else {
+        b = s * a.L;
+        e = b + a.L;
+    }
+    if (a.length)
+        e = min(e, b + max(0, a.length[s]));
+    return DecaySeq{b, e};
+}
+
+// Where a sequence begins, for the search below.
+__device__ __forceinline__ int64_t decay_begin(const DecayArgs &a, int32_t s)
+{
+    return a.offsets ? min(max(a.offsets[s], (int64_t)0), a.rows) : s * a.L;
+}
+
+// The rows that sequence `s` has in cell `cell` of C consecutive rows: piece `id` of
+// cdiv(rows, C) + S.  A path through cells and sequences, which goes to the next sequence
+// or to the next cell at every step, meets every pair that has rows in common, and every
+// sequence in the cell where it begins: sequence s begins at step cell(begin) + s, and these
+// steps ascend.  No list of pieces has to be made, whatever the offsets on the device are.
+struct DecayPiece {
+    int32_t s;
+    int64_t cell, lo, hi;   // hi <= lo: no rows
+    DecaySeq q;
+};
+__device__ __forceinline__ DecayPiece decay_piece(const DecayArgs &a, int64_t id, int32_t C)
+{
+    // how many sequences begin at step id or before, by one wavefront: a 64-ary search
+    const int lane = threadIdx.x & 63;
+    int32_t lo = 0, hi = a.S;
+    while (hi - lo > kWave) {
+        const int32_t step = (hi - lo + kWave - 1) / kWave;
+        const int64_t probe = (int64_t)lo + (int64_t)(lane + 1) * step - 1;
+        const int c = __popcll(__ballot(probe < hi &&
+                                        decay_begin(a, (int32_t)min(probe, (int64_t)hi - 1)) / C +
+                                                probe <= id));
+        lo += c * step;
+        hi = min(lo + step, hi);
+    }
+    const int64_t idx = (int64_t)lo + lane;
+    lo += __popcll(__ballot(idx < hi && decay_begin(a, (int32_t)min(idx, (int64_t)hi - 1)) / C +
+                                                idx <= id));
+    DecayPiece p{max(lo - 1, 0), 0, 0, 0, {0, 0}};
+    if (lo < 1)
+        return p;
+    p.cell = id - p.s;
+    p.q = decay_seq(a, p.s);
+    p.lo = max(p.q.b, p.cell * C);
+    p.hi = min(p.q.e, (p.cell + 1) * C);
+    return p;
+}
+
+// a^n of log a = g: 1 for n = 0, whatever g is.
+__device__ __forceinline__ float decay_pow(float g, float n) { return n == 0.f ? 1.f : expf(n * g); }
+
+}  // namespace tgm

@@ -38,7 +38,9 @@ SYMBOLS = ["tgm_status_str", "tgm_last_device_error", "tgm_version", "tgm_alloc_
            "tgm_norm", "tgm_norm_work_bytes", "tgm_norm_backward",
            "tgm_linear", "tgm_linear_work_bytes", "tgm_linear_backward",
            "tgm_scan", "tgm_scan_carry_rows", "tgm_scan_work_bytes", "tgm_scan_backward",
-           "tgm_scan_step", "tgm_rotary", "tgm_rotary_frequencies", "tgm_xent",
+           "tgm_scan_step", "tgm_rotary", "tgm_rotary_frequencies",
+           "tgm_decay_attn", "tgm_decay_attn_work_bytes", "tgm_decay_attn_backward",
+           "tgm_decay_attn_step", "tgm_xent",
            "tgm_xent_work_bytes", "tgm_xent_backward",
            "tgm_profile_enable", "tgm_profile_reset", "tgm_profile_count", "tgm_profile_get"]
 
@@ -123,6 +125,14 @@ class RotaryDesc(C.Structure):
                 ("dtype", C.c_int32), ("pos_type", C.c_int32), ("layout", C.c_int32),
                 ("inverse", C.c_int32), ("amplitude", C.c_float), ("ld_x", C.c_int64),
                 ("ld_y", C.c_int64)]
+
+
+class DecayAttnDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("S", C.c_int32), ("H", C.c_int32), ("H_kv", C.c_int32),
+                ("d_k", C.c_int32), ("d_v", C.c_int32), ("dtype", C.c_int32),
+                ("reverse", C.c_int32), ("scale", C.c_float), ("ld_q", C.c_int64),
+                ("ld_k", C.c_int64), ("ld_v", C.c_int64), ("ld_o", C.c_int64),
+                ("ld_dq", C.c_int64), ("ld_dk", C.c_int64), ("ld_dv", C.c_int64)]
 
 
 class XentDesc(C.Structure):
@@ -225,6 +235,13 @@ def lib():
             "tgm_rotary": [C.POINTER(RotaryDesc), P, P, P, P, P, V],
             "tgm_rotary_frequencies": [I32, I32, C.c_double, C.c_double, C.c_double, C.c_double,
                                        C.c_double, P, C.POINTER(C.c_float)],
+            "tgm_decay_attn_work_bytes": [I64, I32, I32, I32, I32, I32, I32, I32,
+                                          C.POINTER(C.c_size_t)],
+            "tgm_decay_attn": [C.POINTER(DecayAttnDesc), P, P, P, P, P, P, P, P, P, P, C.c_size_t,
+                               V],
+            "tgm_decay_attn_backward": [C.POINTER(DecayAttnDesc), P, P, P, P, P, P, P, P, P, P, P,
+                                        P, P, P, C.c_size_t, V],
+            "tgm_decay_attn_step": [C.POINTER(DecayAttnDesc), P, P, P, P, P, P, P, P, V],
             "tgm_xent_work_bytes": [I32, I32, I32, I32, I32, C.POINTER(C.c_size_t)],
             "tgm_xent": [C.POINTER(XentDesc), P, P, P, P, P, P, P, P, C.c_size_t, V],
             "tgm_xent_backward": [C.POINTER(XentDesc), P, P, P, P, P, P, P, P, P, P, P,
@@ -1027,3 +1044,104 @@ def tgm_xent_backward(x, w, target, lse, dloss, work, bias=None, dx=None, dw=Non
     d = XentDesc(rows, N, K, dtype_code(dt), lx, lw, ldx, ldw)
     _call("tgm_xent_backward", gpu, stream, C.byref(d), px, pw, pb, pt, pe, pd, pn, pdx, pdw, pdb,
           pk, nk)
+
+
+def tgm_decay_attn_work_bytes(rows, S, heads, d_k, d_v, dtype, kv_heads=None,
+                              backward=False) -> int:
+    return _bytes("tgm_decay_attn_work_bytes", rows, S, heads, kv_heads or heads, d_k, d_v,
+                  dtype_code(dtype), 1 if backward else 0)
+
+
+def _state(name, t, shape, gpu):
+    """Address of an optional dense fp32 table of states."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} is a contiguous float32 tensor of {shape}")
+    if gpu < 0 or t.get_device() != gpu:
+        raise ValueError(f"{name} is on {t.device}: every tensor of a call is on one GPU")
+    return t.data_ptr()
+
+
+def _decay_args(q, k, v, decay, kv_heads):
+    """What the calls share: sizes, device, addresses and strides."""
+    import torch
+    (rows, wq), (_, wk), (_, wv) = _shape2("q", q), _shape2("k", k), _shape2("v", v)
+    if decay is None or decay.dim() != 1:
+        raise ValueError("decay is a vector, a number for each head")
+    H = decay.shape[0]
+    G = H if kv_heads is None else kv_heads
+    if H < 1 or G < 1 or H % G:
+        raise ValueError(f"{H} heads share {G} heads of k and v")
+    if wq % H or wk % G or wv % G or wq // H != wk // G:
+        raise ValueError(f"q, k and v of {wq}, {wk} and {wv} columns are no {H} and {G} heads")
+    gpu, dt = q.get_device(), q.dtype
+    pq, lq = _arg("q", q, dt, (rows, wq), gpu)
+    pk, lk = _arg("k", k, dt, (rows, wk), gpu)
+    pv, lv = _arg("v", v, dt, (rows, wv), gpu)
+    pd, _ = _arg("decay", decay, torch.float32, (H,), gpu)
+    return rows, H, G, wq // H, wv // G, gpu, dt, pq, lq, pk, lk, pv, lv, pd
+
+
+def _sequences(S, offsets, length, gpu):
+    import torch
+    if not 0 <= S < 1 << 31:
+        raise ValueError(f"S is {S}")
+    return (_opt("offsets", offsets, torch.int64, (S + 1,), gpu)[0],
+            _opt("length", length, torch.int32, (S,), gpu)[0])
+
+
+def tgm_decay_attn(q, k, v, decay, o, S, work, scale=1.0, kv_heads=None, offsets=None, length=None,
+                   state=None, state_last=None, reverse=False, stream=None):
+    """S_t = exp(decay) S_(t-1) + k_t v_t^T, o_t = scale q_t S_t for each head, along S
+    sequences: packed by ``offsets`` [S + 1], or padded (rows / S rows each).  q [rows x H
+    d_k], k [rows x kv_heads d_k], v [rows x kv_heads d_v], decay [H] (log a), o [rows x H
+    d_v], states [S, H, d_k, d_v] fp32."""
+    rows, H, G, dk, dv, gpu, dt, pq, lq, pk, lk, pv, lv, pd = _decay_args(q, k, v, decay, kv_heads)
+    pf, pl = _sequences(S, offsets, length, gpu)
+    po, lo = _arg("o", o, dt, (rows, H * dv), gpu)
+    ps = _state("state", state, (S, H, dk, dv), gpu)
+    pe = _state("state_last", state_last, (S, H, dk, dv), gpu)
+    pw, nw = _work_arg(work, gpu)
+    d = DecayAttnDesc(rows, S, H, G, dk, dv, dtype_code(dt), 1 if reverse else 0, scale, lq, lk, lv,
+                      lo, 0, 0, 0)
+    _call("tgm_decay_attn", gpu, stream, C.byref(d), pq, pk, pv, pd, pf, pl, ps, po, pe, pw, nw)
+
+
+def tgm_decay_attn_backward(q, k, v, decay, do, dq, dk, dv, S, work, scale=1.0, kv_heads=None,
+                            offsets=None, length=None, state=None, dstate_last=None, dstate=None,
+                            reverse=False, stream=None):
+    """Gradients of tgm_decay_attn with the same inputs and sequences; dq, dk, dv and dstate
+    are optional."""
+    rows, H, G, nk, nv, gpu, dt, pq, lq, pk, lk, pv, lv, pd = _decay_args(q, k, v, decay, kv_heads)
+    pf, pl = _sequences(S, offsets, length, gpu)
+    po, lo = _arg("do", do, dt, (rows, H * nv), gpu)
+    ps = _state("state", state, (S, H, nk, nv), gpu)
+    pe = _state("dstate_last", dstate_last, (S, H, nk, nv), gpu)
+    pb = _state("dstate", dstate, (S, H, nk, nv), gpu)
+    pdq, ldq = _opt("dq", dq, dt, (rows, H * nk), gpu)
+    pdk, ldk = _opt("dk", dk, dt, (rows, G * nk), gpu)
+    pdv, ldv = _opt("dv", dv, dt, (rows, G * nv), gpu)
+    pw, nw = _work_arg(work, gpu)
+    d = DecayAttnDesc(rows, S, H, G, nk, nv, dtype_code(dt), 1 if reverse else 0, scale, lq, lk, lv,
+                      lo, ldq, ldk, ldv)
+    _call("tgm_decay_attn_backward", gpu, stream, C.byref(d), pq, pk, pv, pd, pf, pl, ps, po, pe,
+          pdq, pdk, pdv, pb, pw, nw)
+
+
+def tgm_decay_attn_step(q, k, v, decay, state, o, scale=1.0, kv_heads=None, slots=None,
+                        n_rows=None, stream=None):
+    """One row of tgm_decay_attn for each row of q, k and v, into ``state``
+    [slots, H, d_k, d_v] in place."""
+    import torch
+    rows, H, G, dk, dv, gpu, dt, pq, lq, pk, lk, pv, lv, pd = _decay_args(q, k, v, decay, kv_heads)
+    if state is None or state.dim() != 4:
+        raise ValueError("state is a table of states [slots, H, d_k, d_v]")
+    S = state.shape[0]
+    ps = _state("state", state, (S, H, dk, dv), gpu)
+    po, lo = _opt("o", o, dt, (rows, H * dv), gpu)
+    pt, _ = _opt("slots", slots, torch.int32, (rows,), gpu)
+    pn, _ = _opt("n_rows", n_rows, torch.int32, (1,), gpu)
+    d = DecayAttnDesc(rows, S, H, G, dk, dv, dtype_code(dt), 0, scale, lq, lk, lv, lo, 0, 0, 0)
+    _call("tgm_decay_attn_step", gpu, stream, C.byref(d), pq, pk, pv, pd, pt, pn, ps, po)
