@@ -93,8 +93,8 @@ __device__ __forceinline__ DecayPiece decay_piece(const DecayArgs &a, int64_t id
     const int64_t idx = (int64_t)lo + lane;
     lo += __popcll(__ballot(idx < hi && decay_begin(a, (int32_t)min(idx, (int64_t)hi - 1)) / C +
                                                 idx <= id));
-    DecayPiece p{max(lo - 1, 0), 0, 0, 0, {0, 0}};
-    if (lo < 1)
+    DecayPiece p{max(lo - 1, 0), -1, 0, 0, {0, 0}};
+    if (lo < 1)   // before the first sequence
         return p;
     p.cell = id - p.s;
     p.q = decay_seq(a, p.s);
@@ -102,6 +102,47 @@ __device__ __forceinline__ DecayPiece decay_piece(const DecayArgs &a, int64_t id
     p.hi = min(p.q.e, (p.cell + 1) * C);
     return p;
 }
+
+struct DecayRun {
+    DecayArgs a;
+    float *states;      // [cells x H x dk x dv]: the state behind each cell's rows (in the
+                        // recurrence's order) where a sequence goes on to the next cell
+    int32_t cell;       // rows of a cell
+    int64_t cells;      // of a padded sequence, 0 for packed ones
+    int64_t ids;        // pieces
+};
+
+// Piece `id` of the sequences: a sequence of no more than a cell's rows in one piece, which
+// the cell that it begins in has; longer ones by cells.  Packed sequences share a grid of
+// cells, padded ones have cells of their own.
+__device__ __forceinline__ DecayPiece decay_piece_of(const DecayRun &r, int64_t id)
+{
+    DecayPiece p;
+    if (r.a.offsets) {
+        p = decay_piece(r.a, id, r.cell);
+        if (p.q.e - p.q.b <= r.cell) {
+            const bool here = p.q.b / r.cell == p.cell;
+            p.lo = here ? p.q.b : 0, p.hi = here ? p.q.e : 0;
+        }
+        return p;
+    }
+    p.s = (int32_t)(id / r.cells), p.cell = id;
+    p.q = decay_seq(r.a, p.s);
+    const int64_t k = id - p.s * r.cells;
+    p.lo = p.q.b + k * r.cell;
+    p.hi = min(p.q.e, p.lo + r.cell);
+    return p;
+}
+// Whether a sequence without rows is the piece's to look after.
+__device__ __forceinline__ bool decay_empty_here(const DecayRun &r, const DecayPiece &p)
+{
+    return p.q.e <= p.q.b && (r.a.offsets ? p.cell == p.q.b / r.cell : p.cell == p.s * r.cells);
+}
+
+// what: 0 states, 1 results of the inputs' type, 2 results in fp32
+tgm_status_t decay_f32(const DecayRun &r, int what, hipStream_t s);
+tgm_status_t decay_bf16(const DecayRun &r, int what, hipStream_t s);
+tgm_status_t decay_f16(const DecayRun &r, int what, hipStream_t s);
 
 // a^n of log a = g: 1 for n = 0, whatever g is.
 __device__ __forceinline__ float decay_pow(float g, float n) { return n == 0.f ? 1.f : expf(n * g); }

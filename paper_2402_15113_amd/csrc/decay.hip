@@ -12,69 +12,61 @@ using namespace tgm;
 
 namespace {
 
-// Row by row: a workgroup has a sequence's head, its state in registers, 256 / RW groups of
-// threads with every (256 / RW)-th of the state's rows and a column each.
-constexpr int kRowThreads = 256;
-template <class T, class O, int RW>
-__global__ __launch_bounds__(kRowThreads) void k_decay_rows(DecayArgs A)
+// The states behind the cells of the sequences that go on, from those of the cells alone: a
+// thread follows four elements of a head's state along a sequence.  Bound by memory.
+__global__ __launch_bounds__(256) void k_decay_walk(DecayRun run)
 {
-    constexpr int G = kRowThreads / RW, NI = kDecayMaxD / G;
-    __shared__ float xs[kDecayMaxD], ys[kDecayMaxD], part[G][RW];
-    const int j = threadIdx.x % RW, g = threadIdx.x / RW;
-    const int32_t h = blockIdx.y;
-    const float decay = A.decay[h], a = decay_pow(decay, 1.f);
-    const bool col = j < A.r;
-    for (int64_t s = blockIdx.x; s < A.S; s += gridDim.x) {
-        const DecaySeq q = decay_seq(A, (int32_t)s);
-        const int64_t n = q.e - q.b, at = (s * A.H + h) * (int64_t)(A.p * A.r);
-        float st[NI];
+    const DecayArgs &A = run.a;
+    const int32_t h = blockIdx.y, size = A.p * A.r;
+    const int32_t at = (int32_t)(blockIdx.z * 256 + threadIdx.x) * 4;
+    const float keep = decay_pow(A.decay[h], (float)run.cell);
+    const int64_t step = A.rev ? -1 : 1;
+    for (int64_t id = blockIdx.x; id < run.ids; id += gridDim.x) {
+        const DecayPiece p = decay_piece_of(run, id);
+        if (p.hi <= p.lo || p.q.e - p.q.b <= run.cell || at >= size)
+            continue;
+        if (A.rev ? p.hi != p.q.e : p.lo != p.q.b)
+            continue;
+        // the sequence's other cells but the last, which leaves no state
+        int64_t left = A.offsets ? (A.rev ? p.cell - p.q.b / run.cell
+                                          : (p.q.e - 1) / run.cell - p.cell)
+                                 : (p.q.e - p.q.b + run.cell - 1) / run.cell - 1;
+        --left;
+        float *s = run.states + (p.cell * A.H + h) * (int64_t)size + at;
+        const int64_t next = step * A.H * size;
+        auto load = [&](const float *from) __attribute__((always_inline)) {
+            f4 v{0.f, 0.f, 0.f, 0.f};
+            if (at + 4 <= size)
+                __builtin_memcpy(&v, from, 16);
+            else
 #pragma unroll
-        for (int u = 0; u < NI; ++u) {
-            const int i = g + u * G;
-            st[u] = A.first && col && i < A.p
-                        ? A.first[at + (A.turned ? (int64_t)j * A.p + i : (int64_t)i * A.r + j)]
-                        : 0.f;
-        }
-        for (int64_t t = 0; t < n; ++t) {
-            const int64_t row = A.rev ? q.e - 1 - t : q.b + t;
-            const float f = t == 0 && A.lag0 == 0 ? 1.f : a;
-            if ((int)threadIdx.x < A.p) {
-                const T *y = (const T *)A.y.p + row * A.y.ld + (int64_t)(h / A.y.share) * A.p;
-                const T *x = (const T *)A.x.p + row * A.x.ld + (int64_t)(h / A.x.share) * A.p;
-                ys[threadIdx.x] = A.c_y * to_f32(y[threadIdx.x]);
-                xs[threadIdx.x] = to_f32(x[threadIdx.x]);
-            }
-            const T *z = (const T *)A.z.p + row * A.z.ld + (int64_t)(h / A.z.share) * A.r;
-            const float zj = col ? to_f32(z[j]) : 0.f;
-            __syncthreads();
-            float o = 0.f;
+                for (int j = 0; j < 3; ++j)
+                    if (at + j < size)
+                        v[j] = from[j];
+            return v;
+        };
+        f4 v = load(s);
+        constexpr int AHEAD = 8;
+        for (; left > 0; left -= AHEAD) {
+            f4 e[AHEAD];
 #pragma unroll
-            for (int u = 0; u < NI; ++u) {
-                const int i = g + u * G;
-                if (i < A.p) {
-                    st[u] = f * st[u] + ys[i] * zj;
-                    o += xs[i] * st[u];
+            for (int u = 0; u < AHEAD; ++u)
+                if (u < left)
+                    e[u] = load(s + (u + 1) * next);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                if (u < left) {
+                    v = v * keep + e[u];
+                    s += next;
+                    if (at + 4 <= size)
+                        __builtin_memcpy(s, &v, 16);
+                    else
+#pragma unroll
+                        for (int j = 0; j < 3; ++j)
+                            if (at + j < size)
+                                s[j] = v[j];
                 }
-            }
-            part[g][j] = o;
-            __syncthreads();
-            if (A.out && g == 0 && col) {
-                for (int k = 1; k < G; ++k)
-                    o += part[k][j];
-                ((O *)A.out)[row * A.ld_out + (int64_t)h * A.r + j] = from_f32<O>(A.c_out * o);
-            }
         }
-        if (A.last) {
-            const float f = A.lag1 && (n || A.lag0) ? a : 1.f;
-#pragma unroll
-            for (int u = 0; u < NI; ++u) {
-                const int i = g + u * G;
-                if (col && i < A.p)
-                    A.last[at + (A.turned ? (int64_t)j * A.p + i : (int64_t)i * A.r + j)] =
-                        f * st[u];
-            }
-        }
-        __syncthreads();
     }
 }
 
@@ -167,78 +159,124 @@ size_t whole(size_t n) { return (n + 255) / 256 * 256; }
 // Workgroups along x for n of them a head: a launch has fewer than 2^32 threads.
 uint32_t across(int64_t n, int32_t H) { return (uint32_t)std::min<int64_t>(n, (1 << 22) / H); }
 
-template <class T, class O> tgm_status_t go_rows(const DecayArgs &a, hipStream_t s)
+// Rows of a cell: sequences of no more are one workgroup's (a head of them), longer ones are
+// divided, which costs a pass over y and z for the states and two over the states.
+constexpr int kCell = 1024;
+int32_t decay_cell(int64_t rows, int32_t S, int32_t H)
 {
-    const dim3 grid(across(a.S, a.H), (uint32_t)a.H);
-    if (a.S == 0)
-        return TGM_OK;
-    if (a.r <= 32)
-        TGM_LAUNCH((k_decay_rows<T, O, 32>), grid, dim3(kRowThreads), 0, s, a);
-    else if (a.r <= 64)
-        TGM_LAUNCH((k_decay_rows<T, O, 64>), grid, dim3(kRowThreads), 0, s, a);
-    else
-        TGM_LAUNCH((k_decay_rows<T, O, 128>), grid, dim3(kRowThreads), 0, s, a);
-    return TGM_OK;
+    (void)rows, (void)S, (void)H;
+    return kCell;
+}
+// Cells, and whether any sequence may have more than one.
+struct DecayPlan {
+    int32_t cell;
+    int64_t cells, ids, padded_cells;
+    bool divided;
+};
+DecayPlan decay_plan(int64_t rows, int32_t S, int32_t H, bool packed)
+{
+    DecayPlan p{};
+    p.cell = decay_cell(rows, S, H);
+    if (packed) {
+        p.cells = cdiv(rows, p.cell), p.ids = p.cells + S, p.divided = p.cells > 1;
+    } else {
+        const int64_t L = S ? rows / S : 0;
+        p.padded_cells = std::max<int64_t>(1, cdiv(L, p.cell));
+        p.cells = p.ids = p.padded_cells * S, p.divided = p.padded_cells > 1;
+    }
+    return p;
 }
 
 struct DecayCall {
     const tgm_decay_attn_desc *d;
     int64_t ld_q, ld_k, ld_v, ld_o, ld_dq, ld_dk, ld_dv;
-    DecayArgs a;   // the sequences, decays and sizes
+    DecayRun run;   // the sequences, decays and sizes
+    bool divided;
     hipStream_t s;
 };
 
-template <class T>
-tgm_status_t forward(DecayCall &c, const void *q, const void *k, const void *v, const float *first,
-                     void *o, float *last)
+template <class T> tgm_status_t go(const DecayRun &r, int what, hipStream_t s)
 {
-    DecayArgs a = c.a;
+    return std::is_same_v<T, float>  ? decay_f32(r, what, s)
+           : std::is_same_v<T, bf16> ? decay_bf16(r, what, s)
+                                     : decay_f16(r, what, s);
+}
+
+// The states behind the cells, into r.states.
+template <class T> tgm_status_t states(const DecayCall &c, const DecayRun &r)
+{
+    if (!c.divided)
+        return TGM_OK;
+    TGM_TRY_STATUS(go<T>(r, 0, c.s));
+    const int64_t z = cdiv((int64_t)r.a.p * r.a.r, 1024);
+    TGM_LAUNCH(k_decay_walk,
+               dim3(across(r.ids, (int32_t)(r.a.H * z)), (uint32_t)r.a.H, (uint32_t)z), dim3(256),
+               0, c.s, r);
+    return TGM_OK;
+}
+
+template <class T>
+tgm_status_t forward(const DecayCall &c, const void *q, const void *k, const void *v,
+                     const float *first, void *o, float *last, char *work)
+{
+    DecayRun r = c.run;
+    DecayArgs &a = r.a;
     const int32_t share = a.H / c.d->H_kv;
     a.x = DecayIn{q, c.ld_q, 1}, a.y = DecayIn{k, c.ld_k, share};
     a.z = DecayIn{v, c.ld_v, share};
     a.p = c.d->d_k, a.r = c.d->d_v, a.out = o, a.ld_out = c.ld_o;
     a.first = first, a.last = last, a.lag0 = 1, a.c_y = 1.f, a.c_out = c.d->scale;
-    return go_rows<T, T>(a, c.s);
+    r.states = (float *)work;
+    TGM_TRY_STATUS(states<T>(c, r));
+    return go<T>(r, 1, c.s);
 }
 
 template <class T>
-tgm_status_t backward(DecayCall &c, const void *q, const void *k, const void *v,
+tgm_status_t backward(const DecayCall &c, const void *q, const void *k, const void *v,
                       const float *first, const void *dO, const float *dlast, void *dq, void *dk,
-                      void *dv, float *dfirst, char *work)
+                      void *dv, float *dfirst, char *work, size_t state_bytes)
 {
     const tgm_decay_attn_desc *d = c.d;
     const int32_t share = d->H / d->H_kv;
     const DecayIn iq{q, c.ld_q, 1}, ik{k, c.ld_k, share}, iv{v, c.ld_v, share}, io{dO, c.ld_o, 1};
-    DecayArgs a = c.a;
+    DecayRun r = c.run;
+    DecayArgs &a = r.a;
+    r.states = (float *)work;
     if (dq) {
+        a.y = ik, a.z = iv, a.p = d->d_k, a.r = d->d_v;
+        a.first = first, a.lag0 = 1, a.c_y = 1.f, a.c_out = d->scale;
+        TGM_TRY_STATUS(states<T>(c, r));
         a.x = io, a.y = iv, a.z = ik, a.p = d->d_v, a.r = d->d_k, a.turned = 1;
-        a.out = dq, a.ld_out = c.ld_dq, a.first = first, a.last = nullptr, a.lag0 = 1;
-        a.c_y = 1.f, a.c_out = d->scale;
-        TGM_TRY_STATUS((go_rows<T, T>(a, c.s)));
+        a.out = dq, a.ld_out = c.ld_dq;
+        TGM_TRY_STATUS(go<T>(r, 1, c.s));
     }
+    if (!dk && !dv && !dfirst)
+        return TGM_OK;
     // the others run against the first one's order
-    a.rev = !c.a.rev, a.first = dlast, a.lag0 = 0, a.c_y = d->scale, a.c_out = 1.f;
-    auto go = [&](void *out, int32_t width, int64_t ld) -> tgm_status_t {
+    a.rev = !c.run.a.rev, a.first = dlast, a.lag0 = 0, a.c_y = d->scale, a.c_out = 1.f;
+    a.x = ik, a.y = iq, a.z = io, a.p = d->d_k, a.r = d->d_v, a.turned = 0;
+    TGM_TRY_STATUS(states<T>(c, r));
+    float *part = (float *)(work + state_bytes);
+    auto results = [&](void *out, int32_t width, int64_t ld) -> tgm_status_t {
         if (share == 1 || !out) {
             a.out = out, a.ld_out = ld;
-            return go_rows<T, T>(a, c.s);
+            return go<T>(r, 1, c.s);
         }
-        a.out = work, a.ld_out = (int64_t)a.H * width;
-        TGM_TRY_STATUS((go_rows<T, float>(a, c.s)));
+        a.out = part, a.ld_out = (int64_t)a.H * width;
+        TGM_TRY_STATUS(go<T>(r, 2, c.s));
         const int64_t ids = cdiv(a.rows, kSharedRows) + a.S;
         TGM_LAUNCH((k_decay_shared<T>), dim3((uint32_t)std::min<int64_t>(ids, 1 << 16)),
-                   dim3(256), 0, c.s, (const float *)work, a, d->H_kv, share, width, ld, (T *)out);
+                   dim3(256), 0, c.s, part, a, d->H_kv, share, width, ld, (T *)out);
         return TGM_OK;
     };
+    if (dv || dfirst) {
+        a.last = dfirst, a.lag1 = 1;
+        TGM_TRY_STATUS(results(dv, d->d_v, c.ld_dv));
+    }
     if (dk) {
         a.x = iv, a.y = io, a.z = iq, a.p = d->d_v, a.r = d->d_k, a.turned = 1;
         a.last = nullptr;
-        TGM_TRY_STATUS(go(dk, d->d_k, c.ld_dk));
-    }
-    if (dv || dfirst) {
-        a.x = ik, a.y = iq, a.z = io, a.p = d->d_k, a.r = d->d_v, a.turned = 0;
-        a.last = dfirst, a.lag1 = 1;
-        TGM_TRY_STATUS(go(dv, d->d_v, c.ld_dv));
+        TGM_TRY_STATUS(results(dk, d->d_k, c.ld_dk));
     }
     return TGM_OK;
 }
@@ -267,19 +305,38 @@ tgm_status_t decay_call(const tgm_decay_attn_desc *d, const float *decay, const 
     for (int64_t ld : {c->ld_q, c->ld_k, c->ld_v, c->ld_o, c->ld_dq, c->ld_dk, c->ld_dv})
         if (ld < 0)
             return TGM_EINVAL;
-    c->a.decay = decay, c->a.offsets = offsets, c->a.length = length;
-    c->a.rows = d->rows, c->a.S = d->S, c->a.H = d->H, c->a.rev = d->reverse != 0;
+    DecayArgs &a = c->run.a;
+    a.decay = decay, a.offsets = offsets, a.length = length;
+    a.rows = d->rows, a.S = d->S, a.H = d->H, a.rev = d->reverse != 0;
     return TGM_OK;
 }
 // Padded sequences divide the rows.
 tgm_status_t decay_lengths(DecayCall *c)
 {
-    if (c->a.offsets)
-        return TGM_OK;
-    if (c->a.S == 0 ? c->a.rows != 0 : c->a.rows % c->a.S != 0)
-        return TGM_EINVAL;
-    c->a.L = c->a.S ? c->a.rows / c->a.S : 0;
+    DecayArgs &a = c->run.a;
+    if (!a.offsets) {
+        if (a.S == 0 ? a.rows != 0 : a.rows % a.S != 0)
+            return TGM_EINVAL;
+        a.L = a.S ? a.rows / a.S : 0;
+    }
+    const DecayPlan p = decay_plan(a.rows, a.S, a.H, a.offsets != nullptr);
+    c->run.cell = p.cell, c->run.cells = p.padded_cells, c->run.ids = p.ids;
+    c->divided = p.divided;
     return TGM_OK;
+}
+// Bytes of the cells' states, whichever form the sequences have.
+size_t state_bytes(int64_t rows, int32_t S, int32_t H, int32_t d_k, int32_t d_v)
+{
+    size_t cells = 0;
+    const DecayPlan packed = decay_plan(rows, S, H, true);
+    if (packed.divided)
+        cells = packed.cells;
+    if (S && rows % S == 0) {
+        const DecayPlan padded = decay_plan(rows, S, H, false);
+        if (padded.divided)
+            cells = std::max(cells, (size_t)padded.cells);
+    }
+    return whole(cells * H * d_k * d_v * 4);
 }
 
 tgm_status_t check_work(size_t need, const void *work, size_t bytes)
@@ -299,7 +356,7 @@ tgm_status_t go_step(const DecayCall &c, const void *q, const void *k, const voi
     d.ld_q = c.ld_q, d.ld_k = c.ld_k, d.ld_v = c.ld_v, d.ld_o = c.ld_o;
     TGM_LAUNCH((k_decay_step<T, VEC, LANES>),
                dim3(across(d.rows, d.H), (uint32_t)d.H), dim3(256), 0, c.s, (const T *)q,
-               (const T *)k, (const T *)v, c.a.decay, slots, n_rows, state, (T *)o, d);
+               (const T *)k, (const T *)v, c.run.a.decay, slots, n_rows, state, (T *)o, d);
     return TGM_OK;
 }
 template <class T>
@@ -324,7 +381,8 @@ extern "C" tgm_status_t tgm_decay_attn_work_bytes(int64_t rows, int32_t S, int32
 {
     if (!bytes || !decay_sizes(rows, S, H, H_kv, d_k, d_v, dtype))
         return TGM_EINVAL;
-    *bytes = backward && H != H_kv ? whole((size_t)rows * H * std::max(d_k, d_v) * 4) : 0;
+    *bytes = state_bytes(rows, S, H, d_k, d_v) +
+             (backward && H != H_kv ? whole((size_t)rows * H * std::max(d_k, d_v) * 4) : 0);
     return TGM_OK;
 }
 
@@ -343,10 +401,11 @@ extern "C" tgm_status_t tgm_decay_attn(const tgm_decay_attn_desc *d, const void 
     TGM_TRY_STATUS(tgm_decay_attn_work_bytes(d->rows, d->S, d->H, d->H_kv, d->d_k, d->d_v, d->dtype,
                                              0, &need));
     TGM_TRY_STATUS(check_work(need, work, work_bytes));
+    char *w = (char *)work;
     switch (d->dtype) {
-    case TGM_F32: return forward<float>(c, q, k, v, state, o, state_last);
-    case TGM_BF16: return forward<bf16>(c, q, k, v, state, o, state_last);
-    default: return forward<f16>(c, q, k, v, state, o, state_last);
+    case TGM_F32: return forward<float>(c, q, k, v, state, o, state_last, w);
+    case TGM_BF16: return forward<bf16>(c, q, k, v, state, o, state_last, w);
+    default: return forward<f16>(c, q, k, v, state, o, state_last, w);
     }
 }
 
@@ -366,13 +425,14 @@ extern "C" tgm_status_t tgm_decay_attn_backward(
                                              1, &need));
     TGM_TRY_STATUS(check_work(need, work, work_bytes));
     char *w = (char *)work;
+    const size_t sb = state_bytes(d->rows, d->S, d->H, d->d_k, d->d_v);
     switch (d->dtype) {
     case TGM_F32:
-        return backward<float>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w);
+        return backward<float>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w, sb);
     case TGM_BF16:
-        return backward<bf16>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w);
+        return backward<bf16>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w, sb);
     default:
-        return backward<f16>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w);
+        return backward<f16>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w, sb);
     }
 }
 

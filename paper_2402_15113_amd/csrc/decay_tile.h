@@ -1,0 +1,559 @@
+// The recurrence of csrc/decay.h by chunks of C rows, on the matrix cores.  Within a chunk,
+// with n rows and i, s counted from its first,
+//   out_i = c_out a^(i + 1) x_i S  +  c_out c_y sum_(s <= i) a^(i - s) (x_i . y_s) z_s,
+//   S    <- a^n S + c_y sum_s a^(n - 1 - s) y_s z_s^T,
+// which is four products instead of C steps.
+//
+// A workgroup has a head of a piece of a sequence and goes from chunk to chunk.  Its
+// wavefronts share the state by columns: each keeps its columns of S (fp32, all p rows) in
+// registers, where the matrix instructions leave them in just the places that the next
+// product's operand has them in, so S never goes through LDS.  What they exchange are the
+// weights a^(i - s) (x_i . y_s), a row of 16 i each, through LDS.
+//
+// 16-bit inputs: the weights and S are rounded once for the products that make out of them.
+// S itself takes a^(n - 1 - s) z_s in parts (three of bf16, two of fp16) whose sum is the
+// fp32 product, so no error of 16 bits is carried along.
+#pragma once
+
+#include "decay.h"
+#include "linear.h"
+
+namespace tgm {
+
+typedef short d4s __attribute__((ext_vector_type(4)));
+
+// C rows of W columns in LDS; rows 16 bytes longer than they have to be start in different
+// banks.
+template <class T, int C, int W> struct DecayTile {
+    static constexpr int VEC = 16 / (int)sizeof(T), PITCH = W * (int)sizeof(T) + 16;
+    static constexpr int BYTES = C * PITCH;
+
+    // 16 bytes along a row: the fragment of rows r0 .. r0 + 15 for step ks of 4 VEC columns
+    static __device__ __forceinline__ Frag<T> along(const char *t, int r0, int ks)
+    {
+        const int lane = threadIdx.x & 63;
+        Frag<T> f;
+        f.v = *reinterpret_cast<const Pack<T, VEC> *>(__builtin_assume_aligned(
+            t + (r0 + (lane & 15)) * PITCH + 16 * (4 * ks + (lane >> 4)), 16));
+        return f;
+    }
+    // The transposed fragment: lane i of 16 has column c0 + i, for step ks of 4 VEC rows.
+    // GAP: 16 columns in four runs of 4 that begin 8 apart.
+    template <bool GAP> static __device__ __forceinline__ Frag<T> across(const char *t, int c0,
+                                                                         int ks)
+    {
+        const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+        Frag<T> f;
+        if constexpr (sizeof(T) == 2) {
+            // 16 lanes read 4 rows of 16 elements; lane i gets the i-th column of them
+            typedef __attribute__((address_space(3))) d4s *lds_d4;
+            d4s v[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const char *p = t + (32 * ks + 8 * q + 4 * u + (i >> 2)) * PITCH +
+                                2 * (c0 + (GAP ? 8 : 4) * (i & 3));
+                v[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_d4)(__attribute__((address_space(3))) void *)const_cast<char *>(p));
+            }
+            __builtin_memcpy(&f.v, v, sizeof(v));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                f.v.v[j] = *reinterpret_cast<const T *>(t + (16 * ks + 4 * q + j) * PITCH +
+                                                        4 * (c0 + i));
+        }
+        return f;
+    }
+};
+
+typedef unsigned d4u __attribute__((ext_vector_type(4), may_alias));
+typedef d4u d4u_any __attribute__((aligned(1)));
+
+// A chunk's rows of one matrix in memory: n of them, row i of the chunk at i ld from `base`,
+// or at (n - 1 - i) ld where the recurrence runs backwards.  63 rows of 2^24 fp32 columns are
+// below 2^32 bytes, so a lane keeps 32 bits for a row's place.
+struct DecayRows {
+    const char *base;
+    uint32_t ld;      // bytes
+    int32_t n, rev;
+    __device__ __forceinline__ uint32_t at(int i) const
+    {
+        return (uint32_t)(rev ? n - 1 - i : i) * ld;
+    }
+};
+
+// A tile on its way from memory: rows past n and columns past the head's width are zeros.
+template <class T, int C, int W, int TH> struct DecayLoad {
+    using Tile = DecayTile<T, C, W>;
+    static constexpr int VEC = Tile::VEC, PER = W / VEC, N = C * PER / TH;
+    static_assert(C * PER % TH == 0, "");
+    d4u v[N];   // of a vector type, which the compiler loads as one (a Pack it takes apart)
+
+    __device__ __forceinline__ void load(const DecayRows &r, int width)
+    {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
+            v[u] = d4u{0, 0, 0, 0};
+            if (row < r.n && c < width) {
+                const char *from = r.base + (r.at(row) + (uint32_t)(c * (int)sizeof(T)));
+                if (c + VEC <= width)
+                    v[u] = *reinterpret_cast<const d4u_any *>(from);
+                else
+                    v[u] = part(reinterpret_cast<const T *>(from), width - c);
+            }
+        }
+    }
+    // the first `some` < VEC elements of a vector
+    static __device__ __forceinline__ d4u part(const T *from, int some)
+    {
+        d4u r{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < VEC - 1; ++j)
+            if (j < some) {
+                if constexpr (sizeof(T) == 4)
+                    r[j] = __builtin_bit_cast(unsigned, from[j]);
+                else
+                    r[j / 2] |= (unsigned)__builtin_bit_cast(uint16_t, from[j]) << (16 * (j & 1));
+            }
+        return r;
+    }
+    __device__ __forceinline__ void store(char *t) const
+    {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int e = u * TH + (int)threadIdx.x;
+            *reinterpret_cast<d4u *>(__builtin_assume_aligned(
+                t + e / PER * Tile::PITCH + 16 * (e % PER), 16)) = v[u];
+        }
+    }
+};
+
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) < INFINITY; }
+// The power of two that brings a largest absolute value (finite, or 0) to 2^13 .. 2^14: fp16 has
+// 13 bits and more below it.
+__device__ __forceinline__ float half_scale(float top)
+{
+    return top > 0.f ? ldexpf(1.f, min(max(13 - ilogbf(top), -100), 100)) : 1.f;
+}
+
+// Which piece and head workgroup `id` takes: every XCD (id % 8) runs of all heads of a
+// piece, whose rows lie side by side and which may share k and v.
+struct DecayPlace {
+    int64_t piece;
+    int32_t head;
+};
+__device__ __forceinline__ DecayPlace decay_place(int64_t id, int64_t ids, int32_t H)
+{
+    const int64_t whole = ids / 8 * 8;
+    if (id < whole * H) {
+        const int64_t m = id / 8;
+        return DecayPlace{m / H * 8 + id % 8, (int32_t)(m % H)};
+    }
+    const int64_t m = id - whole * H;
+    return DecayPlace{whole + m / H, (int32_t)(m % H)};
+}
+
+template <class T> struct DecayChunk {
+    static constexpr int C = sizeof(T) == 4 ? 32 : 64;
+};
+
+// OUT: x and the results; without, the pieces' states alone (for sequences that go on).
+template <class T, class O, int P, int R, bool OUT>
+__global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
+{
+    constexpr int C = DecayChunk<T>::C, NW = R / 16, TH = 64 * NW, TB = C / 16, STEP = 64 / (int)sizeof(T);
+    constexpr int KP = P / STEP, KC = C / STEP, PB = P / 16;
+    constexpr int BLOCKS = STEP / 16;                               // blocks of 16 to a step
+    constexpr int VEC = 16 / (int)sizeof(T);
+    constexpr bool F16 = TypeCode<T>::code == TGM_F16, F32 = sizeof(T) == 4;
+    constexpr int PARTS = F32 ? 1 : F16 ? 2 : 3;
+    using TX = DecayTile<T, C, P>;
+    using TZ = DecayTile<T, C, R>;
+    using TW = DecayTile<T, C, C>;
+    __shared__ __attribute__((aligned(16))) char lx[OUT ? TX::BYTES : 16], ly[TX::BYTES],
+        lz[TZ::BYTES], lw[OUT ? TW::BYTES : 16];
+    __shared__ float row_scale[F16 ? C : 1];
+    const DecayArgs &A = run.a;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int i16 = lane & 15, g = lane >> 4, r0 = 16 * w;
+    // the state's row that element j of block pb of a lane is
+    auto state_row = [&](int pb, int j) {
+        return F32 ? 16 * pb + 4 * g + j : 32 * (pb / 2) + 8 * g + 4 * (pb & 1) + j;
+    };
+    const int64_t all = run.ids * A.H;
+    for (int64_t at = blockIdx.x; at < all; at += gridDim.x) {
+        const DecayPlace place = decay_place(at, run.ids, A.H);
+        const DecayPiece piece = decay_piece_of(run, place.piece);
+        const int32_t h = place.head;
+        const bool empty = decay_empty_here(run, piece);
+        const int64_t rows = piece.hi - piece.lo;
+        const bool begins = empty || (A.rev ? piece.hi == piece.q.e : piece.lo == piece.q.b);
+        const bool ends = empty || (A.rev ? piece.lo == piece.q.b : piece.hi == piece.q.e);
+        if (!empty && rows <= 0)
+            continue;
+        if (OUT ? rows <= 0 && !(ends && A.last) : ends)
+            continue;
+        const float decay = A.decay[h];
+        const int64_t size = (int64_t)A.p * A.r;
+
+        // ---- the state before the piece
+        f4 st[PB];
+        const float *from = nullptr;
+        if (begins)
+            from = A.first ? A.first + ((int64_t)piece.s * A.H + h) * size : nullptr;
+        else if (OUT)
+            from = run.states + ((piece.cell + (A.rev ? 1 : -1)) * A.H + h) * size;
+        const int col = r0 + i16;
+#pragma unroll
+        for (int pb = 0; pb < PB; ++pb) {
+            st[pb] = f4{0.f, 0.f, 0.f, 0.f};
+            const int r = state_row(pb, 0);
+            if (from && col < A.r)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (r + j < A.p)
+                        st[pb][j] = from[A.turned ? col * A.p + r + j : (r + j) * A.r + col];
+        }
+        bool some = from != nullptr;   // a state that is not all zeros
+
+        // rows t0 .. t0 + n - 1 of the piece, in the recurrence's order
+        auto rows_of = [&](const void *p, int64_t ld, int64_t head, int bytes, int64_t t0, int n)
+            __attribute__((always_inline)) {
+                const int64_t low = A.rev ? piece.hi - t0 - n : piece.lo + t0;
+                return DecayRows{(const char *)p + (low * ld + head) * bytes,
+                                 (uint32_t)(ld * bytes), n, A.rev};
+            };
+
+        // ---- weights that every whole chunk has
+        float wd[TB][4], fx[TB], wz[KC][VEC];
+        int lag = begins ? A.lag0 : 1, had_n = -1, had_lag = -1;
+#pragma unroll
+        for (int b = 0; b < TB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int d = 16 * b + i16 - (4 * g + j);
+                wd[b][j] = OUT && d >= 0 ? A.c_out * A.c_y * decay_pow(decay, (float)d) : 0.f;
+            }
+        float whole = 1.f;
+
+        DecayLoad<T, C, P, TH> vx, vy;
+        DecayLoad<T, C, R, TH> vz;
+        auto fetch = [&](int64_t t0) __attribute__((always_inline)) {
+            const int n = (int)min((int64_t)C, rows - t0);
+            constexpr int B = sizeof(T);
+            if constexpr (OUT)
+                vx.load(rows_of(A.x.p, A.x.ld, (int64_t)(h / A.x.share) * A.p, B, t0, n), A.p);
+            vy.load(rows_of(A.y.p, A.y.ld, (int64_t)(h / A.y.share) * A.p, B, t0, n), A.p);
+            vz.load(rows_of(A.z.p, A.z.ld, (int64_t)(h / A.z.share) * A.r, B, t0, n), A.r);
+        };
+        if (rows > 0)
+            fetch(0);
+        for (int64_t t0 = 0; t0 < rows; t0 += C) {
+            const int n = (int)min((int64_t)C, rows - t0), nb = (n + 15) / 16;
+            __syncthreads();   // no one reads the last chunk any more
+            if constexpr (OUT)
+                vx.store(lx);
+            vy.store(ly);
+            vz.store(lz);
+            __syncthreads();
+            const bool more = t0 + C < rows;
+            if (more)
+                fetch(t0 + C);
+            if (n != had_n || lag != had_lag) {
+                had_n = n, had_lag = lag;
+#pragma unroll
+                for (int b = 0; b < TB; ++b)
+                    fx[b] = A.c_out * decay_pow(decay, (float)(16 * b + i16 + lag));
+#pragma unroll
+                for (int k = 0; k < KC; ++k)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        wz[k][e] = A.c_y * decay_pow(decay, (float)max(0, n - 1 - (STEP * k +
+                                                                               VEC * g + e)));
+                whole = decay_pow(decay, (float)(n - 1 + lag));
+            }
+
+            if constexpr (OUT) {
+                // ---- the weights of rows 16 b .. + 15
+                for (int b = w; b < nb; b += NW) {
+                    f4 acc[TB];
+#pragma unroll
+                    for (int s = 0; s < TB; ++s)
+                        acc[s] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int k = 0; k < KP; ++k) {
+                        const Frag<T> fx_ = TX::along(lx, 16 * b, k);
+#pragma unroll
+                        for (int s = 0; s < TB; ++s)
+                            if (s <= b)
+                                acc[s] = mfma(TX::along(ly, 16 * s, k), fx_, acc[s]);
+                    }
+                    float top = 0.f;
+#pragma unroll
+                    for (int s = 0; s < TB; ++s)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            // row i16 of block b, column 4 g + j of block s: wd by their distance
+                            float f = 0.f;
+#pragma unroll
+                            for (int d = 0; d < TB; ++d)
+                                f = b - s == d ? wd[d][j] : f;
+                            const bool in = b > s || (b == s && i16 >= 4 * g + j);
+                            acc[s][j] = in ? acc[s][j] * f : 0.f;
+                            if constexpr (F16)
+                                top = finite(acc[s][j]) ? fmaxf(top, fabsf(acc[s][j])) : top;
+                        }
+                    float scale = 1.f;
+                    if constexpr (F16) {
+                        top = fmaxf(top, __shfl_xor(top, 16));
+                        top = fmaxf(top, __shfl_xor(top, 32));
+                        scale = half_scale(top);
+                        if (g == 0)
+                            row_scale[16 * b + i16] = 1.f / scale;
+                    }
+#pragma unroll
+                    for (int s = 0; s < TB; ++s)
+                        if (s <= (b | (BLOCKS - 1))) {
+                            Pack<T, 4> q;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                q.v[j] = from_f32<T>(F16 ? acc[s][j] * scale : acc[s][j]);
+                            *reinterpret_cast<Pack<T, 4> *>(__builtin_assume_aligned(
+                                lw + (16 * b + i16) * TW::PITCH +
+                                    (16 * s + 4 * g) * (int)sizeof(T),
+                                4 * sizeof(T))) = q;
+                        }
+                }
+                __syncthreads();
+            }
+
+            // ---- this wavefront's columns of z
+            Frag<T> z[KC];
+#pragma unroll
+            for (int k = 0; k < KC; ++k)
+                z[k] = TZ::template across<false>(lz, r0, k);
+
+            if constexpr (OUT) {
+                f4 o[TB];
+                bool spoilt = false;
+                float s_scale = 1.f;
+                if constexpr (F16) {
+                    float top = 0.f;
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float v = fabsf(st[pb][j]);
+                            top = v < INFINITY ? fmaxf(top, v) : top;
+                        }
+                    s_scale = half_scale(group_max<64>(top));
+                }
+                // A weight of zero does not keep what is not finite in a later row of the
+                // chunk from a row's sum.  The last block's sums show whether there may be any:
+                // then such elements of z count as zero, and are added where they belong.
+                for (bool again = false;; again = true) {
+#pragma unroll
+                    for (int b = 0; b < TB; ++b)
+                        o[b] = f4{0.f, 0.f, 0.f, 0.f};
+                    if (some) {
+#pragma unroll
+                        for (int k = 0; k < KP; ++k) {
+                            Frag<T> s;
+#pragma unroll
+                            for (int e = 0; e < VEC; ++e) {
+                                const float v = st[BLOCKS * k + e / 4][e % 4];
+                                s.v.v[e] = from_f32<T>(F16 ? v * s_scale : v);
+                            }
+#pragma unroll
+                            for (int b = 0; b < TB; ++b)
+                                if (b < nb)
+                                    o[b] = mfma(s, TX::along(lx, 16 * b, k), o[b]);
+                        }
+#pragma unroll
+                        for (int b = 0; b < TB; ++b)
+                            o[b] *= F16 ? fx[b] / s_scale : fx[b];
+                    }
+#pragma unroll
+                    for (int b = 0; b < TB; ++b)
+                        if (b < nb) {
+                            f4 c = F16 ? f4{0.f, 0.f, 0.f, 0.f} : o[b];
+#pragma unroll
+                            for (int k = 0; k < KC; ++k)
+                                if (BLOCKS * k <= b)
+                                    c = mfma(z[k], TW::along(lw, 16 * b, k), c);
+                            o[b] = F16 ? o[b] + c * row_scale[16 * b + i16] : c;
+                        }
+                    if (again)
+                        break;
+                    float seen = 0.f;
+#pragma unroll
+                    for (int b = 0; b < TB; ++b)
+                        if (b == nb - 1)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                seen += o[b][j] * 0.f;
+                    if (!__any(seen != 0.f))   // NaN where one is not finite
+                        break;
+                    bool bad = false;
+#pragma unroll
+                    for (int k = 0; k < KC; ++k)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e)
+                            if (!finite(to_f32(z[k].v.v[e])))
+                                bad = true, z[k].v.v[e] = from_f32<T>(0.f);
+                    if (!__any(bad))
+                        break;
+                    spoilt = true;
+                }
+                if (spoilt) {
+#pragma unroll 1
+                    for (int s = 0; s < n; ++s)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float v = to_f32(*reinterpret_cast<const T *>(
+                                lz + s * TZ::PITCH + (r0 + 4 * g + j) * (int)sizeof(T)));
+                            if (finite(v))
+                                continue;
+#pragma unroll
+                            for (int b = 0; b < TB; ++b)
+                                if (16 * b + i16 >= s && b < nb)
+                                    o[b][j] += v * to_f32(*reinterpret_cast<const T *>(
+                                                       lw + (16 * b + i16) * TW::PITCH +
+                                                       s * (int)sizeof(T)));
+                        }
+#pragma unroll
+                    for (int k = 0; k < KC; ++k)
+                        z[k] = TZ::template across<false>(lz, r0, k);
+                }
+                const DecayRows to_rows =
+                    rows_of(A.out, A.ld_out, (int64_t)h * A.r + r0, sizeof(O), t0, n);
+#pragma unroll
+                for (int b = 0; b < TB; ++b) {
+                    const int i = 16 * b + i16, c = r0 + 4 * g;
+                    if (A.out && i < n && c < A.r) {
+                        O *to = reinterpret_cast<O *>(const_cast<char *>(to_rows.base) +
+                                                      (to_rows.at(i) + 4 * g * (uint32_t)sizeof(O)));
+                        Pack<O, 4> q;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            q.v[j] = from_f32<O>(o[b][j]);
+                        if (c + 4 <= A.r)
+                            store_pack(to, q);
+                        else
+#pragma unroll
+                            for (int j = 0; j < 3; ++j)
+                                if (c + j < A.r)
+                                    to[j] = q.v[j];
+                    }
+                }
+            }
+
+            // ---- the state behind the chunk, where anyone reads it
+            if (more || !ends || (OUT && A.last)) {
+                float z_scale = 1.f;
+                if constexpr (F16) {
+                    float top = 0.f;
+#pragma unroll
+                    for (int k = 0; k < KC; ++k)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            const float v = fabsf(to_f32(z[k].v.v[e]) * wz[k][e]);
+                            top = v < INFINITY ? fmaxf(top, v) : top;
+                        }
+                    z_scale = half_scale(group_max<64>(top));
+                }
+                const float keep = F16 ? whole * z_scale : whole;
+                if (some)
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb)
+                        st[pb] *= keep;
+#pragma unroll
+                for (int k = 0; k < KC; ++k)
+                    if (BLOCKS * k < nb) {
+                        Frag<T> part[PARTS];
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            float v = to_f32(z[k].v.v[e]) * wz[k][e];
+                            if constexpr (F16)
+                                v *= z_scale;
+#pragma unroll
+                            for (int u = 0; u < PARTS; ++u) {
+                                part[u].v.v[e] = from_f32<T>(v);
+                                // (what is not finite stays in the first part)
+                                if (u + 1 < PARTS)
+                                    v = finite(v) ? v - to_f32(part[u].v.v[e]) : 0.f;
+                            }
+                        }
+#pragma unroll
+                        for (int pb = 0; pb < PB; ++pb) {
+                            const Frag<T> f = TX::template across<!F32>(
+                                ly, F32 ? 16 * pb : 32 * (pb / 2) + 4 * (pb & 1), k);
+#pragma unroll
+                            for (int u = 0; u < PARTS; ++u)
+                                st[pb] = mfma(f, part[u], st[pb]);
+                        }
+                    }
+                if constexpr (F16)
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb)
+                        st[pb] *= 1.f / z_scale;
+                some = true;
+            }
+            lag = 1;
+        }
+
+        // ---- the state behind the piece
+        float *to = nullptr;
+        float f = 1.f;
+        if (!OUT)
+            to = run.states + (piece.cell * A.H + h) * size;
+        else if (ends && A.last) {
+            to = A.last + ((int64_t)piece.s * A.H + h) * size;
+            if (A.lag1 && !empty)
+                f = decay_pow(decay, 1.f);
+        }
+        if (to && col < A.r)
+#pragma unroll
+            for (int pb = 0; pb < PB; ++pb) {
+                const int r = state_row(pb, 0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (r + j < A.p)
+                        to[A.turned ? col * A.p + r + j : (r + j) * A.r + col] = f * st[pb][j];
+            }
+    }
+}
+
+template <class T, class O, int P, int R, bool OUT>
+tgm_status_t launch_decay(const DecayRun &r, hipStream_t s)
+{
+    constexpr int TH = 4 * R;
+    const int64_t n = std::min<int64_t>(r.ids * r.a.H, 1 << 22);
+    if (n > 0)
+        TGM_LAUNCH((k_decay<T, O, P, R, OUT>), dim3((uint32_t)n), dim3(TH), 0, s, r);
+    return TGM_OK;
+}
+template <class T, class O, bool OUT> tgm_status_t pick_decay(const DecayRun &r, hipStream_t s)
+{
+    const int p = r.a.p, q = r.a.r;
+    if (p <= 32 && q <= 32)
+        return launch_decay<T, O, 32, 32, OUT>(r, s);
+    if (p <= 64)
+        return q <= 64 ? launch_decay<T, O, 64, 64, OUT>(r, s)
+                       : launch_decay<T, O, 64, 128, OUT>(r, s);
+    return q <= 64 ? launch_decay<T, O, 128, 64, OUT>(r, s)
+                   : launch_decay<T, O, 128, 128, OUT>(r, s);
+}
+// what: 0 states, 1 results of type T, 2 results in fp32
+template <class T> tgm_status_t run_decay(const DecayRun &r, int what, hipStream_t s)
+{
+    if (what == 0)
+        return pick_decay<T, float, false>(r, s);
+    if constexpr (sizeof(T) == 2)
+        if (what == 2)
+            return pick_decay<T, float, true>(r, s);
+    return pick_decay<T, T, true>(r, s);
+}
+
+}  // namespace tgm

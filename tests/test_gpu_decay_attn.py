@@ -163,6 +163,14 @@ def test_long(tgm, dtype, reverse):
     go(tgm, packed([3, 1100, 700, 0, 40], behind=5), 2, 1, 40, 24, TYPES[dtype], reverse=reverse)
 
 
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_longer(tgm, dtype, reverse):
+    """A sequence over several cells of rows, with states handed along them."""
+    go(tgm, packed([700, 4500, 2], before=100), 1, 1, 16, 20, TYPES[dtype], reverse=reverse)
+    go(tgm, padded([3000, 2047, 1, 2300], 3000), 1, 1, 12, 16, TYPES[dtype], reverse=reverse)
+
+
 @pytest.mark.parametrize("dtype", list(TYPES))
 def test_shortened(tgm, dtype):
     go(tgm, packed([30, 200, 5, 70], cut=[0, 130, 9, -1]), 2, 2, 48, 48, TYPES[dtype])
