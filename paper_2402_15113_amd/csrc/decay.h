@@ -144,7 +144,11 @@ tgm_status_t decay_f32(const DecayRun &r, int what, hipStream_t s);
 tgm_status_t decay_bf16(const DecayRun &r, int what, hipStream_t s);
 tgm_status_t decay_f16(const DecayRun &r, int what, hipStream_t s);
 
-// a^n of log a = g: 1 for n = 0, whatever g is.
-__device__ __forceinline__ float decay_pow(float g, float n) { return n == 0.f ? 1.f : expf(n * g); }
+// a^n, from log2 a: 1 for n = 0, whatever a is.
+__device__ __forceinline__ float decay_log2(float g) { return g * 1.44269504088896340736f; }
+__device__ __forceinline__ float decay_pow(float g2, float n)
+{
+    return n == 0.f ? 1.f : __builtin_amdgcn_exp2f(n * g2);
+}
 
 }  // namespace tgm

@@ -19,7 +19,7 @@ __global__ __launch_bounds__(256) void k_decay_walk(DecayRun run)
     const DecayArgs &A = run.a;
     const int32_t h = blockIdx.y, size = A.p * A.r;
     const int32_t at = (int32_t)(blockIdx.z * 256 + threadIdx.x) * 4;
-    const float keep = decay_pow(A.decay[h], (float)run.cell);
+    const float keep = decay_pow(decay_log2(A.decay[h]), (float)run.cell);
     const int64_t step = A.rev ? -1 : 1;
     for (int64_t id = blockIdx.x; id < run.ids; id += gridDim.x) {
         const DecayPiece p = decay_piece_of(run, id);
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256) void k_decay_step(const T *__restrict__ q,
     const int32_t n = rows_in_use((int32_t)d.rows, n_rows);
     const int32_t h = blockIdx.y, hk = h / (d.H / d.H_kv);
     const int c = threadIdx.x % LANES * VEC, g = threadIdx.x / LANES;
-    const float a = decay_pow(decay[h], 1.f);
+    const float a = decay_pow(decay_log2(decay[h]), 1.f);
     for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
         const int32_t slot = slots ? slots[row] : (int32_t)row;
         const bool kept = slot >= 0 && slot < d.S;

@@ -15,6 +15,8 @@
 // fp32 product, so no error of 16 bits is carried along.
 #pragma once
 
+#include <type_traits>
+
 #include "decay.h"
 #include "linear.h"
 
@@ -91,16 +93,46 @@ template <class T, int C, int W, int TH> struct DecayLoad {
 
     __device__ __forceinline__ void load(const DecayRows &r, int width)
     {
+        // past the ends: the last one again, for zeros
+        if (width % VEC == 0) {
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-            const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
-            v[u] = d4u{0, 0, 0, 0};
-            if (row < r.n && c < width) {
-                const char *from = r.base + (r.at(row) + (uint32_t)(c * (int)sizeof(T)));
-                if (c + VEC <= width)
-                    v[u] = *reinterpret_cast<const d4u_any *>(from);
-                else
-                    v[u] = part(reinterpret_cast<const T *>(from), width - c);
+            for (int u = 0; u < N; ++u) {
+                const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
+                v[u] = *reinterpret_cast<const d4u_any *>(
+                    r.base + (r.at(min(row, r.n - 1)) +
+                              (uint32_t)(min(c, width - VEC) * (int)sizeof(T))));
+            }
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
+                if (row >= r.n || c >= width)
+                    v[u] = d4u{0, 0, 0, 0};
+            }
+        } else if (width > VEC) {
+            // the last vector of a row moves back to its end, and its elements forward
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
+                v[u] = *reinterpret_cast<const d4u_any *>(
+                    r.base + (r.at(min(row, r.n - 1)) +
+                              (uint32_t)(min(c, width - VEC) * (int)sizeof(T))));
+            }
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
+                const int back = max(0, c - (width - VEC));
+                v[u] = __builtin_bit_cast(d4u, __builtin_bit_cast(unsigned __int128, v[u]) >>
+                                                   (8 * (int)sizeof(T) * min(back, VEC - 1)));
+                if (row >= r.n || c >= width)
+                    v[u] = d4u{0, 0, 0, 0};
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
+                v[u] = d4u{0, 0, 0, 0};
+                if (row < r.n && c == 0)
+                    v[u] = part(reinterpret_cast<const T *>(r.base + r.at(row)), width);
             }
         }
     }
@@ -162,10 +194,10 @@ template <class T> struct DecayChunk {
 template <class T, class O, int P, int R, bool OUT>
 __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
 {
-    constexpr int C = DecayChunk<T>::C, NW = R / 16, TH = 64 * NW, TB = C / 16, STEP = 64 / (int)sizeof(T);
-    constexpr int KP = P / STEP, KC = C / STEP, PB = P / 16;
-    constexpr int BLOCKS = STEP / 16;                               // blocks of 16 to a step
-    constexpr int VEC = 16 / (int)sizeof(T);
+    constexpr int C = DecayChunk<T>::C, NW = R / 16, TH = 64 * NW, TB = C / 16;
+    constexpr int STEP = 64 / (int)sizeof(T);       // elements of a fragment's sum
+    constexpr int BLOCKS = STEP / 16;               // blocks of 16 in them
+    constexpr int KP = P / STEP, PB = P / 16, VEC = 16 / (int)sizeof(T);
     constexpr bool F16 = TypeCode<T>::code == TGM_F16, F32 = sizeof(T) == 4;
     constexpr int PARTS = F32 ? 1 : F16 ? 2 : 3;
     using TX = DecayTile<T, C, P>;
@@ -194,28 +226,8 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
             continue;
         if (OUT ? rows <= 0 && !(ends && A.last) : ends)
             continue;
-        const float decay = A.decay[h];
+        const float decay = decay_log2(A.decay[h]);
         const int64_t size = (int64_t)A.p * A.r;
-
-        // ---- the state before the piece
-        f4 st[PB];
-        const float *from = nullptr;
-        if (begins)
-            from = A.first ? A.first + ((int64_t)piece.s * A.H + h) * size : nullptr;
-        else if (OUT)
-            from = run.states + ((piece.cell + (A.rev ? 1 : -1)) * A.H + h) * size;
-        const int col = r0 + i16;
-#pragma unroll
-        for (int pb = 0; pb < PB; ++pb) {
-            st[pb] = f4{0.f, 0.f, 0.f, 0.f};
-            const int r = state_row(pb, 0);
-            if (from && col < A.r)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (r + j < A.p)
-                        st[pb][j] = from[A.turned ? col * A.p + r + j : (r + j) * A.r + col];
-        }
-        bool some = from != nullptr;   // a state that is not all zeros
 
         // rows t0 .. t0 + n - 1 of the piece, in the recurrence's order
         auto rows_of = [&](const void *p, int64_t ld, int64_t head, int bytes, int64_t t0, int n)
@@ -224,19 +236,6 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                 return DecayRows{(const char *)p + (low * ld + head) * bytes,
                                  (uint32_t)(ld * bytes), n, A.rev};
             };
-
-        // ---- weights that every whole chunk has
-        float wd[TB][4], fx[TB], wz[KC][VEC];
-        int lag = begins ? A.lag0 : 1, had_n = -1, had_lag = -1;
-#pragma unroll
-        for (int b = 0; b < TB; ++b)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int d = 16 * b + i16 - (4 * g + j);
-                wd[b][j] = OUT && d >= 0 ? A.c_out * A.c_y * decay_pow(decay, (float)d) : 0.f;
-            }
-        float whole = 1.f;
-
         DecayLoad<T, C, P, TH> vx, vy;
         DecayLoad<T, C, R, TH> vz;
         auto fetch = [&](int64_t t0) __attribute__((always_inline)) {
@@ -249,58 +248,68 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
         };
         if (rows > 0)
             fetch(0);
-        for (int64_t t0 = 0; t0 < rows; t0 += C) {
-            const int n = (int)min((int64_t)C, rows - t0), nb = (n + 15) / 16;
-            __syncthreads();   // no one reads the last chunk any more
-            if constexpr (OUT)
-                vx.store(lx);
-            vy.store(ly);
-            vz.store(lz);
-            __syncthreads();
-            const bool more = t0 + C < rows;
-            if (more)
-                fetch(t0 + C);
-            if (n != had_n || lag != had_lag) {
-                had_n = n, had_lag = lag;
-#pragma unroll
-                for (int b = 0; b < TB; ++b)
-                    fx[b] = A.c_out * decay_pow(decay, (float)(16 * b + i16 + lag));
-#pragma unroll
-                for (int k = 0; k < KC; ++k)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        wz[k][e] = A.c_y * decay_pow(decay, (float)max(0, n - 1 - (STEP * k +
-                                                                               VEC * g + e)));
-                whole = decay_pow(decay, (float)(n - 1 + lag));
-            }
 
-            if constexpr (OUT) {
-                // ---- the weights of rows 16 b .. + 15
-                for (int b = w; b < nb; b += NW) {
-                    f4 acc[TB];
+        // ---- the state before the piece
+        f4 st[PB];
+        const float *from = nullptr;
+        if (begins)
+            from = A.first ? A.first + ((int64_t)piece.s * A.H + h) * size : nullptr;
+        else if (OUT)
+            from = run.states + ((piece.cell + (A.rev ? 1 : -1)) * A.H + h) * size;
+        const int col = r0 + i16;
+        // where element (r, col) of a state lies: 32 bits, formed where it is used
+        uint32_t s_col = (uint32_t)col * (A.turned ? (uint32_t)A.p : 1u) * 4u;
+        const uint32_t s_row = (A.turned ? 1u : (uint32_t)A.r) * 4u;
+        asm volatile("" : "+v"(s_col));
 #pragma unroll
-                    for (int s = 0; s < TB; ++s)
+        for (int pb = 0; pb < PB; ++pb)
+            st[pb] = f4{0.f, 0.f, 0.f, 0.f};
+        if (from && col < A.r)
+#pragma unroll
+            for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int r = state_row(pb, j);
+                    const float v = *reinterpret_cast<const float *>(
+                        reinterpret_cast<const char *>(from) +
+                        (s_col + (uint32_t)min(r, A.p - 1) * s_row));
+                    st[pb][j] = r < A.p ? v : 0.f;
+                }
+        bool some = from != nullptr;     // a state that is not all zeros
+        int lag = begins ? A.lag0 : 1;   // its weight at the chunk's first row: a^lag
+
+        // A chunk of n rows, NB blocks of 16 of them (the last may be shorter); NB is known so
+        // that no branch stands between a fragment's read and its product.
+        auto chunk = [&](auto blocks, int64_t t0, int n, bool more) __attribute__((always_inline)) {
+            constexpr int NB = decltype(blocks)::value, KC = (NB + BLOCKS - 1) / BLOCKS;
+            if constexpr (OUT) {
+                // ---- the weights of rows 16 b .. + 15 and NS blocks of s a wavefront
+                constexpr int NS = F16 || NW < NB * 2 ? NB : NW >= NB * NB ? 1 : NB * NB / NW;
+                constexpr int TASKS = NB * (NB / NS);
+                const float c_w = A.c_out * A.c_y;
+#pragma unroll 1
+                for (int task = w; task < TASKS; task += NW) {
+                    const int b = task % NB, s0 = task / NB * NS;
+                    f4 acc[NS];
+#pragma unroll
+                    for (int s = 0; s < NS; ++s)
                         acc[s] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int k = 0; k < KP; ++k) {
-                        const Frag<T> fx_ = TX::along(lx, 16 * b, k);
+                        const Frag<T> fx = TX::along(lx, 16 * b, k);
 #pragma unroll
-                        for (int s = 0; s < TB; ++s)
-                            if (s <= b)
-                                acc[s] = mfma(TX::along(ly, 16 * s, k), fx_, acc[s]);
+                        for (int s = 0; s < NS; ++s)
+                            acc[s] = mfma(TX::along(ly, 16 * (s0 + s), k), fx, acc[s]);
                     }
                     float top = 0.f;
 #pragma unroll
-                    for (int s = 0; s < TB; ++s)
+                    for (int s = 0; s < NS; ++s)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            // row i16 of block b, column 4 g + j of block s: wd by their distance
-                            float f = 0.f;
-#pragma unroll
-                            for (int d = 0; d < TB; ++d)
-                                f = b - s == d ? wd[d][j] : f;
-                            const bool in = b > s || (b == s && i16 >= 4 * g + j);
-                            acc[s][j] = in ? acc[s][j] * f : 0.f;
+                            // row i16 of block b, column 4 g + j of block s0 + s
+                            const int d = 16 * (b - s0 - s) + i16 - (4 * g + j);
+                            const float f = c_w * decay_pow(decay, (float)max(d, 0));
+                            acc[s][j] = d >= 0 ? acc[s][j] * f : 0.f;
                             if constexpr (F16)
                                 top = finite(acc[s][j]) ? fmaxf(top, fabsf(acc[s][j])) : top;
                         }
@@ -312,18 +321,22 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                         if (g == 0)
                             row_scale[16 * b + i16] = 1.f / scale;
                     }
+                    char *to = lw + (16 * b + i16) * TW::PITCH + (16 * s0 + 4 * g) * (int)sizeof(T);
 #pragma unroll
-                    for (int s = 0; s < TB; ++s)
-                        if (s <= (b | (BLOCKS - 1))) {
-                            Pack<T, 4> q;
+                    for (int s = 0; s < NS; ++s) {
+                        Pack<T, 4> q;
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                q.v[j] = from_f32<T>(F16 ? acc[s][j] * scale : acc[s][j]);
-                            *reinterpret_cast<Pack<T, 4> *>(__builtin_assume_aligned(
-                                lw + (16 * b + i16) * TW::PITCH +
-                                    (16 * s + 4 * g) * (int)sizeof(T),
-                                4 * sizeof(T))) = q;
-                        }
+                        for (int j = 0; j < 4; ++j)
+                            q.v[j] = from_f32<T>(F16 ? acc[s][j] * scale : acc[s][j]);
+                        *reinterpret_cast<Pack<T, 4> *>(__builtin_assume_aligned(
+                            to + 16 * s * (int)sizeof(T), 4 * sizeof(T))) = q;
+                    }
+                    if constexpr (NB % BLOCKS) {   // the rest of a fragment's sum
+                        Pack<T, 4> q;
+                        __builtin_memset(&q, 0, sizeof(q));
+                        *reinterpret_cast<Pack<T, 4> *>(__builtin_assume_aligned(
+                            to + 16 * NB * (int)sizeof(T), 4 * sizeof(T))) = q;
+                    }
                 }
                 __syncthreads();
             }
@@ -335,7 +348,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                 z[k] = TZ::template across<false>(lz, r0, k);
 
             if constexpr (OUT) {
-                f4 o[TB];
+                f4 o[NB];
                 bool spoilt = false;
                 float s_scale = 1.f;
                 if constexpr (F16) {
@@ -352,9 +365,10 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                 // A weight of zero does not keep what is not finite in a later row of the
                 // chunk from a row's sum.  The last block's sums show whether there may be any:
                 // then such elements of z count as zero, and are added where they belong.
-                for (bool again = false;; again = true) {
+#pragma unroll 1
+                for (;;) {
 #pragma unroll
-                    for (int b = 0; b < TB; ++b)
+                    for (int b = 0; b < NB; ++b)
                         o[b] = f4{0.f, 0.f, 0.f, 0.f};
                     if (some) {
 #pragma unroll
@@ -366,45 +380,40 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                                 s.v.v[e] = from_f32<T>(F16 ? v * s_scale : v);
                             }
 #pragma unroll
-                            for (int b = 0; b < TB; ++b)
-                                if (b < nb)
-                                    o[b] = mfma(s, TX::along(lx, 16 * b, k), o[b]);
+                            for (int b = 0; b < NB; ++b)
+                                o[b] = mfma(s, TX::along(lx, 16 * b, k), o[b]);
                         }
 #pragma unroll
-                        for (int b = 0; b < TB; ++b)
-                            o[b] *= F16 ? fx[b] / s_scale : fx[b];
+                        for (int b = 0; b < NB; ++b) {
+                            const float f =
+                                A.c_out * decay_pow(decay, (float)(16 * b + i16 + lag));
+                            o[b] *= F16 ? f / s_scale : f;
+                        }
                     }
 #pragma unroll
-                    for (int b = 0; b < TB; ++b)
-                        if (b < nb) {
-                            f4 c = F16 ? f4{0.f, 0.f, 0.f, 0.f} : o[b];
+                    for (int b = 0; b < NB; ++b) {
+                        f4 c = F16 ? f4{0.f, 0.f, 0.f, 0.f} : o[b];
 #pragma unroll
-                            for (int k = 0; k < KC; ++k)
-                                if (BLOCKS * k <= b)
-                                    c = mfma(z[k], TW::along(lw, 16 * b, k), c);
-                            o[b] = F16 ? o[b] + c * row_scale[16 * b + i16] : c;
-                        }
-                    if (again)
-                        break;
+                        for (int k = 0; k < KC; ++k)
+                            if (BLOCKS * k <= b)
+                                c = mfma(z[k], TW::along(lw, 16 * b, k), c);
+                        o[b] = F16 ? o[b] + c * row_scale[16 * b + i16] : c;
+                    }
                     float seen = 0.f;
 #pragma unroll
-                    for (int b = 0; b < TB; ++b)
-                        if (b == nb - 1)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                seen += o[b][j] * 0.f;
-                    if (!__any(seen != 0.f))   // NaN where one is not finite
+                    for (int j = 0; j < 4; ++j)
+                        seen += o[NB - 1][j] * 0.f;
+                    if (spoilt || !__any(seen != 0.f))   // NaN where one is not finite
                         break;
-                    bool bad = false;
 #pragma unroll
                     for (int k = 0; k < KC; ++k)
 #pragma unroll
                         for (int e = 0; e < VEC; ++e)
                             if (!finite(to_f32(z[k].v.v[e])))
-                                bad = true, z[k].v.v[e] = from_f32<T>(0.f);
-                    if (!__any(bad))
+                                spoilt = true, z[k].v.v[e] = from_f32<T>(0.f);
+                    spoilt = __any(spoilt);
+                    if (!spoilt)
                         break;
-                    spoilt = true;
                 }
                 if (spoilt) {
 #pragma unroll 1
@@ -416,8 +425,8 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                             if (finite(v))
                                 continue;
 #pragma unroll
-                            for (int b = 0; b < TB; ++b)
-                                if (16 * b + i16 >= s && b < nb)
+                            for (int b = 0; b < NB; ++b)
+                                if (16 * b + i16 >= s)
                                     o[b][j] += v * to_f32(*reinterpret_cast<const T *>(
                                                        lw + (16 * b + i16) * TW::PITCH +
                                                        s * (int)sizeof(T)));
@@ -426,31 +435,43 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                     for (int k = 0; k < KC; ++k)
                         z[k] = TZ::template across<false>(lz, r0, k);
                 }
-                const DecayRows to_rows =
-                    rows_of(A.out, A.ld_out, (int64_t)h * A.r + r0, sizeof(O), t0, n);
+                if (A.out) {
+                    const DecayRows to_rows =
+                        rows_of(A.out, A.ld_out, (int64_t)h * A.r + r0, sizeof(O), t0, n);
+                    const int c = r0 + 4 * g;
+                    auto to = [&](int b) __attribute__((always_inline)) {
+                        return reinterpret_cast<O *>(
+                            const_cast<char *>(to_rows.base) +
+                            (to_rows.at(16 * b + i16) + 4 * g * (uint32_t)sizeof(O)));
+                    };
+                    if (c + 4 <= A.r) {
 #pragma unroll
-                for (int b = 0; b < TB; ++b) {
-                    const int i = 16 * b + i16, c = r0 + 4 * g;
-                    if (A.out && i < n && c < A.r) {
-                        O *to = reinterpret_cast<O *>(const_cast<char *>(to_rows.base) +
-                                                      (to_rows.at(i) + 4 * g * (uint32_t)sizeof(O)));
-                        Pack<O, 4> q;
+                        for (int b = 0; b < NB; ++b) {
+                            Pack<O, 4> q;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            q.v[j] = from_f32<O>(o[b][j]);
-                        if (c + 4 <= A.r)
-                            store_pack(to, q);
-                        else
+                            for (int j = 0; j < 4; ++j)
+                                q.v[j] = from_f32<O>(o[b][j]);
+                            if (16 * b + i16 < n)
+                                store_pack(to(b), q);
+                        }
+                    } else if (c < A.r) {
 #pragma unroll
-                            for (int j = 0; j < 3; ++j)
-                                if (c + j < A.r)
-                                    to[j] = q.v[j];
+                        for (int b = 0; b < NB; ++b)
+                            if (16 * b + i16 < n)
+#pragma unroll
+                                for (int j = 0; j < 3; ++j)
+                                    if (c + j < A.r)
+                                        to(b)[j] = from_f32<O>(o[b][j]);
                     }
                 }
             }
 
             // ---- the state behind the chunk, where anyone reads it
             if (more || !ends || (OUT && A.last)) {
+                auto weight = [&](int k, int e) __attribute__((always_inline)) {
+                    const int s = STEP * k + VEC * g + e;
+                    return A.c_y * decay_pow(decay, (float)max(0, n - 1 - s));
+                };
                 float z_scale = 1.f;
                 if constexpr (F16) {
                     float top = 0.f;
@@ -458,42 +479,42 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                     for (int k = 0; k < KC; ++k)
 #pragma unroll
                         for (int e = 0; e < VEC; ++e) {
-                            const float v = fabsf(to_f32(z[k].v.v[e]) * wz[k][e]);
+                            const float v = fabsf(to_f32(z[k].v.v[e]) * weight(k, e));
                             top = v < INFINITY ? fmaxf(top, v) : top;
                         }
                     z_scale = half_scale(group_max<64>(top));
                 }
+                const float whole = decay_pow(decay, (float)(n - 1 + lag));
                 const float keep = F16 ? whole * z_scale : whole;
                 if (some)
 #pragma unroll
                     for (int pb = 0; pb < PB; ++pb)
                         st[pb] *= keep;
 #pragma unroll
-                for (int k = 0; k < KC; ++k)
-                    if (BLOCKS * k < nb) {
-                        Frag<T> part[PARTS];
+                for (int k = 0; k < KC; ++k) {
+                    Frag<T> part[PARTS];
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            float v = to_f32(z[k].v.v[e]) * wz[k][e];
-                            if constexpr (F16)
-                                v *= z_scale;
+                    for (int e = 0; e < VEC; ++e) {
+                        float v = to_f32(z[k].v.v[e]) * weight(k, e);
+                        if constexpr (F16)
+                            v *= z_scale;
 #pragma unroll
-                            for (int u = 0; u < PARTS; ++u) {
-                                part[u].v.v[e] = from_f32<T>(v);
-                                // (what is not finite stays in the first part)
-                                if (u + 1 < PARTS)
-                                    v = finite(v) ? v - to_f32(part[u].v.v[e]) : 0.f;
-                            }
-                        }
-#pragma unroll
-                        for (int pb = 0; pb < PB; ++pb) {
-                            const Frag<T> f = TX::template across<!F32>(
-                                ly, F32 ? 16 * pb : 32 * (pb / 2) + 4 * (pb & 1), k);
-#pragma unroll
-                            for (int u = 0; u < PARTS; ++u)
-                                st[pb] = mfma(f, part[u], st[pb]);
+                        for (int u = 0; u < PARTS; ++u) {
+                            part[u].v.v[e] = from_f32<T>(v);
+                            // (what is not finite stays in the first part)
+                            if (u + 1 < PARTS)
+                                v = finite(v) ? v - to_f32(part[u].v.v[e]) : 0.f;
                         }
                     }
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb) {
+                        const Frag<T> f = TX::template across<!F32>(
+                            ly, F32 ? 16 * pb : 32 * (pb / 2) + 4 * (pb & 1), k);
+#pragma unroll
+                        for (int u = 0; u < PARTS; ++u)
+                            st[pb] = mfma(f, part[u], st[pb]);
+                    }
+                }
                 if constexpr (F16)
 #pragma unroll
                     for (int pb = 0; pb < PB; ++pb)
@@ -501,7 +522,31 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                 some = true;
             }
             lag = 1;
-        }
+        };
+
+        auto turn = [&](auto blocks, int64_t t0, int n) __attribute__((always_inline)) {
+            __syncthreads();   // no one reads the last chunk any more
+            if constexpr (OUT)
+                vx.store(lx);
+            vy.store(ly);
+            vz.store(lz);
+            __syncthreads();
+            const bool more = t0 + C < rows;
+            if (more)
+                fetch(t0 + C);
+            chunk(blocks, t0, n, more);
+        };
+        int64_t t0 = 0;
+#pragma unroll 1
+        for (; t0 + C <= rows; t0 += C)
+            turn(std::integral_constant<int, TB>{}, t0, C);
+        const int n = (int)(rows - t0);
+        if (n > C / 2)
+            turn(std::integral_constant<int, TB>{}, t0, n);
+        else if (n > 16)
+            turn(std::integral_constant<int, TB / 2 < 1 ? 1 : TB / 2>{}, t0, n);
+        else if (n > 0)
+            turn(std::integral_constant<int, 1>{}, t0, n);
 
         // ---- the state behind the piece
         float *to = nullptr;
@@ -513,15 +558,17 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
             if (A.lag1 && !empty)
                 f = decay_pow(decay, 1.f);
         }
+        asm volatile("" : "+v"(s_col));
         if (to && col < A.r)
 #pragma unroll
-            for (int pb = 0; pb < PB; ++pb) {
-                const int r = state_row(pb, 0);
+            for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (r + j < A.p)
-                        to[A.turned ? col * A.p + r + j : (r + j) * A.r + col] = f * st[pb][j];
-            }
+                for (int j = 0; j < 4; ++j) {
+                    const int r = state_row(pb, j);
+                    if (r < A.p)
+                        *reinterpret_cast<float *>(reinterpret_cast<char *>(to) +
+                                                   (s_col + (uint32_t)r * s_row)) = f * st[pb][j];
+                }
     }
 }
 
