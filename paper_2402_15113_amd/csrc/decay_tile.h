@@ -93,18 +93,21 @@ template <class T, int C, int W, int TH> struct DecayLoad {
 
     __device__ __forceinline__ void load(const DecayRows &r, int width)
     {
+        // (formed anew: the places of three forms of a load would stay in registers)
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
         // past the ends: the last one again, for zeros
         if (width % VEC == 0) {
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
+                const int e = u * TH + tid, row = e / PER, c = e % PER * VEC;
                 v[u] = *reinterpret_cast<const d4u_any *>(
                     r.base + (r.at(min(row, r.n - 1)) +
                               (uint32_t)(min(c, width - VEC) * (int)sizeof(T))));
             }
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
+                const int e = u * TH + tid, row = e / PER, c = e % PER * VEC;
                 if (row >= r.n || c >= width)
                     v[u] = d4u{0, 0, 0, 0};
             }
@@ -112,14 +115,14 @@ template <class T, int C, int W, int TH> struct DecayLoad {
             // the last vector of a row moves back to its end, and its elements forward
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
+                const int e = u * TH + tid, row = e / PER, c = e % PER * VEC;
                 v[u] = *reinterpret_cast<const d4u_any *>(
                     r.base + (r.at(min(row, r.n - 1)) +
                               (uint32_t)(min(c, width - VEC) * (int)sizeof(T))));
             }
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
+                const int e = u * TH + tid, row = e / PER, c = e % PER * VEC;
                 const int back = max(0, c - (width - VEC));
                 v[u] = __builtin_bit_cast(d4u, __builtin_bit_cast(unsigned __int128, v[u]) >>
                                                    (8 * (int)sizeof(T) * min(back, VEC - 1)));
@@ -129,7 +132,7 @@ template <class T, int C, int W, int TH> struct DecayLoad {
         } else {
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                const int e = u * TH + (int)threadIdx.x, row = e / PER, c = e % PER * VEC;
+                const int e = u * TH + tid, row = e / PER, c = e % PER * VEC;
                 v[u] = d4u{0, 0, 0, 0};
                 if (row < r.n && c == 0)
                     v[u] = part(reinterpret_cast<const T *>(r.base + r.at(row)), width);
@@ -199,7 +202,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
     constexpr int BLOCKS = STEP / 16;               // blocks of 16 in them
     constexpr int KP = P / STEP, PB = P / 16, VEC = 16 / (int)sizeof(T);
     constexpr bool F16 = TypeCode<T>::code == TGM_F16, F32 = sizeof(T) == 4;
-    constexpr int PARTS = F32 ? 1 : F16 ? 2 : 3;
+    constexpr int PARTS = F32 ? 1 : F16 ? 2 : 3, GROUP = PB < 4 ? PB : 4;
     using TX = DecayTile<T, C, P>;
     using TZ = DecayTile<T, C, R>;
     using TW = DecayTile<T, C, C>;
@@ -208,10 +211,10 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
     __shared__ float row_scale[F16 ? C : 1];
     const DecayArgs &A = run.a;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int i16 = lane & 15, g = lane >> 4, r0 = 16 * w;
-    // the state's row that element j of block pb of a lane is
-    auto state_row = [&](int pb, int j) {
-        return F32 ? 16 * pb + 4 * g + j : 32 * (pb / 2) + 8 * g + 4 * (pb & 1) + j;
+    const int lane_row = lane & 15, lane_group = lane >> 4, r0 = 16 * w;
+    // the state's row that element j of block pb of a lane is, q its group of 16
+    auto state_row = [](int pb, int j, int q) {
+        return F32 ? 16 * pb + 4 * q + j : 32 * (pb / 2) + 8 * q + 4 * (pb & 1) + j;
     };
     const int64_t all = run.ids * A.H;
     for (int64_t at = blockIdx.x; at < all; at += gridDim.x) {
@@ -256,11 +259,13 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
             from = A.first ? A.first + ((int64_t)piece.s * A.H + h) * size : nullptr;
         else if (OUT)
             from = run.states + ((piece.cell + (A.rev ? 1 : -1)) * A.H + h) * size;
-        const int col = r0 + i16;
-        // where element (r, col) of a state lies: 32 bits, formed where it is used
-        uint32_t s_col = (uint32_t)col * (A.turned ? (uint32_t)A.p : 1u) * 4u;
+        const int col = r0 + lane_row;
+        // where element (r, col) of a state lies: 32 bits, formed where it is used (all of
+        // them would stay in registers for the next piece)
+        const uint32_t s_col = (uint32_t)col * (A.turned ? (uint32_t)A.p : 1u) * 4u;
         const uint32_t s_row = (A.turned ? 1u : (uint32_t)A.r) * 4u;
-        asm volatile("" : "+v"(s_col));
+        int q = lane_group;
+        asm volatile("" : "+v"(q));
 #pragma unroll
         for (int pb = 0; pb < PB; ++pb)
             st[pb] = f4{0.f, 0.f, 0.f, 0.f};
@@ -269,19 +274,29 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
             for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int r = state_row(pb, j);
+                    const int r = state_row(pb, j, q);
                     const float v = *reinterpret_cast<const float *>(
                         reinterpret_cast<const char *>(from) +
                         (s_col + (uint32_t)min(r, A.p - 1) * s_row));
                     st[pb][j] = r < A.p ? v : 0.f;
                 }
+        float shared_weight[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            shared_weight[e] = __builtin_bit_cast(
+                float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(
+                           int, decay_pow(decay, (float)(VEC - 1 - e)))));
         bool some = from != nullptr;     // a state that is not all zeros
         int lag = begins ? A.lag0 : 1;   // its weight at the chunk's first row: a^lag
 
         // A chunk of n rows, NB blocks of 16 of them (the last may be shorter); NB is known so
         // that no branch stands between a fragment's read and its product.
-        auto chunk = [&](auto blocks, int64_t t0, int n, bool more) __attribute__((always_inline)) {
+        auto chunk = [&](auto blocks, auto full, int64_t t0, int n, bool more) __attribute__((always_inline)) {
             constexpr int NB = decltype(blocks)::value, KC = (NB + BLOCKS - 1) / BLOCKS;
+            // formed anew in every chunk: all that follows from a lane's place would stay in
+            // registers, four times over
+            int i16 = lane_row, g = lane_group;
+            asm volatile("" : "+v"(i16), "+v"(g));
             if constexpr (OUT) {
                 // ---- the weights of rows 16 b .. + 15 and NS blocks of s a wavefront
                 constexpr int NS = F16 || NW < NB * 2 ? NB : NW >= NB * NB ? 1 : NB * NB / NW;
@@ -468,9 +483,20 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
 
             // ---- the state behind the chunk, where anyone reads it
             if (more || !ends || (OUT && A.last)) {
+                // c_y a^(n - 1 - s), s = STEP k + VEC g + e; of whole chunks as a lane's factor
+                // times one that all lanes share
+                float lane_weight[KC];
+                if constexpr (full)
+#pragma unroll
+                    for (int k = 0; k < KC; ++k)
+                        lane_weight[k] =
+                            A.c_y * decay_pow(decay, (float)(C - VEC - STEP * k - VEC * g));
                 auto weight = [&](int k, int e) __attribute__((always_inline)) {
-                    const int s = STEP * k + VEC * g + e;
-                    return A.c_y * decay_pow(decay, (float)max(0, n - 1 - s));
+                    if constexpr (full)
+                        return lane_weight[k] * shared_weight[e];
+                    else
+                        return A.c_y * decay_pow(decay, (float)max(0, n - 1 - (STEP * k +
+                                                                               VEC * g + e)));
                 };
                 float z_scale = 1.f;
                 if constexpr (F16) {
@@ -501,18 +527,25 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
 #pragma unroll
                         for (int u = 0; u < PARTS; ++u) {
                             part[u].v.v[e] = from_f32<T>(v);
-                            // (what is not finite stays in the first part)
                             if (u + 1 < PARTS)
-                                v = finite(v) ? v - to_f32(part[u].v.v[e]) : 0.f;
+                                v -= to_f32(part[u].v.v[e]);
                         }
                     }
+                    // (products into one block wait for each other)
 #pragma unroll
-                    for (int pb = 0; pb < PB; ++pb) {
-                        const Frag<T> f = TX::template across<!F32>(
-                            ly, F32 ? 16 * pb : 32 * (pb / 2) + 4 * (pb & 1), k);
+                    for (int p4 = 0; p4 < PB; p4 += GROUP) {
+                        Frag<T> f[GROUP];
+#pragma unroll
+                        for (int i = 0; i < GROUP; ++i) {
+                            const int pb = p4 + i;
+                            f[i] = TX::template across<!F32>(
+                                ly, F32 ? 16 * pb : 32 * (pb / 2) + 4 * (pb & 1), k);
+                        }
 #pragma unroll
                         for (int u = 0; u < PARTS; ++u)
-                            st[pb] = mfma(f, part[u], st[pb]);
+#pragma unroll
+                            for (int i = 0; i < GROUP; ++i)
+                                st[p4 + i] = mfma(f[i], part[u], st[p4 + i]);
                     }
                 }
                 if constexpr (F16)
@@ -524,7 +557,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
             lag = 1;
         };
 
-        auto turn = [&](auto blocks, int64_t t0, int n) __attribute__((always_inline)) {
+        auto turn = [&](auto blocks, auto full, int64_t t0, int n) __attribute__((always_inline)) {
             __syncthreads();   // no one reads the last chunk any more
             if constexpr (OUT)
                 vx.store(lx);
@@ -534,19 +567,19 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
             const bool more = t0 + C < rows;
             if (more)
                 fetch(t0 + C);
-            chunk(blocks, t0, n, more);
+            chunk(blocks, full, t0, n, more);
         };
         int64_t t0 = 0;
 #pragma unroll 1
         for (; t0 + C <= rows; t0 += C)
-            turn(std::integral_constant<int, TB>{}, t0, C);
+            turn(std::integral_constant<int, TB>{}, std::true_type{}, t0, C);
         const int n = (int)(rows - t0);
         if (n > C / 2)
-            turn(std::integral_constant<int, TB>{}, t0, n);
+            turn(std::integral_constant<int, TB>{}, std::false_type{}, t0, n);
         else if (n > 16)
-            turn(std::integral_constant<int, TB / 2 < 1 ? 1 : TB / 2>{}, t0, n);
+            turn(std::integral_constant<int, TB / 2 < 1 ? 1 : TB / 2>{}, std::false_type{}, t0, n);
         else if (n > 0)
-            turn(std::integral_constant<int, 1>{}, t0, n);
+            turn(std::integral_constant<int, 1>{}, std::false_type{}, t0, n);
 
         // ---- the state behind the piece
         float *to = nullptr;
@@ -558,13 +591,13 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
             if (A.lag1 && !empty)
                 f = decay_pow(decay, 1.f);
         }
-        asm volatile("" : "+v"(s_col));
+        asm volatile("" : "+v"(q));
         if (to && col < A.r)
 #pragma unroll
             for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int r = state_row(pb, j);
+                    const int r = state_row(pb, j, q);
                     if (r < A.p)
                         *reinterpret_cast<float *>(reinterpret_cast<char *>(to) +
                                                    (s_col + (uint32_t)r * s_row)) = f * st[pb][j];
