@@ -24,27 +24,25 @@ namespace tgm {
 
 typedef short d4s __attribute__((ext_vector_type(4)));
 
-// C rows of W columns in LDS; rows 16 bytes longer than they have to be start in different
-// banks.
+// C rows of W columns in LDS.  Rows are so much longer than they have to be that both kinds
+// of read meet different banks: 16 bytes of 8 neighbouring rows, and (16 bits) 32 bytes of 4,
+// or (32 bits) 64 bytes of every 4th of 16.
 template <class T, int C, int W> struct DecayTile {
-    static constexpr int VEC = 16 / (int)sizeof(T), PITCH = W * (int)sizeof(T) + 16;
+    static constexpr int VEC = 16 / (int)sizeof(T);
+    static constexpr int PITCH = W * (int)sizeof(T) + (sizeof(T) == 2 ? 32 : 16);
     static constexpr int BYTES = C * PITCH;
 
     // 16 bytes along a row: the fragment of rows r0 .. r0 + 15 for step ks of 4 VEC columns
-    static __device__ __forceinline__ Frag<T> along(const char *t, int r0, int ks)
+    static __device__ __forceinline__ Frag<T> along(const char *t, int r0, int ks, int i, int q)
     {
-        const int lane = threadIdx.x & 63;
         Frag<T> f;
         f.v = *reinterpret_cast<const Pack<T, VEC> *>(__builtin_assume_aligned(
-            t + (r0 + (lane & 15)) * PITCH + 16 * (4 * ks + (lane >> 4)), 16));
+            t + (r0 + i) * PITCH + 16 * (4 * ks + q), 16));
         return f;
     }
     // The transposed fragment: lane i of 16 has column c0 + i, for step ks of 4 VEC rows.
-    // GAP: 16 columns in four runs of 4 that begin 8 apart.
-    template <bool GAP> static __device__ __forceinline__ Frag<T> across(const char *t, int c0,
-                                                                         int ks)
+    static __device__ __forceinline__ Frag<T> across(const char *t, int c0, int ks, int i, int q)
     {
-        const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
         Frag<T> f;
         if constexpr (sizeof(T) == 2) {
             // 16 lanes read 4 rows of 16 elements; lane i gets the i-th column of them
@@ -52,8 +50,8 @@ template <class T, int C, int W> struct DecayTile {
             d4s v[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const char *p = t + (32 * ks + 8 * q + 4 * u + (i >> 2)) * PITCH +
-                                2 * (c0 + (GAP ? 8 : 4) * (i & 3));
+                const char *p =
+                    t + (32 * ks + 8 * q + 4 * u + (i >> 2)) * PITCH + 2 * (c0 + 4 * (i & 3));
                 v[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                     (lds_d4)(__attribute__((address_space(3))) void *)const_cast<char *>(p));
             }
@@ -65,6 +63,23 @@ template <class T, int C, int W> struct DecayTile {
                                                         4 * (c0 + i));
         }
         return f;
+    }
+    // x lies in another order, 16-bit columns 16 h + 4 q + r of every 32 at 8 q + 4 h + r: the
+    // order in which a lane holds two blocks of the state, so that `along` reads what their
+    // product takes.  The columns as they are, for the product with y:
+    static __device__ __forceinline__ Frag<T> along_x(const char *t, int r0, int ks, int i, int q)
+    {
+        if constexpr (sizeof(T) == 4) {
+            return along(t, r0, ks, i, q);
+        } else {
+            const char *p = t + (r0 + i) * PITCH + 64 * ks + 32 * (q & 1) + 8 * (q >> 1);
+            const uint64_t lo = *reinterpret_cast<const uint64_t *>(p);
+            const uint64_t hi = *reinterpret_cast<const uint64_t *>(p + 16);
+            Frag<T> f;
+            __builtin_memcpy(&f.v, &lo, 8);
+            __builtin_memcpy((char *)&f.v + 8, &hi, 8);
+            return f;
+        }
     }
 };
 
@@ -96,8 +111,15 @@ template <class T, int C, int W, int TH> struct DecayLoad {
         // (formed anew: the places of three forms of a load would stay in registers)
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
-        // past the ends: the last one again, for zeros
-        if (width % VEC == 0) {
+        if (r.n == C && width == W) {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int e = u * TH + tid;
+                v[u] = *reinterpret_cast<const d4u_any *>(
+                    r.base + (r.at(e / PER) + (uint32_t)(e % PER * 16)));
+            }
+        } else if (width % VEC == 0) {
+            // past the ends: the last one again, for zeros
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const int e = u * TH + tid, row = e / PER, c = e % PER * VEC;
@@ -153,13 +175,22 @@ template <class T, int C, int W, int TH> struct DecayLoad {
             }
         return r;
     }
-    __device__ __forceinline__ void store(char *t) const
+    // X: in x's order
+    template <bool X> __device__ __forceinline__ void store(char *t) const
     {
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            const int e = u * TH + (int)threadIdx.x;
-            *reinterpret_cast<d4u *>(__builtin_assume_aligned(
-                t + e / PER * Tile::PITCH + 16 * (e % PER), 16)) = v[u];
+            const int e = u * TH + (int)threadIdx.x, m = e % PER;
+            char *row = t + e / PER * Tile::PITCH;
+            if constexpr (X && sizeof(T) == 2) {
+                // columns 8 m .. + 7 of every 32: h = m / 2, q = 2 (m % 2) and the next
+                typedef unsigned d2u __attribute__((ext_vector_type(2), may_alias));
+                char *to = row + 64 * (m >> 2) + 32 * (m & 1) + 8 * ((m >> 1) & 1);
+                *reinterpret_cast<d2u *>(to) = d2u{v[u].x, v[u].y};
+                *reinterpret_cast<d2u *>(to + 16) = d2u{v[u].z, v[u].w};
+            } else {
+                *reinterpret_cast<d4u *>(__builtin_assume_aligned(row + 16 * m, 16)) = v[u];
+            }
         }
     }
 };
@@ -208,14 +239,14 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
     using TW = DecayTile<T, C, C>;
     __shared__ __attribute__((aligned(16))) char lx[OUT ? TX::BYTES : 16], ly[TX::BYTES],
         lz[TZ::BYTES], lw[OUT ? TW::BYTES : 16];
+    // c_out c_y a^d at C + d for the distances d >= 0 within a chunk, zeros below
+    __shared__ float by_distance[OUT ? 2 * C : 1];
     __shared__ float row_scale[F16 ? C : 1];
     const DecayArgs &A = run.a;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int lane_row = lane & 15, lane_group = lane >> 4, r0 = 16 * w;
     // the state's row that element j of block pb of a lane is, q its group of 16
-    auto state_row = [](int pb, int j, int q) {
-        return F32 ? 16 * pb + 4 * q + j : 32 * (pb / 2) + 8 * q + 4 * (pb & 1) + j;
-    };
+    auto state_row = [](int pb, int j, int q) { return 16 * pb + 4 * q + j; };
     const int64_t all = run.ids * A.H;
     for (int64_t at = blockIdx.x; at < all; at += gridDim.x) {
         const DecayPlace place = decay_place(at, run.ids, A.H);
@@ -286,6 +317,12 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
             shared_weight[e] = __builtin_bit_cast(
                 float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(
                            int, decay_pow(decay, (float)(VEC - 1 - e)))));
+        if constexpr (OUT) {
+            __syncthreads();   // no one reads the last piece's any more
+            for (int i = threadIdx.x; i < 2 * C; i += TH)
+                by_distance[i] =
+                    i < C ? 0.f : A.c_out * A.c_y * decay_pow(decay, (float)(i - C));
+        }
         bool some = from != nullptr;     // a state that is not all zeros
         int lag = begins ? A.lag0 : 1;   // its weight at the chunk's first row: a^lag
 
@@ -301,7 +338,6 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                 // ---- the weights of rows 16 b .. + 15 and NS blocks of s a wavefront
                 constexpr int NS = F16 || NW < NB * 2 ? NB : NW >= NB * NB ? 1 : NB * NB / NW;
                 constexpr int TASKS = NB * (NB / NS);
-                const float c_w = A.c_out * A.c_y;
 #pragma unroll 1
                 for (int task = w; task < TASKS; task += NW) {
                     const int b = task % NB, s0 = task / NB * NS;
@@ -311,20 +347,20 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                         acc[s] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int k = 0; k < KP; ++k) {
-                        const Frag<T> fx = TX::along(lx, 16 * b, k);
+                        const Frag<T> fx = TX::along_x(lx, 16 * b, k, i16, g);
 #pragma unroll
                         for (int s = 0; s < NS; ++s)
-                            acc[s] = mfma(TX::along(ly, 16 * (s0 + s), k), fx, acc[s]);
+                            acc[s] = mfma(TX::along(ly, 16 * (s0 + s), k, i16, g), fx, acc[s]);
                     }
                     float top = 0.f;
 #pragma unroll
                     for (int s = 0; s < NS; ++s)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            // row i16 of block b, column 4 g + j of block s0 + s
+                            // row i16 of block b, column 4 g + j of block s0 + s (a product
+                            // with a later row is none, whatever it is)
                             const int d = 16 * (b - s0 - s) + i16 - (4 * g + j);
-                            const float f = c_w * decay_pow(decay, (float)max(d, 0));
-                            acc[s][j] = d >= 0 ? acc[s][j] * f : 0.f;
+                            acc[s][j] = d >= 0 ? acc[s][j] * by_distance[C + d] : 0.f;
                             if constexpr (F16)
                                 top = finite(acc[s][j]) ? fmaxf(top, fabsf(acc[s][j])) : top;
                         }
@@ -360,7 +396,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
             Frag<T> z[KC];
 #pragma unroll
             for (int k = 0; k < KC; ++k)
-                z[k] = TZ::template across<false>(lz, r0, k);
+                z[k] = TZ::across(lz, r0, k, i16, g);
 
             if constexpr (OUT) {
                 f4 o[NB];
@@ -396,7 +432,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                             }
 #pragma unroll
                             for (int b = 0; b < NB; ++b)
-                                o[b] = mfma(s, TX::along(lx, 16 * b, k), o[b]);
+                                o[b] = mfma(s, TX::along(lx, 16 * b, k, i16, g), o[b]);
                         }
 #pragma unroll
                         for (int b = 0; b < NB; ++b) {
@@ -411,7 +447,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
 #pragma unroll
                         for (int k = 0; k < KC; ++k)
                             if (BLOCKS * k <= b)
-                                c = mfma(z[k], TW::along(lw, 16 * b, k), c);
+                                c = mfma(z[k], TW::along(lw, 16 * b, k, i16, g), c);
                         o[b] = F16 ? o[b] + c * row_scale[16 * b + i16] : c;
                     }
                     float seen = 0.f;
@@ -448,7 +484,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                         }
 #pragma unroll
                     for (int k = 0; k < KC; ++k)
-                        z[k] = TZ::template across<false>(lz, r0, k);
+                        z[k] = TZ::across(lz, r0, k, i16, g);
                 }
                 if (A.out) {
                     const DecayRows to_rows =
@@ -466,7 +502,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
 #pragma unroll
                             for (int j = 0; j < 4; ++j)
                                 q.v[j] = from_f32<O>(o[b][j]);
-                            if (16 * b + i16 < n)
+                            if (full || 16 * b + i16 < n)
                                 store_pack(to(b), q);
                         }
                     } else if (c < A.r) {
@@ -538,8 +574,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
 #pragma unroll
                         for (int i = 0; i < GROUP; ++i) {
                             const int pb = p4 + i;
-                            f[i] = TX::template across<!F32>(
-                                ly, F32 ? 16 * pb : 32 * (pb / 2) + 4 * (pb & 1), k);
+                            f[i] = TX::across(ly, 16 * pb, k, i16, g);
                         }
 #pragma unroll
                         for (int u = 0; u < PARTS; ++u)
@@ -560,9 +595,9 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
         auto turn = [&](auto blocks, auto full, int64_t t0, int n) __attribute__((always_inline)) {
             __syncthreads();   // no one reads the last chunk any more
             if constexpr (OUT)
-                vx.store(lx);
-            vy.store(ly);
-            vz.store(lz);
+                vx.template store<true>(lx);
+            vy.template store<false>(ly);
+            vz.template store<false>(lz);
             __syncthreads();
             const bool more = t0 + C < rows;
             if (more)
