@@ -40,7 +40,9 @@ template <class T, int C, int W> struct DecayTile {
             t + (r0 + i) * PITCH + 16 * (4 * ks + q), 16));
         return f;
     }
-    // The transposed fragment: lane i of 16 has column c0 + i, for step ks of 4 VEC rows.
+    // The transposed fragment: lane i of 16 has column c0 + i, for step ks of 4 VEC rows; of
+    // 16-bit ones a lane has rows 4 q + r and 16 + 4 q + r of 32, so that the lanes that read
+    // together have 8 neighbouring rows, in banks of their own.
     static __device__ __forceinline__ Frag<T> across(const char *t, int c0, int ks, int i, int q)
     {
         Frag<T> f;
@@ -51,7 +53,7 @@ template <class T, int C, int W> struct DecayTile {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const char *p =
-                    t + (32 * ks + 8 * q + 4 * u + (i >> 2)) * PITCH + 2 * (c0 + 4 * (i & 3));
+                    t + (32 * ks + 16 * u + 4 * q + (i >> 2)) * PITCH + 2 * (c0 + 4 * (i & 3));
                 v[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                     (lds_d4)(__attribute__((address_space(3))) void *)const_cast<char *>(p));
             }
@@ -64,9 +66,10 @@ template <class T, int C, int W> struct DecayTile {
         }
         return f;
     }
-    // x lies in another order, 16-bit columns 16 h + 4 q + r of every 32 at 8 q + 4 h + r: the
-    // order in which a lane holds two blocks of the state, so that `along` reads what their
-    // product takes.  The columns as they are, for the product with y:
+    // x and the weights lie in another order, 16-bit columns 16 h + 4 q + r of every 32 at 8 q +
+    // 4 h + r: the order in which a lane holds two blocks of the state, and the rows of z, so
+    // that `along` reads what their products take.  x's columns as they are, for the product
+    // with y:
     static __device__ __forceinline__ Frag<T> along_x(const char *t, int r0, int ks, int i, int q)
     {
         if constexpr (sizeof(T) == 4) {
@@ -245,6 +248,9 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
     const DecayArgs &A = run.a;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int lane_row = lane & 15, lane_group = lane >> 4, r0 = 16 * w;
+    // element e of a fragment of z is row STEP k + 4 g + row_of(e)
+    auto row_of = [](int e) { return e < 4 ? e : 12 + e; };
+    constexpr int LAST = F32 ? 3 : 19;
     // the state's row that element j of block pb of a lane is, q its group of 16
     auto state_row = [](int pb, int j, int q) { return 16 * pb + 4 * q + j; };
     const int64_t all = run.ids * A.H;
@@ -316,7 +322,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
         for (int e = 0; e < VEC; ++e)
             shared_weight[e] = __builtin_bit_cast(
                 float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(
-                           int, decay_pow(decay, (float)(VEC - 1 - e)))));
+                           int, decay_pow(decay, (float)(LAST - row_of(e))))));
         if constexpr (OUT) {
             __syncthreads();   // no one reads the last piece's any more
             for (int i = threadIdx.x; i < 2 * C; i += TH)
@@ -372,21 +378,26 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                         if (g == 0)
                             row_scale[16 * b + i16] = 1.f / scale;
                     }
-                    char *to = lw + (16 * b + i16) * TW::PITCH + (16 * s0 + 4 * g) * (int)sizeof(T);
+                    // columns 16 s + 4 g .. + 3, in their order
+                    auto to = [&](int s) __attribute__((always_inline)) {
+                        return reinterpret_cast<Pack<T, 4> *>(__builtin_assume_aligned(
+                            lw + (16 * b + i16) * TW::PITCH +
+                                (F32 ? 16 * s + 4 * g : 32 * (s >> 1) + 8 * g + 4 * (s & 1)) *
+                                    (int)sizeof(T),
+                            4 * sizeof(T)));
+                    };
 #pragma unroll
                     for (int s = 0; s < NS; ++s) {
                         Pack<T, 4> q;
 #pragma unroll
                         for (int j = 0; j < 4; ++j)
                             q.v[j] = from_f32<T>(F16 ? acc[s][j] * scale : acc[s][j]);
-                        *reinterpret_cast<Pack<T, 4> *>(__builtin_assume_aligned(
-                            to + 16 * s * (int)sizeof(T), 4 * sizeof(T))) = q;
+                        *to(s0 + s) = q;
                     }
                     if constexpr (NB % BLOCKS) {   // the rest of a fragment's sum
                         Pack<T, 4> q;
                         __builtin_memset(&q, 0, sizeof(q));
-                        *reinterpret_cast<Pack<T, 4> *>(__builtin_assume_aligned(
-                            to + 16 * NB * (int)sizeof(T), 4 * sizeof(T))) = q;
+                        *to(NB) = q;
                     }
                 }
                 __syncthreads();
@@ -468,7 +479,9 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                 }
                 if (spoilt) {
 #pragma unroll 1
-                    for (int s = 0; s < n; ++s)
+                    for (int s = 0; s < n; ++s) {
+                        const int place =
+                            F32 ? s : (s & ~31) + 8 * ((s >> 2) & 3) + 4 * ((s >> 4) & 1) + (s & 3);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float v = to_f32(*reinterpret_cast<const T *>(
@@ -480,8 +493,9 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                                 if (16 * b + i16 >= s)
                                     o[b][j] += v * to_f32(*reinterpret_cast<const T *>(
                                                        lw + (16 * b + i16) * TW::PITCH +
-                                                       s * (int)sizeof(T)));
+                                                       place * (int)sizeof(T)));
                         }
+                    }
 #pragma unroll
                     for (int k = 0; k < KC; ++k)
                         z[k] = TZ::across(lz, r0, k, i16, g);
@@ -519,20 +533,20 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
 
             // ---- the state behind the chunk, where anyone reads it
             if (more || !ends || (OUT && A.last)) {
-                // c_y a^(n - 1 - s), s = STEP k + VEC g + e; of whole chunks as a lane's factor
-                // times one that all lanes share
+                // c_y a^(n - 1 - s) for row s of element e of z[k]; of whole chunks as a lane's
+                // factor times one that all lanes share
                 float lane_weight[KC];
                 if constexpr (full)
 #pragma unroll
                     for (int k = 0; k < KC; ++k)
                         lane_weight[k] =
-                            A.c_y * decay_pow(decay, (float)(C - VEC - STEP * k - VEC * g));
+                            A.c_y * decay_pow(decay, (float)(C - LAST - 1 - STEP * k - 4 * g));
                 auto weight = [&](int k, int e) __attribute__((always_inline)) {
                     if constexpr (full)
                         return lane_weight[k] * shared_weight[e];
                     else
-                        return A.c_y * decay_pow(decay, (float)max(0, n - 1 - (STEP * k +
-                                                                               VEC * g + e)));
+                        return A.c_y * decay_pow(decay, (float)max(0, n - 1 - STEP * k - 4 * g -
+                                                                          row_of(e)));
                 };
                 float z_scale = 1.f;
                 if constexpr (F16) {
