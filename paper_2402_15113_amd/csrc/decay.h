@@ -66,6 +66,25 @@ __device__ __forceinline__ int64_t decay_begin(const DecayArgs &a, int32_t s)
     return a.offsets ? min(max(a.offsets[s], (int64_t)0), a.rows) : s * a.L;
 }
 
+// How many sequences have key(s) <= v, by one wavefront: a 64-ary search.  Keys ascend where
+// the offsets make sense; whatever they hold, it ends and stays in [0, S].
+template <class Key>
+__device__ __forceinline__ int32_t decay_count(int32_t S, int64_t v, Key key)
+{
+    const int lane = threadIdx.x & 63;
+    int32_t lo = 0, hi = S;
+    while (hi - lo > kWave) {
+        const int32_t step = (hi - lo + kWave - 1) / kWave;
+        const int64_t probe = (int64_t)lo + (int64_t)(lane + 1) * step - 1;
+        const int c =
+            __popcll(__ballot(probe < hi && key((int32_t)min(probe, (int64_t)hi - 1)) <= v));
+        lo += c * step;
+        hi = min(lo + step, hi);
+    }
+    const int64_t idx = (int64_t)lo + lane;
+    return lo + __popcll(__ballot(idx < hi && key((int32_t)min(idx, (int64_t)hi - 1)) <= v));
+}
+
 // The rows that sequence `s` has in cell `cell` of C consecutive rows: piece `id` of
 // cdiv(rows, C) + S.  A path through cells and sequences, which goes to the next sequence
 // or to the next cell at every step, meets every pair that has rows in common, and every
@@ -78,21 +97,7 @@ struct DecayPiece {
 };
 __device__ __forceinline__ DecayPiece decay_piece(const DecayArgs &a, int64_t id, int32_t C)
 {
-    // how many sequences begin at step id or before, by one wavefront: a 64-ary search
-    const int lane = threadIdx.x & 63;
-    int32_t lo = 0, hi = a.S;
-    while (hi - lo > kWave) {
-        const int32_t step = (hi - lo + kWave - 1) / kWave;
-        const int64_t probe = (int64_t)lo + (int64_t)(lane + 1) * step - 1;
-        const int c = __popcll(__ballot(probe < hi &&
-                                        decay_begin(a, (int32_t)min(probe, (int64_t)hi - 1)) / C +
-                                                probe <= id));
-        lo += c * step;
-        hi = min(lo + step, hi);
-    }
-    const int64_t idx = (int64_t)lo + lane;
-    lo += __popcll(__ballot(idx < hi && decay_begin(a, (int32_t)min(idx, (int64_t)hi - 1)) / C +
-                                                idx <= id));
+    const int32_t lo = decay_count(a.S, id, [&](int32_t s) { return decay_begin(a, s) / C + s; });
     DecayPiece p{max(lo - 1, 0), -1, 0, 0, {0, 0}};
     if (lo < 1)   // before the first sequence
         return p;
@@ -144,11 +149,15 @@ tgm_status_t decay_f32(const DecayRun &r, int what, hipStream_t s);
 tgm_status_t decay_bf16(const DecayRun &r, int what, hipStream_t s);
 tgm_status_t decay_f16(const DecayRun &r, int what, hipStream_t s);
 
-// a^n, from log2 a: 1 for n = 0, whatever a is.
-__device__ __forceinline__ float decay_log2(float g) { return g * 1.44269504088896340736f; }
+// a^n from log2 a, which is kept finite so that a^0 is 1 also where a is 0.
+__device__ __forceinline__ float decay_log2(float g)
+{
+    const float g2 = g * 1.44269504088896340736f;
+    return g2 < -1e30f ? -1e30f : g2;
+}
 __device__ __forceinline__ float decay_pow(float g2, float n)
 {
-    return n == 0.f ? 1.f : __builtin_amdgcn_exp2f(n * g2);
+    return __builtin_amdgcn_exp2f(n * g2);
 }
 
 }  // namespace tgm

@@ -13,58 +13,64 @@ using namespace tgm;
 namespace {
 
 // The states behind the cells of the sequences that go on, from those of the cells alone: a
-// thread follows four elements of a head's state along a sequence.  Bound by memory.
+// thread follows an element of a head's state along the sequence that begins in its cell and
+// leaves it.  Bound by memory.
 __global__ __launch_bounds__(256) void k_decay_walk(DecayRun run)
 {
     const DecayArgs &A = run.a;
     const int32_t h = blockIdx.y, size = A.p * A.r;
-    const int32_t at = (int32_t)(blockIdx.z * 256 + threadIdx.x) * 4;
+    constexpr int EACH = 4, AHEAD = 8;   // elements of a thread, cells that are loaded together
+    const int32_t at = (int32_t)(blockIdx.z * 256 * EACH + threadIdx.x);
     const float keep = decay_pow(decay_log2(A.decay[h]), (float)run.cell);
-    const int64_t step = A.rev ? -1 : 1;
-    for (int64_t id = blockIdx.x; id < run.ids; id += gridDim.x) {
-        const DecayPiece p = decay_piece_of(run, id);
-        if (p.hi <= p.lo || p.q.e - p.q.b <= run.cell || at >= size)
-            continue;
-        if (A.rev ? p.hi != p.q.e : p.lo != p.q.b)
-            continue;
-        // the sequence's other cells but the last, which leaves no state
-        int64_t left = A.offsets ? (A.rev ? p.cell - p.q.b / run.cell
-                                          : (p.q.e - 1) / run.cell - p.cell)
-                                 : (p.q.e - p.q.b + run.cell - 1) / run.cell - 1;
-        --left;
-        float *s = run.states + (p.cell * A.H + h) * (int64_t)size + at;
-        const int64_t next = step * A.H * size;
-        auto load = [&](const float *from) __attribute__((always_inline)) {
-            f4 v{0.f, 0.f, 0.f, 0.f};
-            if (at + 4 <= size)
-                __builtin_memcpy(&v, from, 16);
-            else
+    const int64_t C = run.cell, cells = A.offsets ? (A.rows + C - 1) / C : run.ids;
+    for (int64_t cell = blockIdx.x; cell < cells; cell += gridDim.x) {
+        int64_t left;   // cells that the sequence goes on to, but for its last
+        if (A.offsets) {
+            // the sequence of the cell's last row (first, if backwards)
+            const int64_t row = A.rev ? cell * C : min((cell + 1) * C, A.rows) - 1;
+            const int32_t n = decay_count(A.S, row, [&](int32_t s) { return decay_begin(A, s); });
+            if (n < 1)
+                continue;
+            const DecaySeq q = decay_seq(A, n - 1);
+            if (q.e - q.b <= C || row < q.b || row >= q.e)
+                continue;
+            const int64_t first = q.b / C, last = (q.e - 1) / C;
+            if (cell != (A.rev ? last : first))
+                continue;
+            left = last - first - 1;
+        } else {
+            const int32_t s = (int32_t)(cell / run.cells);
+            const DecaySeq q = decay_seq(A, s);
+            const int64_t n = (q.e - q.b + C - 1) / C;
+            if (cell - s * run.cells != (A.rev ? n - 1 : 0))
+                continue;
+            left = n - 2;
+        }
+        float *s = run.states + (cell * A.H + h) * (int64_t)size + at;
+        const int64_t next = (A.rev ? -1 : 1) * (int64_t)A.H * size;
+        const int32_t mine = min(EACH, (size - at + 255) / 256);
+        float v[EACH];
 #pragma unroll
-                for (int j = 0; j < 3; ++j)
-                    if (at + j < size)
-                        v[j] = from[j];
-            return v;
-        };
-        f4 v = load(s);
-        constexpr int AHEAD = 8;
+        for (int k = 0; k < EACH; ++k)
+            v[k] = k < mine ? s[256 * k] : 0.f;
         for (; left > 0; left -= AHEAD) {
-            f4 e[AHEAD];
+            float e[AHEAD][EACH];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u)
-                if (u < left)
-                    e[u] = load(s + (u + 1) * next);
+#pragma unroll
+                for (int k = 0; k < EACH; ++k)
+                    if (u < left && k < mine)
+                        e[u][k] = s[(u + 1) * next + 256 * k];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u)
                 if (u < left) {
-                    v = v * keep + e[u];
                     s += next;
-                    if (at + 4 <= size)
-                        __builtin_memcpy(s, &v, 16);
-                    else
 #pragma unroll
-                        for (int j = 0; j < 3; ++j)
-                            if (at + j < size)
-                                s[j] = v[j];
+                    for (int k = 0; k < EACH; ++k)
+                        if (k < mine) {
+                            v[k] = v[k] * keep + e[u][k];
+                            s[256 * k] = v[k];
+                        }
                 }
         }
     }
@@ -161,11 +167,11 @@ uint32_t across(int64_t n, int32_t H) { return (uint32_t)std::min<int64_t>(n, (1
 
 // Rows of a cell: sequences of no more are one workgroup's (a head of them), longer ones are
 // divided, which costs a pass over y and z for the states and two over the states.
-constexpr int kCell = 1024;
-int32_t decay_cell(int64_t rows, int32_t S, int32_t H)
+// As long as 1,024 workgroups or so are left, two rounds of two a CU: us of the whole call with
+// cells of 512, 1,024, 2,048 and 4,096 rows, 262,147 rows of 8 heads of 128 bf16: TUNE.
+int32_t decay_cell(int64_t rows, int32_t H)
 {
-    (void)rows, (void)S, (void)H;
-    return kCell;
+    return (int32_t)std::min<int64_t>(4096, std::max<int64_t>(256, cdiv(rows * H, 1024 * 64) * 64));
 }
 // Cells, and whether any sequence may have more than one.
 struct DecayPlan {
@@ -176,7 +182,7 @@ struct DecayPlan {
 DecayPlan decay_plan(int64_t rows, int32_t S, int32_t H, bool packed)
 {
     DecayPlan p{};
-    p.cell = decay_cell(rows, S, H);
+    p.cell = decay_cell(rows, H);
     if (packed) {
         p.cells = cdiv(rows, p.cell), p.ids = p.cells + S, p.divided = p.cells > 1;
     } else {
@@ -209,8 +215,9 @@ template <class T> tgm_status_t states(const DecayCall &c, const DecayRun &r)
         return TGM_OK;
     TGM_TRY_STATUS(go<T>(r, 0, c.s));
     const int64_t z = cdiv((int64_t)r.a.p * r.a.r, 1024);
+    const int64_t cells = r.a.offsets ? cdiv(r.a.rows, r.cell) : r.ids;
     TGM_LAUNCH(k_decay_walk,
-               dim3(across(r.ids, (int32_t)(r.a.H * z)), (uint32_t)r.a.H, (uint32_t)z), dim3(256),
+               dim3(across(cells, (int32_t)(r.a.H * z)), (uint32_t)r.a.H, (uint32_t)z), dim3(256),
                0, c.s, r);
     return TGM_OK;
 }

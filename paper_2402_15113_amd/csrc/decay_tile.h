@@ -105,8 +105,8 @@ struct DecayRows {
 // A tile on its way from memory: rows past n and columns past the head's width are zeros.
 template <class T, int C, int W, int TH> struct DecayLoad {
     using Tile = DecayTile<T, C, W>;
-    static constexpr int VEC = Tile::VEC, PER = W / VEC, N = C * PER / TH;
-    static_assert(C * PER % TH == 0, "");
+    static constexpr int VEC = Tile::VEC, PER = W / VEC, N = (C * PER + TH - 1) / TH;
+    static constexpr bool EVEN = C * PER % TH == 0;   // else the last threads have none
     d4u v[N];   // of a vector type, which the compiler loads as one (a Pack it takes apart)
 
     __device__ __forceinline__ void load(const DecayRows &r, int width)
@@ -114,7 +114,7 @@ template <class T, int C, int W, int TH> struct DecayLoad {
         // (formed anew: the places of three forms of a load would stay in registers)
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
-        if (r.n == C && width == W) {
+        if (EVEN && r.n == C && width == W) {
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const int e = u * TH + tid;
@@ -185,6 +185,8 @@ template <class T, int C, int W, int TH> struct DecayLoad {
         for (int u = 0; u < N; ++u) {
             const int e = u * TH + (int)threadIdx.x, m = e % PER;
             char *row = t + e / PER * Tile::PITCH;
+            if (!EVEN && e >= C * PER)
+                continue;
             if constexpr (X && sizeof(T) == 2) {
                 // columns 8 m .. + 7 of every 32: h = m / 2, q = 2 (m % 2) and the next
                 typedef unsigned d2u __attribute__((ext_vector_type(2), may_alias));
@@ -223,15 +225,22 @@ __device__ __forceinline__ DecayPlace decay_place(int64_t id, int64_t ids, int32
     return DecayPlace{whole + m / H, (int32_t)(m % H)};
 }
 
-template <class T> struct DecayChunk {
-    static constexpr int C = sizeof(T) == 4 ? 32 : 64;
-};
+// Rows of a chunk: 32, so that two workgroups a CU fit its registers, and 64 for the states alone
+// of few 16-bit columns.
+template <class T, int P, bool OUT> constexpr int decay_chunk()
+{
+    return !OUT && sizeof(T) == 2 && P <= 64 ? 64 : 32;
+}
 
 // OUT: x and the results; without, the pieces' states alone (for sequences that go on).
-template <class T, class O, int P, int R, bool OUT>
-__global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
+// PIPE: two chunks in LDS, the weights of the next one formed beside the results of this one:
+// for sizes of which a CU holds one workgroup, whose wavefronts would all wait for the same
+// thing at the same time.
+template <class T, class O, int P, int R, bool OUT, bool PIPE>
+__global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
 {
-    constexpr int C = DecayChunk<T>::C, NW = R / 16, TH = 64 * NW, TB = C / 16;
+    constexpr int BUFS = PIPE ? 2 : 1;
+    constexpr int C = decay_chunk<T, P, OUT>(), NW = R / 16, TH = 64 * NW, TB = C / 16;
     constexpr int STEP = 64 / (int)sizeof(T);       // elements of a fragment's sum
     constexpr int BLOCKS = STEP / 16;               // blocks of 16 in them
     constexpr int KP = P / STEP, PB = P / 16, VEC = 16 / (int)sizeof(T);
@@ -240,11 +249,11 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
     using TX = DecayTile<T, C, P>;
     using TZ = DecayTile<T, C, R>;
     using TW = DecayTile<T, C, C>;
-    __shared__ __attribute__((aligned(16))) char lx[OUT ? TX::BYTES : 16], ly[TX::BYTES],
-        lz[TZ::BYTES], lw[OUT ? TW::BYTES : 16];
+    __shared__ __attribute__((aligned(16))) char lx_[OUT ? BUFS * TX::BYTES : 16],
+        ly_[BUFS * TX::BYTES], lz_[BUFS * TZ::BYTES], lw_[OUT ? BUFS * TW::BYTES : 16];
     // c_out c_y a^d at C + d for the distances d >= 0 within a chunk, zeros below
     __shared__ float by_distance[OUT ? 2 * C : 1];
-    __shared__ float row_scale[F16 ? C : 1];
+    __shared__ float row_scale[F16 ? BUFS * C : 1];
     const DecayArgs &A = run.a;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int lane_row = lane & 15, lane_group = lane >> 4, r0 = 16 * w;
@@ -317,14 +326,19 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                         (s_col + (uint32_t)min(r, A.p - 1) * s_row));
                     st[pb][j] = r < A.p ? v : 0.f;
                 }
-        float shared_weight[VEC];
+        // of whole chunks as a lane's factor times one that all lanes share
+        float lane_weight[C / STEP], shared_weight[VEC];
+#pragma unroll
+        for (int k = 0; k < C / STEP; ++k)
+            lane_weight[k] =
+                A.c_y * decay_pow(decay, (float)(C - LAST - 1 - STEP * k - 4 * lane_group));
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
             shared_weight[e] = __builtin_bit_cast(
                 float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(
                            int, decay_pow(decay, (float)(LAST - row_of(e))))));
+        __syncthreads();   // no one reads the last piece's chunks any more
         if constexpr (OUT) {
-            __syncthreads();   // no one reads the last piece's any more
             for (int i = threadIdx.x; i < 2 * C; i += TH)
                 by_distance[i] =
                     i < C ? 0.f : A.c_out * A.c_y * decay_pow(decay, (float)(i - C));
@@ -332,76 +346,90 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
         bool some = from != nullptr;     // a state that is not all zeros
         int lag = begins ? A.lag0 : 1;   // its weight at the chunk's first row: a^lag
 
-        // A chunk of n rows, NB blocks of 16 of them (the last may be shorter); NB is known so
-        // that no branch stands between a fragment's read and its product.
-        auto chunk = [&](auto blocks, auto full, int64_t t0, int n, bool more) __attribute__((always_inline)) {
-            constexpr int NB = decltype(blocks)::value, KC = (NB + BLOCKS - 1) / BLOCKS;
-            // formed anew in every chunk: all that follows from a lane's place would stay in
-            // registers, four times over
+        // The weights of a chunk of NB blocks of 16 rows (the last may be shorter); NB is known
+        // so that no branch stands between a fragment's read and its product.  What follows
+        // from a lane's place is formed anew in every chunk: all of it would stay in
+        // registers, several times over.
+        auto scores = [&](auto blocks, int buf) __attribute__((always_inline)) {
+            constexpr int NB = decltype(blocks)::value;
+            const char *lx = lx_ + buf * TX::BYTES, *ly = ly_ + buf * TX::BYTES;
+            char *lw = lw_ + buf * (OUT ? TW::BYTES : 0);
             int i16 = lane_row, g = lane_group;
             asm volatile("" : "+v"(i16), "+v"(g));
-            if constexpr (OUT) {
-                // ---- the weights of rows 16 b .. + 15 and NS blocks of s a wavefront
-                constexpr int NS = F16 || NW < NB * 2 ? NB : NW >= NB * NB ? 1 : NB * NB / NW;
-                constexpr int TASKS = NB * (NB / NS);
-#pragma unroll 1
-                for (int task = w; task < TASKS; task += NW) {
-                    const int b = task % NB, s0 = task / NB * NS;
-                    f4 acc[NS];
+            // rows 16 b .. + 15 and NS blocks of s a wavefront
+            constexpr int NS = F16 || NW < NB * 2 ? NB : NW >= NB * NB ? 1 : NB * NB / NW;
+            constexpr int TASKS = NB * (NB / NS);
+            auto task_of = [&](int task) __attribute__((always_inline)) {
+                const int b = task % NB, s0 = task / NB * NS;
+                f4 acc[NS];
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+                    acc[s] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < KP; ++k) {
+                    const Frag<T> fx = TX::along_x(lx, 16 * b, k, i16, g);
 #pragma unroll
                     for (int s = 0; s < NS; ++s)
-                        acc[s] = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int k = 0; k < KP; ++k) {
-                        const Frag<T> fx = TX::along_x(lx, 16 * b, k, i16, g);
-#pragma unroll
-                        for (int s = 0; s < NS; ++s)
-                            acc[s] = mfma(TX::along(ly, 16 * (s0 + s), k, i16, g), fx, acc[s]);
-                    }
-                    float top = 0.f;
-#pragma unroll
-                    for (int s = 0; s < NS; ++s)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            // row i16 of block b, column 4 g + j of block s0 + s (a product
-                            // with a later row is none, whatever it is)
-                            const int d = 16 * (b - s0 - s) + i16 - (4 * g + j);
-                            acc[s][j] = d >= 0 ? acc[s][j] * by_distance[C + d] : 0.f;
-                            if constexpr (F16)
-                                top = finite(acc[s][j]) ? fmaxf(top, fabsf(acc[s][j])) : top;
-                        }
-                    float scale = 1.f;
-                    if constexpr (F16) {
-                        top = fmaxf(top, __shfl_xor(top, 16));
-                        top = fmaxf(top, __shfl_xor(top, 32));
-                        scale = half_scale(top);
-                        if (g == 0)
-                            row_scale[16 * b + i16] = 1.f / scale;
-                    }
-                    // columns 16 s + 4 g .. + 3, in their order
-                    auto to = [&](int s) __attribute__((always_inline)) {
-                        return reinterpret_cast<Pack<T, 4> *>(__builtin_assume_aligned(
-                            lw + (16 * b + i16) * TW::PITCH +
-                                (F32 ? 16 * s + 4 * g : 32 * (s >> 1) + 8 * g + 4 * (s & 1)) *
-                                    (int)sizeof(T),
-                            4 * sizeof(T)));
-                    };
-#pragma unroll
-                    for (int s = 0; s < NS; ++s) {
-                        Pack<T, 4> q;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            q.v[j] = from_f32<T>(F16 ? acc[s][j] * scale : acc[s][j]);
-                        *to(s0 + s) = q;
-                    }
-                    if constexpr (NB % BLOCKS) {   // the rest of a fragment's sum
-                        Pack<T, 4> q;
-                        __builtin_memset(&q, 0, sizeof(q));
-                        *to(NB) = q;
-                    }
+                        acc[s] = mfma(TX::along(ly, 16 * (s0 + s), k, i16, g), fx, acc[s]);
                 }
-                __syncthreads();
-            }
+                float top = 0.f;
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        // row i16 of block b, column 4 g + j of block s0 + s (a product
+                        // with a later row is none, whatever it is)
+                        const int d = 16 * (b - s0 - s) + i16 - (4 * g + j);
+                        acc[s][j] = d >= 0 ? acc[s][j] * by_distance[C + d] : 0.f;
+                        if constexpr (F16)
+                            top = finite(acc[s][j]) ? fmaxf(top, fabsf(acc[s][j])) : top;
+                    }
+                float scale = 1.f;
+                if constexpr (F16) {
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    scale = half_scale(top);
+                    if (g == 0)
+                        row_scale[buf * C + 16 * b + i16] = 1.f / scale;
+                }
+                // columns 16 s + 4 g .. + 3, in their order
+                auto to = [&](int s) __attribute__((always_inline)) {
+                    return reinterpret_cast<Pack<T, 4> *>(__builtin_assume_aligned(
+                        lw + (16 * b + i16) * TW::PITCH +
+                            (F32 ? 16 * s + 4 * g : 32 * (s >> 1) + 8 * g + 4 * (s & 1)) *
+                                (int)sizeof(T),
+                        4 * sizeof(T)));
+                };
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    Pack<T, 4> q;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        q.v[j] = from_f32<T>(F16 ? acc[s][j] * scale : acc[s][j]);
+                    *to(s0 + s) = q;
+                }
+                if constexpr (NB % BLOCKS) {   // the rest of a fragment's sum
+                    Pack<T, 4> q;
+                    __builtin_memset(&q, 0, sizeof(q));
+                    *to(NB) = q;
+                }
+            };
+            if constexpr (TASKS == NW)
+                task_of(w);
+            else
+#pragma unroll 1
+                for (int task = w; task < TASKS; task += NW)
+                    task_of(task);
+        };
+
+        // The results of n rows and the state behind them.
+        auto rest = [&](auto blocks, auto full, int buf, int64_t t0, int n, bool more)
+            __attribute__((always_inline)) {
+            constexpr int NB = decltype(blocks)::value, KC = (NB + BLOCKS - 1) / BLOCKS;
+            const char *lx = lx_ + buf * TX::BYTES, *ly = ly_ + buf * TX::BYTES;
+            const char *lz = lz_ + buf * TZ::BYTES, *lw = lw_ + buf * (OUT ? TW::BYTES : 0);
+            int i16 = lane_row, g = lane_group;
+            asm volatile("" : "+v"(i16), "+v"(g));
 
             // ---- this wavefront's columns of z
             Frag<T> z[KC];
@@ -459,7 +487,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
                         for (int k = 0; k < KC; ++k)
                             if (BLOCKS * k <= b)
                                 c = mfma(z[k], TW::along(lw, 16 * b, k, i16, g), c);
-                        o[b] = F16 ? o[b] + c * row_scale[16 * b + i16] : c;
+                        o[b] = F16 ? o[b] + c * row_scale[buf * C + 16 * b + i16] : c;
                     }
                     float seen = 0.f;
 #pragma unroll
@@ -533,14 +561,7 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
 
             // ---- the state behind the chunk, where anyone reads it
             if (more || !ends || (OUT && A.last)) {
-                // c_y a^(n - 1 - s) for row s of element e of z[k]; of whole chunks as a lane's
-                // factor times one that all lanes share
-                float lane_weight[KC];
-                if constexpr (full)
-#pragma unroll
-                    for (int k = 0; k < KC; ++k)
-                        lane_weight[k] =
-                            A.c_y * decay_pow(decay, (float)(C - LAST - 1 - STEP * k - 4 * g));
+                // c_y a^(n - 1 - s) for row s of element e of z[k]
                 auto weight = [&](int k, int e) __attribute__((always_inline)) {
                     if constexpr (full)
                         return lane_weight[k] * shared_weight[e];
@@ -606,29 +627,70 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
             lag = 1;
         };
 
-        auto turn = [&](auto blocks, auto full, int64_t t0, int n) __attribute__((always_inline)) {
-            __syncthreads();   // no one reads the last chunk any more
+        auto put = [&](int buf) __attribute__((always_inline)) {
             if constexpr (OUT)
-                vx.template store<true>(lx);
-            vy.template store<false>(ly);
-            vz.template store<false>(lz);
-            __syncthreads();
-            const bool more = t0 + C < rows;
-            if (more)
-                fetch(t0 + C);
-            chunk(blocks, full, t0, n, more);
+                vx.template store<true>(lx_ + buf * TX::BYTES);
+            vy.template store<false>(ly_ + buf * TX::BYTES);
+            vz.template store<false>(lz_ + buf * TZ::BYTES);
+        };
+        using All = std::integral_constant<int, TB>;
+        using Half = std::integral_constant<int, TB / 2 < 1 ? 1 : TB / 2>;
+        using One = std::integral_constant<int, 1>;
+        // by the blocks that n rows have
+        auto by_blocks = [&](int n, auto f) __attribute__((always_inline)) {
+            if (n > C / 2)
+                f(All{});
+            else if (n > 16)
+                f(Half{});
+            else
+                f(One{});
         };
         int64_t t0 = 0;
+        int buf = 0;
+        if (rows > 0)
+            put(0);
+        __syncthreads();
+        if constexpr (PIPE) {
+            if (rows > C) {
+                fetch(C);
+                scores(All{}, 0);
+            } else if (rows > 0) {
+                by_blocks((int)rows, [&](auto nb) { scores(nb, 0); });
+            }
 #pragma unroll 1
-        for (; t0 + C <= rows; t0 += C)
-            turn(std::integral_constant<int, TB>{}, std::true_type{}, t0, C);
-        const int n = (int)(rows - t0);
-        if (n > C / 2)
-            turn(std::integral_constant<int, TB>{}, std::false_type{}, t0, n);
-        else if (n > 16)
-            turn(std::integral_constant<int, TB / 2 < 1 ? 1 : TB / 2>{}, std::false_type{}, t0, n);
-        else if (n > 0)
-            turn(std::integral_constant<int, 1>{}, std::false_type{}, t0, n);
+            for (; t0 + C < rows; t0 += C, buf ^= 1) {
+                put(buf ^ 1);
+                __syncthreads();
+                if (t0 + 2 * C < rows)
+                    fetch(t0 + 2 * C);
+                scores(All{}, buf ^ 1);
+                rest(All{}, std::true_type{}, buf, t0, C, true);
+                __syncthreads();
+            }
+            __syncthreads();
+        } else {
+#pragma unroll 1
+            for (; t0 + C < rows; t0 += C) {
+                fetch(t0 + C);
+                if constexpr (OUT) {
+                    scores(All{}, 0);
+                    __syncthreads();
+                }
+                rest(All{}, std::true_type{}, 0, t0, C, true);
+                __syncthreads();
+                put(0);
+                __syncthreads();
+            }
+            if constexpr (OUT) {
+                if (rows > 0)
+                    by_blocks((int)(rows - t0), [&](auto nb) { scores(nb, 0); });
+                __syncthreads();
+            }
+        }
+        if (rows > 0) {
+            const int n = (int)(rows - t0);
+            by_blocks(n, [&](auto nb) { rest(nb, std::false_type{}, buf, t0, n, false); });
+        }
 
         // ---- the state behind the piece
         float *to = nullptr;
@@ -654,25 +716,26 @@ __global__ __launch_bounds__(4 * R, 2) void k_decay(DecayRun run)
     }
 }
 
-template <class T, class O, int P, int R, bool OUT>
+template <class T, class O, int P, int R, bool OUT, bool PIPE = false>
 tgm_status_t launch_decay(const DecayRun &r, hipStream_t s)
 {
     constexpr int TH = 4 * R;
     const int64_t n = std::min<int64_t>(r.ids * r.a.H, 1 << 22);
     if (n > 0)
-        TGM_LAUNCH((k_decay<T, O, P, R, OUT>), dim3((uint32_t)n), dim3(TH), 0, s, r);
+        TGM_LAUNCH((k_decay<T, O, P, R, OUT, PIPE>), dim3((uint32_t)n), dim3(TH), 0, s, r);
     return TGM_OK;
 }
 template <class T, class O, bool OUT> tgm_status_t pick_decay(const DecayRun &r, hipStream_t s)
 {
     const int p = r.a.p, q = r.a.r;
+    constexpr bool PIPE = false;
     if (p <= 32 && q <= 32)
         return launch_decay<T, O, 32, 32, OUT>(r, s);
     if (p <= 64)
         return q <= 64 ? launch_decay<T, O, 64, 64, OUT>(r, s)
-                       : launch_decay<T, O, 64, 128, OUT>(r, s);
+                       : launch_decay<T, O, 64, 128, OUT, PIPE>(r, s);
     return q <= 64 ? launch_decay<T, O, 128, 64, OUT>(r, s)
-                   : launch_decay<T, O, 128, 128, OUT>(r, s);
+                   : launch_decay<T, O, 128, 128, OUT, PIPE>(r, s);
 }
 // what: 0 states, 1 results of type T, 2 results in fp32
 template <class T> tgm_status_t run_decay(const DecayRun &r, int what, hipStream_t s)
