@@ -115,6 +115,7 @@ struct DecayRun {
     int32_t cell;       // rows of a cell
     int64_t cells;      // of a padded sequence, 0 for packed ones
     int64_t ids;        // pieces
+    bool brief;         // sequences of few rows for the most part
 };
 
 // Piece `id` of the sequences: a sequence of no more than a cell's rows in one piece, which

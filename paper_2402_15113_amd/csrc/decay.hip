@@ -329,6 +329,7 @@ tgm_status_t decay_lengths(DecayCall *c)
     const DecayPlan p = decay_plan(a.rows, a.S, a.H, a.offsets != nullptr);
     c->run.cell = p.cell, c->run.cells = p.padded_cells, c->run.ids = p.ids;
     c->divided = p.divided;
+    c->run.brief = a.rows <= (int64_t)48 * a.S;
     return TGM_OK;
 }
 // Bytes of the cells' states, whichever form the sequences have.

@@ -178,12 +178,21 @@ template <class T, int C, int W, int TH> struct DecayLoad {
             }
         return r;
     }
+    // Waits for the loads, here and not behind stores that follow.
+    __device__ __forceinline__ void arrive() const
+    {
+#pragma unroll
+        for (int u = 0; u < N; ++u)
+            asm volatile("" ::"v"(v[u]));
+    }
     // X: in x's order
     template <bool X> __device__ __forceinline__ void store(char *t) const
     {
+        int tid = threadIdx.x;   // formed anew, as in load
+        asm volatile("" : "+v"(tid));
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            const int e = u * TH + (int)threadIdx.x, m = e % PER;
+            const int e = u * TH + tid, m = e % PER;
             char *row = t + e / PER * Tile::PITCH;
             if (!EVEN && e >= C * PER)
                 continue;
@@ -233,13 +242,9 @@ template <class T, int P, bool OUT> constexpr int decay_chunk()
 }
 
 // OUT: x and the results; without, the pieces' states alone (for sequences that go on).
-// PIPE: two chunks in LDS, the weights of the next one formed beside the results of this one:
-// for sizes of which a CU holds one workgroup, whose wavefronts would all wait for the same
-// thing at the same time.
-template <class T, class O, int P, int R, bool OUT, bool PIPE>
+template <class T, class O, int P, int R, bool OUT>
 __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
 {
-    constexpr int BUFS = PIPE ? 2 : 1;
     constexpr int C = decay_chunk<T, P, OUT>(), NW = R / 16, TH = 64 * NW, TB = C / 16;
     constexpr int STEP = 64 / (int)sizeof(T);       // elements of a fragment's sum
     constexpr int BLOCKS = STEP / 16;               // blocks of 16 in them
@@ -249,11 +254,11 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
     using TX = DecayTile<T, C, P>;
     using TZ = DecayTile<T, C, R>;
     using TW = DecayTile<T, C, C>;
-    __shared__ __attribute__((aligned(16))) char lx_[OUT ? BUFS * TX::BYTES : 16],
-        ly_[BUFS * TX::BYTES], lz_[BUFS * TZ::BYTES], lw_[OUT ? BUFS * TW::BYTES : 16];
+    __shared__ __attribute__((aligned(16))) char lx[OUT ? TX::BYTES : 16], ly[TX::BYTES],
+        lz[TZ::BYTES], lw[OUT ? TW::BYTES : 16];
     // c_out c_y a^d at C + d for the distances d >= 0 within a chunk, zeros below
     __shared__ float by_distance[OUT ? 2 * C : 1];
-    __shared__ float row_scale[F16 ? BUFS * C : 1];
+    __shared__ float row_scale[F16 ? C : 1];
     const DecayArgs &A = run.a;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int lane_row = lane & 15, lane_group = lane >> 4, r0 = 16 * w;
@@ -337,7 +342,7 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
             shared_weight[e] = __builtin_bit_cast(
                 float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(
                            int, decay_pow(decay, (float)(LAST - row_of(e))))));
-        __syncthreads();   // no one reads the last piece's chunks any more
+        lds_barrier();   // no one reads the last piece's chunks any more
         if constexpr (OUT) {
             for (int i = threadIdx.x; i < 2 * C; i += TH)
                 by_distance[i] =
@@ -350,10 +355,8 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
         // so that no branch stands between a fragment's read and its product.  What follows
         // from a lane's place is formed anew in every chunk: all of it would stay in
         // registers, several times over.
-        auto scores = [&](auto blocks, int buf) __attribute__((always_inline)) {
+        auto scores = [&](auto blocks) __attribute__((always_inline)) {
             constexpr int NB = decltype(blocks)::value;
-            const char *lx = lx_ + buf * TX::BYTES, *ly = ly_ + buf * TX::BYTES;
-            char *lw = lw_ + buf * (OUT ? TW::BYTES : 0);
             int i16 = lane_row, g = lane_group;
             asm volatile("" : "+v"(i16), "+v"(g));
             // rows 16 b .. + 15 and NS blocks of s a wavefront
@@ -390,7 +393,7 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
                     top = fmaxf(top, __shfl_xor(top, 32));
                     scale = half_scale(top);
                     if (g == 0)
-                        row_scale[buf * C + 16 * b + i16] = 1.f / scale;
+                        row_scale[16 * b + i16] = 1.f / scale;
                 }
                 // columns 16 s + 4 g .. + 3, in their order
                 auto to = [&](int s) __attribute__((always_inline)) {
@@ -423,11 +426,9 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
         };
 
         // The results of n rows and the state behind them.
-        auto rest = [&](auto blocks, auto full, int buf, int64_t t0, int n, bool more)
+        auto rest = [&](auto blocks, auto full, int64_t t0, int n, bool more)
             __attribute__((always_inline)) {
             constexpr int NB = decltype(blocks)::value, KC = (NB + BLOCKS - 1) / BLOCKS;
-            const char *lx = lx_ + buf * TX::BYTES, *ly = ly_ + buf * TX::BYTES;
-            const char *lz = lz_ + buf * TZ::BYTES, *lw = lw_ + buf * (OUT ? TW::BYTES : 0);
             int i16 = lane_row, g = lane_group;
             asm volatile("" : "+v"(i16), "+v"(g));
 
@@ -487,7 +488,7 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
                         for (int k = 0; k < KC; ++k)
                             if (BLOCKS * k <= b)
                                 c = mfma(z[k], TW::along(lw, 16 * b, k, i16, g), c);
-                        o[b] = F16 ? o[b] + c * row_scale[buf * C + 16 * b + i16] : c;
+                        o[b] = F16 ? o[b] + c * row_scale[16 * b + i16] : c;
                     }
                     float seen = 0.f;
 #pragma unroll
@@ -528,6 +529,9 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
                     for (int k = 0; k < KC; ++k)
                         z[k] = TZ::across(lz, r0, k, i16, g);
                 }
+                // the next chunk is there: its wait would be for these stores too
+                if (more)
+                    vx.arrive(), vy.arrive(), vz.arrive();
                 if (A.out) {
                     const DecayRows to_rows =
                         rows_of(A.out, A.ld_out, (int64_t)h * A.r + r0, sizeof(O), t0, n);
@@ -627,14 +631,14 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
             lag = 1;
         };
 
-        auto put = [&](int buf) __attribute__((always_inline)) {
+        auto put = [&]() __attribute__((always_inline)) {
             if constexpr (OUT)
-                vx.template store<true>(lx_ + buf * TX::BYTES);
-            vy.template store<false>(ly_ + buf * TX::BYTES);
-            vz.template store<false>(lz_ + buf * TZ::BYTES);
+                vx.template store<true>(lx);
+            vy.template store<false>(ly);
+            vz.template store<false>(lz);
         };
         using All = std::integral_constant<int, TB>;
-        using Half = std::integral_constant<int, TB / 2 < 1 ? 1 : TB / 2>;
+        using Half = std::integral_constant<int, TB / 2>;
         using One = std::integral_constant<int, 1>;
         // by the blocks that n rows have
         auto by_blocks = [&](int n, auto f) __attribute__((always_inline)) {
@@ -645,51 +649,30 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
             else
                 f(One{});
         };
-        int64_t t0 = 0;
-        int buf = 0;
         if (rows > 0)
-            put(0);
-        __syncthreads();
-        if constexpr (PIPE) {
-            if (rows > C) {
-                fetch(C);
-                scores(All{}, 0);
-            } else if (rows > 0) {
-                by_blocks((int)rows, [&](auto nb) { scores(nb, 0); });
-            }
+            put();
+        lds_barrier();
+        int64_t t0 = 0;
 #pragma unroll 1
-            for (; t0 + C < rows; t0 += C, buf ^= 1) {
-                put(buf ^ 1);
-                __syncthreads();
-                if (t0 + 2 * C < rows)
-                    fetch(t0 + 2 * C);
-                scores(All{}, buf ^ 1);
-                rest(All{}, std::true_type{}, buf, t0, C, true);
-                __syncthreads();
-            }
-            __syncthreads();
-        } else {
-#pragma unroll 1
-            for (; t0 + C < rows; t0 += C) {
-                fetch(t0 + C);
-                if constexpr (OUT) {
-                    scores(All{}, 0);
-                    __syncthreads();
-                }
-                rest(All{}, std::true_type{}, 0, t0, C, true);
-                __syncthreads();
-                put(0);
-                __syncthreads();
-            }
+        for (; t0 + C < rows; t0 += C) {
+            fetch(t0 + C);
             if constexpr (OUT) {
-                if (rows > 0)
-                    by_blocks((int)(rows - t0), [&](auto nb) { scores(nb, 0); });
-                __syncthreads();
+                scores(All{});
+                lds_barrier();
             }
+            rest(All{}, std::true_type{}, t0, C, true);
+            lds_barrier();
+            put();
+            lds_barrier();
+        }
+        if constexpr (OUT) {
+            if (rows > 0)
+                by_blocks((int)(rows - t0), [&](auto nb) { scores(nb); });
+            lds_barrier();
         }
         if (rows > 0) {
             const int n = (int)(rows - t0);
-            by_blocks(n, [&](auto nb) { rest(nb, std::false_type{}, buf, t0, n, false); });
+            by_blocks(n, [&](auto nb) { rest(nb, std::false_type{}, t0, n, false); });
         }
 
         // ---- the state behind the piece
@@ -716,26 +699,370 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
     }
 }
 
-template <class T, class O, int P, int R, bool OUT, bool PIPE = false>
+// Short sequences: a wavefront has a head of a piece and all columns of its state, chunks of 16
+// rows, and everything in registers.  The weights a^(i - s) (x_i . y_s) of 16 rows are left by
+// the matrix instructions where the next product takes them, so nothing goes through LDS and
+// no wavefront waits for another; a chunk of 10 rows costs a fifth of the instructions that
+// the workgroup of k_decay spends on it.
+template <class T, class O, int P, int R>
+__global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
+{
+    constexpr int STEP = 64 / (int)sizeof(T), BLOCKS = STEP / 16, KP = P / STEP, PB = P / 16;
+    constexpr int CB = R / 16, VEC = 16 / (int)sizeof(T), B = sizeof(T);
+    constexpr bool F16 = TypeCode<T>::code == TGM_F16, F32 = sizeof(T) == 4;
+    constexpr int PARTS = F32 ? 1 : F16 ? 2 : 3;
+    const DecayArgs &A = run.a;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int64_t all = run.ids * A.H;
+    for (int64_t at = (int64_t)blockIdx.x * 4 + w; at < all; at += (int64_t)gridDim.x * 4) {
+        // (formed anew: what follows from it would stay in registers)
+        int i16 = lane & 15, g = lane >> 4;
+        asm volatile("" : "+v"(i16), "+v"(g));
+        const DecayPlace place = decay_place(at, run.ids, A.H);
+        const DecayPiece piece = decay_piece_of(run, place.piece);
+        const int32_t h = place.head;
+        const bool empty = decay_empty_here(run, piece);
+        const int64_t rows = piece.hi - piece.lo;
+        const bool begins = empty || (A.rev ? piece.hi == piece.q.e : piece.lo == piece.q.b);
+        const bool ends = empty || (A.rev ? piece.lo == piece.q.b : piece.hi == piece.q.e);
+        if ((!empty && rows <= 0) || (rows <= 0 && !(ends && A.last)))
+            continue;
+        const float decay = decay_log2(A.decay[h]);
+        const int64_t size = (int64_t)A.p * A.r;
+        const float *from = nullptr;
+        if (begins)
+            from = A.first ? A.first + ((int64_t)piece.s * A.H + h) * size : nullptr;
+        else
+            from = run.states + ((piece.cell + (A.rev ? 1 : -1)) * A.H + h) * size;
+        // Element (r, c) of a state: what all lanes share is the base, so that a lane keeps one
+        // place for each block of columns.
+        const uint32_t s_col = (A.turned ? (uint32_t)A.p : 1u) * 4u;
+        const uint32_t s_row = (A.turned ? 1u : (uint32_t)A.r) * 4u;
+        auto each = [&](auto f) __attribute__((always_inline)) {
+            uint32_t lane_at[CB];
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+                lane_at[cb] = (uint32_t)(16 * cb + i16) * s_col + (uint32_t)(4 * g) * s_row;
+#pragma unroll
+            for (int pb = 0; pb < PB; ++pb) {
+                const bool whole = 16 * pb + 16 <= A.p;
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb)
+                    if (16 * cb + i16 < A.r)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (whole || 16 * pb + 4 * g + j < A.p)
+                                f(pb, cb, j, (size_t)(16 * pb + j) * s_row, lane_at[cb]);
+            }
+        };
+        f4 st[PB][CB];
+#pragma unroll
+        for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+                st[pb][cb] = f4{0.f, 0.f, 0.f, 0.f};
+        if (from)
+            each([&](int pb, int cb, int j, size_t base, uint32_t mine)
+                     __attribute__((always_inline)) {
+                         st[pb][cb][j] = *reinterpret_cast<const float *>(
+                             reinterpret_cast<const char *>(from) + base + mine);
+                     });
+        bool some = from != nullptr;
+        int lag = begins ? A.lag0 : 1;
+
+        auto rows_of = [&](const void *p, int64_t ld, int64_t head, int bytes, int64_t t0, int n)
+            __attribute__((always_inline)) {
+                const int64_t low = A.rev ? piece.hi - t0 - n : piece.lo + t0;
+                return DecayRows{(const char *)p + (low * ld + head) * bytes,
+                                 (uint32_t)(ld * bytes), n, A.rev};
+            };
+        // 4 neighbouring columns from c on of row i16, zeros where there are none
+        auto load4 = [&](const DecayRows &r, int c, int width) __attribute__((always_inline)) {
+            Pack<T, 4> v;
+            __builtin_memset(&v, 0, sizeof(v));
+            if (i16 < r.n && c < width) {
+                const T *p = reinterpret_cast<const T *>(r.base + (r.at(i16) + (uint32_t)(c * B)));
+                if (c + 4 <= width)
+                    v = load_pack<T, 4>(p);
+                else
+#pragma unroll
+                    for (int j = 0; j < 3; ++j)
+                        if (c + j < width)
+                            v.v[j] = p[j];
+            }
+            return v;
+        };
+        // the fragment for step k: 16-bit columns 16 h + 4 g + r of 32, the state's order
+        auto along = [&](const DecayRows &r, int k, int width) __attribute__((always_inline)) {
+            Frag<T> f;
+#pragma unroll
+            for (int u = 0; u < BLOCKS; ++u) {
+                const Pack<T, 4> v = load4(r, STEP * k + 16 * u + 4 * g, width);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    f.v.v[4 * u + j] = v.v[j];
+            }
+            return f;
+        };
+        // the transposed one: column 16 b + i16, rows 4 g .. + 3
+        auto across = [&](const DecayRows &r, int b, int width) __attribute__((always_inline)) {
+            Frag<T> f;
+            const int c = 16 * b + i16;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                f.v.v[e] = from_f32<T>(0.f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = 4 * g + j;
+                const T v = *reinterpret_cast<const T *>(
+                    r.base + (r.at(min(row, r.n - 1)) + (uint32_t)(min(c, width - 1) * B)));
+                f.v.v[j] = row < r.n && c < width ? v : from_f32<T>(0.f);
+            }
+            return f;
+        };
+#pragma unroll 1
+        for (int64_t t0 = 0; t0 < rows; t0 += 16) {
+            const int n = (int)min((int64_t)16, rows - t0);
+            const bool more = t0 + 16 < rows;
+            const DecayRows rx = rows_of(A.x.p, A.x.ld, (int64_t)(h / A.x.share) * A.p, B, t0, n);
+            const DecayRows ry = rows_of(A.y.p, A.y.ld, (int64_t)(h / A.y.share) * A.p, B, t0, n);
+            const DecayRows rz = rows_of(A.z.p, A.z.ld, (int64_t)(h / A.z.share) * A.r, B, t0, n);
+            Frag<T> x[KP], y[KP], z[CB];
+#pragma unroll
+            for (int k = 0; k < KP; ++k)
+                x[k] = along(rx, k, A.p), y[k] = along(ry, k, A.p);
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+                z[cb] = across(rz, cb, A.r);
+            const bool onward = more || !ends || A.last;   // the state behind the chunk is read
+            Frag<T> yt[PB];
+            if (onward)
+#pragma unroll
+                for (int pb = 0; pb < PB; ++pb)
+                    yt[pb] = across(ry, pb, A.p);
+
+            // ---- the weights of row i16 and rows 4 g .. + 3
+            f4 acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < KP; ++k)
+                acc = mfma(y[k], x[k], acc);
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int d = i16 - (4 * g + j);
+                const float f = A.c_out * A.c_y * decay_pow(decay, (float)max(d, 0));
+                acc[j] = d >= 0 ? acc[j] * f : 0.f;
+                if constexpr (F16)
+                    top = finite(acc[j]) ? fmaxf(top, fabsf(acc[j])) : top;
+            }
+            float w_scale = 1.f;
+            if constexpr (F16) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                w_scale = half_scale(top);
+            }
+            Frag<T> wf;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                wf.v.v[e] = from_f32<T>(e >= 4 ? 0.f : F16 ? acc[e % 4] * w_scale : acc[e % 4]);
+
+            // ---- the results
+            f4 o[CB];
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+                o[cb] = f4{0.f, 0.f, 0.f, 0.f};
+            if (some) {
+                float s_scale = 1.f;
+                if constexpr (F16) {
+                    float most = 0.f;
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float v = fabsf(st[pb][cb][j]);
+                                most = v < INFINITY ? fmaxf(most, v) : most;
+                            }
+                    s_scale = half_scale(group_max<64>(most));
+                }
+#pragma unroll
+                for (int k = 0; k < KP; ++k)
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb) {
+                        Frag<T> s;
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            const float v = st[BLOCKS * k + e / 4][cb][e % 4];
+                            s.v.v[e] = from_f32<T>(F16 ? v * s_scale : v);
+                        }
+                        o[cb] = mfma(s, x[k], o[cb]);
+                    }
+                const float f = A.c_out * decay_pow(decay, (float)(i16 + lag));
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb)
+                    o[cb] *= F16 ? f / s_scale : f;
+            }
+            // what is not finite in z counts as zero, and is added where it belongs (k_decay)
+            bool spoilt = false;
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    spoilt |= !finite(to_f32(z[cb].v.v[j]));
+            spoilt = __any(spoilt);
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb) {
+                Frag<T> c = z[cb];
+                if (spoilt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (!finite(to_f32(c.v.v[j])))
+                            c.v.v[j] = from_f32<T>(0.f);
+                if constexpr (F16) {
+                    const f4 p = mfma(c, wf, f4{0.f, 0.f, 0.f, 0.f});
+                    o[cb] += p * (1.f / w_scale);
+                } else {
+                    o[cb] = mfma(c, wf, o[cb]);
+                }
+            }
+            if (spoilt)
+#pragma unroll 1
+                for (int s = 0; s < n; ++s) {
+                    const float w0 = __shfl(acc[0], 16 * (s >> 2) + i16);
+                    const float w1 = __shfl(acc[1], 16 * (s >> 2) + i16);
+                    const float w2 = __shfl(acc[2], 16 * (s >> 2) + i16);
+                    const float w3 = __shfl(acc[3], 16 * (s >> 2) + i16);
+                    const float ws = s & 2 ? (s & 1 ? w3 : w2) : s & 1 ? w1 : w0;
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int c = 16 * cb + 4 * g + j;
+                            if (c < A.r) {
+                                const float v = to_f32(*reinterpret_cast<const T *>(
+                                    rz.base + (rz.at(s) + (uint32_t)(c * B))));
+                                if (!finite(v) && i16 >= s)
+                                    o[cb][j] += v * ws;
+                            }
+                        }
+                }
+            if (A.out && i16 < n) {
+                const DecayRows ro =
+                    rows_of(A.out, A.ld_out, (int64_t)h * A.r, sizeof(O), t0, n);
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    const int c = 16 * cb + 4 * g;
+                    O *to = reinterpret_cast<O *>(const_cast<char *>(ro.base) +
+                                                  (ro.at(i16) + (uint32_t)(c * (int)sizeof(O))));
+                    Pack<O, 4> q;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        q.v[j] = from_f32<O>(o[cb][j]);
+                    if (c + 4 <= A.r)
+                        store_pack(to, q);
+                    else
+#pragma unroll
+                        for (int j = 0; j < 3; ++j)
+                            if (c + j < A.r)
+                                to[j] = q.v[j];
+                }
+            }
+
+            // ---- the state behind the chunk
+            if (onward) {
+                float v[CB][4], most = 0.f, z_scale = 1.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float f = A.c_y * decay_pow(decay, (float)max(0, n - 1 - (4 * g + j)));
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb) {
+                        v[cb][j] = to_f32(z[cb].v.v[j]) * f;
+                        if constexpr (F16)
+                            most = finite(v[cb][j]) ? fmaxf(most, fabsf(v[cb][j])) : most;
+                    }
+                }
+                if constexpr (F16)
+                    z_scale = half_scale(group_max<64>(most));
+                const float whole = decay_pow(decay, (float)(n - 1 + lag));
+                const float keep = F16 ? whole * z_scale : whole;
+                if (some)
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                        for (int cb = 0; cb < CB; ++cb)
+                            st[pb][cb] *= keep;
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    Frag<T> part[PARTS];
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        float u = e >= 4 ? 0.f : F16 ? v[cb][e % 4] * z_scale : v[cb][e % 4];
+#pragma unroll
+                        for (int k = 0; k < PARTS; ++k) {
+                            part[k].v.v[e] = from_f32<T>(u);
+                            if (k + 1 < PARTS)
+                                u -= to_f32(part[k].v.v[e]);
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+                        for (int pb = 0; pb < PB; ++pb)
+                            st[pb][cb] = mfma(yt[pb], part[k], st[pb][cb]);
+                }
+                if constexpr (F16)
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                        for (int cb = 0; cb < CB; ++cb)
+                            st[pb][cb] *= 1.f / z_scale;
+                some = true;
+            }
+            lag = 1;
+        }
+        if (ends && A.last) {
+            char *to = reinterpret_cast<char *>(A.last + ((int64_t)piece.s * A.H + h) * size);
+            const float f = A.lag1 && !empty ? decay_pow(decay, 1.f) : 1.f;
+            each([&](int pb, int cb, int j, size_t base, uint32_t mine)
+                     __attribute__((always_inline)) {
+                         *reinterpret_cast<float *>(to + base + mine) = f * st[pb][cb][j];
+                     });
+        }
+    }
+}
+
+template <class T, class O, int P, int R, bool OUT>
 tgm_status_t launch_decay(const DecayRun &r, hipStream_t s)
 {
     constexpr int TH = 4 * R;
     const int64_t n = std::min<int64_t>(r.ids * r.a.H, 1 << 22);
     if (n > 0)
-        TGM_LAUNCH((k_decay<T, O, P, R, OUT, PIPE>), dim3((uint32_t)n), dim3(TH), 0, s, r);
+        TGM_LAUNCH((k_decay<T, O, P, R, OUT>), dim3((uint32_t)n), dim3(TH), 0, s, r);
+    return TGM_OK;
+}
+template <class T, class O, int P, int R>
+tgm_status_t launch_short(const DecayRun &r, hipStream_t s)
+{
+    const int64_t n = std::min<int64_t>(cdiv(r.ids * r.a.H, 4), 1 << 22);
+    if (n > 0)
+        TGM_LAUNCH((k_decay_short<T, O, P, R>), dim3((uint32_t)n), dim3(256), 0, s, r);
     return TGM_OK;
 }
 template <class T, class O, bool OUT> tgm_status_t pick_decay(const DecayRun &r, hipStream_t s)
 {
     const int p = r.a.p, q = r.a.r;
-    constexpr bool PIPE = false;
+    if constexpr (OUT)
+        if (r.brief && p <= 64 && q <= 64)
+            return p <= 32 && q <= 32 ? launch_short<T, O, 32, 32>(r, s)
+                                      : launch_short<T, O, 64, 64>(r, s);
     if (p <= 32 && q <= 32)
         return launch_decay<T, O, 32, 32, OUT>(r, s);
     if (p <= 64)
         return q <= 64 ? launch_decay<T, O, 64, 64, OUT>(r, s)
-                       : launch_decay<T, O, 64, 128, OUT, PIPE>(r, s);
+                       : launch_decay<T, O, 64, 128, OUT>(r, s);
     return q <= 64 ? launch_decay<T, O, 128, 64, OUT>(r, s)
-                   : launch_decay<T, O, 128, 128, OUT, PIPE>(r, s);
+                   : launch_decay<T, O, 128, 128, OUT>(r, s);
 }
 // what: 0 states, 1 results of type T, 2 results in fp32
 template <class T> tgm_status_t run_decay(const DecayRun &r, int what, hipStream_t s)
