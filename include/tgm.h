@@ -956,7 +956,7 @@ typedef struct {
     int64_t ld_dx, ld_dw;   /* tgm_xent_backward only */
 } tgm_xent_desc;
 /* For tgm_xent (backward 0) and tgm_xent_backward (1: a piece of the classes' gradients in
- * dtype, 256 MB or 1,024 classes, whichever is more, and fp32 sums of dx). */
+ * dtype, up to 512 MB or 1,024 classes, whichever is more, and fp32 sums of dx). */
 tgm_status_t tgm_xent_work_bytes(int32_t rows, int32_t N, int32_t K, int32_t dtype,
                                  int32_t backward, size_t *bytes);
 tgm_status_t tgm_xent(const tgm_xent_desc *d, const void *x, const void *W, const void *bias,

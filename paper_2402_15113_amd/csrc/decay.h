@@ -110,9 +110,10 @@ __device__ __forceinline__ DecayPiece decay_piece(const DecayArgs &a, int64_t id
 
 struct DecayRun {
     DecayArgs a;
-    float *states;      // [cells x H x dk x dv]: the state behind each cell's rows (in the
+    float *states;      // [H x all_cells x dk x dv]: the state behind each cell's rows (in the
                         // recurrence's order) where a sequence goes on to the next cell
     int32_t cell;       // rows of a cell
+    int64_t all_cells;
     int64_t cells;      // of a padded sequence, 0 for packed ones
     int64_t ids;        // pieces
     bool brief;         // sequences of few rows for the most part

@@ -19,10 +19,10 @@ __global__ __launch_bounds__(256) void k_decay_walk(DecayRun run)
 {
     const DecayArgs &A = run.a;
     const int32_t h = blockIdx.y, size = A.p * A.r;
-    constexpr int EACH = 4, AHEAD = 8;   // elements of a thread, cells that are loaded together
+    constexpr int EACH = 2, AHEAD = 8;   // elements of a thread, cells that are loaded together
     const int32_t at = (int32_t)(blockIdx.z * 256 * EACH + threadIdx.x);
     const float keep = decay_pow(decay_log2(A.decay[h]), (float)run.cell);
-    const int64_t C = run.cell, cells = A.offsets ? (A.rows + C - 1) / C : run.ids;
+    const int64_t C = run.cell, cells = run.all_cells;
     for (int64_t cell = blockIdx.x; cell < cells; cell += gridDim.x) {
         int64_t left;   // cells that the sequence goes on to, but for its last
         if (A.offsets) {
@@ -46,32 +46,49 @@ __global__ __launch_bounds__(256) void k_decay_walk(DecayRun run)
                 continue;
             left = n - 2;
         }
-        float *s = run.states + (cell * A.H + h) * (int64_t)size + at;
-        const int64_t next = (A.rev ? -1 : 1) * (int64_t)A.H * size;
-        const int32_t mine = min(EACH, (size - at + 255) / 256);
-        float v[EACH];
+        if (left <= 0)
+            continue;
+        float *s = run.states + (h * run.all_cells + cell) * (int64_t)size;
+        const int64_t next = (A.rev ? -1 : 1) * (int64_t)size;
+        int32_t mine[EACH];   // past the state's end: the last element again, which is not stored
+        float v[EACH], e[2][AHEAD][EACH];
 #pragma unroll
         for (int k = 0; k < EACH; ++k)
-            v[k] = k < mine ? s[256 * k] : 0.f;
-        for (; left > 0; left -= AHEAD) {
-            float e[AHEAD][EACH];
+            mine[k] = min(at + 256 * k, size - 1), v[k] = s[mine[k]];
+        // cells c + 1 .. c + AHEAD, past the last one that one again
+        auto load = [&](float (&to)[AHEAD][EACH], int64_t c) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
+            for (int u = 0; u < AHEAD; ++u) {
+                const float *p = s + min(c + 1 + u, left) * next;
 #pragma unroll
                 for (int k = 0; k < EACH; ++k)
-                    if (u < left && k < mine)
-                        e[u][k] = s[(u + 1) * next + 256 * k];
+                    to[u][k] = p[mine[k]];
+            }
+        };
+        auto follow = [&](const float (&from)[AHEAD][EACH], int64_t c)
+            __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-                if (u < left) {
-                    s += next;
+                for (int u = 0; u < AHEAD; ++u)
+                    if (c + 1 + u <= left) {
+                        float *p = s + (c + 1 + u) * next;
 #pragma unroll
-                    for (int k = 0; k < EACH; ++k)
-                        if (k < mine) {
-                            v[k] = v[k] * keep + e[u][k];
-                            s[256 * k] = v[k];
+                        for (int k = 0; k < EACH; ++k) {
+                            v[k] = v[k] * keep + from[u][k];
+                            if (at + 256 * k < size)
+                                p[mine[k]] = v[k];
                         }
-                }
+                    }
+            };
+        // the next cells' loads go before these cells' stores, which are waited for in order
+        load(e[0], 0);
+        for (int64_t c = 0; c < left; c += 2 * AHEAD) {
+            if (c + AHEAD < left)
+                load(e[1], c + AHEAD);
+            follow(e[0], c);
+            if (c + 2 * AHEAD < left)
+                load(e[0], c + 2 * AHEAD);
+            if (c + AHEAD < left)
+                follow(e[1], c + AHEAD);
         }
     }
 }
@@ -214,10 +231,9 @@ template <class T> tgm_status_t states(const DecayCall &c, const DecayRun &r)
     if (!c.divided)
         return TGM_OK;
     TGM_TRY_STATUS(go<T>(r, 0, c.s));
-    const int64_t z = cdiv((int64_t)r.a.p * r.a.r, 1024);
-    const int64_t cells = r.a.offsets ? cdiv(r.a.rows, r.cell) : r.ids;
+    const int64_t z = cdiv((int64_t)r.a.p * r.a.r, 512);
     TGM_LAUNCH(k_decay_walk,
-               dim3(across(cells, (int32_t)(r.a.H * z)), (uint32_t)r.a.H, (uint32_t)z), dim3(256),
+               dim3(across(r.all_cells, (int32_t)(r.a.H * z)), (uint32_t)r.a.H, (uint32_t)z), dim3(256),
                0, c.s, r);
     return TGM_OK;
 }
@@ -328,6 +344,7 @@ tgm_status_t decay_lengths(DecayCall *c)
     }
     const DecayPlan p = decay_plan(a.rows, a.S, a.H, a.offsets != nullptr);
     c->run.cell = p.cell, c->run.cells = p.padded_cells, c->run.ids = p.ids;
+    c->run.all_cells = p.cells;
     c->divided = p.divided;
     c->run.brief = a.rows <= (int64_t)48 * a.S;
     return TGM_OK;

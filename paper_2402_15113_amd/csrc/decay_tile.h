@@ -114,12 +114,13 @@ template <class T, int C, int W, int TH> struct DecayLoad {
         // (formed anew: the places of three forms of a load would stay in registers)
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
-        if (EVEN && r.n == C && width == W) {
+        if (r.n == C && width == W) {
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const int e = u * TH + tid;
-                v[u] = *reinterpret_cast<const d4u_any *>(
-                    r.base + (r.at(e / PER) + (uint32_t)(e % PER * 16)));
+                if (EVEN || e < C * PER)
+                    v[u] = *reinterpret_cast<const d4u_any *>(
+                        r.base + (r.at(e / PER) + (uint32_t)(e % PER * 16)));
             }
         } else if (width % VEC == 0) {
             // past the ends: the last one again, for zeros
@@ -309,7 +310,7 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
         if (begins)
             from = A.first ? A.first + ((int64_t)piece.s * A.H + h) * size : nullptr;
         else if (OUT)
-            from = run.states + ((piece.cell + (A.rev ? 1 : -1)) * A.H + h) * size;
+            from = run.states + (h * run.all_cells + piece.cell + (A.rev ? 1 : -1)) * size;
         const int col = r0 + lane_row;
         // where element (r, col) of a state lies: 32 bits, formed where it is used (all of
         // them would stay in registers for the next piece)
@@ -679,7 +680,7 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
         float *to = nullptr;
         float f = 1.f;
         if (!OUT)
-            to = run.states + (piece.cell * A.H + h) * size;
+            to = run.states + (h * run.all_cells + piece.cell) * size;
         else if (ends && A.last) {
             to = A.last + ((int64_t)piece.s * A.H + h) * size;
             if (A.lag1 && !empty)
@@ -733,7 +734,7 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
         if (begins)
             from = A.first ? A.first + ((int64_t)piece.s * A.H + h) * size : nullptr;
         else
-            from = run.states + ((piece.cell + (A.rev ? 1 : -1)) * A.H + h) * size;
+            from = run.states + (h * run.all_cells + piece.cell + (A.rev ? 1 : -1)) * size;
         // Element (r, c) of a state: what all lanes share is the base, so that a lane keeps one
         // place for each block of columns.
         const uint32_t s_col = (A.turned ? (uint32_t)A.p : 1u) * 4u;

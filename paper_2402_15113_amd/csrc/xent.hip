@@ -19,7 +19,8 @@ namespace {
 
 constexpr int kMaxDim = 1 << 20;
 
-// lse and loss of 64 rows a workgroup; its 16 wavefronts share the runs of columns.
+// lse and loss of 16 rows a workgroup, 64 threads a row with every 64th run of columns.  Bound by
+// memory and, with few rows, its latency: 514 runs of 8,192 rows (34 MB): TUNE.
 __global__ __launch_bounds__(1024) void k_xent_loss(const f2 *__restrict__ part, int32_t runs,
                                                     int32_t rows, int32_t classes,
                                                     const int32_t *__restrict__ n_rows,
@@ -28,32 +29,32 @@ __global__ __launch_bounds__(1024) void k_xent_loss(const f2 *__restrict__ part,
                                                     float *__restrict__ loss,
                                                     float *__restrict__ lse)
 {
-    __shared__ f2 lds[16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int64_t m = (int64_t)blockIdx.x * 64 + lane;
+    constexpr int ROWS = 16, LANES = 64;
+    __shared__ f2 lds[LANES][ROWS + 1];
+    const int row = threadIdx.x % ROWS, lane = threadIdx.x / ROWS;
+    const int64_t m = (int64_t)blockIdx.x * ROWS + row;
     const bool on = m < rows_in_use(rows, n_rows);
     // the sum relative to the largest so far; -infinity: nothing yet (or no more than NaN)
-    float top = -INFINITY, sum = 0.f;
-    auto join = [&](f2 p) __attribute__((always_inline)) {
-        const float t = fmaxf(top, p.x);
-        if (t == -INFINITY) {
-            sum += p.y;
-        } else {
-            sum = sum * expf(top - t) + p.y * expf(p.x - t);
-            top = t;
-        }
+    auto join = [](f2 a, f2 b) __attribute__((always_inline)) {
+        const float t = fmaxf(a.x, b.x);
+        return t == -INFINITY ? f2{t, a.y + b.y}
+                              : f2{t, a.y * expf(a.x - t) + b.y * expf(b.x - t)};
     };
+    f2 all{-INFINITY, 0.f};
     if (on)
-#pragma unroll 4
-        for (int r = w; r < runs; r += 16)
-            join(part[(int64_t)r * rows + m]);
-    lds[w][lane] = f2{top, sum};
-    __syncthreads();
-    if (w || !on)
+#pragma unroll 8
+        for (int r = lane; r < runs; r += LANES)
+            all = join(all, part[(int64_t)r * rows + m]);
+    lds[lane][row] = all;
+    for (int half = LANES / 2; half; half /= 2) {
+        __syncthreads();
+        if (lane < half)
+            lds[lane][row] = join(lds[lane][row], lds[lane + half][row]);
+    }
+    if (lane || !on)
         return;
-    for (int k = 1; k < 16; ++k)
-        join(lds[k][lane]);
-    const float l = top == -INFINITY ? (sum == 0.f ? top : sum) : top + logf(sum);
+    all = lds[0][row];
+    const float l = all.x == -INFINITY ? (all.y == 0.f ? all.x : all.y) : all.x + logf(all.y);
     const int32_t t = target[m];
     if (lse)
         lse[m] = l;
@@ -150,8 +151,26 @@ __global__ __launch_bounds__(256) void k_xent_dx(const float *__restrict__ sum, 
 }
 
 // ---------------------------------------------------------------- host
-// Classes of a piece: dz of one takes 256 MB or so, of which the caches hold most between
-// the product that writes it and the two that read it.
+// Classes of a piece: dz of one takes 512 MB at most (or 1,024 classes).  Of the multiples of 256
+// up to there the one whose tiles of 256 x 256 fill their rounds of 256 CUs best, in the logits'
+// product (with sums of K) and in dW's (with sums of the rows): 8,192 rows x 65,537 x 2,048
+// bf16 in pieces of 16,384: TUNE.
+int32_t xent_piece(int32_t rows, int32_t N, int32_t K, int64_t most)
+{
+    if (N <= most)
+        return N;
+    const int64_t rt = cdiv(rows, 256), kt = cdiv(K, 256);
+    int64_t best = most;
+    double least = 1e300;
+    for (int64_t n = most; n >= 1024 && 2 * n >= most; n -= 256) {
+        const int64_t tiles = n / 256;
+        const double cost = (double)(cdiv(tiles * rt, 256) * K + cdiv(tiles * kt, 256) * rows) /
+                            (double)n;
+        if (cost < 0.99 * least)
+            least = cost, best = n;
+    }
+    return (int32_t)best;
+}
 struct XentPlan {
     int32_t piece, last;      // classes of every piece, and of the last one
     int64_t pieces, ld_dz;
@@ -162,10 +181,8 @@ XentPlan xent_plan(int32_t rows, int32_t N, int32_t K, int code)
 {
     XentPlan p{};
     const int64_t eb = elem_bytes(code), R = std::max(rows, 1);
-    int64_t most = ((int64_t)256 << 20) / (R * eb) / 256 * 256;
-    most = std::max<int64_t>(most, 1024);
-    p.pieces = cdiv(N, most);
-    p.piece = p.pieces == 1 ? N : (int32_t)(cdiv(cdiv(N, p.pieces), 256) * 256);
+    const int64_t most = std::max<int64_t>(((int64_t)512 << 20) / (R * eb) / 256 * 256, 1024);
+    p.piece = xent_piece(rows, N, K, most);
     p.pieces = cdiv(N, p.piece);
     p.last = (int32_t)(N - (p.pieces - 1) * p.piece);
     p.ld_dz = cdiv(p.piece, 16) * 16;
@@ -233,7 +250,7 @@ tgm_status_t forward(const tgm_xent_desc *d, const int64_t *ld, const void *x, c
     e.at_target = (float *)(work + whole((size_t)xent_parts(d->N) * d->rows * sizeof(f2)));
     XentRuns r;
     TGM_TRY_STATUS(sums_of<T>(p, e, &r));
-    TGM_LAUNCH(k_xent_loss, dim3((uint32_t)cdiv(d->rows, 64)), dim3(1024), 0, s, e.part,
+    TGM_LAUNCH(k_xent_loss, dim3((uint32_t)cdiv(d->rows, 16)), dim3(1024), 0, s, e.part,
                r.columns, d->rows, d->N, n_rows, target, e.at_target, loss, lse);
     return TGM_OK;
 }
