@@ -301,6 +301,7 @@ struct LinearProduct {
     LinearOut o;
     float *work;             // for the partial sums of linear_splits() parts
     hipStream_t s;
+    int32_t parts = 0;       // of the small tile's sums, where not by linear_plan()
 };
 
 // Tiled products (csrc/linear_tile.h); which: 0 forward (P = W, Q = x, results of
@@ -317,6 +318,10 @@ struct LinearPlan {
     int parts;
 };
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, int code);
+inline LinearPlan linear_plan(const LinearProduct &p, int code)
+{
+    return p.parts ? LinearPlan{false, p.parts} : linear_plan(p.o.M, p.o.N, p.K, code);
+}
 // Bytes that the parts of a product need.
 size_t linear_split_bytes(int64_t M, int64_t N, int64_t K, int code);
 

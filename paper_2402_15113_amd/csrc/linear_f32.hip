@@ -8,7 +8,7 @@ namespace {
 // of them the SIMDs come out even (12,000 x 200 outputs of the framework's gates).
 template <bool PK, bool QK, bool DIRECT> tgm_status_t go(const LinearProduct &p)
 {
-    const LinearPlan l = linear_plan(p.o.M, p.o.N, p.K, TGM_F32);
+    const LinearPlan l = linear_plan(p, TGM_F32);
     return l.large ? launch_tile<float, float, PK, QK, 128, 128, 2, 2, DIRECT>(p, l.parts)
                    : launch_tile<float, float, PK, QK, 64, 64, 1, 4, DIRECT>(p, l.parts);
 }

@@ -390,8 +390,10 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
 #pragma unroll 1
         for (int32_t s = quick;;) {
             H h;
+            // (zeros behind the sum's end, whose products would add nothing)
+            const int halves = K - (s0 + s) * BK > BK / 2 ? 2 : 1;
 #pragma unroll 1
-            for (int c = 0; c < 2; ++c) {
+            for (int c = 0; c < halves; ++c) {
 #pragma unroll
                 for (int a = 0; a < NA; ++a)
                     h.read(lds[0], lds[0] + LP::BYTES, wn, wm, c, a);

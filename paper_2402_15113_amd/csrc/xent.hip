@@ -171,6 +171,25 @@ int32_t xent_piece(int32_t rows, int32_t N, int32_t K, int64_t most)
     }
     return (int32_t)best;
 }
+// Parts of the sums of dx and dW in fp32, where the small tile takes them: workgroups by the
+// thousand, five a CU, since a few more than CUs leave most of them idle for half of the time.
+// 12,000 rows x 9,228 x 100, dx (376 tiles): TUNE.
+int32_t xent_split(int64_t M, int64_t N, int64_t K, int code)
+{
+    const LinearPlan l = linear_plan(M, N, K, code);
+    if (code != TGM_F32 || l.large)
+        return l.large ? 0 : l.parts;
+    const int64_t tiles = cdiv(M, 64) * cdiv(N, 64), steps = cdiv(K, 32);
+    return (int32_t)std::max<int64_t>(l.parts, std::min<int64_t>({2048 / tiles, steps / 16, 16}));
+}
+size_t xent_split_bytes(int64_t M, int64_t N, int64_t K, int code)
+{
+    if (M <= 0 || K <= 0)
+        return 0;
+    const int32_t parts = xent_split(M, N, K, code);
+    return parts > 1 ? (size_t)parts * M * ((N + 3) / 4 * 4) * 4
+                     : linear_split_bytes(M, N, K, code);
+}
 struct XentPlan {
     int32_t piece, last;      // classes of every piece, and of the last one
     int64_t pieces, ld_dz;
@@ -191,8 +210,8 @@ XentPlan xent_plan(int32_t rows, int32_t N, int32_t K, int code)
     p.scale = code == TGM_F16 ? whole((size_t)(64 + round_up(K, 4)) * 4) : 0;
     p.db = whole((size_t)xent_db_parts(rows, code) * p.piece * 4);
     for (int32_t n : {p.piece, p.last})
-        p.split = std::max({p.split, linear_split_bytes(rows, K, n, code),
-                            linear_split_bytes(n, K, rows, code)});
+        p.split = std::max({p.split, xent_split_bytes(rows, K, n, code),
+                            xent_split_bytes(n, K, rows, code)});
     p.all = p.dz + p.sum + p.scale + p.db + p.split;
     return p;
 }
@@ -294,6 +313,7 @@ tgm_status_t backward(const tgm_xent_desc *d, const int64_t *ld, const void *x, 
         if (dx && d->rows) {
             LinearProduct p{w, dz, ld[1], plan.ld_dz, n, nullptr, {}, split, s};
             p.o.M = d->rows, p.o.N = d->K, p.o.n_rows = n_rows, p.o.sn = unscale;
+            p.parts = xent_split(d->rows, d->K, n, code);
             if (plan.pieces == 1) {
                 p.o.y = dx, p.o.ld_y = ld[2];
                 TGM_TRY_STATUS(tile_of_type<T>(p, 1, code));
@@ -317,6 +337,7 @@ tgm_status_t backward(const tgm_xent_desc *d, const int64_t *ld, const void *x, 
         if (dW) {
             LinearProduct p{x, dz, ld[0], plan.ld_dz, d->rows, n_rows, {}, split, s};
             p.o.M = n, p.o.N = d->K, p.o.sn = unscale;
+            p.parts = d->rows ? xent_split(n, d->K, d->rows, code) : 0;
             // dz's rows have whole vectors
             p.o.pad_m = round_up(n, 16 / (int)sizeof(T)) - n;
             p.o.y = (T *)dW + n0 * ld[3], p.o.ld_y = ld[3];

@@ -11,9 +11,16 @@
 namespace tgm {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-// exp(d) of a difference from a maximum: its rounding is 2^-24 of d, which is large only
-// where the result is small.
-__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+// exp(z - m).  For results of 32 bits by the difference, whose rounding is 2^-24 of it, large
+// only where the result is small; for 16 bits in one step, with 2^-24 of m besides.
+template <bool FULL> struct ExpFrom {
+    float m;   // times -log2(e) unless FULL
+    __device__ __forceinline__ explicit ExpFrom(float from) : m(FULL ? from : -from * kLog2e) {}
+    __device__ __forceinline__ float operator()(float z) const
+    {
+        return __builtin_amdgcn_exp2f(FULL ? (z - m) * kLog2e : fmaf(z, kLog2e, m));
+    }
+};
 
 struct XentSums {
     using Args = XentArgs;
@@ -55,12 +62,13 @@ struct XentSums {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
             const float ref = fabsf(top) == INFINITY ? 0.f : top;
+            const ExpFrom<sizeof(T) == 4> exp_of(ref);
             float sum = 0.f;
 #pragma unroll
             for (int a = 0; a < NA; ++a)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    sum += exp_of(acc[a][b][j] - ref);
+                    sum += exp_of(acc[a][b][j]);
             sum += __shfl_xor(sum, 16);
             sum += __shfl_xor(sum, 32);
             if (m < M) {
@@ -89,10 +97,11 @@ struct XentGrad {
                                                   f4 (&acc)[NA][MA], int32_t n0, int32_t m0,
                                                   int32_t, int32_t run, int32_t M)
     {
-        const int lane = threadIdx.x & 63, n1 = n0 + 4 * (lane >> 4);
+        const int lane = threadIdx.x & 63, g = lane >> 4, n1 = n0 + 4 * g;
         const float scale = e.scale ? e.scale[0] : 1.f;
         float l[MA], dl[MA];
         int32_t at[MA];
+        bool here = false;   // a row's target is among the columns
 #pragma unroll
         for (int b = 0; b < MA; ++b) {
             const int32_t m = min(m0 + 16 * b + (lane & 15), M - 1), t = e.target[m];
@@ -101,45 +110,104 @@ struct XentGrad {
             // rows that have no part in the loss
             if (t < 0 || t >= e.classes || l[b] == -INFINITY || m0 + 16 * b + (lane & 15) >= M)
                 at[b] = INT32_MIN;
+            here |= at[b] >= 0 && at[b] < 16 * NA;
         }
+        if (e.bias)
 #pragma unroll
-        for (int a = 0; a < NA; ++a) {
-            const int32_t n = n1 + 16 * a;
-            f4 bias{0.f, 0.f, 0.f, 0.f}, sum{0.f, 0.f, 0.f, 0.f};
-            if (e.bias)
+            for (int a = 0; a < NA; ++a)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float bias = to_f32(((const T *)e.bias)[min(n1 + 16 * a + j, o.N - 1)]);
+#pragma unroll
+                    for (int b = 0; b < MA; ++b)
+                        acc[a][b][j] += bias;
+                }
+        // softmax, less 1 at the target where one is here (few tiles have any)
+#pragma unroll
+        for (int b = 0; b < MA; ++b) {
+            const ExpFrom<sizeof(T) == 4> exp_of(l[b]);
+#pragma unroll
+            for (int a = 0; a < NA; ++a)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    bias[j] = to_f32(((const T *)e.bias)[min(n + j, o.N - 1)]);
+                    acc[a][b][j] = exp_of(acc[a][b][j]);
+        }
+        if (__any(here))
 #pragma unroll
-            for (int b = 0; b < MA; ++b) {
-                const int32_t m = m0 + 16 * b + (lane & 15);
-                Pack<T, 4> out;
+            for (int b = 0; b < MA; ++b)
+#pragma unroll
+                for (int a = 0; a < NA; ++a)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        acc[a][b][j] -= at[b] == 16 * a + j ? 1.f : 0.f;
+#pragma unroll
+        for (int b = 0; b < MA; ++b)
+#pragma unroll
+            for (int a = 0; a < NA; ++a)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[a][b][j] = at[b] == INT32_MIN ? 0.f : acc[a][b][j] * dl[b];
+        if (e.db)
+#pragma unroll
+            for (int a = 0; a < NA; ++a)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    float d = exp_of(acc[a][b][j] + bias[j] - l[b]);
-                    d = (at[b] == 16 * a + j ? d - 1.f : d) * dl[b];
-                    d = at[b] == INT32_MIN ? 0.f : d;
-                    sum[j] += d;
-                    out.v[j] = from_f32<T>(d);
-                }
-                T *dz = (T *)e.dz + (int64_t)m * e.ld_dz + n;
-                if (m < M) {
-                    if (n + 4 <= o.N)
-                        store_pack(dz, out);
-                    else
+                    float sum = 0.f;
 #pragma unroll
-                        for (int j = 0; j < 3; ++j)
-                            if (n + j < o.N)
-                                dz[j] = out.v[j];
+                    for (int b = 0; b < MA; ++b)
+                        sum += acc[a][b][j];
+                    sum = row16_sum(sum);
+                    if ((lane & 15) == 0 && n1 + 16 * a + j < o.N)
+                        e.db[(int64_t)run * o.N + n1 + 16 * a + j] = sum;
+                }
+        T *dz = (T *)e.dz + (int64_t)(m0 + (lane & 15)) * e.ld_dz + n0;
+        const bool whole = n0 + 16 * NA <= o.N;
+#pragma unroll
+        for (int b = 0; b < MA; ++b, dz += 16 * e.ld_dz) {
+            if (m0 + 16 * b + (lane & 15) >= M)
+                continue;
+            if constexpr (sizeof(T) == 2 && NA % 2 == 0) {
+                // A lane has 4 columns of a block and of the next one.  Of two neighbouring
+                // groups of lanes the first takes 8 of the one and the second 8 of the other:
+                // stores of 16 bytes, 64 a row.
+                if (whole) {
+#pragma unroll
+                    for (int a = 0; a < NA; a += 2) {
+                        uint32_t x[2], y[2];
+                        Pack<T, 4> p, q;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            p.v[j] = from_f32<T>(acc[a][b][j]),
+                            q.v[j] = from_f32<T>(acc[a + 1][b][j]);
+                        __builtin_memcpy(x, &p, 8);
+                        __builtin_memcpy(y, &q, 8);
+                        uint32_t out[4];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const auto r = __builtin_amdgcn_permlane16_swap(x[k], y[k], false,
+                                                                            false);
+                            out[k] = r[0], out[2 + k] = r[1];
+                        }
+                        __builtin_memcpy(dz + 16 * (a + (g & 1)) + 8 * (g >> 1), out, 16);
+                    }
+                    continue;
                 }
             }
-            if (e.db)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float s = row16_sum(sum[j]);
-                    if ((lane & 15) == 0 && n + j < o.N)
-                        e.db[(int64_t)run * o.N + n + j] = s;
-                }
+            for (int a = 0; a < NA; ++a) {
+                const int32_t n = n1 + 16 * a;
+                Pack<T, 4> out;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    out.v[j] = from_f32<T>(acc[a][b][j]);
+                if (n + 4 <= o.N)
+                    store_pack(dz + 16 * a + 4 * g, out);
+                else
+#pragma unroll
+                    for (int j = 0; j < 3; ++j)
+                        if (n + j < o.N)
+                            dz[16 * a + 4 * g + j] = out.v[j];
+            }
         }
     }
 };
@@ -184,7 +252,7 @@ tgm_status_t xent_product(const LinearProduct &p, const XentArgs &e, XentRuns *r
 // dx of 16-bit operands with fp32 results.
 template <class T> tgm_status_t xent_dx(const LinearProduct &p)
 {
-    const LinearPlan l = linear_plan(p.o.M, p.o.N, p.K, TypeCode<T>::code);
+    const LinearPlan l = linear_plan(p, TypeCode<T>::code);
     if (!direct<T, false, true>(p))
         return launch_tile<T, float, false, true, 128, 128, 2, 2, false>(p, l.parts);
     return l.large ? launch_tile<T, float, false, true, 256, 256, 2, 4, true>(p, l.parts)
