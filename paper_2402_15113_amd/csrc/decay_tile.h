@@ -700,11 +700,19 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
     }
 }
 
-// Short sequences: a wavefront has a head of a piece and all columns of its state, chunks of 16
-// rows, and everything in registers.  The weights a^(i - s) (x_i . y_s) of 16 rows are left by
-// the matrix instructions where the next product takes them, so nothing goes through LDS and
-// no wavefront waits for another; a chunk of 10 rows costs a fifth of the instructions that
-// the workgroup of k_decay spends on it.
+// Between a wavefront's lanes' writes to LDS and its other lanes' reads of them, and back: LDS
+// serves a wavefront in order, only the compiler has to be kept from moving them.
+__device__ __forceinline__ void exchange()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
+// Short sequences: a wavefront has a head of a piece and all columns of its state, and chunks of
+// 16 rows.  The weights a^(i - s) (x_i . y_s) of 16 rows are left by the matrix instructions where
+// the next product takes them; LDS, of which every wavefront has its own, turns y and z; no
+// wavefront waits for another.
 template <class T, class O, int P, int R>
 __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
 {
@@ -712,8 +720,12 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
     constexpr int CB = R / 16, VEC = 16 / (int)sizeof(T), B = sizeof(T);
     constexpr bool F16 = TypeCode<T>::code == TGM_F16, F32 = sizeof(T) == 4;
     constexpr int PARTS = F32 ? 1 : F16 ? 2 : 3;
+    using TY = DecayTile<T, 16, P>;
+    using TZ = DecayTile<T, 16, R>;
+    __shared__ __attribute__((aligned(16))) char lds[4][TY::BYTES + TZ::BYTES];
     const DecayArgs &A = run.a;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    char *ly = lds[w], *lz = ly + TY::BYTES;
     const int64_t all = run.ids * A.H;
     for (int64_t at = (int64_t)blockIdx.x * 4 + w; at < all; at += (int64_t)gridDim.x * 4) {
         // (formed anew: what follows from it would stay in registers)
@@ -762,12 +774,30 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb)
                 st[pb][cb] = f4{0.f, 0.f, 0.f, 0.f};
-        if (from)
+        if (from && A.turned) {   // 4 rows of a column are neighbours
+#pragma unroll
+            for (int pb = 0; pb < PB; ++pb)
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb) {
+                    const int r = 16 * pb + 4 * g, c = 16 * cb + i16;
+                    const float *p = from + (c * A.p + r);
+                    if (c < A.r && r + 4 <= A.p)
+                        __builtin_memcpy(&st[pb][cb], p, 16);
+                    else if (c < A.r)
+#pragma unroll
+                        for (int j = 0; j < 3; ++j)
+                            if (r + j < A.p)
+                                st[pb][cb][j] = p[j];
+                }
+        } else if (from)
             each([&](int pb, int cb, int j, size_t base, uint32_t mine)
                      __attribute__((always_inline)) {
                          st[pb][cb][j] = *reinterpret_cast<const float *>(
                              reinterpret_cast<const char *>(from) + base + mine);
                      });
+        // Where one chunk is all, the state behind it is formed with rows and columns exchanged:
+        // then a lane has 4 columns of a row, which are neighbours in memory.
+        const bool exchanged = rows > 0 && rows <= 16 && ends && A.last && !A.turned;
         bool some = from != nullptr;
         int lag = begins ? A.lag0 : 1;
 
@@ -777,47 +807,48 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
                 return DecayRows{(const char *)p + (low * ld + head) * bytes,
                                  (uint32_t)(ld * bytes), n, A.rev};
             };
-        // 4 neighbouring columns from c on of row i16, zeros where there are none
-        auto load4 = [&](const DecayRows &r, int c, int width) __attribute__((always_inline)) {
-            Pack<T, 4> v;
+        // columns 16 b + 4 g .. + 3 of row i16 for all b, zeros where there are none
+        auto fetch = [&](auto &v, const DecayRows &r, int width) __attribute__((always_inline)) {
+            constexpr int N = sizeof(v) / sizeof(v[0]);
             __builtin_memset(&v, 0, sizeof(v));
-            if (i16 < r.n && c < width) {
-                const T *p = reinterpret_cast<const T *>(r.base + (r.at(i16) + (uint32_t)(c * B)));
-                if (c + 4 <= width)
-                    v = load_pack<T, 4>(p);
-                else
+            if (i16 < r.n) {
+                const char *row = r.base + (r.at(i16) + (uint32_t)(4 * g * B));
 #pragma unroll
-                    for (int j = 0; j < 3; ++j)
-                        if (c + j < width)
-                            v.v[j] = p[j];
+                for (int b = 0; b < N; ++b) {
+                    const T *from4 = reinterpret_cast<const T *>(row + 16 * b * B);
+                    if (16 * b + 16 <= width || 16 * b + 4 * g + 4 <= width)
+                        v[b] = load_pack<T, 4>(from4);
+                    else
+#pragma unroll
+                        for (int j = 0; j < 3; ++j)
+                            if (16 * b + 4 * g + j < width)
+                                v[b].v[j] = from4[j];
+                }
             }
-            return v;
         };
         // the fragment for step k: 16-bit columns 16 h + 4 g + r of 32, the state's order
-        auto along = [&](const DecayRows &r, int k, int width) __attribute__((always_inline)) {
+        auto along = [&](const Pack<T, 4> *v, int k) __attribute__((always_inline)) {
             Frag<T> f;
-#pragma unroll
-            for (int u = 0; u < BLOCKS; ++u) {
-                const Pack<T, 4> v = load4(r, STEP * k + 16 * u + 4 * g, width);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    f.v.v[4 * u + j] = v.v[j];
-            }
-            return f;
-        };
-        // the transposed one: column 16 b + i16, rows 4 g .. + 3
-        auto across = [&](const DecayRows &r, int b, int width) __attribute__((always_inline)) {
-            Frag<T> f;
-            const int c = 16 * b + i16;
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                f.v.v[e] = from_f32<T>(0.f);
+                f.v.v[e] = v[BLOCKS * k + e / 4].v[e % 4];
+            return f;
+        };
+        // the transposed one: column c0 + i16, rows 4 g .. + 3
+        auto across = [&](const char *t, int pitch, int c0) __attribute__((always_inline)) {
+            Frag<T> f;
+            __builtin_memset(&f, 0, sizeof(f));
+            if constexpr (F32) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int row = 4 * g + j;
-                const T v = *reinterpret_cast<const T *>(
-                    r.base + (r.at(min(row, r.n - 1)) + (uint32_t)(min(c, width - 1) * B)));
-                f.v.v[j] = row < r.n && c < width ? v : from_f32<T>(0.f);
+                for (int j = 0; j < 4; ++j)
+                    f.v.v[j] =
+                        *reinterpret_cast<const T *>(t + (4 * g + j) * pitch + 4 * (c0 + i16));
+            } else {
+                typedef __attribute__((address_space(3))) d4s *lds_d4;
+                const char *p = t + (4 * g + (i16 >> 2)) * pitch + 2 * (c0 + 4 * (i16 & 3));
+                const d4s v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_d4)(__attribute__((address_space(3))) void *)const_cast<char *>(p));
+                __builtin_memcpy(&f.v, &v, sizeof(v));
             }
             return f;
         };
@@ -828,25 +859,34 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
             const DecayRows rx = rows_of(A.x.p, A.x.ld, (int64_t)(h / A.x.share) * A.p, B, t0, n);
             const DecayRows ry = rows_of(A.y.p, A.y.ld, (int64_t)(h / A.y.share) * A.p, B, t0, n);
             const DecayRows rz = rows_of(A.z.p, A.z.ld, (int64_t)(h / A.z.share) * A.r, B, t0, n);
-            Frag<T> x[KP], y[KP], z[CB];
+            Pack<T, 4> px[PB], py[PB], pz[CB];
+            fetch(px, rx, A.p);
+            fetch(py, ry, A.p);
+            fetch(pz, rz, A.r);
+            exchange();   // (no lane reads the last chunk any more)
+#pragma unroll
+            for (int b = 0; b < PB; ++b)
+                *reinterpret_cast<Pack<T, 4> *>(__builtin_assume_aligned(
+                    ly + i16 * TY::PITCH + (16 * b + 4 * g) * B, 4 * B)) = py[b];
+#pragma unroll
+            for (int b = 0; b < CB; ++b)
+                *reinterpret_cast<Pack<T, 4> *>(__builtin_assume_aligned(
+                    lz + i16 * TZ::PITCH + (16 * b + 4 * g) * B, 4 * B)) = pz[b];
+            exchange();
+            Frag<T> x[KP], z[CB];
 #pragma unroll
             for (int k = 0; k < KP; ++k)
-                x[k] = along(rx, k, A.p), y[k] = along(ry, k, A.p);
+                x[k] = along(px, k);
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb)
-                z[cb] = across(rz, cb, A.r);
+                z[cb] = across(lz, TZ::PITCH, 16 * cb);
             const bool onward = more || !ends || A.last;   // the state behind the chunk is read
-            Frag<T> yt[PB];
-            if (onward)
-#pragma unroll
-                for (int pb = 0; pb < PB; ++pb)
-                    yt[pb] = across(ry, pb, A.p);
 
             // ---- the weights of row i16 and rows 4 g .. + 3
             f4 acc{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int k = 0; k < KP; ++k)
-                acc = mfma(y[k], x[k], acc);
+                acc = mfma(along(py, k), x[k], acc);
             float top = 0.f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -941,8 +981,8 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
                         for (int j = 0; j < 4; ++j) {
                             const int c = 16 * cb + 4 * g + j;
                             if (c < A.r) {
-                                const float v = to_f32(*reinterpret_cast<const T *>(
-                                    rz.base + (rz.at(s) + (uint32_t)(c * B))));
+                                const float v = to_f32(
+                                    *reinterpret_cast<const T *>(lz + s * TZ::PITCH + c * B));
                                 if (!finite(v) && i16 >= s)
                                     o[cb][j] += v * ws;
                             }
@@ -987,12 +1027,19 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
                     z_scale = half_scale(group_max<64>(most));
                 const float whole = decay_pow(decay, (float)(n - 1 + lag));
                 const float keep = F16 ? whole * z_scale : whole;
-                if (some)
+                Frag<T> yt[PB];
+#pragma unroll
+                for (int pb = 0; pb < PB; ++pb)
+                    yt[pb] = across(ly, TY::PITCH, 16 * pb);
+                if (some && !exchanged)
 #pragma unroll
                     for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
                         for (int cb = 0; cb < CB; ++cb)
                             st[pb][cb] *= keep;
+                float *to = A.last + ((int64_t)piece.s * A.H + h) * size;
+                const float f =
+                    (A.lag1 ? decay_pow(decay, 1.f) : 1.f) * (F16 ? 1.f / z_scale : 1.f);
 #pragma unroll
                 for (int cb = 0; cb < CB; ++cb) {
                     Frag<T> part[PARTS];
@@ -1006,23 +1053,65 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
                                 u -= to_f32(part[k].v.v[e]);
                         }
                     }
+                    if (!exchanged) {
+#pragma unroll
+                        for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+                            for (int pb = 0; pb < PB; ++pb)
+                                st[pb][cb] = mfma(yt[pb], part[k], st[pb][cb]);
+                        continue;
+                    }
+                    const int c = 16 * cb + 4 * g;
+                    f4 r[PB];
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb) {
+                        const int row = 16 * pb + i16;
+                        r[pb] = f4{0.f, 0.f, 0.f, 0.f};
+                        if (from && row < A.p) {
+                            const float *p = from + (row * A.r + c);
+                            if (c + 4 <= A.r)
+                                __builtin_memcpy(&r[pb], p, 16);
+                            else
+#pragma unroll
+                                for (int j = 0; j < 3; ++j)
+                                    if (c + j < A.r)
+                                        r[pb][j] = p[j];
+                            r[pb] *= keep;
+                        }
+                    }
 #pragma unroll
                     for (int k = 0; k < PARTS; ++k)
 #pragma unroll
                         for (int pb = 0; pb < PB; ++pb)
-                            st[pb][cb] = mfma(yt[pb], part[k], st[pb][cb]);
+                            r[pb] = mfma(part[k], yt[pb], r[pb]);
+#pragma unroll
+                    for (int pb = 0; pb < PB; ++pb) {
+                        const int row = 16 * pb + i16;
+                        float *p = to + (row * A.r + c);
+                        r[pb] *= f;
+                        if (row < A.p) {
+                            if (c + 4 <= A.r)
+                                __builtin_memcpy(p, &r[pb], 16);
+                            else
+#pragma unroll
+                                for (int j = 0; j < 3; ++j)
+                                    if (c + j < A.r)
+                                        p[j] = r[pb][j];
+                        }
+                    }
                 }
                 if constexpr (F16)
+                    if (!exchanged)
 #pragma unroll
-                    for (int pb = 0; pb < PB; ++pb)
+                        for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
-                        for (int cb = 0; cb < CB; ++cb)
-                            st[pb][cb] *= 1.f / z_scale;
+                            for (int cb = 0; cb < CB; ++cb)
+                                st[pb][cb] *= 1.f / z_scale;
                 some = true;
             }
             lag = 1;
         }
-        if (ends && A.last) {
+        if (ends && A.last && !exchanged) {
             char *to = reinterpret_cast<char *>(A.last + ((int64_t)piece.s * A.H + h) * size);
             const float f = A.lag1 && !empty ? decay_pow(decay, 1.f) : 1.f;
             each([&](int pb, int cb, int j, size_t base, uint32_t mine)
