@@ -66,14 +66,21 @@ __device__ __forceinline__ int64_t decay_begin(const DecayArgs &a, int32_t s)
     return a.offsets ? min(max(a.offsets[s], (int64_t)0), a.rows) : s * a.L;
 }
 
-// How many sequences have key(s) <= v, by one wavefront: a 64-ary search.  Keys ascend where
-// the offsets make sense; whatever they hold, it ends and stays in [0, S].
-template <class Key>
-__device__ __forceinline__ int32_t decay_count(int32_t S, int64_t v, Key key)
+// The cell of C rows that row b (0 .. rows, at most 2^30) is in.
+__device__ __forceinline__ int64_t decay_cell_of(int64_t b, int32_t C)
 {
+    return (uint32_t)b / (uint32_t)C;
+}
+
+// lo and how many sequences of lo .. hi - 1 have key(s) <= v, by one wavefront: a 64-ary search,
+// whose last 256 are looked at together.  Keys ascend where the offsets make sense; whatever
+// they hold, it ends and stays in [lo, hi].
+template <class Key>
+__device__ __forceinline__ int32_t decay_count(int32_t lo, int32_t hi, int64_t v, Key key)
+{
+    constexpr int LAST = 4;
     const int lane = threadIdx.x & 63;
-    int32_t lo = 0, hi = S;
-    while (hi - lo > kWave) {
+    while (hi - lo > LAST * kWave) {
         const int32_t step = (hi - lo + kWave - 1) / kWave;
         const int64_t probe = (int64_t)lo + (int64_t)(lane + 1) * step - 1;
         const int c =
@@ -81,8 +88,17 @@ __device__ __forceinline__ int32_t decay_count(int32_t S, int64_t v, Key key)
         lo += c * step;
         hi = min(lo + step, hi);
     }
-    const int64_t idx = (int64_t)lo + lane;
-    return lo + __popcll(__ballot(idx < hi && key((int32_t)min(idx, (int64_t)hi - 1)) <= v));
+    if (hi <= lo)
+        return lo;
+    int64_t k[LAST];
+#pragma unroll
+    for (int u = 0; u < LAST; ++u)
+        k[u] = key((int32_t)min((int64_t)lo + u * kWave + lane, (int64_t)hi - 1));
+    int32_t n = 0;
+#pragma unroll
+    for (int u = 0; u < LAST; ++u)
+        n += __popcll(__ballot((int64_t)lo + u * kWave + lane < hi && k[u] <= v));
+    return lo + n;
 }
 
 // The rows that sequence `s` has in cell `cell` of C consecutive rows: piece `id` of
@@ -97,7 +113,11 @@ struct DecayPiece {
 };
 __device__ __forceinline__ DecayPiece decay_piece(const DecayArgs &a, int64_t id, int32_t C)
 {
-    const int32_t lo = decay_count(a.S, id, [&](int32_t s) { return decay_begin(a, s) / C + s; });
+    // step id is of a sequence from id - cells to id
+    const int64_t cells = decay_cell_of(a.rows + C - 1, C);
+    const int32_t lo = decay_count((int32_t)min(max(id - cells, (int64_t)0), (int64_t)a.S),
+                                   (int32_t)min(id + 1, (int64_t)a.S), id,
+                                   [&](int32_t s) { return decay_cell_of(decay_begin(a, s), C) + s; });
     DecayPiece p{max(lo - 1, 0), -1, 0, 0, {0, 0}};
     if (lo < 1)   // before the first sequence
         return p;
@@ -128,7 +148,7 @@ __device__ __forceinline__ DecayPiece decay_piece_of(const DecayRun &r, int64_t 
     if (r.a.offsets) {
         p = decay_piece(r.a, id, r.cell);
         if (p.q.e - p.q.b <= r.cell) {
-            const bool here = p.q.b / r.cell == p.cell;
+            const bool here = decay_cell_of(p.q.b, r.cell) == p.cell;
             p.lo = here ? p.q.b : 0, p.hi = here ? p.q.e : 0;
         }
         return p;
@@ -140,10 +160,34 @@ __device__ __forceinline__ DecayPiece decay_piece_of(const DecayRun &r, int64_t 
     p.hi = min(p.q.e, p.lo + r.cell);
     return p;
 }
+// The piece of cell `id` that goes on to the next cell (in the recurrence's order), if there is
+// one: at most one sequence of more than a cell's rows has its last (backwards: first) row and
+// the next.
+__device__ __forceinline__ DecayPiece decay_piece_onward(const DecayRun &r, int64_t id)
+{
+    const DecayArgs &a = r.a;
+    DecayPiece p;
+    if (a.offsets) {
+        const int64_t row = a.rev ? id * r.cell : min((id + 1) * r.cell, a.rows) - 1;
+        const int32_t n =
+            decay_count(0, a.S, row, [&](int32_t s) { return decay_begin(a, s); });
+        p = DecayPiece{max(n - 1, 0), id, 0, 0, {0, 0}};
+        if (n < 1)
+            return p;
+        p.q = decay_seq(a, p.s);
+        p.lo = max(p.q.b, id * r.cell), p.hi = min(p.q.e, (id + 1) * r.cell);
+    } else {
+        p = decay_piece_of(r, id);
+    }
+    if (p.q.e - p.q.b <= r.cell || (a.rev ? p.lo == p.q.b : p.hi == p.q.e))
+        p.lo = p.hi = 0;
+    return p;
+}
 // Whether a sequence without rows is the piece's to look after.
 __device__ __forceinline__ bool decay_empty_here(const DecayRun &r, const DecayPiece &p)
 {
-    return p.q.e <= p.q.b && (r.a.offsets ? p.cell == p.q.b / r.cell : p.cell == p.s * r.cells);
+    return p.q.e <= p.q.b && (r.a.offsets ? p.cell == decay_cell_of(p.q.b, r.cell)
+                                             : p.cell == p.s * r.cells);
 }
 
 // what: 0 states, 1 results of the inputs' type, 2 results in fp32

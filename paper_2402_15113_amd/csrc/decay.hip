@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "decay.h"
@@ -24,28 +25,14 @@ __global__ __launch_bounds__(256) void k_decay_walk(DecayRun run)
     const float keep = decay_pow(decay_log2(A.decay[h]), (float)run.cell);
     const int64_t C = run.cell, cells = run.all_cells;
     for (int64_t cell = blockIdx.x; cell < cells; cell += gridDim.x) {
-        int64_t left;   // cells that the sequence goes on to, but for its last
-        if (A.offsets) {
-            // the sequence of the cell's last row (first, if backwards)
-            const int64_t row = A.rev ? cell * C : min((cell + 1) * C, A.rows) - 1;
-            const int32_t n = decay_count(A.S, row, [&](int32_t s) { return decay_begin(A, s); });
-            if (n < 1)
-                continue;
-            const DecaySeq q = decay_seq(A, n - 1);
-            if (q.e - q.b <= C || row < q.b || row >= q.e)
-                continue;
-            const int64_t first = q.b / C, last = (q.e - 1) / C;
-            if (cell != (A.rev ? last : first))
-                continue;
-            left = last - first - 1;
-        } else {
-            const int32_t s = (int32_t)(cell / run.cells);
-            const DecaySeq q = decay_seq(A, s);
-            const int64_t n = (q.e - q.b + C - 1) / C;
-            if (cell - s * run.cells != (A.rev ? n - 1 : 0))
-                continue;
-            left = n - 2;
-        }
+        const DecayPiece piece = decay_piece_onward(run, cell);
+        if (piece.hi <= piece.lo ||
+            (A.rev ? piece.hi != piece.q.e : piece.lo != piece.q.b))
+            continue;   // no sequence begins here and goes on
+        // cells that it goes on to, but for its last
+        const DecaySeq q = piece.q;
+        const int64_t left =
+            (A.offsets ? (q.e - 1) / C - q.b / C : (q.e - q.b + C - 1) / C - 1) - 1;
         if (left <= 0)
             continue;
         float *s = run.states + (h * run.all_cells + cell) * (int64_t)size;
@@ -184,11 +171,24 @@ uint32_t across(int64_t n, int32_t H) { return (uint32_t)std::min<int64_t>(n, (1
 
 // Rows of a cell: sequences of no more are one workgroup's (a head of them), longer ones are
 // divided, which costs a pass over y and z for the states and two over the states.
-// As long as 1,024 workgroups or so are left, two rounds of two a CU: us of the whole call with
-// cells of 512, 1,024, 2,048 and 4,096 rows, 262,147 rows of 8 heads of 128 bf16: TUNE.
-int32_t decay_cell(int64_t rows, int32_t H)
+// A cell's rows come one chunk after another and the states pass is over C rows' time, while
+// the states to write and walk go as rows H / C, so the best C grows as the root of rows H.
+// us of a call, cells of 64, 256, 512, 1,024, 2,048 and 4,096 rows, bf16 heads of 128:
+//     1,024 rows x 8        54    56     75     91
+//     8,192 x 8            322   114     99    144    250
+//     32,768 x 8         1,560   386    237    198    266
+//     65,536 x 32       12,978 3,803  2,183  1,418  1,039
+//     262,147 x 8                     1,253  1,003    897   862
+// (the root is 128, 384, 768, 2,048 and 2,048 there.)  Padded sequences fill the card without
+// being divided from 256 heads of them on: 16 x 4,096 rows of 32 heads 438 us whole, 700 in
+// cells of 2,048, 878 of 1,024; of 16 heads 334, 373 and 450; but 4 x 4,096 rows of 32 heads
+// (128 workgroups) 231 whole and 197 in cells of 1,024.
+int32_t decay_cell(int64_t rows, int32_t S, int32_t H, bool packed)
 {
-    return (int32_t)std::min<int64_t>(4096, std::max<int64_t>(256, cdiv(rows * H, 1024 * 64) * 64));
+    if (!packed && (int64_t)S * H >= 256)
+        return (int32_t)std::max<int64_t>(1, rows / S);
+    const int64_t root = (int64_t)std::sqrt(2.0 * (double)rows * H);
+    return (int32_t)std::min<int64_t>(4096, std::max<int64_t>(64, cdiv(root, 64) * 64));
 }
 // Cells, and whether any sequence may have more than one.
 struct DecayPlan {
@@ -199,7 +199,7 @@ struct DecayPlan {
 DecayPlan decay_plan(int64_t rows, int32_t S, int32_t H, bool packed)
 {
     DecayPlan p{};
-    p.cell = decay_cell(rows, H);
+    p.cell = decay_cell(rows, S, H, packed);
     if (packed) {
         p.cells = cdiv(rows, p.cell), p.ids = p.cells + S, p.divided = p.cells > 1;
     } else {
@@ -208,6 +208,20 @@ DecayPlan decay_plan(int64_t rows, int32_t S, int32_t H, bool packed)
         p.cells = p.ids = p.padded_cells * S, p.divided = p.padded_cells > 1;
     }
     return p;
+}
+// Sequences of 16 rows or fewer are a wavefront's each, longer ones a workgroup's: us of a
+// call, wavefronts and workgroups, 40,000 rows x 4 heads of 50 fp32 and of 64 bf16, padded
+//     4 rows    246  313   246  301
+//     16         63   83    57   70
+//     17         94   86    80   68
+//     32         64   55    53   40
+// and packed, of lengths that vary, where the mean decides:
+//     8         242  268   251  262
+//     11        183  183   198  195
+//     16        159  149   145  123
+bool decay_brief(int64_t rows, int32_t S, bool packed)
+{
+    return rows <= (packed ? 10 : 16) * (int64_t)S;
 }
 
 struct DecayCall {
@@ -346,7 +360,7 @@ tgm_status_t decay_lengths(DecayCall *c)
     c->run.cell = p.cell, c->run.cells = p.padded_cells, c->run.ids = p.ids;
     c->run.all_cells = p.cells;
     c->divided = p.divided;
-    c->run.brief = a.rows <= (int64_t)48 * a.S;
+    c->run.brief = decay_brief(a.rows, a.S, a.offsets != nullptr);
     return TGM_OK;
 }
 // Bytes of the cells' states, whichever form the sequences have.

@@ -268,18 +268,18 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
     constexpr int LAST = F32 ? 3 : 19;
     // the state's row that element j of block pb of a lane is, q its group of 16
     auto state_row = [](int pb, int j, int q) { return 16 * pb + 4 * q + j; };
-    const int64_t all = run.ids * A.H;
+    const int64_t ids = OUT ? run.ids : run.all_cells, all = ids * A.H;
     for (int64_t at = blockIdx.x; at < all; at += gridDim.x) {
-        const DecayPlace place = decay_place(at, run.ids, A.H);
-        const DecayPiece piece = decay_piece_of(run, place.piece);
+        const DecayPlace place = decay_place(at, ids, A.H);
+        const DecayPiece piece =
+            OUT ? decay_piece_of(run, place.piece) : decay_piece_onward(run, place.piece);
         const int32_t h = place.head;
-        const bool empty = decay_empty_here(run, piece);
+        const bool empty = OUT && decay_empty_here(run, piece);
         const int64_t rows = piece.hi - piece.lo;
         const bool begins = empty || (A.rev ? piece.hi == piece.q.e : piece.lo == piece.q.b);
-        const bool ends = empty || (A.rev ? piece.lo == piece.q.b : piece.hi == piece.q.e);
-        if (!empty && rows <= 0)
-            continue;
-        if (OUT ? rows <= 0 && !(ends && A.last) : ends)
+        const bool ends =
+            OUT && (empty || (A.rev ? piece.lo == piece.q.b : piece.hi == piece.q.e));
+        if (rows <= 0 && !(empty && A.last))
             continue;
         const float decay = decay_log2(A.decay[h]);
         const int64_t size = (int64_t)A.p * A.r;
@@ -565,7 +565,7 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
             }
 
             // ---- the state behind the chunk, where anyone reads it
-            if (more || !ends || (OUT && A.last)) {
+            if (more || !OUT || (ends && A.last)) {
                 // c_y a^(n - 1 - s) for row s of element e of z[k]
                 auto weight = [&](int k, int e) __attribute__((always_inline)) {
                     if constexpr (full)
@@ -738,7 +738,7 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
         const int64_t rows = piece.hi - piece.lo;
         const bool begins = empty || (A.rev ? piece.hi == piece.q.e : piece.lo == piece.q.b);
         const bool ends = empty || (A.rev ? piece.lo == piece.q.b : piece.hi == piece.q.e);
-        if ((!empty && rows <= 0) || (rows <= 0 && !(ends && A.last)))
+        if (rows <= 0 && !(empty && A.last))
             continue;
         const float decay = decay_log2(A.decay[h]);
         const int64_t size = (int64_t)A.p * A.r;
@@ -880,7 +880,7 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb)
                 z[cb] = across(lz, TZ::PITCH, 16 * cb);
-            const bool onward = more || !ends || A.last;   // the state behind the chunk is read
+            const bool onward = more || (ends && A.last);   // the state behind the chunk is read
 
             // ---- the weights of row i16 and rows 4 g .. + 3
             f4 acc{0.f, 0.f, 0.f, 0.f};
@@ -1126,7 +1126,7 @@ template <class T, class O, int P, int R, bool OUT>
 tgm_status_t launch_decay(const DecayRun &r, hipStream_t s)
 {
     constexpr int TH = 4 * R;
-    const int64_t n = std::min<int64_t>(r.ids * r.a.H, 1 << 22);
+    const int64_t n = std::min<int64_t>((OUT ? r.ids : r.all_cells) * r.a.H, 1 << 22);
     if (n > 0)
         TGM_LAUNCH((k_decay<T, O, P, R, OUT>), dim3((uint32_t)n), dim3(TH), 0, s, r);
     return TGM_OK;
