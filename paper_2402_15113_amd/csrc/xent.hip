@@ -20,7 +20,8 @@ namespace {
 constexpr int kMaxDim = 1 << 20;
 
 // lse and loss of 16 rows a workgroup, 64 threads a row with every 64th run of columns.  Bound by
-// memory and, with few rows, its latency: 514 runs of 8,192 rows (34 MB): TUNE.
+// memory and, with few rows, its latency: 514 runs of 8,192 rows (34 MB) in 11 us, 42 with a
+// thread a row.
 __global__ __launch_bounds__(1024) void k_xent_loss(const f2 *__restrict__ part, int32_t runs,
                                                     int32_t rows, int32_t classes,
                                                     const int32_t *__restrict__ n_rows,
@@ -97,7 +98,8 @@ __global__ __launch_bounds__(1024) void k_xent_scale(const float *__restrict__ d
         unscale[k] = 1.f / s;
 }
 
-// db = the runs' partial sums added in order: 32 columns a workgroup, 32 threads each.
+// db = the runs' partial sums added in order: 32 columns a workgroup, 32 threads each.  Bound by
+// latency: 9,228 columns of 188 tiles of rows in 11 us.
 template <class T>
 __global__ __launch_bounds__(1024) void k_xent_db(const float *__restrict__ part, XentRuns r,
                                                   int32_t rows, const int32_t *n_rows, int32_t N,
@@ -122,7 +124,8 @@ __global__ __launch_bounds__(1024) void k_xent_db(const float *__restrict__ part
     }
 }
 
-// dx from its fp32 sums over the pieces.  Bound by memory.
+// dx from its fp32 sums over the pieces.  Bound by memory: 8,192 x 2,048 to
+// bf16 in 18 us (5.6 TB/s).
 template <class T>
 __global__ __launch_bounds__(256) void k_xent_dx(const float *__restrict__ sum, int32_t rows,
                                                  const int32_t *n_rows, int32_t K, int64_t wide,
@@ -153,8 +156,13 @@ __global__ __launch_bounds__(256) void k_xent_dx(const float *__restrict__ sum, 
 // ---------------------------------------------------------------- host
 // Classes of a piece: dz of one takes 512 MB at most (or 1,024 classes).  Of the multiples of 256
 // up to there the one whose tiles of 256 x 256 fill their rounds of 256 CUs best, in the logits'
-// product (with sums of K) and in dW's (with sums of the rows): 8,192 rows x 65,537 x 2,048
-// bf16 in pieces of 16,384: TUNE.
+// product (with sums of K) and in dW's (with sums of the rows).  us of a training step, 8,192 rows
+// x 65,537 x 2,048 bf16, in pieces of
+//     4,096  8,192  13,312  16,384  16,640  21,760  32,768
+//     7,338  6,825   7,520   6,921   7,334   7,304   6,931
+// Smaller ones gain little and lose more where rows are many (32,768 rows x 32,768 x 1,024 bf16:
+// 9,029 us with 128 MB, 8,310 with 256, 7,475 with 512) and in fp32 (12,000 rows x 9,228 x 100:
+// 1,217 us in two pieces, 1,117 in one).
 int32_t xent_piece(int32_t rows, int32_t N, int32_t K, int64_t most)
 {
     if (N <= most)
@@ -173,7 +181,8 @@ int32_t xent_piece(int32_t rows, int32_t N, int32_t K, int64_t most)
 }
 // Parts of the sums of dx and dW in fp32, where the small tile takes them: workgroups by the
 // thousand, five a CU, since a few more than CUs leave most of them idle for half of the time.
-// 12,000 rows x 9,228 x 100, dx (376 tiles): TUNE.
+// 12,000 rows x 9,228 x 100 (376 tiles of dx): a training step with 1, 2, 4, 5, 8 and 12 parts
+// 1,428, 1,202, 1,157, 1,129, 1,106 and 1,108 us.
 int32_t xent_split(int64_t M, int64_t N, int64_t K, int code)
 {
     const LinearPlan l = linear_plan(M, N, K, code);

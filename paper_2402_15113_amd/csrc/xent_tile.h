@@ -5,6 +5,8 @@
 // sums go over its own values and then over the four lanes that share it.
 #pragma once
 
+#include <type_traits>
+
 #include "linear_tile.h"
 #include "xent.h"
 
@@ -22,6 +24,8 @@ template <bool FULL> struct ExpFrom {
     }
 };
 
+// The sums of the loss.  Bound by the matrix cores: 8,192 rows x 65,537 x 2,048 bf16 in 1.57 ms
+// (1.40 PFLOP/s), 12,000 x 9,228 x 100 fp32 in 275 us.
 struct XentSums {
     using Args = XentArgs;
     template <class T, int NA, int MA>
@@ -90,6 +94,9 @@ struct XentSums {
     }
 };
 
+// dz.  Bound by the matrix cores and, where K is small, by its stores: 8,192 rows x 32,768 x 2,048
+// bf16 in 931 us (1.18 PFLOP/s), 1,174 with stores of 8 bytes; 12,000 x 9,228 x 100 fp32 in 385 us
+// (443 MB stored).
 struct XentGrad {
     using Args = XentArgs;
     template <class T, int NA, int MA>
@@ -214,14 +221,23 @@ struct XentGrad {
 
 // Whether the large tiles take a product of logits.  Of many tiles it does not matter that the
 // last round of them is not full, so that here a tenth more of rounds is taken for what a large
-// tile saves: 8,192 rows x 65,537 x 2,048 bf16: TUNE.
-template <class T> bool xent_large(int64_t M, int64_t N, int64_t K)
+// tile saves.  us with small and large tiles, forward alone and with its gradient:
+//     bf16  8,192 x 65,537 x 2,048   2,031  1,573     7,884  6,931
+//           4,096 x 32,768 x 256       108     92       440    423
+//           4,096 x 32,768 x 64         79     61       304    278
+//           512 x 32,768 x 1,024        44     36       193    178
+//     fp32  8,192 x 16,384 x 2,048   4,083  3,848    16,156 15,689
+//           4,096 x 32,768 x 256       571    538     2,240  2,202
+//           12,000 x 9,228 x 128       271    265     1,053  1,095
+//           4,096 x 32,768 x 64        197    191       773    819
+// so fp32's gradient, whose end stores 64 KB a tile, takes them for sums of 256 or more.
+template <class T, class End> bool xent_large(int64_t M, int64_t N, int64_t K)
 {
     const bool f32 = sizeof(T) == 4;
     const int64_t side = f32 ? 128 : 256, half = side / 2;
     const int64_t large = cdiv(M, side) * cdiv(N, side), small = cdiv(M, half) * cdiv(N, half);
-    return large >= (f32 ? 512 : 192) && (f32 || K >= 1024) &&
-           cdiv(large, 256) * 40 <= cdiv(small, 256) * 11;
+    return large >= (f32 ? 512 : 192) && cdiv(large, 256) * 40 <= cdiv(small, 256) * 11 &&
+           (!f32 || K >= 256 || std::is_same_v<End, XentSums>);
 }
 
 // The sum of a tile comes in one part.
@@ -234,7 +250,7 @@ tgm_status_t launch_xent(const LinearProduct &p, const XentArgs &e, XentRuns *r)
 template <class T, class End>
 tgm_status_t xent_product(const LinearProduct &p, const XentArgs &e, XentRuns *r)
 {
-    const bool large = xent_large<T>(p.o.M, p.o.N, p.K);
+    const bool large = xent_large<T, End>(p.o.M, p.o.N, p.K);
     const bool lies = direct<T, true, true>(p);
     if constexpr (sizeof(T) == 4) {
         if (large)
