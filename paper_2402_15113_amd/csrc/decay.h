@@ -111,21 +111,39 @@ struct DecayPiece {
     int64_t cell, lo, hi;   // hi <= lo: no rows
     DecaySeq q;
 };
-__device__ __forceinline__ DecayPiece decay_piece(const DecayArgs &a, int64_t id, int32_t C)
+// The sequences that may be a step's, from .lo to .hi - 1, and a sequence's first step.
+struct DecaySteps {
+    int32_t lo, hi;
+};
+__device__ __forceinline__ DecaySteps decay_steps(const DecayArgs &a, int64_t id, int32_t C)
 {
-    // step id is of a sequence from id - cells to id
     const int64_t cells = decay_cell_of(a.rows + C - 1, C);
-    const int32_t lo = decay_count((int32_t)min(max(id - cells, (int64_t)0), (int64_t)a.S),
-                                   (int32_t)min(id + 1, (int64_t)a.S), id,
-                                   [&](int32_t s) { return decay_cell_of(decay_begin(a, s), C) + s; });
-    DecayPiece p{max(lo - 1, 0), -1, 0, 0, {0, 0}};
-    if (lo < 1)   // before the first sequence
+    return DecaySteps{(int32_t)min(max(id - cells, (int64_t)0), (int64_t)a.S),
+                      (int32_t)min(id + 1, (int64_t)a.S)};
+}
+__device__ __forceinline__ int64_t decay_step_of(const DecayArgs &a, int32_t s, int32_t C)
+{
+    return decay_cell_of(decay_begin(a, s), C) + s;
+}
+// n sequences have begun at step id or before.
+__device__ __forceinline__ DecayPiece decay_piece(const DecayArgs &a, int64_t id, int32_t C,
+                                                  int32_t n)
+{
+    DecayPiece p{max(n - 1, 0), -1, 0, 0, {0, 0}};
+    if (n < 1)   // before the first sequence
         return p;
     p.cell = id - p.s;
     p.q = decay_seq(a, p.s);
     p.lo = max(p.q.b, p.cell * C);
     p.hi = min(p.q.e, (p.cell + 1) * C);
     return p;
+}
+__device__ __forceinline__ DecayPiece decay_piece(const DecayArgs &a, int64_t id, int32_t C)
+{
+    const DecaySteps t = decay_steps(a, id, C);
+    return decay_piece(a, id, C, decay_count(t.lo, t.hi, id, [&](int32_t s) {
+                           return decay_step_of(a, s, C);
+                       }));
 }
 
 struct DecayRun {
@@ -136,29 +154,49 @@ struct DecayRun {
     int64_t all_cells;
     int64_t cells;      // of a padded sequence, 0 for packed ones
     int64_t ids;        // pieces
+    const int32_t *order;   // [ids], the pieces with rows, long ones first, then -1; may be null
     bool brief;         // sequences of few rows for the most part
 };
 
 // Piece `id` of the sequences: a sequence of no more than a cell's rows in one piece, which
 // the cell that it begins in has; longer ones by cells.  Packed sequences share a grid of
 // cells, padded ones have cells of their own.
-__device__ __forceinline__ DecayPiece decay_piece_of(const DecayRun &r, int64_t id)
+__device__ __forceinline__ DecayPiece decay_whole(const DecayRun &r, DecayPiece p)
+{
+    if (p.q.e - p.q.b <= r.cell) {
+        const bool here = decay_cell_of(p.q.b, r.cell) == p.cell;
+        p.lo = here ? p.q.b : 0, p.hi = here ? p.q.e : 0;
+    }
+    return p;
+}
+__device__ __forceinline__ DecayPiece decay_padded_piece(const DecayRun &r, int64_t id)
 {
     DecayPiece p;
-    if (r.a.offsets) {
-        p = decay_piece(r.a, id, r.cell);
-        if (p.q.e - p.q.b <= r.cell) {
-            const bool here = decay_cell_of(p.q.b, r.cell) == p.cell;
-            p.lo = here ? p.q.b : 0, p.hi = here ? p.q.e : 0;
-        }
-        return p;
-    }
     p.s = (int32_t)(id / r.cells), p.cell = id;
     p.q = decay_seq(r.a, p.s);
     const int64_t k = id - p.s * r.cells;
     p.lo = p.q.b + k * r.cell;
     p.hi = min(p.q.e, p.lo + r.cell);
     return p;
+}
+__device__ __forceinline__ DecayPiece decay_piece_of(const DecayRun &r, int64_t id)
+{
+    return r.a.offsets ? decay_whole(r, decay_piece(r.a, id, r.cell)) : decay_padded_piece(r, id);
+}
+// The same by a single thread.
+__device__ __forceinline__ DecayPiece decay_piece_alone(const DecayRun &r, int64_t id)
+{
+    if (!r.a.offsets)
+        return decay_padded_piece(r, id);
+    DecaySteps t = decay_steps(r.a, id, r.cell);
+    while (t.lo < t.hi) {
+        const int32_t mid = t.lo + (t.hi - t.lo) / 2;
+        if (decay_step_of(r.a, mid, r.cell) <= id)
+            t.lo = mid + 1;
+        else
+            t.hi = mid;
+    }
+    return decay_whole(r, decay_piece(r.a, id, r.cell, t.lo));
 }
 // The piece of cell `id` that goes on to the next cell (in the recurrence's order), if there is
 // one: at most one sequence of more than a cell's rows has its last (backwards: first) row and
@@ -177,7 +215,7 @@ __device__ __forceinline__ DecayPiece decay_piece_onward(const DecayRun &r, int6
         p.q = decay_seq(a, p.s);
         p.lo = max(p.q.b, id * r.cell), p.hi = min(p.q.e, (id + 1) * r.cell);
     } else {
-        p = decay_piece_of(r, id);
+        p = decay_padded_piece(r, id);
     }
     if (p.q.e - p.q.b <= r.cell || (a.rev ? p.lo == p.q.b : p.hi == p.q.e))
         p.lo = p.hi = 0;

@@ -82,6 +82,47 @@ __global__ __launch_bounds__(256) void k_decay_walk(DecayRun run)
     }
 }
 
+// The pieces that have something to do, those of most rows first (by 32nds of a cell), for the
+// results pass of sequences of uneven lengths: otherwise a long piece that begins last is waited
+// for.  The order within a length is any, and no result depends on it.  One workgroup; bound by
+// the latency of each thread's searches: 109 pieces 5 us.
+constexpr int kOrderThreads = 1024, kOrderEach = 8, kOrderLengths = 33;
+__global__ __launch_bounds__(kOrderThreads) void k_decay_order(DecayRun run, int32_t *order)
+{
+    __shared__ int32_t place[kOrderLengths + 1];
+    if (threadIdx.x <= kOrderLengths)
+        place[threadIdx.x] = 0;
+    __syncthreads();
+    int length[kOrderEach];   // 0: the longest; the last: nothing to do
+#pragma unroll
+    for (int u = 0; u < kOrderEach; ++u) {
+        const int64_t id = u * kOrderThreads + threadIdx.x;
+        if (id >= run.ids)
+            continue;
+        const DecayPiece p = decay_piece_alone(run, id);
+        const int64_t rows = p.hi - p.lo;
+        length[u] = rows > 0 ? kOrderLengths - 2 - (int)(32 * (rows - 1) / run.cell)
+                    : decay_empty_here(run, p) ? kOrderLengths - 1
+                                               : kOrderLengths;
+        atomicAdd(&place[length[u]], 1);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int i = 0, n = 0; i <= kOrderLengths; ++i) {
+            const int32_t here = place[i];
+            place[i] = n;
+            n += here;
+        }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kOrderEach; ++u) {
+        const int64_t id = u * kOrderThreads + threadIdx.x;
+        if (id < run.ids)
+            order[atomicAdd(&place[length[u]], 1)] =
+                length[u] == kOrderLengths ? -1 : (int32_t)id;
+    }
+}
+
 // The gradient of a head of k or v that several heads of q share: theirs added in order, for
 // the rows of sequences.  Bound by memory: 65,536 rows of 16 heads of 128, four to one (604 MB):
 // 155 us, 3.9 TB/s; of 64, 78 us.
@@ -229,11 +270,44 @@ bool decay_brief(int64_t rows, int32_t S, bool packed)
     return rows <= (packed ? 10 : 16) * (int64_t)S;
 }
 
+// Bytes of the pieces' order, 0 where none is made: it costs a launch and pays where pieces of a
+// chunk's rows and more come after each other on a CU.  us of a training step with and without:
+//     65,536 rows of 16 heads of 64 and 128 bf16 in 64 sequences   1,506  1,797
+//     65,536 x 4 heads of 64 in 200, fp32                            557    707
+//     20,000 x 8 heads of 64 in 12, fp32                             419    484
+//     40,000 x 4 heads of 64 in 833 (48 rows), fp32                  314    372
+//     in 1,250 (32)                                                  373    388
+//     in 1,666 (24)                                                  435    435
+//     in 2,500 (16)                                                  554    539
+size_t order_bytes(const DecayPlan &p, int64_t rows, int32_t S, int32_t H)
+{
+    return S > 1 && p.ids <= kOrderThreads * kOrderEach && p.ids * H > 256 && rows >= 32 * p.ids
+               ? (size_t)p.ids * 4
+               : 0;
+}
+
+// Bytes of the cells' states and of the pieces' order, whichever form the sequences have.
+struct DecayBytes {
+    size_t states, order;
+};
+DecayBytes decay_bytes(int64_t rows, int32_t S, int32_t H, int32_t d_k, int32_t d_v)
+{
+    size_t cells = 0, order = 0;
+    auto add = [&](const DecayPlan &p) {
+        cells = std::max(cells, p.divided ? (size_t)p.cells : 0);
+        order = std::max(order, order_bytes(p, rows, S, H));
+    };
+    add(decay_plan(rows, S, H, true));
+    if (S && rows % S == 0)
+        add(decay_plan(rows, S, H, false));
+    return DecayBytes{whole(cells * H * d_k * d_v * 4), whole(order)};
+}
+
 struct DecayCall {
     const tgm_decay_attn_desc *d;
     int64_t ld_q, ld_k, ld_v, ld_o, ld_dq, ld_dk, ld_dv;
     DecayRun run;   // the sequences, decays and sizes
-    bool divided;
+    bool divided, ordered;
     hipStream_t s;
 };
 
@@ -244,6 +318,17 @@ template <class T> tgm_status_t go(const DecayRun &r, int what, hipStream_t s)
                                      : decay_f16(r, what, s);
 }
 
+// The work space's parts, and the order.
+tgm_status_t begin(const DecayCall &c, DecayRun *r, char *work, DecayBytes b)
+{
+    r->states = (float *)work;
+    if (c.ordered) {
+        TGM_LAUNCH(k_decay_order, dim3(1), dim3(kOrderThreads), 0, c.s, *r,
+                   (int32_t *)(work + b.states));
+        r->order = (int32_t *)(work + b.states);
+    }
+    return TGM_OK;
+}
 // The states behind the cells, into r.states.
 template <class T> tgm_status_t states(const DecayCall &c, const DecayRun &r)
 {
@@ -259,7 +344,7 @@ template <class T> tgm_status_t states(const DecayCall &c, const DecayRun &r)
 
 template <class T>
 tgm_status_t forward(const DecayCall &c, const void *q, const void *k, const void *v,
-                     const float *first, void *o, float *last, char *work)
+                     const float *first, void *o, float *last, char *work, DecayBytes b)
 {
     DecayRun r = c.run;
     DecayArgs &a = r.a;
@@ -268,7 +353,7 @@ tgm_status_t forward(const DecayCall &c, const void *q, const void *k, const voi
     a.z = DecayIn{v, c.ld_v, share};
     a.p = c.d->d_k, a.r = c.d->d_v, a.out = o, a.ld_out = c.ld_o;
     a.first = first, a.last = last, a.lag0 = 1, a.c_y = 1.f, a.c_out = c.d->scale;
-    r.states = (float *)work;
+    TGM_TRY_STATUS(begin(c, &r, work, b));
     TGM_TRY_STATUS(states<T>(c, r));
     return go<T>(r, 1, c.s);
 }
@@ -276,14 +361,14 @@ tgm_status_t forward(const DecayCall &c, const void *q, const void *k, const voi
 template <class T>
 tgm_status_t backward(const DecayCall &c, const void *q, const void *k, const void *v,
                       const float *first, const void *dO, const float *dlast, void *dq, void *dk,
-                      void *dv, float *dfirst, char *work, size_t state_bytes)
+                      void *dv, float *dfirst, char *work, DecayBytes b)
 {
     const tgm_decay_attn_desc *d = c.d;
     const int32_t share = d->H / d->H_kv;
     const DecayIn iq{q, c.ld_q, 1}, ik{k, c.ld_k, share}, iv{v, c.ld_v, share}, io{dO, c.ld_o, 1};
     DecayRun r = c.run;
     DecayArgs &a = r.a;
-    r.states = (float *)work;
+    TGM_TRY_STATUS(begin(c, &r, work, b));
     if (dq) {
         a.y = ik, a.z = iv, a.p = d->d_k, a.r = d->d_v;
         a.first = first, a.lag0 = 1, a.c_y = 1.f, a.c_out = d->scale;
@@ -298,7 +383,7 @@ tgm_status_t backward(const DecayCall &c, const void *q, const void *k, const vo
     a.rev = !c.run.a.rev, a.first = dlast, a.lag0 = 0, a.c_y = d->scale, a.c_out = 1.f;
     a.x = ik, a.y = iq, a.z = io, a.p = d->d_k, a.r = d->d_v, a.turned = 0;
     TGM_TRY_STATUS(states<T>(c, r));
-    float *part = (float *)(work + state_bytes);
+    float *part = (float *)(work + b.states + b.order);
     auto results = [&](void *out, int32_t width, int64_t ld) -> tgm_status_t {
         if (share == 1 || !out) {
             a.out = out, a.ld_out = ld;
@@ -365,24 +450,10 @@ tgm_status_t decay_lengths(DecayCall *c)
     c->run.cell = p.cell, c->run.cells = p.padded_cells, c->run.ids = p.ids;
     c->run.all_cells = p.cells;
     c->divided = p.divided;
+    c->ordered = (a.offsets || a.length) && order_bytes(p, a.rows, a.S, a.H);
     c->run.brief = decay_brief(a.rows, a.S, a.offsets != nullptr);
     return TGM_OK;
 }
-// Bytes of the cells' states, whichever form the sequences have.
-size_t state_bytes(int64_t rows, int32_t S, int32_t H, int32_t d_k, int32_t d_v)
-{
-    size_t cells = 0;
-    const DecayPlan packed = decay_plan(rows, S, H, true);
-    if (packed.divided)
-        cells = packed.cells;
-    if (S && rows % S == 0) {
-        const DecayPlan padded = decay_plan(rows, S, H, false);
-        if (padded.divided)
-            cells = std::max(cells, (size_t)padded.cells);
-    }
-    return whole(cells * H * d_k * d_v * 4);
-}
-
 tgm_status_t check_work(size_t need, const void *work, size_t bytes)
 {
     if (!need)
@@ -431,7 +502,8 @@ extern "C" tgm_status_t tgm_decay_attn_work_bytes(int64_t rows, int32_t S, int32
 {
     if (!bytes || !decay_sizes(rows, S, H, H_kv, d_k, d_v, dtype))
         return TGM_EINVAL;
-    *bytes = state_bytes(rows, S, H, d_k, d_v) +
+    const DecayBytes b = decay_bytes(rows, S, H, d_k, d_v);
+    *bytes = b.states + b.order +
              (backward && H != H_kv ? whole((size_t)rows * H * std::max(d_k, d_v) * 4) : 0);
     return TGM_OK;
 }
@@ -451,11 +523,12 @@ extern "C" tgm_status_t tgm_decay_attn(const tgm_decay_attn_desc *d, const void 
     TGM_TRY_STATUS(tgm_decay_attn_work_bytes(d->rows, d->S, d->H, d->H_kv, d->d_k, d->d_v, d->dtype,
                                              0, &need));
     TGM_TRY_STATUS(check_work(need, work, work_bytes));
+    const DecayBytes b = decay_bytes(d->rows, d->S, d->H, d->d_k, d->d_v);
     char *w = (char *)work;
     switch (d->dtype) {
-    case TGM_F32: return forward<float>(c, q, k, v, state, o, state_last, w);
-    case TGM_BF16: return forward<bf16>(c, q, k, v, state, o, state_last, w);
-    default: return forward<f16>(c, q, k, v, state, o, state_last, w);
+    case TGM_F32: return forward<float>(c, q, k, v, state, o, state_last, w, b);
+    case TGM_BF16: return forward<bf16>(c, q, k, v, state, o, state_last, w, b);
+    default: return forward<f16>(c, q, k, v, state, o, state_last, w, b);
     }
 }
 
@@ -475,14 +548,14 @@ extern "C" tgm_status_t tgm_decay_attn_backward(
                                              1, &need));
     TGM_TRY_STATUS(check_work(need, work, work_bytes));
     char *w = (char *)work;
-    const size_t sb = state_bytes(d->rows, d->S, d->H, d->d_k, d->d_v);
+    const DecayBytes b = decay_bytes(d->rows, d->S, d->H, d->d_k, d->d_v);
     switch (d->dtype) {
     case TGM_F32:
-        return backward<float>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w, sb);
+        return backward<float>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w, b);
     case TGM_BF16:
-        return backward<bf16>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w, sb);
+        return backward<bf16>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w, b);
     default:
-        return backward<f16>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w, sb);
+        return backward<f16>(c, q, k, v, state, dO, dstate_last, dq, dk, dv, dstate, w, b);
     }
 }
 

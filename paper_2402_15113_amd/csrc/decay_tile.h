@@ -18,7 +18,7 @@
 // through LDS), of which 16 wavefronts a CU do not hide all; q, k, v and o pass once here and k
 // and v once more for the states.  bf16, 262,147 rows of 8 heads of 128: results 540 us (2.1 GB,
 // 4.0 TB/s), states 262 us (1.1 GB, 4.1 TB/s); 65,536 rows of 16 heads of 64 and 128 in 64
-// sequences: results 400 us, dq 254, dv 440 and dk 265 (fp32, for four heads each), states 54.
+// sequences: results 281 us, dq 181, dv 308 and dk 188 (fp32, for four heads each), states 54.
 // fp32, 4,000 sequences of 11 rows of 2 heads of 50 with their states: 86 us (200 MB).
 #pragma once
 
@@ -251,9 +251,18 @@ template <class T, int P, bool OUT> constexpr int decay_chunk()
     return !OUT && sizeof(T) == 2 && P <= 64 ? 64 : 32;
 }
 
+// Wavefronts of a SIMD that registers are kept for: two workgroups of 512 threads or four of 256
+// fit a CU; three of those with 128 x 64 columns in fp32 and fp16, which would not be kept in 128
+// registers.  us with 3 and 4: 262,144 rows of 8 heads fp32 1,438 and 1,484, a training step of
+// 65,536 rows of heads of 64 and 128 fp16 1,002 and 1,082; of bf16 dq and dk of 16 heads 425 and 382.
+template <class T, int P, int R, bool OUT> constexpr int decay_waves()
+{
+    return OUT && P == 128 && R == 64 && TypeCode<T>::code != TGM_BF16 ? 3 : 4;
+}
+
 // OUT: x and the results; without, the pieces' states alone (for sequences that go on).
 template <class T, class O, int P, int R, bool OUT>
-__global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
+__global__ __launch_bounds__(4 * R, (decay_waves<T, P, R, OUT>())) void k_decay(DecayRun run)
 {
     constexpr int C = decay_chunk<T, P, OUT>(), NW = R / 16, TH = 64 * NW, TB = C / 16;
     constexpr int STEP = 64 / (int)sizeof(T);       // elements of a fragment's sum
@@ -280,8 +289,10 @@ __global__ __launch_bounds__(4 * R, 4) void k_decay(DecayRun run)
     const int64_t ids = OUT ? run.ids : run.all_cells, all = ids * A.H;
     for (int64_t at = blockIdx.x; at < all; at += gridDim.x) {
         const DecayPlace place = decay_place(at, ids, A.H);
-        const DecayPiece piece =
-            OUT ? decay_piece_of(run, place.piece) : decay_piece_onward(run, place.piece);
+        const int64_t id = OUT && run.order ? run.order[place.piece] : place.piece;
+        if (id < 0)
+            continue;
+        const DecayPiece piece = OUT ? decay_piece_of(run, id) : decay_piece_onward(run, id);
         const int32_t h = place.head;
         const bool empty = OUT && decay_empty_here(run, piece);
         const int64_t rows = piece.hi - piece.lo;

@@ -335,6 +335,38 @@ def test_many_sequences(tgm):
     go(tgm, packed(lengths), 1, 1, 4, 4, torch.float32)
 
 
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_short_sequences(tgm, dtype, reverse):
+    """Few rows each for the most part, packed and padded, and a sequence of many among them."""
+    few = [(5 * i) % 9 for i in range(120)]
+    go(tgm, packed(few + [230, 16, 17] + few[::-1]), 2, 1, 50, 50, TYPES[dtype], reverse=reverse)
+    go(tgm, packed(few, before=2, behind=3), 3, 3, 17, 31, TYPES[dtype], reverse=reverse, pad=1)
+    go(tgm, padded([16, 0, 3, 20, 9, 1], 16), 2, 2, 64, 40, TYPES[dtype], reverse=reverse)
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_uneven_lengths(tgm, dtype, reverse):
+    """Many heads and sequences of many rows, taken in the order of their lengths: more pieces
+    than workgroups of a CU each, some without rows, some of part of a cell."""
+    go(tgm, packed([40, 0, 900, 310, 1, 700, 33], before=5, behind=60), 32, 8, 8, 12,
+       TYPES[dtype], reverse=reverse)
+    go(tgm, padded([200, 0, 64, 17, 199, -5, 300, 1, 150, 33], 200), 32, 32, 12, 8, TYPES[dtype],
+       reverse=reverse, state=False)
+
+
+def test_uneven_offsets_that_make_no_sense(tgm):
+    """As above: other memory is not touched."""
+    dt, rows = torch.bfloat16, 1100
+    for off in ([500, 20, 800, 10], [-40, 300, 5000, 900], [900, 900, -1, 2 ** 62]):
+        seqs = (dict(offsets=torch.tensor(off).cuda(), length=None), [0] * 3, [0] * 3, rows)
+        d, out, _ = both(tgm, seqs, 64, 16, 32, 48, dt, pad=8)
+        torch.cuda.synchronize()
+        for n in ("o", "dq", "dk", "dv"):
+            assert (out[n]._base[:, out[n].shape[1]:].float() == 7).all()
+
+
 def test_captured_and_two_streams(tgm):
     dt, H, G, dk, dv = torch.bfloat16, 4, 2, 64, 64
     seqs = packed([700, 0, 90, 300], behind=6)
