@@ -14,71 +14,90 @@ using namespace tgm;
 namespace {
 
 // The states behind the cells of the sequences that go on, from those of the cells alone: a
-// thread follows an element of a head's state along the sequence that begins in its cell and
-// leaves it.  A chain of cells has to be followed in order, so that what bounds it is how many
-// loads are under way: two elements a thread, eight cells ahead, double buffered.  129 cells of 8
-// heads of 128 x 128 (135 MB): 89 us, 1.5 TB/s; 45 cells of 16 heads of 64 x 128, 27 us.
+// thread follows EACH elements of a head's state along a sequence of more rows than a cell.  The
+// cells have to be followed in order, so that what bounds it is how many loads are under way: 16 a
+// thread, double buffered.  129 cells of 8 heads of 128 x 128 (135 MB): 31 us, 4.4 TB/s; 45 cells of 16
+// heads of 64 x 128 under 64 sequences 17.
+// Its workgroups go by sequences where there are no more than four to a cell, else by cells, in
+// which those that begin and go on have to be searched for (by cells alone 89 and 29 us), and
+// since most of many have nothing to follow, they are fewer, of 8 elements a thread (with 2: 34).
+bool decay_by_sequence(const DecayRun &r) { return r.a.S <= 4 * r.all_cells; }
+
+template <bool BY_SEQUENCE, int EACH>
 __global__ __launch_bounds__(256) void k_decay_walk(DecayRun run)
 {
     const DecayArgs &A = run.a;
     const int32_t h = blockIdx.y, size = A.p * A.r;
-    constexpr int EACH = 2, AHEAD = 8;   // elements of a thread, cells that are loaded together
     const int32_t at = (int32_t)(blockIdx.z * 256 * EACH + threadIdx.x);
     const float keep = decay_pow(decay_log2(A.decay[h]), (float)run.cell);
-    const int64_t C = run.cell, cells = run.all_cells;
-    for (int64_t cell = blockIdx.x; cell < cells; cell += gridDim.x) {
-        const DecayPiece piece = decay_piece_onward(run, cell);
-        if (piece.hi <= piece.lo ||
-            (A.rev ? piece.hi != piece.q.e : piece.lo != piece.q.b))
-            continue;   // no sequence begins here and goes on
-        // cells that it goes on to, but for its last
-        const DecaySeq q = piece.q;
-        const int64_t left =
-            (A.offsets ? (q.e - 1) / C - q.b / C : (q.e - q.b + C - 1) / C - 1) - 1;
+    const int64_t C = run.cell, n = BY_SEQUENCE ? A.S : run.all_cells;
+    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+        DecaySeq q;
+        if constexpr (BY_SEQUENCE) {
+            q = decay_seq(A, (int32_t)i);
+            if (q.e - q.b <= C)
+                continue;
+        } else {
+            const DecayPiece piece = decay_piece_onward(run, i);
+            q = piece.q;
+            if (piece.hi <= piece.lo || (A.rev ? piece.hi != q.e : piece.lo != q.b))
+                continue;   // no sequence begins here and goes on
+        }
+        const int64_t first = A.offsets ? q.b / C : q.b / A.L * run.cells;
+        const int64_t last = A.offsets ? (q.e - 1) / C : first + (q.e - q.b - 1) / C;
+        const int64_t left = last - first - 1;   // cells that it goes on to, but for its last
         if (left <= 0)
             continue;
-        float *s = run.states + (h * run.all_cells + cell) * (int64_t)size;
+        float *s = run.states + (h * run.all_cells + (A.rev ? last : first)) * (int64_t)size;
         const int64_t next = (A.rev ? -1 : 1) * (int64_t)size;
         int32_t mine[EACH];   // past the state's end: the last element again, which is not stored
-        float v[EACH], e[2][AHEAD][EACH];
+        float v[EACH];
 #pragma unroll
         for (int k = 0; k < EACH; ++k)
             mine[k] = min(at + 256 * k, size - 1), v[k] = s[mine[k]];
-        // cells c + 1 .. c + AHEAD, past the last one that one again
-        auto load = [&](float (&to)[AHEAD][EACH], int64_t c) __attribute__((always_inline)) {
+        auto along = [&](auto ahead) __attribute__((always_inline)) {
+            constexpr int AHEAD = decltype(ahead)::value;
+            float e[2][AHEAD][EACH];
+            // cells c + 1 .. c + AHEAD, past the last one that one again
+            auto load = [&](float (&to)[AHEAD][EACH], int64_t c) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const float *p = s + min(c + 1 + u, left) * next;
+                for (int u = 0; u < AHEAD; ++u) {
+                    const float *p = s + min(c + 1 + u, left) * next;
 #pragma unroll
-                for (int k = 0; k < EACH; ++k)
-                    to[u][k] = p[mine[k]];
+                    for (int k = 0; k < EACH; ++k)
+                        to[u][k] = p[mine[k]];
+                }
+            };
+            auto follow = [&](const float (&from)[AHEAD][EACH], int64_t c)
+                __attribute__((always_inline)) {
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u)
+                        if (c + 1 + u <= left) {
+                            float *p = s + (c + 1 + u) * next;
+#pragma unroll
+                            for (int k = 0; k < EACH; ++k) {
+                                v[k] = v[k] * keep + from[u][k];
+                                if (at + 256 * k < size)
+                                    p[mine[k]] = v[k];
+                            }
+                        }
+                };
+            // the next cells' loads go before these cells' stores, which are waited for in order
+            load(e[0], 0);
+            for (int64_t c = 0; c < left; c += 2 * AHEAD) {
+                if (c + AHEAD < left)
+                    load(e[1], c + AHEAD);
+                follow(e[0], c);
+                if (c + 2 * AHEAD < left)
+                    load(e[0], c + 2 * AHEAD);
+                if (c + AHEAD < left)
+                    follow(e[1], c + AHEAD);
             }
         };
-        auto follow = [&](const float (&from)[AHEAD][EACH], int64_t c)
-            __attribute__((always_inline)) {
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u)
-                    if (c + 1 + u <= left) {
-                        float *p = s + (c + 1 + u) * next;
-#pragma unroll
-                        for (int k = 0; k < EACH; ++k) {
-                            v[k] = v[k] * keep + from[u][k];
-                            if (at + 256 * k < size)
-                                p[mine[k]] = v[k];
-                        }
-                    }
-            };
-        // the next cells' loads go before these cells' stores, which are waited for in order
-        load(e[0], 0);
-        for (int64_t c = 0; c < left; c += 2 * AHEAD) {
-            if (c + AHEAD < left)
-                load(e[1], c + AHEAD);
-            follow(e[0], c);
-            if (c + 2 * AHEAD < left)
-                load(e[0], c + 2 * AHEAD);
-            if (c + AHEAD < left)
-                follow(e[1], c + AHEAD);
-        }
+        if (left <= 2)
+            along(std::integral_constant<int, 2>{});
+        else
+            along(std::integral_constant<int, 16 / EACH>{});
     }
 }
 
@@ -345,10 +364,19 @@ template <class T> tgm_status_t states(const DecayCall &c, const DecayRun &r)
     if (!c.divided)
         return TGM_OK;
     TGM_TRY_STATUS(go<T>(r, 0, c.s));
-    const int64_t z = cdiv((int64_t)r.a.p * r.a.r, 512);
-    TGM_LAUNCH(k_decay_walk,
-               dim3(across(r.all_cells, (int32_t)(r.a.H * z)), (uint32_t)r.a.H, (uint32_t)z), dim3(256),
-               0, c.s, r);
+    const bool by_sequence = decay_by_sequence(r);
+    const int64_t n = by_sequence ? r.a.S : r.all_cells, size = (int64_t)r.a.p * r.a.r;
+    const bool many = n * r.a.H * cdiv(size, 512) > 4096;
+    const int64_t z = cdiv(size, many ? 2048 : 512);
+    const dim3 grid(across(n, (int32_t)(r.a.H * z)), (uint32_t)r.a.H, (uint32_t)z);
+    if (by_sequence && many)
+        TGM_LAUNCH((k_decay_walk<true, 8>), grid, dim3(256), 0, c.s, r);
+    else if (by_sequence)
+        TGM_LAUNCH((k_decay_walk<true, 2>), grid, dim3(256), 0, c.s, r);
+    else if (many)
+        TGM_LAUNCH((k_decay_walk<false, 8>), grid, dim3(256), 0, c.s, r);
+    else
+        TGM_LAUNCH((k_decay_walk<false, 2>), grid, dim3(256), 0, c.s, r);
     return TGM_OK;
 }
 
