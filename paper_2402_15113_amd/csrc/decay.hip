@@ -249,13 +249,15 @@ uint32_t across(int64_t n, int32_t H) { return (uint32_t)std::min<int64_t>(n, (1
 // A cell's rows come one chunk after another and the states pass is over C rows' time, while
 // the states to write and walk go as rows H / C, so the best C grows as the root of rows H.
 // us of a call, cells of 64, 256, 512, 1,024, 2,048 and 4,096 rows, bf16 heads of 128:
-//     1,024 rows x 8        54    56     75     91
-//     8,192 x 8            322   114     99    144    250
-//     32,768 x 8         1,560   386    237    198    266
-//     65,536 x 32       12,978 3,803  2,183  1,418  1,039
-//     262,147 x 8                     1,253  1,003    897   862
-// (the root is 128, 384, 768, 2,048 and 2,048 there.)  Padded sequences fill the card without
-// being divided from 256 heads of them on: 16 x 4,096 rows of 32 heads 438 us whole, 700 in
+//     1,024 rows x 8        40     51     78     92
+//     16,384 x 8           177     92    100    148    260
+//     65,536 x 8           844    362    276    234    279
+//     65,536 x 32        3,400  1,338  1,070    930    868
+//     262,144 x 1          991    275    187    183    272
+//     262,147 x 8                            932    860    840
+// (the root is 128, 512, 1,024, 2,048, 768 and 2,048 there: 44, 102, 242, 860, 200 and 860 us.)
+// Padded sequences fill the card without being divided from 256 heads of them on: 16 x 4,096
+// rows of 32 heads 438 us whole, 700 in
 // cells of 2,048, 878 of 1,024; of 16 heads 334, 373 and 450; but 4 x 4,096 rows of 32 heads
 // (128 workgroups) 231 whole and 197 in cells of 1,024.
 int32_t decay_cell(int64_t rows, int32_t S, int32_t H, bool packed)
