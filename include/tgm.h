@@ -882,7 +882,8 @@ tgm_status_t tgm_rotary_frequencies(int32_t rot, int32_t scaling, double base, d
  * head h / (H / H_kv) of k and v.  decay [H] fp32 on the device holds log a: 0 forgets
  * nothing, -infinity everything but the row itself (positive ones grow).  state and
  * state_last [S x H x d_k x d_v] are dense fp32 (state_last may be NULL): what each sequence
- * starts from and ends with (state's for a sequence without rows).  The sequences are packed by
+ * starts from and ends with (state's for a sequence without rows); they are two tables, as a
+ * sequence's end may be written before its beginning is read.  The sequences are packed by
  * offsets or padded, and shortened by length, as for tgm_scan; what rows of no sequence
  * hold does not matter, and their o is left as it is.  reverse != 0 runs every sequence
  * from its last row to its first.
@@ -893,7 +894,7 @@ tgm_status_t tgm_rotary_frequencies(int32_t rot, int32_t scaling, double base, d
  * later rows only; where the formula has an infinity there may be NaN.
  * rows <= 2^30, H <= 4096, 1 <= d_k, d_v <= 128.
  * Errors: TGM_EINVAL (null, sizes, types, strides, S < 0, S = 0 with rows in the padded form
- * or rows not divisible by it), TGM_ESIZE (work). */
+ * or rows not divisible by it, state_last = state), TGM_ESIZE (work). */
 typedef struct {
     int64_t rows;
     int32_t S, H, H_kv, d_k, d_v;
@@ -919,8 +920,8 @@ tgm_status_t tgm_decay_attn(const tgm_decay_attn_desc *d, const void *q, const v
  *   dstate = a G_1  (dstate_last for a sequence without rows).
  * dq, dk, dv of type dtype, laid out as q, k, v (rows of no sequence are left as they are):
  * dk and dv of a head of k and v are added over the heads that share it, in fp32.  dstate
- * fp32.  Each may be NULL.  The decays are constants: they have no gradient.  Errors as
- * tgm_decay_attn. */
+ * fp32, another table than dstate_last.  Each may be NULL.  The decays are constants: they have no
+ * gradient.  Errors as tgm_decay_attn. */
 tgm_status_t tgm_decay_attn_backward(const tgm_decay_attn_desc *d, const void *q, const void *k,
                                      const void *v, const float *decay, const int64_t *offsets,
                                      const int32_t *length, const float *state, const void *dO,

@@ -81,12 +81,12 @@ __device__ __forceinline__ int32_t decay_count(int32_t lo, int32_t hi, int64_t v
     constexpr int LAST = 4;
     const int lane = threadIdx.x & 63;
     while (hi - lo > LAST * kWave) {
-        const int32_t step = (hi - lo + kWave - 1) / kWave;
+        const int32_t step = (int32_t)(((int64_t)hi - lo + kWave - 1) / kWave);
         const int64_t probe = (int64_t)lo + (int64_t)(lane + 1) * step - 1;
         const int c =
             __popcll(__ballot(probe < hi && key((int32_t)min(probe, (int64_t)hi - 1)) <= v));
         lo += c * step;
-        hi = min(lo + step, hi);
+        hi = (int32_t)min((int64_t)lo + step, (int64_t)hi);
     }
     if (hi <= lo)
         return lo;

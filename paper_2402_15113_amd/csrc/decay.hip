@@ -562,7 +562,7 @@ extern "C" tgm_status_t tgm_decay_attn(const tgm_decay_attn_desc *d, const void 
     DecayCall c{};
     TGM_TRY_STATUS(decay_call(d, decay, offsets, length, stream, &c));
     TGM_TRY_STATUS(decay_lengths(&c));
-    if (d->rows && (!q || !k || !v || !o))
+    if ((d->rows && (!q || !k || !v || !o)) || (state && state == state_last))
         return TGM_EINVAL;
     size_t need = 0;
     TGM_TRY_STATUS(tgm_decay_attn_work_bytes(d->rows, d->S, d->H, d->H_kv, d->d_k, d->d_v, d->dtype,
@@ -586,7 +586,7 @@ extern "C" tgm_status_t tgm_decay_attn_backward(
     DecayCall c{};
     TGM_TRY_STATUS(decay_call(d, decay, offsets, length, stream, &c));
     TGM_TRY_STATUS(decay_lengths(&c));
-    if (d->rows && (!q || !k || !v || !dO))
+    if ((d->rows && (!q || !k || !v || !dO)) || (dstate && dstate == dstate_last))
         return TGM_EINVAL;
     size_t need = 0;
     TGM_TRY_STATUS(tgm_decay_attn_work_bytes(d->rows, d->S, d->H, d->H_kv, d->d_k, d->d_v, d->dtype,

@@ -73,6 +73,19 @@ def test_pointers_and_work():
                                  None) == tgm.TGM_OK
 
 
+def test_states_are_two_tables():
+    """A sequence's last state may be written before another workgroup has read its first."""
+    L, E = tgm.lib(), tgm.TGM_EINVAL
+    other = 2 * X
+    work = lambda b: tgm.tgm_decay_attn_work_bytes(96, 3, 4, 32, 16, torch.bfloat16, kv_heads=2,
+                                                   backward=b)
+    for last, want in ((X, E), (other, tgm.TGM_ESIZE)):
+        assert work(False) and L.tgm_decay_attn(desc(), X, X, X, X, X, None, X, X, last, X,
+                                                work(False) - 1, None) == want
+        assert L.tgm_decay_attn_backward(desc(), X, X, X, X, X, None, X, X, X, X, X, X, last, X,
+                                         work(True) - 1, None) == want
+
+
 def test_work_bytes():
     f = tgm.tgm_decay_attn_work_bytes
     for bad in ((-1, 1, 1, 1, 1), (1, -1, 1, 1, 1), (1, 1, 0, 1, 1), (1, 1, 1, 0, 1),
