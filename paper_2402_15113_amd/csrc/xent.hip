@@ -35,11 +35,15 @@ __global__ __launch_bounds__(1024) void k_xent_loss(const f2 *__restrict__ part,
     const int row = threadIdx.x % ROWS, lane = threadIdx.x / ROWS;
     const int64_t m = (int64_t)blockIdx.x * ROWS + row;
     const bool on = m < rows_in_use(rows, n_rows);
-    // the sum relative to the largest so far; -infinity: nothing yet (or no more than NaN)
+    // the sum relative to the largest so far; -infinity: nothing yet (or no more than NaN); beside
+    // an infinite one the others are nothing, if they are numbers
     auto join = [](f2 a, f2 b) __attribute__((always_inline)) {
         const float t = fmaxf(a.x, b.x);
-        return t == -INFINITY ? f2{t, a.y + b.y}
-                              : f2{t, a.y * expf(a.x - t) + b.y * expf(b.x - t)};
+        const bool far = fabsf(t) == INFINITY;
+        auto part = [&](f2 v) __attribute__((always_inline)) {
+            return far ? (v.x == t ? v.y : v.y * 0.f) : v.y * expf(v.x - t);
+        };
+        return f2{t, part(a) + part(b)};
     };
     f2 all{-INFINITY, 0.f};
     if (on)

@@ -77,7 +77,7 @@ struct XentSums {
             sum += __shfl_xor(sum, 32);
             if (m < M) {
                 if (lane < 16)
-                    e.part[(int64_t)run * e.rows + m] = f2{top == -INFINITY ? top : ref, sum};
+                    e.part[(int64_t)run * e.rows + m] = f2{top, sum};
                 // (a target may be any number)
                 const int32_t at = (int32_t)((uint32_t)e.target[m] - (uint32_t)(e.n_first + n1));
                 if (at >= 0 && at < 16 * NA && (at & 15) < 4) {

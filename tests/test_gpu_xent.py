@@ -307,3 +307,22 @@ def test_captured_and_two_streams(tgm):
         for name in outs[0]:
             assert torch.equal(outs[0][name], outs[1][name]), name
             assert torch.equal(outs[0][name], outs[2][name]), name
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N", [40, 700])
+def test_infinite_logit_beside_large_ones(tgm, dtype, N):
+    """exp(-300) is zero in 32 bits: nothing, beside an infinite sum, and not NaN."""
+    dt, rows, K = TYPES[dtype], 70, 16
+    x, w = torch.zeros(rows, K, device="cuda", dtype=dt), torch.zeros(N, K, device="cuda", dtype=dt)
+    bias = torch.zeros(N, device="cuda", dtype=dt)
+    bias[3], bias[N - 1] = math.inf, 300.0
+    target = torch.full((rows,), N - 1, device="cuda", dtype=torch.int32)
+    target[0] = 3
+    loss, lse = (torch.zeros(rows, device="cuda") for _ in range(2))
+    tgm.tgm_xent(x, w, target, loss, work(tgm, rows, N, K, dt, False), lse=lse, bias=bias)
+    assert (lse == math.inf).all() and (loss[1:] == math.inf).all() and torch.isnan(loss[0])
+    # NaN goes through all the same, wherever it is
+    w[N // 2, 0], x[5, 0] = math.nan, 1.0
+    tgm.tgm_xent(x, w, target, loss, work(tgm, rows, N, K, dt, False), lse=lse, bias=bias)
+    assert torch.isnan(lse).all()
