@@ -408,6 +408,38 @@ def test_captured_and_two_streams(tgm):
             assert torch.equal(outs[0][name], outs[2][name]), name
 
 
+def test_captured_uneven_lengths(tgm):
+    """The order of the pieces is made anew in every replay."""
+    dt, H, G, d = torch.bfloat16, 32, 8, 16
+    seqs = packed([40, 0, 900, 310, 1, 700, 33], before=5, behind=60)
+    how, begin, end, rows = seqs
+    S = len(begin)
+    m = make(seqs, H, G, d, d, dt, state=False)
+    ks = [work(tgm, rows, S, H, d, d, dt, G, False) for _ in range(2)]
+    outs = [torch.zeros(rows, H * d, device="cuda", dtype=dt) for _ in range(2)]
+    call = lambda i: tgm.tgm_decay_attn(m["q"], m["k"], m["v"], m["decay"], outs[i], S, ks[i],
+                                        kv_heads=G, **how)
+    call(0)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(0)
+    for i in range(4):
+        ends = [0, 400 * i, 400 * i, 1300, 1301 + 100 * i, 1800, 1801, rows - i]
+        how["offsets"].copy_(torch.tensor(ends))
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        call(1)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[1])
+        ref = decayref.run(m["q"], m["k"], m["v"], m["decay"], 1.0, H, G,
+                           decayref.chains(ends[:-1], ends[1:], False))
+        tol = decayref.tolerance("o", ref, dt)
+        check("o", outs[0], ref["o"], tol + rounded(ref["o"].abs() + tol, dt))
+
+
 # ------------------------------------------------------------------- single rows
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("H,G,dk,dv", [(1, 1, 1, 1), (2, 2, 50, 50), (4, 1, 128, 128), (3, 3, 7, 33),
