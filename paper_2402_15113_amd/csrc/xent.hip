@@ -33,8 +33,7 @@ __global__ __launch_bounds__(1024) void k_xent_loss(const f2 *__restrict__ part,
     constexpr int ROWS = 16, LANES = 64;
     __shared__ f2 lds[LANES][ROWS + 1];
     const int row = threadIdx.x % ROWS, lane = threadIdx.x / ROWS;
-    const int64_t m = (int64_t)blockIdx.x * ROWS + row;
-    const bool on = m < rows_in_use(rows, n_rows);
+    const int32_t R = rows_in_use(rows, n_rows);
     // the sum relative to the largest so far; -infinity: nothing yet (or no more than NaN); beside
     // an infinite one the others are nothing, if they are numbers
     auto join = [](f2 a, f2 b) __attribute__((always_inline)) {
@@ -45,28 +44,32 @@ __global__ __launch_bounds__(1024) void k_xent_loss(const f2 *__restrict__ part,
         };
         return f2{t, part(a) + part(b)};
     };
-    f2 all{-INFINITY, 0.f};
-    if (on)
+    for (int64_t m0 = (int64_t)blockIdx.x * ROWS; m0 < R; m0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t m = m0 + row;
+        const bool on = m < R;
+        f2 all{-INFINITY, 0.f};
+        if (on)
 #pragma unroll 8
-        for (int r = lane; r < runs; r += LANES)
-            all = join(all, part[(int64_t)r * rows + m]);
-    lds[lane][row] = all;
-    for (int half = LANES / 2; half; half /= 2) {
-        __syncthreads();
-        if (lane < half)
-            lds[lane][row] = join(lds[lane][row], lds[lane + half][row]);
-    }
-    if (lane || !on)
-        return;
-    all = lds[0][row];
-    const float l = all.x == -INFINITY ? (all.y == 0.f ? all.x : all.y) : all.x + logf(all.y);
-    const int32_t t = target[m];
-    if (lse)
-        lse[m] = l;
-    if (loss) {
-        const float z = t >= 0 && t < classes ? at_target[m] : 0.f;
-        // a class that is left out has probability 0, wherever the others are
-        loss[m] = t < 0 || t >= classes ? 0.f : z == -INFINITY && l == l ? INFINITY : l - z;
+            for (int r = lane; r < runs; r += LANES)
+                all = join(all, part[(int64_t)r * rows + m]);
+        lds[lane][row] = all;
+        for (int half = LANES / 2; half; half /= 2) {
+            __syncthreads();
+            if (lane < half)
+                lds[lane][row] = join(lds[lane][row], lds[lane + half][row]);
+        }
+        if (lane || !on)
+            continue;   // (what is read behind the last barrier is this wavefront's own)
+        all = lds[0][row];
+        const float l = all.x == -INFINITY ? (all.y == 0.f ? all.x : all.y) : all.x + logf(all.y);
+        const int32_t t = target[m];
+        if (lse)
+            lse[m] = l;
+        if (loss) {
+            const float z = t >= 0 && t < classes ? at_target[m] : 0.f;
+            // a class that is left out has probability 0, wherever the others are
+            loss[m] = t < 0 || t >= classes ? 0.f : z == -INFINITY && l == l ? INFINITY : l - z;
+        }
     }
 }
 
@@ -282,8 +285,9 @@ tgm_status_t forward(const tgm_xent_desc *d, const int64_t *ld, const void *x, c
     e.at_target = (float *)(work + whole((size_t)xent_parts(d->N) * d->rows * sizeof(f2)));
     XentRuns r;
     TGM_TRY_STATUS(sums_of<T>(p, e, &r));
-    TGM_LAUNCH(k_xent_loss, dim3((uint32_t)cdiv(d->rows, 16)), dim3(1024), 0, s, e.part,
-               r.columns, d->rows, d->N, n_rows, target, e.at_target, loss, lse);
+    // (a launch has fewer than 2^32 threads)
+    TGM_LAUNCH(k_xent_loss, dim3((uint32_t)std::min<int64_t>(cdiv(d->rows, 16), 1 << 21)),
+               dim3(1024), 0, s, e.part, r.columns, d->rows, d->N, n_rows, target, e.at_target, loss, lse);
     return TGM_OK;
 }
 

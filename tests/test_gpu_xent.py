@@ -326,3 +326,27 @@ def test_infinite_logit_beside_large_ones(tgm, dtype, N):
     w[N // 2, 0], x[5, 0] = math.nan, 1.0
     tgm.tgm_xent(x, w, target, loss, work(tgm, rows, N, K, dt, False), lse=lse, bias=bias)
     assert torch.isnan(lse).all()
+
+
+def test_very_many_rows(tgm):
+    """More rows than a launch has groups of 16 of: two classes of one channel, whose loss is
+    log(1 + e^-z) for the first."""
+    rows, f32 = (1 << 26) + 100, torch.float32
+    x = (torch.arange(rows, device="cuda") % 1024 / 256.0)[:, None].contiguous()
+    w = torch.tensor([[1.0], [0.0]], device="cuda")
+    target = torch.zeros(rows, device="cuda", dtype=torch.int32)
+    loss, lse = (torch.full((rows,), -1.0, device="cuda") for _ in range(2))
+    tgm.tgm_xent(x, w, target, loss, work(tgm, rows, 2, 1, f32, False), lse=lse)
+    for some in (slice(0, 1 << 20), slice(rows - (1 << 20), rows)):
+        z = x[some, 0].double()
+        # two exponentials, their sum, a logarithm and a difference, of values below 5
+        tol = torch.full_like(z, 40 * U)
+        check("lse", lse[some], torch.log(1 + z.exp()).cpu(), tol.cpu())
+        check("loss", loss[some], torch.log(1 + (-z).exp()).cpu(), tol.cpu())
+    assert (loss >= 0).all() and (lse > 0).all()
+    dx = torch.full_like(x, 7.0)
+    tgm.tgm_xent_backward(x, w, target, lse, torch.ones_like(lse),
+                          work(tgm, rows, 2, 1, f32, True), dx=dx)
+    z = x[-1000:, 0].double()
+    check("dx", dx[-1000:, 0], (-1 / (1 + z.exp())).cpu(), torch.full((1000,), 60 * U).double())
+    assert (dx < 0).all() and (dx > -0.6).all()
