@@ -111,7 +111,8 @@ struct DecayPiece {
     int64_t cell, lo, hi;   // hi <= lo: no rows
     DecaySeq q;
 };
-// The sequences that may be a step's, from .lo to .hi - 1, and a sequence's first step.
+// The sequences whose first step may be the last one up to step `id`: lo .. hi - 1.  (A sequence's
+// first step is its own number and at most as many cells more.)
 struct DecaySteps {
     int32_t lo, hi;
 };
@@ -121,6 +122,7 @@ __device__ __forceinline__ DecaySteps decay_steps(const DecayArgs &a, int64_t id
     return DecaySteps{(int32_t)min(max(id - cells, (int64_t)0), (int64_t)a.S),
                       (int32_t)min(id + 1, (int64_t)a.S)};
 }
+// Sequence s's first step.
 __device__ __forceinline__ int64_t decay_step_of(const DecayArgs &a, int32_t s, int32_t C)
 {
     return decay_cell_of(decay_begin(a, s), C) + s;
@@ -158,9 +160,7 @@ struct DecayRun {
     bool brief;         // sequences of few rows for the most part
 };
 
-// Piece `id` of the sequences: a sequence of no more than a cell's rows in one piece, which
-// the cell that it begins in has; longer ones by cells.  Packed sequences share a grid of
-// cells, padded ones have cells of their own.
+// A sequence of no more than a cell's rows is one piece, which the cell that it begins in has.
 __device__ __forceinline__ DecayPiece decay_whole(const DecayRun &r, DecayPiece p)
 {
     if (p.q.e - p.q.b <= r.cell) {
@@ -179,6 +179,8 @@ __device__ __forceinline__ DecayPiece decay_padded_piece(const DecayRun &r, int6
     p.hi = min(p.q.e, p.lo + r.cell);
     return p;
 }
+// Piece `id` of the sequences: whole sequences, and longer ones by cells.  Packed sequences
+// share a grid of cells, padded ones have cells of their own.
 __device__ __forceinline__ DecayPiece decay_piece_of(const DecayRun &r, int64_t id)
 {
     return r.a.offsets ? decay_whole(r, decay_piece(r.a, id, r.cell)) : decay_padded_piece(r, id);
@@ -225,7 +227,7 @@ __device__ __forceinline__ DecayPiece decay_piece_onward(const DecayRun &r, int6
 __device__ __forceinline__ bool decay_empty_here(const DecayRun &r, const DecayPiece &p)
 {
     return p.q.e <= p.q.b && (r.a.offsets ? p.cell == decay_cell_of(p.q.b, r.cell)
-                                             : p.cell == p.s * r.cells);
+                                           : p.cell == p.s * r.cells);
 }
 
 // what: 0 states, 1 results of the inputs' type, 2 results in fp32
