@@ -18,8 +18,8 @@
 // through LDS), of which 16 wavefronts a CU do not hide all; q, k, v and o pass once here and k
 // and v once more for the states.  bf16, 262,147 rows of 8 heads of 128: results 540 us (2.1 GB,
 // 4.0 TB/s), states 262 us (1.1 GB, 4.1 TB/s); 65,536 rows of 16 heads of 64 and 128 in 64
-// sequences: results 281 us, dq 181, dv 308 and dk 188 (fp32, for four heads each), states 54.
-// fp32, 4,000 sequences of 11 rows of 2 heads of 50 with their states: 86 us (200 MB).
+// sequences: results 267 us, dq 153, dv 292 and dk 173 (fp32, for four heads each), states 54.
+// fp32, 4,000 sequences of 11 rows of 2 heads of 50 with their states: 81 us (200 MB).
 #pragma once
 
 #include <type_traits>
