@@ -943,7 +943,8 @@ tgm_status_t tgm_decay_attn_step(const tgm_decay_attn_desc *d, const void *q, co
  *   z = x W^T + bias,  lse_r = log sum_n exp z_rn,  loss_r = lse_r - z_(r, target_r).
  * x [rows x K], W [N x K] and bias [N] (may be NULL: zero) have type dtype (f32, bf16 or
  * f16), target [rows] int32, loss and lse [rows] fp32 (one of them may be NULL).  A row whose
- * target is outside [0, N) has no part in the loss: loss 0, no gradient, an lse all the same.
+ * target is outside [0, N) has no part in the loss: loss 0, no gradient whatever its x holds (its
+ * dx is 0 as long as W is finite), an lse all the same.
  * Products are exact and added in fp32, logits and exponentials fp32.  A bias of -infinity leaves
  * a class out: probability 0, loss +infinity where it is the target.  Where every logit of a
  * row is -infinity, lse is -infinity, the loss +infinity and the row has no gradient.
@@ -957,7 +958,8 @@ typedef struct {
     int64_t ld_dx, ld_dw;   /* tgm_xent_backward only */
 } tgm_xent_desc;
 /* For tgm_xent (backward 0) and tgm_xent_backward (1: a piece of the classes' gradients in
- * dtype, up to 512 MB or 1,024 classes, whichever is more, and fp32 sums of dx). */
+ * dtype, up to 512 MB or 1,024 classes, whichever is more, fp32 sums of dx, and a copy of x, which
+ * is made where rows without a gradient are not finite). */
 tgm_status_t tgm_xent_work_bytes(int32_t rows, int32_t N, int32_t K, int32_t dtype,
                                  int32_t backward, size_t *bytes);
 tgm_status_t tgm_xent(const tgm_xent_desc *d, const void *x, const void *W, const void *bias,

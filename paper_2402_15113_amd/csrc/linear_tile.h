@@ -334,6 +334,17 @@ template <class T, class O, class LP, class LQ, int NA, int MA> struct Half8 {
 struct LinearEnd {
     struct Args {};
 };
+// C itself, of another P (lying on 16 bytes) where the device has found that it takes one.
+struct LinearEither {
+    struct Args {
+        const void *P;
+        int64_t ld_p;
+        const int32_t *take;
+    };
+};
+template <class End>
+constexpr bool is_linear =
+    std::is_same_v<End, LinearEnd> || std::is_same_v<End, LinearEither>;
 
 template <class T, class O, bool PK, bool QK, int BN, int BM, int NW, int MW, bool DIRECT,
           class End = LinearEnd>
@@ -362,6 +373,9 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
     const int32_t ns = (int32_t)max((int64_t)0, min(steps - s0, per));
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int wn = (w % NW) * (BN / NW), wm = (w / NW) * (BM / MW);
+    if constexpr (std::is_same_v<End, LinearEither>)
+        if (*end.take)
+            P = (const T *)end.P, ld_p = end.ld_p;
 
     const int used = min(NA, (o.N - n0 - wn + SIDE - 1) / SIDE);
     OP p;
@@ -505,7 +519,7 @@ __global__ __launch_bounds__(64 * NW * MW, 2) void k_linear_tile(
         step(s, no{}, no{});
     }
 
-    if constexpr (!std::is_same_v<End, LinearEnd>) {
+    if constexpr (!is_linear<End>) {
         End::template finish<T, NA, MA>(end, o, acc, n0 + wn, m0 + wm, t.n * NW + w % NW,
                                         t.m * MW + w / NW, M);
         return;

@@ -44,5 +44,9 @@ tgm_status_t xent_grad_f16(const LinearProduct &p, const XentArgs &e, XentRuns *
 // dx of a piece of the classes in fp32, added to what is there.
 tgm_status_t xent_dx_bf16(const LinearProduct &p);
 tgm_status_t xent_dx_f16(const LinearProduct &p);
+// dW, of another x (dense rows of ld, on 16 bytes) where *take is not zero.
+tgm_status_t xent_dw_f32(const LinearProduct &p, const void *x, int64_t ld, const int32_t *take);
+tgm_status_t xent_dw_bf16(const LinearProduct &p, const void *x, int64_t ld, const int32_t *take);
+tgm_status_t xent_dw_f16(const LinearProduct &p, const void *x, int64_t ld, const int32_t *take);
 
 }  // namespace tgm

@@ -274,5 +274,28 @@ template <class T> tgm_status_t xent_dx(const LinearProduct &p)
     return l.large ? launch_tile<T, float, false, true, 256, 256, 2, 4, true>(p, l.parts)
                    : launch_tile<T, float, false, true, 128, 128, 2, 2, true>(p, l.parts);
 }
+// dW, of another x where the device has found that it takes one.
+template <class T, int BN, int BM, int NW, int MW, bool DIRECT>
+tgm_status_t launch_dw(const LinearProduct &p, int parts, const LinearEither::Args &x)
+{
+    return launch_tile<T, T, false, false, BN, BM, NW, MW, DIRECT, LinearEither>(p, parts, x);
+}
+template <class T> tgm_status_t xent_dw(const LinearProduct &p, const LinearEither::Args &x)
+{
+    const LinearPlan l = linear_plan(p, TypeCode<T>::code);
+    const bool lies = direct<T, false, false>(p);
+    if constexpr (sizeof(T) == 4) {
+        if (l.large)
+            return lies ? launch_dw<T, 128, 128, 2, 2, true>(p, l.parts, x)
+                        : launch_dw<T, 128, 128, 2, 2, false>(p, l.parts, x);
+        return lies ? launch_dw<T, 64, 64, 1, 4, true>(p, l.parts, x)
+                    : launch_dw<T, 64, 64, 1, 4, false>(p, l.parts, x);
+    } else {
+        if (!lies)
+            return launch_dw<T, 128, 128, 2, 2, false>(p, l.parts, x);
+        return l.large ? launch_dw<T, 256, 256, 2, 4, true>(p, l.parts, x)
+                       : launch_dw<T, 128, 128, 2, 2, true>(p, l.parts, x);
+    }
+}
 
 }  // namespace tgm

@@ -350,3 +350,117 @@ def test_very_many_rows(tgm):
     z = x[-1000:, 0].double()
     check("dx", dx[-1000:, 0], (-1 / (1 + z.exp())).cpu(), torch.full((1000,), 60 * U).double())
     assert (dx < 0).all() and (dx > -0.6).all()
+
+
+# ---- rows that have no part in the loss
+def spoil(x, rows_of_x, seed):
+    """What is not finite in one column of some of the rows, in all columns of others."""
+    for i, r in enumerate(rows_of_x):
+        if i % 3 == 0:
+            x[r] = (math.nan, math.inf, -math.inf)[i // 3 % 3]
+        elif i % 3 == 1:
+            x[r, (seed + i) % x.shape[1]] = (math.nan, math.inf)[i // 3 % 2]
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,N,K,pad", [(1, 5, 3, 0), (70, 130, 40, 0), (200, 1000, 100, 3),
+                                          (130, 300, 65, 1), (3600, 3700, 264, 0)])
+def test_rows_without_a_target_may_hold_anything(tgm, rows, N, K, pad, dtype):
+    """Loss 0 and no gradient, whatever their x holds: the same results as of zeros there."""
+    dt = TYPES[dtype]
+    x, w = strided(randn(1, rows, K), dt, pad), strided(randn(2, N, K) / K ** 0.5, dt, pad)
+    t = torch.randint(0, N, (rows,), generator=torch.Generator().manual_seed(3)).to(torch.int32)
+    out_rows = list(range(0, rows, 3))
+    t[out_rows] = torch.tensor([-1, N, -2 ** 31, 2 ** 31 - 1]).to(torch.int32)[
+        torch.arange(len(out_rows)) % 4]
+    t, dl = t.cuda(), randn(4, rows).cuda()
+    dl[out_rows[0]] = math.nan
+    bias = randn(5, N).cuda().to(dt)
+    got = []
+    for some in (False, True):
+        x[out_rows] = 0
+        if some:
+            spoil(x, out_rows, 7)
+        loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        tgm.tgm_xent(x, w, t, loss, work(tgm, rows, N, K, dt, False), lse=lse, bias=bias)
+        o = dict(loss=loss, dx=strided(torch.full((rows, K), 7.0), dt, pad),
+                 dw=strided(torch.full((N, K), 7.0), dt, pad), db=torch.full_like(bias, 7.0))
+        tgm.tgm_xent_backward(x, w, t, lse, dl, work(tgm, rows, N, K, dt, True), bias=bias,
+                              dx=o["dx"], dw=o["dw"], db=o["db"])
+        assert (loss[out_rows] == 0).all() and (o["dx"][out_rows] == 0).all()
+        assert untouched(o["dx"], K) and untouched(o["dw"], K)
+        got.append(o)
+    for name in got[0]:
+        assert torch.isfinite(got[1][name]).all(), name
+        assert torch.equal(got[0][name], got[1][name]), name
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_rows_of_nothing_left_may_hold_anything(tgm, dtype):
+    """A row whose every logit is -infinity by its own x has no gradient either."""
+    dt, rows, N, K = TYPES[dtype], 40, 60, 16
+    x, w = randn(1, rows, K).cuda().to(dt), randn(2, N, K).abs().cuda().to(dt) + 0.5
+    x[5] = -math.inf
+    t = torch.arange(rows, dtype=torch.int32, device="cuda")
+    loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    tgm.tgm_xent(x, w, t, loss, work(tgm, rows, N, K, dt, False), lse=lse)
+    assert lse[5] == -math.inf and loss[5] == math.inf
+    dw, dx = torch.empty_like(w), torch.empty_like(x)
+    tgm.tgm_xent_backward(x, w, t, lse, torch.ones(rows, device="cuda"),
+                          work(tgm, rows, N, K, dt, True), dx=dx, dw=dw)
+    assert torch.isfinite(dw).all() and (dx[5] == 0).all()
+
+
+def test_what_is_not_finite_elsewhere_goes_through(tgm):
+    """NaN in a row that has a target is in that column of dW; a row behind the count is not."""
+    rows, N, K = 90, 70, 24
+    x, w = randn(1, rows, K).cuda(), randn(2, N, K).cuda()
+    t = (torch.arange(rows, dtype=torch.int32, device="cuda") % N)
+    t[3] = -1
+    x[3] = math.nan
+    nr = torch.tensor([80], dtype=torch.int32, device="cuda")
+    x[85] = math.nan
+    for bad in (False, True):
+        if bad:
+            x[11, 4] = math.nan
+        loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        tgm.tgm_xent(x, w, t, loss, work(tgm, rows, N, K, torch.float32, False), lse=lse,
+                     n_rows=nr)
+        dw = torch.empty_like(w)
+        tgm.tgm_xent_backward(x, w, t, lse, torch.ones(rows, device="cuda"),
+                              work(tgm, rows, N, K, torch.float32, True), dw=dw, n_rows=nr)
+        # (the row's logits are NaN, so all columns are)
+        assert torch.isnan(dw).all() if bad else torch.isfinite(dw).all()
+
+
+def test_captured_with_ignored_rows(tgm):
+    """Whether rows have to be kept out is found anew in every replay."""
+    dt, rows, N, K = torch.bfloat16, 300, 500, 64
+    x, w = randn(1, rows, K).cuda().to(dt), randn(2, N, K).cuda().to(dt)
+    t = torch.randint(0, N, (rows,), generator=torch.Generator().manual_seed(3)).to(
+        torch.int32).cuda()
+    lse, dl = torch.zeros(rows, device="cuda"), randn(4, rows).cuda()
+    n = max(tgm.tgm_xent_work_bytes(rows, N, K, dt), tgm.tgm_xent_work_bytes(rows, N, K, dt, True))
+    ks = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    dws = [torch.zeros_like(w) for _ in range(2)]
+
+    def call(i):
+        tgm.tgm_xent(x, w, t, None, ks[i], lse=lse)
+        tgm.tgm_xent_backward(x, w, t, lse, dl, ks[i], dw=dws[i])
+
+    call(0)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(0)
+    for i in range(4):
+        x.copy_(randn(20 + i, rows, K))
+        t.copy_(torch.randint(0, N, (rows,), generator=torch.Generator().manual_seed(i)))
+        if i % 2:
+            t[i::7] = -1
+            x[i::7] = math.nan
+        torch.cuda.synchronize()
+        g.replay()
+        call(1)
+        torch.cuda.synchronize()
+        assert torch.isfinite(dws[0]).all() and torch.equal(dws[0], dws[1])
