@@ -11,8 +11,12 @@
 // weights a^(i - s) (x_i . y_s), a row of 16 i each, through LDS.
 //
 // 16-bit inputs: the weights and S are rounded once for the products that make out of them.
-// S itself takes a^(n - 1 - s) z_s in parts (three of bf16, two of fp16) whose sum is the
-// fp32 product, so no error of 16 bits is carried along.
+// S itself takes a^(n - 1 - s) z_s in parts, so that no error of 16 bits is carried along: three
+// of bf16, whose sum is the fp32 product, or two of fp16, whose sum is off by 2^-23 of it.  fp16
+// is narrow, so its numbers come times powers of two: one for a row of weights, one for a column of
+// S (a lane has one column of S and of z), one for a column of z, whose second parts have another
+// 2^12.  What is below 2^-27 of the largest of its row of weights or column of S loses bits to
+// fp16's smallest steps; of a column of z, what is below 2^-29 of its largest in the chunk.
 //
 // What bounds it: the chain from chunk to chunk (loads, weights, results, state, two exchanges
 // through LDS), of which 16 wavefronts a CU do not hide all; q, k, v and o pass once here and k
@@ -219,11 +223,24 @@ template <class T, int C, int W, int TH> struct DecayLoad {
 
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) < INFINITY; }
 // The power of two that brings a largest absolute value (finite, or 0) to 2^13 .. 2^14: fp16 has
-// 13 bits and more below it.
+// all its bits from there down to 2^-14.
 __device__ __forceinline__ float half_scale(float top)
 {
-    return top > 0.f ? ldexpf(1.f, min(max(13 - ilogbf(top), -100), 100)) : 1.f;
+    return top > 0.f ? ldexpf(1.f, min(max(13 - ilogbf(top), -126), 100)) : 1.f;
 }
+// 1 / v of a power of two from 2^-126 to 2^126.
+__device__ __forceinline__ float one_over(float v)
+{
+    return __uint_as_float(0x7f000000u - __float_as_uint(v));
+}
+// The largest of the four lanes that hold a column.
+__device__ __forceinline__ float column_max(float v)
+{
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+// What fp16's second part is held times besides: its smallest steps are 2^-36, not 2^-24.
+constexpr float kLowPart = 4096.f;
 
 // Which piece and head workgroup `id` takes: every XCD (id % 8) runs of all heads of a
 // piece, whose rows lie side by side and which may share k and v.
@@ -341,8 +358,9 @@ __global__ __launch_bounds__(4 * R, (decay_waves<T, P, R, OUT>())) void k_decay(
 #pragma unroll
         for (int pb = 0; pb < PB; ++pb)
             st[pb] = f4{0.f, 0.f, 0.f, 0.f};
-        // (turned: 4 rows of a column are neighbours.  A training step of 1,000 x 40 rows of 4 heads
-        // of 128 x 104 fp16 843 us, 1,115 by single elements)
+        // (turned: 4 rows of a column are neighbours.  By single elements a training step of 1,000 x
+        // 40 rows of 4 heads of 128 x 104 fp16 took 1,115 us, so 843; with fp16's scales by columns
+        // 876.)
         if (from && A.turned) {
 #pragma unroll
             for (int pb = 0; pb < PB; ++pb) {
@@ -478,8 +496,10 @@ __global__ __launch_bounds__(4 * R, (decay_waves<T, P, R, OUT>())) void k_decay(
             if constexpr (OUT) {
                 f4 o[NB];
                 bool spoilt = false;
+                // of the state's column that the lane has.  (Formed without a state too, registers
+                // spill, and a training step of 4,000 sequences of 11 rows takes 435 us for 340.)
                 float s_scale = 1.f;
-                if constexpr (F16) {
+                if (F16 && some) {
                     float top = 0.f;
 #pragma unroll
                     for (int pb = 0; pb < PB; ++pb)
@@ -488,7 +508,7 @@ __global__ __launch_bounds__(4 * R, (decay_waves<T, P, R, OUT>())) void k_decay(
                             const float v = fabsf(st[pb][j]);
                             top = v < INFINITY ? fmaxf(top, v) : top;
                         }
-                    s_scale = half_scale(group_max<64>(top));
+                    s_scale = half_scale(column_max(top));
                 }
                 // A weight of zero does not keep what is not finite in a later row of the
                 // chunk from a row's sum.  The last block's sums show whether there may be any:
@@ -511,11 +531,19 @@ __global__ __launch_bounds__(4 * R, (decay_waves<T, P, R, OUT>())) void k_decay(
                             for (int b = 0; b < NB; ++b)
                                 o[b] = mfma(s, TX::along(lx, 16 * b, k, i16, g), o[b]);
                         }
+                        if constexpr (F16)   // 1 over the scales of the four columns that o has
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float back = __shfl(one_over(s_scale), 4 * g + j);
+#pragma unroll
+                                for (int b = 0; b < NB; ++b)
+                                    o[b][j] *= back;
+                            }
 #pragma unroll
                         for (int b = 0; b < NB; ++b) {
                             const float f =
                                 A.c_out * decay_pow(decay, (float)(16 * b + i16 + lag));
-                            o[b] *= F16 ? f / s_scale : f;
+                            o[b] *= f;
                         }
                     }
 #pragma unroll
@@ -620,49 +648,81 @@ __global__ __launch_bounds__(4 * R, (decay_waves<T, P, R, OUT>())) void k_decay(
                             const float v = fabsf(to_f32(z[k].v.v[e]) * weight(k, e));
                             top = v < INFINITY ? fmaxf(top, v) : top;
                         }
-                    z_scale = half_scale(group_max<64>(top));
+                    z_scale = half_scale(column_max(top));
                 }
                 const float whole = decay_pow(decay, (float)(n - 1 + lag));
-                const float keep = F16 ? whole * z_scale : whole;
-                if (some)
+                if (!F16 && some)
 #pragma unroll
                     for (int pb = 0; pb < PB; ++pb)
-                        st[pb] *= keep;
+                        st[pb] *= whole;
+                // (products into one block wait for each other)
+                if constexpr (F16) {
+                    // both parts' sums apart, for their scales, which the state may not hold
+                    constexpr int PAIR = GROUP / 2;
+                    const float back = one_over(z_scale), keep = some ? whole : 0.f;
+                    Frag<T> high_part[KC], low_part[KC];
 #pragma unroll
-                for (int k = 0; k < KC; ++k) {
-                    Frag<T> part[PARTS];
+                    for (int k = 0; k < KC; ++k)
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        float v = to_f32(z[k].v.v[e]) * weight(k, e);
-                        if constexpr (F16)
-                            v *= z_scale;
-#pragma unroll
-                        for (int u = 0; u < PARTS; ++u) {
-                            part[u].v.v[e] = from_f32<T>(v);
-                            if (u + 1 < PARTS)
-                                v -= to_f32(part[u].v.v[e]);
+                        for (int e = 0; e < VEC; ++e) {
+                            const float v = to_f32(z[k].v.v[e]) * weight(k, e) * z_scale;
+                            high_part[k].v.v[e] = from_f32<T>(v);
+                            low_part[k].v.v[e] =
+                                from_f32<T>((v - to_f32(high_part[k].v.v[e])) * kLowPart);
                         }
+#pragma unroll
+                    for (int p2 = 0; p2 < PB; p2 += PAIR) {
+                        f4 high[PAIR], low[PAIR];
+#pragma unroll
+                        for (int i = 0; i < PAIR; ++i)
+                            high[i] = low[i] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int k = 0; k < KC; ++k) {
+                            Frag<T> f[PAIR];
+#pragma unroll
+                            for (int i = 0; i < PAIR; ++i)
+                                f[i] = TX::across(ly, 16 * (p2 + i), k, i16, g);
+#pragma unroll
+                            for (int i = 0; i < PAIR; ++i)
+                                low[i] = mfma(f[i], low_part[k], low[i]);
+#pragma unroll
+                            for (int i = 0; i < PAIR; ++i)
+                                high[i] = mfma(f[i], high_part[k], high[i]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < PAIR; ++i)
+                            st[p2 + i] = st[p2 + i] * keep + (high[i] + low[i] / kLowPart) * back;
                     }
-                    // (products into one block wait for each other)
+                } else {
 #pragma unroll
-                    for (int p4 = 0; p4 < PB; p4 += GROUP) {
-                        Frag<T> f[GROUP];
+                    for (int k = 0; k < KC; ++k) {
+                        Frag<T> part[PARTS];
 #pragma unroll
-                        for (int i = 0; i < GROUP; ++i) {
-                            const int pb = p4 + i;
-                            f[i] = TX::across(ly, 16 * pb, k, i16, g);
+                        for (int e = 0; e < VEC; ++e) {
+                            float v = to_f32(z[k].v.v[e]) * weight(k, e);
+#pragma unroll
+                            for (int u = 0; u < PARTS; ++u) {
+                                part[u].v.v[e] = from_f32<T>(v);
+                                if (u + 1 < PARTS)
+                                    v -= to_f32(part[u].v.v[e]);
+                            }
                         }
 #pragma unroll
-                        for (int u = 0; u < PARTS; ++u)
+                        for (int p4 = 0; p4 < PB; p4 += GROUP) {
+                            Frag<T> f[GROUP];
 #pragma unroll
-                            for (int i = 0; i < GROUP; ++i)
-                                st[p4 + i] = mfma(f[i], part[u], st[p4 + i]);
+                            for (int i = 0; i < GROUP; ++i) {
+                                const int pb = p4 + i;
+                                f[i] = TX::across(ly, 16 * pb, k, i16, g);
+                            }
+#pragma unroll
+                            for (int u = 0; u < PARTS; ++u)
+#pragma unroll
+                                for (int i = 0; i < GROUP; ++i)
+                                    st[p4 + i] = mfma(f[i], part[u], st[p4 + i]);
+                        }
                     }
                 }
-                if constexpr (F16)
-#pragma unroll
-                    for (int pb = 0; pb < PB; ++pb)
-                        st[pb] *= 1.f / z_scale;
                 some = true;
             }
             lag = 1;
@@ -952,20 +1012,20 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
             for (int cb = 0; cb < CB; ++cb)
                 o[cb] = f4{0.f, 0.f, 0.f, 0.f};
             if (some) {
-                float s_scale = 1.f;
-                if constexpr (F16) {
-                    float most = 0.f;
+                float s_scale[CB];   // of the lane's columns
+                if constexpr (F16)
 #pragma unroll
-                    for (int pb = 0; pb < PB; ++pb)
+                    for (int cb = 0; cb < CB; ++cb) {
+                        float most = 0.f;
 #pragma unroll
-                        for (int cb = 0; cb < CB; ++cb)
+                        for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 const float v = fabsf(st[pb][cb][j]);
                                 most = v < INFINITY ? fmaxf(most, v) : most;
                             }
-                    s_scale = half_scale(group_max<64>(most));
-                }
+                        s_scale[cb] = half_scale(column_max(most));
+                    }
 #pragma unroll
                 for (int k = 0; k < KP; ++k)
 #pragma unroll
@@ -974,14 +1034,19 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
 #pragma unroll
                         for (int e = 0; e < VEC; ++e) {
                             const float v = st[BLOCKS * k + e / 4][cb][e % 4];
-                            s.v.v[e] = from_f32<T>(F16 ? v * s_scale : v);
+                            s.v.v[e] = from_f32<T>(F16 ? v * s_scale[cb] : v);
                         }
                         o[cb] = mfma(s, x[k], o[cb]);
                     }
                 const float f = A.c_out * decay_pow(decay, (float)(i16 + lag));
 #pragma unroll
-                for (int cb = 0; cb < CB; ++cb)
-                    o[cb] *= F16 ? f / s_scale : f;
+                for (int cb = 0; cb < CB; ++cb) {
+                    if constexpr (F16)   // 1 over the scales of the four columns that o has
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            o[cb][j] *= __shfl(one_over(s_scale[cb]), 4 * g + j);
+                    o[cb] *= f;
+                }
             }
             // what is not finite in z counts as zero, and is added where it belongs (k_decay)
             bool spoilt = false;
@@ -1051,7 +1116,10 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
 
             // ---- the state behind the chunk
             if (onward) {
-                float v[CB][4], most = 0.f, z_scale = 1.f;
+                float v[CB][4], most[CB], z_scale[CB];
+#pragma unroll
+                for (int cb = 0; cb < CB; ++cb)
+                    most[cb] = 0.f, z_scale[cb] = 1.f;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float f = A.c_y * decay_pow(decay, (float)max(0, n - 1 - (4 * g + j)));
@@ -1059,49 +1127,70 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
                     for (int cb = 0; cb < CB; ++cb) {
                         v[cb][j] = to_f32(z[cb].v.v[j]) * f;
                         if constexpr (F16)
-                            most = finite(v[cb][j]) ? fmaxf(most, fabsf(v[cb][j])) : most;
+                            most[cb] =
+                                finite(v[cb][j]) ? fmaxf(most[cb], fabsf(v[cb][j])) : most[cb];
                     }
                 }
                 if constexpr (F16)
-                    z_scale = half_scale(group_max<64>(most));
+#pragma unroll
+                    for (int cb = 0; cb < CB; ++cb)
+                        z_scale[cb] = half_scale(column_max(most[cb]));
                 const float whole = decay_pow(decay, (float)(n - 1 + lag));
-                const float keep = F16 ? whole * z_scale : whole;
                 Frag<T> yt[PB];
 #pragma unroll
                 for (int pb = 0; pb < PB; ++pb)
                     yt[pb] = across(ly, TY::PITCH, 16 * pb);
-                if (some && !exchanged)
+                if (some && !exchanged)   // (F16 too: its parts' sums are apart)
 #pragma unroll
                     for (int pb = 0; pb < PB; ++pb)
 #pragma unroll
                         for (int cb = 0; cb < CB; ++cb)
-                            st[pb][cb] *= keep;
+                            st[pb][cb] *= whole;
                 float *to = A.last + ((int64_t)piece.s * A.H + h) * size;
-                const float f =
-                    (A.lag1 ? decay_pow(decay, 1.f) : 1.f) * (F16 ? 1.f / z_scale : 1.f);
+                const float f = A.lag1 ? decay_pow(decay, 1.f) : 1.f;
 #pragma unroll
                 for (int cb = 0; cb < CB; ++cb) {
                     Frag<T> part[PARTS];
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
-                        float u = e >= 4 ? 0.f : F16 ? v[cb][e % 4] * z_scale : v[cb][e % 4];
+                        float u = e >= 4 ? 0.f : F16 ? v[cb][e % 4] * z_scale[cb] : v[cb][e % 4];
 #pragma unroll
                         for (int k = 0; k < PARTS; ++k) {
                             part[k].v.v[e] = from_f32<T>(u);
                             if (k + 1 < PARTS)
                                 u -= to_f32(part[k].v.v[e]);
+                            if constexpr (F16)
+                                u *= kLowPart;
                         }
                     }
+                    f4 high[PB], low[PB];   // F16: the parts' sums, for their scales
                     if (!exchanged) {
-#pragma unroll
-                        for (int k = 0; k < PARTS; ++k)
+                        if constexpr (F16) {
+                            const float back = one_over(z_scale[cb]);
 #pragma unroll
                             for (int pb = 0; pb < PB; ++pb)
-                                st[pb][cb] = mfma(yt[pb], part[k], st[pb][cb]);
+                                low[pb] = mfma(yt[pb], part[1], f4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                            for (int pb = 0; pb < PB; ++pb)
+                                high[pb] = mfma(yt[pb], part[0], f4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                            for (int pb = 0; pb < PB; ++pb)
+                                st[pb][cb] += (high[pb] + low[pb] / kLowPart) * back;
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+                                for (int pb = 0; pb < PB; ++pb)
+                                    st[pb][cb] = mfma(yt[pb], part[k], st[pb][cb]);
+                        }
                         continue;
                     }
                     const int c = 16 * cb + 4 * g;
-                    f4 r[PB];
+                    f4 r[PB], back;   // 1 over the scales of the lane's four columns
+                    if constexpr (F16)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            back[j] = __shfl(one_over(z_scale[cb]), 4 * g + j);
 #pragma unroll
                     for (int pb = 0; pb < PB; ++pb) {
                         const int row = 16 * pb + i16;
@@ -1115,14 +1204,26 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
                                 for (int j = 0; j < 3; ++j)
                                     if (c + j < A.r)
                                         r[pb][j] = p[j];
-                            r[pb] *= keep;
+                            r[pb] *= whole;
                         }
                     }
-#pragma unroll
-                    for (int k = 0; k < PARTS; ++k)
+                    if constexpr (F16) {
 #pragma unroll
                         for (int pb = 0; pb < PB; ++pb)
-                            r[pb] = mfma(part[k], yt[pb], r[pb]);
+                            low[pb] = mfma(part[1], yt[pb], f4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                        for (int pb = 0; pb < PB; ++pb)
+                            high[pb] = mfma(part[0], yt[pb], f4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                        for (int pb = 0; pb < PB; ++pb)
+                            r[pb] += (high[pb] + low[pb] / kLowPart) * back;
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+                            for (int pb = 0; pb < PB; ++pb)
+                                r[pb] = mfma(part[k], yt[pb], r[pb]);
+                    }
 #pragma unroll
                     for (int pb = 0; pb < PB; ++pb) {
                         const int row = 16 * pb + i16;
@@ -1139,13 +1240,6 @@ __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
                         }
                     }
                 }
-                if constexpr (F16)
-                    if (!exchanged)
-#pragma unroll
-                        for (int pb = 0; pb < PB; ++pb)
-#pragma unroll
-                            for (int cb = 0; cb < CB; ++cb)
-                                st[pb][cb] *= 1.f / z_scale;
                 some = true;
             }
             lag = 1;

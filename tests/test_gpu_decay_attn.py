@@ -490,3 +490,57 @@ def test_step_not_finite(tgm):
     tgm.tgm_decay_attn_step(q, k, v, torch.tensor([-0.1, -0.2]).cuda(), state, o)
     bad = torch.isnan(o)
     assert bad[1, d + 5] and int(bad.sum()) == 1 and int(torch.isnan(state).sum()) == 1
+
+
+# ---- sizes that differ by columns and rows
+def sized(t, heads, exponents):
+    """Columns of each head times powers of two."""
+    R = t.shape[0]
+    f = torch.exp2(torch.tensor(exponents, dtype=torch.float32))
+    v = t.view(R, heads, -1)
+    return (v * f[torch.arange(v.shape[2]) % len(exponents)]).reshape(R, -1)
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("lengths,dk,dv", [([150, 0, 40], 40, 56), ([6, 16, 1, 9], 40, 56),
+                                           ([700, 33], 64, 64), ([70], 128, 128), ([90, 5], 128, 64)])
+def test_columns_of_mixed_sizes(tgm, lengths, dk, dv, dtype, reverse):
+    """A column of a state keeps its own precision beside one 2^21 times as large."""
+    dt, H, G = TYPES[dtype], 2, 1
+    seqs = packed(lengths)
+    d = make(seqs, H, G, dk, dv, torch.float32, seed=11)
+    far = [10.0, -11.0, 0.0, -5.0, 9.0]
+    d["v"], d["do"] = sized(d["v"].cpu(), G, far), sized(d["do"].cpu(), H, far[::-1])
+    d["k"], d["q"] = sized(d["k"].cpu(), G, [6.0, -4.0, 0.0]), sized(d["q"].cpu(), H, [0.0, 6.0])
+    for n in ("q", "k", "v", "do"):
+        d[n] = d[n].to(dt).cuda()
+    d["state"] = d["dlast"] = None
+    # results of fp16's range: o has q k v, dk q v do
+    go(tgm, seqs, H, G, dk, dv, dt, reverse=reverse, d=d, scale=2.0 ** -12)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("n,w", [(31, 32), (16, 16), (60, 64)])
+def test_rows_of_mixed_sizes(tgm, n, w, dtype):
+    """Rows of a chunk that go to rows of the state of their own (k is 1 in a column of its
+    own) keep their precision beside rows 2^22 times as large."""
+    dt = TYPES[dtype]
+    seqs = packed([n])
+    d = make(seqs, 1, 1, w, w, dt, state=False, decay=[-2.0 ** -6])
+    k = torch.zeros(n, w)
+    k[torch.arange(n), torch.arange(n)] = 1.0
+    f = torch.exp2(torch.where(torch.arange(n) % 2 == 0, 11.0, -11.0))[:, None]
+    d["k"], d["v"] = k.to(dt).cuda(), (randn(3, n, w) * f).to(dt).cuda()
+    d["q"], d["do"] = (randn(4, n, w) * 2.0 ** -6).to(dt).cuda(), k.flip(0).to(dt).cuda()
+    go(tgm, seqs, 1, 1, w, w, dt, d=d, scale=1.0)
+
+
+@pytest.mark.parametrize("n", [9, 40])
+def test_states_far_above(tgm, n):
+    """fp16 rows that read a first state above 2^116 (fp32 holds it) by a small scale."""
+    dt, w = torch.float16, 16
+    seqs = packed([n] * 4)
+    d = make(seqs, 1, 1, w, w, dt, decay=[-2.0 ** -8])
+    d["state"], d["dlast"] = d["state"] * 2.0 ** 117, d["dlast"] * 2.0 ** 117
+    go(tgm, seqs, 1, 1, w, w, dt, d=d, scale=2.0 ** -112, what=())
