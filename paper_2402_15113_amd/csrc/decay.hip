@@ -568,6 +568,8 @@ extern "C" tgm_status_t tgm_decay_attn(const tgm_decay_attn_desc *d, const void 
     TGM_TRY_STATUS(tgm_decay_attn_work_bytes(d->rows, d->S, d->H, d->H_kv, d->d_k, d->d_v, d->dtype,
                                              0, &need));
     TGM_TRY_STATUS(check_work(need, work, work_bytes));
+    if (d->S == 0)   // packed rows of no sequence
+        return TGM_OK;
     const DecayBytes b = decay_bytes(d->rows, d->S, d->H, d->d_k, d->d_v);
     char *w = (char *)work;
     switch (d->dtype) {
@@ -592,6 +594,8 @@ extern "C" tgm_status_t tgm_decay_attn_backward(
     TGM_TRY_STATUS(tgm_decay_attn_work_bytes(d->rows, d->S, d->H, d->H_kv, d->d_k, d->d_v, d->dtype,
                                              1, &need));
     TGM_TRY_STATUS(check_work(need, work, work_bytes));
+    if (d->S == 0)
+        return TGM_OK;
     char *w = (char *)work;
     const DecayBytes b = decay_bytes(d->rows, d->S, d->H, d->d_k, d->d_v);
     switch (d->dtype) {

@@ -115,3 +115,20 @@ def test_binding():
         tgm._state("state", torch.zeros(2, 4, 2, 2), (2, 4, 2, 3), 0)
     with pytest.raises(ValueError, match="S is"):
         tgm._sequences(-1, None, None, 0)
+
+
+@pytest.mark.parametrize("kw", [dict(rows=200), dict(rows=200, H=2), dict(rows=0),
+                                dict(rows=1 << 20, H_kv=4)])
+def test_no_sequences(kw):
+    """Packed rows of no sequence at all: nothing to do, and nothing that is launched."""
+    L, kw = tgm.lib(), dict(dict(S=0), **kw)
+    assert L.tgm_decay_attn(desc(**kw), X, X, X, X, X, None, X, X, None, X, BIG,
+                            None) == tgm.TGM_OK
+    assert L.tgm_decay_attn_backward(desc(**kw), X, X, X, X, X, None, X, X, X, X, X, X, None, X,
+                                     BIG, None) == tgm.TGM_OK
+    # what the calls ask for is checked all the same
+    if kw["rows"]:
+        assert L.tgm_decay_attn(desc(**kw), None, X, X, X, X, None, X, X, None, X, BIG,
+                                None) == tgm.TGM_EINVAL
+        assert L.tgm_decay_attn_backward(desc(**kw), X, X, X, X, X, None, X, None, X, X, X, X,
+                                         None, X, BIG, None) == tgm.TGM_EINVAL

@@ -544,3 +544,20 @@ def test_states_far_above(tgm, n):
     d = make(seqs, 1, 1, w, w, dt, decay=[-2.0 ** -8])
     d["state"], d["dlast"] = d["state"] * 2.0 ** 117, d["dlast"] * 2.0 ** 117
     go(tgm, seqs, 1, 1, w, w, dt, d=d, scale=2.0 ** -112, what=())
+
+
+@pytest.mark.parametrize("rows,H,G", [(200, 2, 2), (5000, 4, 1), (0, 2, 1)])
+def test_rows_of_no_sequence_alone(tgm, rows, H, G):
+    """Not one sequence: nothing is written, and a capture of the calls goes through."""
+    seqs = packed([], behind=rows)
+    d, out, _ = both(tgm, seqs, H, G, 16, 8, torch.bfloat16, state=False)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        o = torch.full_like(out["o"], 7.0)
+        tgm.tgm_decay_attn(d["q"], d["k"], d["v"], d["decay"], o, 0,
+                           work(tgm, rows, 0, H, 16, 8, torch.bfloat16, G, False), kv_heads=G,
+                           **seqs[0])
+    g.replay()
+    torch.cuda.synchronize()
+    for t in [o] + [out[n] for n in ("o", "dq", "dk", "dv")]:
+        assert (t.float() == 7).all()
