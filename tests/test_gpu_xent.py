@@ -464,3 +464,50 @@ def test_captured_with_ignored_rows(tgm):
         call(1)
         torch.cuda.synchronize()
         assert torch.isfinite(dws[0]).all() and torch.equal(dws[0], dws[1])
+
+
+# ---- tables of several pieces
+def in_pieces(tgm, rows, N, K, dtype):
+    """Whether the work space is too small for dz of all classes."""
+    return tgm.tgm_xent_work_bytes(rows, N, K, dtype, backward=True) < \
+        rows * N * torch.finfo(dtype).bits // 8
+
+
+@pytest.mark.parametrize("dtype,rows,N,K,n_rows", [
+    ("f32", 16384, 12809, 65, 16001), ("bf16", 32768, 12809, 65, 32001),
+    ("f16", 32768, 12809, 65, 32001), ("f32", 16384, 17160, 64, None),
+    ("bf16", 32768, 11456, 72, None), ("f16", 32768, 17161, 64, None)])
+def test_several_pieces(tgm, dtype, rows, N, K, n_rows):
+    """dx adds the pieces, and every piece has its own targets, bias and rows of dW."""
+    assert in_pieces(tgm, rows, N, K, TYPES[dtype]), "all classes are one piece"
+    go(tgm, rows, N, K, TYPES[dtype], n_rows=n_rows, pad=K % 2)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_many_pieces(tgm, dtype):
+    """Many rows: pieces of 1,024 classes, the last one of a few; rows that are kept out too."""
+    rows, N, K = 300000, 2 * 1024 + 37, 8
+    dt = TYPES[dtype]
+    assert in_pieces(tgm, rows, N, K, dt), "all classes are one piece"
+    go(tgm, rows, N, K, dt, n_rows=299990)
+
+
+@pytest.mark.parametrize("dtype,rows", [("f32", 140001), ("bf16", 280001), ("f16", 280001)])
+def test_pieces_with_rows_kept_out(tgm, dtype, rows):
+    """Every piece's dW takes the rows of x that have a part in the loss, and no others."""
+    N, K, dt = 1500, 9, TYPES[dtype]
+    assert in_pieces(tgm, rows, N, K, dt), "all classes are one piece"
+    x, w = randn(1, rows, K).cuda().to(dt), randn(2, N, K).cuda().to(dt)
+    t = torch.randint(0, N, (rows,), generator=torch.Generator().manual_seed(3)).to(
+        torch.int32).cuda()
+    t[5::11] = -1
+    dl, got = randn(4, rows).cuda(), []
+    for fill in (0.0, math.nan):
+        x[5::11] = fill
+        lse = torch.empty(rows, device="cuda")
+        tgm.tgm_xent(x, w, t, None, work(tgm, rows, N, K, dt, False), lse=lse)
+        dw, dx = torch.full_like(w, 7.0), torch.full_like(x, 7.0)
+        tgm.tgm_xent_backward(x, w, t, lse, dl, work(tgm, rows, N, K, dt, True), dw=dw, dx=dx)
+        got.append((dw, dx))
+    assert torch.isfinite(got[1][0]).all() and torch.equal(got[0][0], got[1][0])
+    assert (got[1][1][5::11] == 0).all() and torch.equal(got[0][1], got[1][1])
