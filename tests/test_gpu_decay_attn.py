@@ -561,3 +561,54 @@ def test_rows_of_no_sequence_alone(tgm, rows, H, G):
     torch.cuda.synchronize()
     for t in [o] + [out[n] for n in ("o", "dq", "dk", "dv")]:
         assert (t.float() == 7).all()
+
+
+# ---- states handed along many cells
+def walk_is_wide(rows, S, H, size):
+    """Whether the walk over the cells' states has the work for which it takes 2,048 elements a
+    workgroup: over sequences or cells, whichever it goes by, at least so many workgroups of
+    512."""
+    cells = -(-rows // min(4096, max(64, -(-int((2 * rows * H) ** 0.5) // 64) * 64)))
+    by_sequence = S <= 4 * cells
+    return by_sequence, (S if by_sequence else cells) * H * -(-size // 512) > 4096
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_walk_by_sequences(tgm, dtype, reverse):
+    """Wide states of many heads: uneven sequences over several cells of rows, and states that
+    are no whole number of a workgroup's elements."""
+    lengths = [20 + (37 * i) % 300 for i in range(24)]
+    lengths[3], lengths[9], lengths[20] = 2900, 0, 1500
+    seqs, H, dk, dv = packed(lengths, before=30, behind=3), 16, 64, 100
+    assert walk_is_wide(seqs[3], len(lengths), H, dk * dv) == (True, True)
+    go(tgm, seqs, H, 16, dk, dv, TYPES[dtype], reverse=reverse)
+
+
+@pytest.mark.parametrize("reverse", [False, True])
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_walk_by_cells(tgm, dtype, reverse):
+    """More than four sequences to a cell, most of them short, two of them over several cells."""
+    short = [(7 * i) % 5 for i in range(60)]
+    seqs = packed(short[:40] + [1900] + short[40:] + [950, 1, 3], behind=40)
+    H, dk, dv = 16, 128, 126
+    assert walk_is_wide(seqs[3], len(seqs[1]), H, dk * dv) == (False, True)
+    go(tgm, seqs, H, 16, dk, dv, TYPES[dtype], reverse=reverse)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_sequences_alone(tgm, dtype):
+    """Each sequence's results are those of a call with that sequence alone, within both calls'
+    tolerances (how its rows come into chunks and cells may differ)."""
+    dt, lengths, H, G, d = TYPES[dtype], [64, 0, 90, 10, 700], 2, 1, 64
+    how, begin, end, rows = packed(lengths)
+    m, out, ref = go(tgm, (how, begin, end, rows), H, G, d, d, dt)
+    for s, (b, e) in enumerate(zip(begin, end)):
+        alone = {n: m[n][b:e] for n in ("q", "k", "v", "do")}
+        alone.update(decay=m["decay"], state=m["state"][s:s + 1], dlast=m["dlast"][s:s + 1])
+        _, got, _ = both(tgm, packed([e - b]), H, G, d, d, dt, d=alone)
+        for n in got:
+            tol = decayref.tolerance(n, ref, dt)
+            tol = tol + rounded(ref[n].abs() + tol, torch.float32 if "state" in n else dt)
+            at = slice(s, s + 1) if "state" in n else slice(b, e)
+            check(n, got[n], out[n][at].cpu().to(F64), 2 * tol[at])
