@@ -36,7 +36,7 @@ struct RotaryArgs {
 
 // cos and sin of pos omega.  The angle is formed and taken modulo a quarter turn in fp64
 // (a position of 10^9 keeps 2e-7 of a radian), the rest, within pi / 4, goes by the power
-// series in fp32: the first term left out is below 2e-9 and 1e-10.
+// series in fp32: the first term left out is below 1.8e-9 and 1.2e-10.
 __device__ __forceinline__ f2 turn_of(double pos, double omega)
 {
     const double t = pos * omega;

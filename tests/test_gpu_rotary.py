@@ -176,3 +176,18 @@ def test_captured(tgm):
         tgm.tgm_rotary(x, z, 4, omega, pos)
         torch.cuda.synchronize()
         assert torch.equal(y, z)
+
+
+def test_more_rows_than_the_grid(tgm):
+    """Every workgroup takes a row, and the first ones a second one, whose angles come in the
+    place of the first one's: both ends against fp64."""
+    rows, d, some = (1 << 20) + 100, 512, 300
+    x = torch.randn(rows, d, device="cuda", generator=torch.Generator("cuda").manual_seed(5)).to(
+        torch.bfloat16)
+    omega = (10000.0 ** (-2 * torch.arange(d // 2, dtype=F64) / d)).cuda()
+    for layout in ("half", "interleaved"):
+        y = torch.full_like(x, 7.0)
+        tgm.tgm_rotary(x, y, 1, omega, layout=layout)
+        for at in (slice(0, some), slice((1 << 20) - some, (1 << 20) + 100)):
+            ref, tol = reference(x[at], 1, omega, torch.arange(rows)[at], layout, 1.0, False)
+            check("y", y[at], ref, tol + rounded(ref.abs() + tol, torch.bfloat16))
