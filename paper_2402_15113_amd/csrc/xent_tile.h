@@ -15,12 +15,19 @@ namespace tgm {
 constexpr float kLog2e = 1.44269504088896340736f;
 // exp(z - m).  For results of 32 bits by the difference, whose rounding is 2^-24 of it, large
 // only where the result is small; for 16 bits in one step, with 2^-24 of m besides.
+// (From 2^100 on differences are 0 or at least 2^76: whatever factor they get, the exponential is
+// that of 0, or 0, or infinite, and log2(e) m could leave fp32, as that of bf16's lowest value does.)
 template <bool FULL> struct ExpFrom {
-    float m;   // times -log2(e) unless FULL
-    __device__ __forceinline__ explicit ExpFrom(float from) : m(FULL ? from : -from * kLog2e) {}
+    float m, f;   // m times -f unless FULL
+    __device__ __forceinline__ explicit ExpFrom(float from)
+        : m(from), f(FULL || fabsf(from) < 0x1p100f ? kLog2e : 0x1p-10f)
+    {
+        if (!FULL)
+            m *= -f;
+    }
     __device__ __forceinline__ float operator()(float z) const
     {
-        return __builtin_amdgcn_exp2f(FULL ? (z - m) * kLog2e : fmaf(z, kLog2e, m));
+        return __builtin_amdgcn_exp2f(FULL ? (z - m) * f : fmaf(z, f, m));
     }
 };
 

@@ -511,3 +511,28 @@ def test_pieces_with_rows_kept_out(tgm, dtype, rows):
         got.append((dw, dx))
     assert torch.isfinite(got[1][0]).all() and torch.equal(got[0][0], got[1][0])
     assert (got[1][1][5::11] == 0).all() and torch.equal(got[0][1], got[1][1])
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("N", [40, 700])
+def test_every_class_at_the_lowest_value(tgm, dtype, N):
+    """A mask of the type's lowest value over all classes: equal logits of that size are finite,
+    as is everything that is made of them; one class that is not masked has all the probability."""
+    dt, rows, K = TYPES[dtype], 70, 16
+    x, w = randn(1, rows, K).cuda().to(dt), randn(2, N, K).cuda().to(dt)
+    low = torch.finfo(dt).min
+    t = torch.full((rows,), 7, dtype=torch.int32, device="cuda")
+    dl = torch.ones(rows, device="cuda")
+    for open_class in (None, 7):
+        bias = torch.full((N,), low, device="cuda", dtype=dt)
+        if open_class is not None:
+            bias[open_class] = 0.5
+        loss, lse = (torch.empty(rows, device="cuda") for _ in range(2))
+        tgm.tgm_xent(x, w, t, loss, work(tgm, rows, N, K, dt, False), lse=lse, bias=bias)
+        out = dict(dx=torch.empty_like(x), dw=torch.empty_like(w), db=torch.empty_like(bias))
+        tgm.tgm_xent_backward(x, w, t, lse, dl, work(tgm, rows, N, K, dt, True), bias=bias, **out)
+        ref = reference(x, w, t, bias, dl)
+        for name, got in (("lse", lse), ("loss", loss)):
+            r, e = (v.cpu() for v in ref[name])
+            check(name, got, r, e)
+        assert all(torch.isfinite(v.float()).all() for v in out.values())
