@@ -216,11 +216,11 @@ extern "C" tgm_status_t tgm_rotary_frequencies(int32_t rot, int32_t scaling, dou
         !(original > 0 && std::isfinite(original) && seldom >= 0 && often > seldom &&
           std::isfinite(often)))
         return TGM_EINVAL;
-    if (scaling == TGM_ROTARY_BASE && rot > 2)
-        base *= std::pow(factor, rot / (rot - 2.0));
     *amplitude = scaling == TGM_ROTARY_PARTS ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
     for (int j = 0; j < rot / 2; ++j) {
-        const double w = std::pow(base, -2.0 * j / rot);
+        double w = std::pow(base, -2.0 * j / rot);
+        if (scaling == TGM_ROTARY_BASE && j)   // (the new base may be past fp64's range)
+            w *= std::pow(factor, -2.0 * j / (rot - 2.0));
         double keep = 1;
         if (scaling == TGM_ROTARY_LINEAR)
             keep = 0;

@@ -75,6 +75,19 @@ def test_frequencies(rot):
     assert np.allclose(w[~often & ~seldom], mid[~often & ~seldom], rtol=1e-13, atol=0)
 
 
+@pytest.mark.parametrize("rot", [2, 4, 64, 1024])
+@pytest.mark.parametrize("base,factor", [(1e300, 1e10), (10000.0, 1e300), (1e-300, 1e308)])
+def test_base_past_the_numbers(rot, base, factor):
+    """base factor^(rot / (rot - 2)) may be more than fp64 holds where its roots are not."""
+    w, a = tgm.tgm_rotary_frequencies(rot, "base", base=base, factor=factor)
+    j = np.arange(rot // 2)
+    grow = math.log(factor) / (rot - 2) if rot > 2 else 0.0
+    # (exponents of some hundred: their rounding is that many steps of the result)
+    want = -2 * j * (math.log(base) / rot + grow)
+    assert a == 1 and w[0] == 1 and (w > 0).all()
+    assert np.allclose(np.log(w), want, rtol=1e-12, atol=1e-12)
+
+
 @pytest.mark.parametrize("bad", [
     dict(rot=3), dict(rot=0), dict(rot=-2), dict(rot=1026), dict(base=0.0), dict(base=-1.0),
     dict(base=math.inf), dict(base=math.nan), dict(scaling="linear", factor=0.5),
