@@ -824,8 +824,8 @@ tgm_status_t tgm_scan_step(const tgm_scan_desc *d, const void *g, const void *x,
                            const int32_t *slots, const int32_t *n_rows, float *state, void *y,
                            void *stream);
 
-/* Rotary positions: in each of H heads of d columns, the first rot columns are pairs
- * (x_a, x_b) that are turned by the angle p omega_j, p the row's position:
+/* Rotary positions (Su et al., 2021): in each of H heads of d columns, the first rot columns
+ * are pairs (x_a, x_b) that are turned by the angle p omega_j, p the row's position:
  *   y_a = A (x_a cos - x_b sin),  y_b = A (x_b cos + x_a sin),  j = 0 .. rot / 2 - 1,
  * a = j, b = j + rot / 2 (TGM_ROTARY_HALF) or a = 2 j, b = 2 j + 1
  * (TGM_ROTARY_INTERLEAVED), A = amplitude; the other columns are copied.  inverse != 0
@@ -855,12 +855,14 @@ tgm_status_t tgm_rotary(const tgm_rotary_desc *d, const void *x, const double *o
 /* The frequencies of rot / 2 pairs, omega_j = base^(-2 j / rot), and the amplitude of
  * cos and sin, for histories `factor` >= 1 times as long as those that a model has seen:
  *   TGM_ROTARY_PLAIN   as they are;
- *   TGM_ROTARY_LINEAR  omega_j / factor;
+ *   TGM_ROTARY_LINEAR  omega_j / factor (position interpolation: Chen et al., 2023);
  *   TGM_ROTARY_BASE    base factor^(rot / (rot - 2)) for base, which divides the lowest
- *                      frequency by factor and leaves the highest;
+ *                      frequency by factor and leaves the highest (published as NTK-aware
+ *                      scaling, 2023);
  *   TGM_ROTARY_PARTS   pairs that turn at least `often` times within `original` positions
  *                      keep theirs, those that turn at most `seldom` times have it divided,
- *                      a line between; amplitude 0.1 ln(factor) + 1 (else 1).
+ *                      a line between; amplitude 0.1 ln(factor) + 1 (else 1) (YaRN: Peng et
+ *                      al., 2023).
  * HOST arrays omega [rot / 2] and amplitude [1]; touches no device.  Errors: TGM_EINVAL. */
 #define TGM_ROTARY_PLAIN 0
 #define TGM_ROTARY_LINEAR 1

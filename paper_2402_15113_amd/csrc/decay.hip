@@ -176,10 +176,11 @@ __global__ __launch_bounds__(256) void k_decay_shared(const float *__restrict__ 
     }
 }
 
-// One row for each of n states of a table.  A workgroup has a head of one: a thread reads
-// and writes VEC neighbouring columns of every G-th row of the state.  Bound by memory: 192 states
-// of 16 heads of 128 x 128 (403 MB) 87 us, 4.6 TB/s; 600 of 2 heads of 50 x 50 take 10 us, the
-// call's own time.
+// One row for each of n states of a table.  A workgroup has a head of one: a thread reads and
+// writes VEC neighbouring columns of every G-th row of the state.  Bound by memory: 192 states of
+// 16 heads of 128 x 128 (403 MB) 87 us, 4.6 TB/s.  600 of 2 heads of 50 x 50 (24 MB) take 9 us,
+// three times what their bytes do: 13 rows a thread, each loaded when the one before is stored,
+// since both are of the one table.
 template <class T, int VEC, int LANES>
 __global__ __launch_bounds__(256) void k_decay_step(const T *__restrict__ q,
                                                     const T *__restrict__ k,

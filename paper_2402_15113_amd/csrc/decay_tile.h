@@ -10,20 +10,22 @@
 // product's operand has them in, so S never goes through LDS.  What they exchange are the
 // weights a^(i - s) (x_i . y_s), a row of 16 i each, through LDS.
 //
-// 16-bit inputs: the weights and S are rounded once for the products that make out of them.
-// S itself takes a^(n - 1 - s) z_s in parts, so that no error of 16 bits is carried along: three
-// of bf16, whose sum is the fp32 product, or two of fp16, whose sum is off by 2^-23 of it.  fp16
-// is narrow, so its numbers come times powers of two: one for a row of weights, one for a column of
-// S (a lane has one column of S and of z), one for a column of z, whose second parts have another
+// 16-bit inputs: the weights and S are rounded once for the products that make out of them. S
+// itself takes a^(n - 1 - s) z_s in parts, so that no error of 16 bits is carried along: three of
+// bf16, whose sum is the fp32 product, or two of fp16, whose sum is off by 2^-23 of it.  fp16 is
+// narrow, so its numbers come times powers of two: one for a row of weights, one for a column of S
+// (a lane has one column of S and of z), one for a column of z, whose second parts have another
 // 2^12.  What is below 2^-27 of the largest of its row of weights or column of S loses bits to
 // fp16's smallest steps; of a column of z, what is below 2^-29 of its largest in the chunk.
 //
 // What bounds it: the chain from chunk to chunk (loads, weights, results, state, two exchanges
-// through LDS), of which 16 wavefronts a CU do not hide all; q, k, v and o pass once here and k
-// and v once more for the states.  bf16, 262,147 rows of 8 heads of 128: results 540 us (2.1 GB,
-// 4.0 TB/s), states 262 us (1.1 GB, 4.1 TB/s); 65,536 rows of 16 heads of 64 and 128 in 64
-// sequences: results 267 us, dq 153, dv 292 and dk 173 (fp32, for four heads each), states 54.
-// fp32, 4,000 sequences of 11 rows of 2 heads of 50 with their states: 81 us (200 MB).
+// through LDS), of which 16 wavefronts a CU do not hide all; q, k, v and o pass once here and k and
+// v once more for the states.  bf16, 262,147 rows of 8 heads of 128: results 553 us at least and
+// 624 in the median (2.1 GB, 3.9 TB/s), states 265 and 291 (1.1 GB, 4.1 TB/s); 65,536 rows of 16
+// heads of 64 and 128 in 64 sequences, at least: results 266 us, dq 152, dv 293 and dk 174 (fp32,
+// for four heads each), states 54.  fp32, 262,147 rows of 8 heads of 128: results 1,558 us at least
+// (171 G operations, 110 TFLOP/s), states 692 (99 TFLOP/s); 4,000 sequences of 11 rows of 2 heads
+// of 50 with their states 80 (200 MB).
 #pragma once
 
 #include <type_traits>
@@ -270,8 +272,10 @@ template <class T, int P, bool OUT> constexpr int decay_chunk()
 
 // Wavefronts of a SIMD that registers are kept for: two workgroups of 512 threads or four of 256
 // fit a CU; three of those with 128 x 64 columns in fp32 and fp16, which would not be kept in 128
-// registers.  us with 3 and 4: 262,144 rows of 8 heads fp32 1,438 and 1,484, a training step of
-// 65,536 rows of heads of 64 and 128 fp16 1,002 and 1,082; of bf16 dq and dk of 16 heads 425 and 382.
+// registers.  us with 3 and 4: 262,144 rows of 8 heads of 128 x 64 fp32 1,338 and 1,377; a training
+// step of 65,536 rows of 8 heads of 64 and 128 in 64 sequences fp16 834 and 907, of 16 heads, 4 of
+// k and v, bf16 1,375 and 1,361.  With 4, kernels of 128 columns spill vector registers around
+// their pieces: bf16 45 (128 x 64) and 36 (128 x 128), fp16 19 to 21 and fp32 13 (128 x 128).
 template <class T, int P, int R, bool OUT> constexpr int decay_waves()
 {
     return OUT && P == 128 && R == 64 && TypeCode<T>::code != TGM_BF16 ? 3 : 4;
@@ -805,13 +809,15 @@ __device__ __forceinline__ void exchange()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
 }
 
-// Short sequences: a wavefront has a head of a piece and all columns of its state, and chunks of
-// 16 rows.  The weights a^(i - s) (x_i . y_s) of 16 rows are left by the matrix instructions where
-// the next product takes them; LDS, of which every wavefront has its own, turns y and z; no
-// wavefront waits for another.  Bound by the latency of each sequence's loads, of which the 8
-// wavefronts a CU that a state in registers leaves room for do not cover all: 12,000 sequences of
-// 10 rows of 2 heads of 50 fp32 with their states (431 MB) in 165 us, 2.6 TB/s; without the
-// states behind them 83.  (States moved through LDS, 16 bytes a lane side by side: 177 us.)
+// Short sequences: a wavefront has a head of a piece and all columns of its state, and chunks of 16
+// rows.  The weights a^(i - s) (x_i . y_s) of 16 rows are left by the matrix instructions where the
+// next product takes them; LDS, of which every wavefront has its own, turns y and z; no wavefront
+// waits for another.  Bound by each sequence's loads, several thousand instructions and stores, one
+// after another, of which the 8 wavefronts a CU that a state in registers leaves room for (211
+// vector registers, 241 scalar ones in lanes of others) do not cover all; the state is kept there
+// also where there is none before and one chunk is all.  12,000 sequences of 10 rows of 2 heads of
+// 50 fp32 with their states (431 MB) in 163 us, 2.6 TB/s; without the states behind them 83.
+// (States moved through LDS, 16 bytes a lane side by side: 177 us.)
 template <class T, class O, int P, int R>
 __global__ __launch_bounds__(256, 2) void k_decay_short(DecayRun run)
 {

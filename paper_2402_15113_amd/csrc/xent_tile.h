@@ -31,8 +31,8 @@ template <bool FULL> struct ExpFrom {
     }
 };
 
-// The sums of the loss.  Bound by the matrix cores: 8,192 rows x 65,537 x 2,048 bf16 in 1.57 ms
-// (1.40 PFLOP/s), 12,000 x 9,228 x 100 fp32 in 275 us.
+// The sums of the loss.  Bound by the matrix cores: 8,192 rows x 65,537 x 2,048 bf16 in 1.59 ms
+// (1.39 PFLOP/s), 12,000 x 9,228 x 100 fp32 in 275 us.
 struct XentSums {
     using Args = XentArgs;
     template <class T, int NA, int MA>
@@ -102,7 +102,7 @@ struct XentSums {
 };
 
 // dz.  Bound by the matrix cores and, where K is small, by its stores: 8,192 rows x 32,768 x 2,048
-// bf16 in 931 us (1.18 PFLOP/s), 1,174 with stores of 8 bytes; 12,000 x 9,228 x 100 fp32 in 385 us
+// bf16 in 931 us (1.18 PFLOP/s), 1,174 with stores of 8 bytes; 12,000 x 9,228 x 100 fp32 in 360 us
 // (443 MB stored).
 struct XentGrad {
     using Args = XentArgs;
