@@ -889,13 +889,14 @@ tgm_status_t tgm_rotary_frequencies(int32_t rot, int32_t scaling, double base, d
  * offsets or padded, and shortened by length, as for tgm_scan; what rows of no sequence
  * hold does not matter, and their o is left as it is.  reverse != 0 runs every sequence
  * from its last row to its first.
- * Products are added in fp32, and states are fp32, to which 16-bit rows add products rounded to
- * 24 bits (f16: 22); the weights a^(t-s) scale q_t k_s of 16-bit rows within some rows, and
- * the state that q_t reads there, are rounded to 16 bits, about 1.4 times the error that rounding o
- * has.  f16 has these times powers of two, one for each row of weights and each column of a state
- * (of its transpose for dq and dk): a weight or an element below 2^-27 of the largest of its row
- * or column, and a product below 2^-29 of the largest of its column within 64 rows, lose bits.  A row that is not finite reaches its own and
- * later rows only; where the formula has an infinity there may be NaN.
+ * Products are added in fp32, and states are fp32, to which 16-bit rows add products rounded
+ * to 24 bits (f16: 22); the weights a^(t-s) scale q_t k_s of 16-bit rows within some rows, and
+ * the state that q_t reads there, are rounded to 16 bits, about 1.4 times the error that
+ * rounding o has.  f16 has these times powers of two, one for each row of weights and each
+ * column of a state (of its transpose for dq and dk): a weight or an element below 2^-27 of
+ * the largest of its row or column, and a product below 2^-29 of the largest of its column
+ * within 64 rows, lose bits.  A row that is not finite reaches its own and later rows only;
+ * where the formula has an infinity there may be NaN.
  * rows <= 2^30, H <= 4096, 1 <= d_k, d_v <= 128.
  * Errors: TGM_EINVAL (null, sizes, types, strides, S < 0, S = 0 with rows in the padded form
  * or rows not divisible by it, state_last = state), TGM_ESIZE (work). */
